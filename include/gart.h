@@ -440,6 +440,95 @@ gart_status gart_adam_step(float* param, const float* grad, float* m, float* v, 
  * run on the frame. */
 gart_status gart_frame_status(const gart_frame* frame, uint32_t* flags_host, void* stream);
 
+/* ---- Learned blocks in front of the parameters ----
+ * An appearance model looks a latent code up for every Gaussian, turns the
+ * codes into SH coefficients with linear layers and dropout, and takes
+ * gart_backward's g_sh back into its weights and codes.  These calls are its
+ * operators.
+ *
+ *  - All tensors of a call have one element type; ids and random state aside.
+ *    Sums are formed in 32-bit floats and rounded once, when they are stored.
+ *  - Matrices are row-major with a row stride in elements of at least the
+ *    column count; an input whose stride is 0 is one row repeated.  Rows and
+ *    columns are below 2^31, and offsets are 64 bits.  A size may be 0.
+ *    Data must be aligned to the element size; nothing more is needed.
+ *  - An output may not overlap another output or an input, except where a
+ *    call names one it may be equal to (the same data and stride).
+ *  - The calls only enqueue kernels (they may be captured in a HIP graph) and
+ *    give the same bits for the same inputs.  scratch is caller-owned device
+ *    memory, 16-byte aligned, used by one stream at a time, with nothing kept
+ *    in it between calls.  INVALID_ARG for NULL, mismatched or overlapping
+ *    arguments, before anything is launched. */
+
+typedef enum { GART_DTYPE_F32 = 0, GART_DTYPE_BF16 = 1, GART_DTYPE_F16 = 2 } gart_dtype;
+
+typedef enum {
+  GART_ACT_NONE = 0,
+  GART_ACT_RELU = 1, /* max(z, 0) */
+  GART_ACT_SILU = 2, /* z / (1 + exp(-z)) */
+  GART_ACT_GELU = 3  /* 0.5 z (1 + tanh(sqrt(2 / pi) (z + 0.044715 z^3))) */
+} gart_activation;
+
+/* A matrix in device memory.  Host struct, passed by pointer. */
+typedef struct {
+  void* data;
+  int64_t rows, cols;
+  int64_t stride; /* elements from one row to the next */
+} gart_matrix;
+
+/* out[i,:] = scale * table[ids[i],:] for i < out.rows; a zero row where ids[i]
+ * is outside [0, table.rows) (a Gaussian without a code).  ids: device int32,
+ * or int64 if ids64 is non-zero, [out.rows]. */
+gart_status gart_embedding(const gart_matrix* table, const void* ids, int32_t ids64, float scale, gart_dtype dtype,
+                           const gart_matrix* out, void* stream);
+
+/* Scratch of gart_embedding_backward for n ids, vocab table rows of dim. */
+size_t gart_embedding_scratch_bytes(int64_t n, int64_t vocab, int64_t dim);
+
+/* Gradient of gart_embedding with respect to the table:
+ *   g_table[v,:] = scale * sum over i with ids[i] = v of dl_dout[i,:]
+ * for every v < g_table.rows (zero for rows no id names).  Rows are summed in
+ * an order fixed by the ids alone, so the result is deterministic. */
+gart_status gart_embedding_backward(const void* ids, int32_t ids64, const gart_matrix* dl_dout, float scale,
+                                    gart_dtype dtype, const gart_matrix* g_table, void* scratch,
+                                    size_t scratch_bytes, void* stream);
+
+/* Scratch of gart_linear for rows x inputs times inputs x outputs (0 if it needs none). */
+size_t gart_linear_scratch_bytes(int64_t rows, int64_t inputs, int64_t outputs, gart_dtype dtype);
+
+/* y = act(x weight^T + bias) + residual, with x [rows, inputs], weight
+ * [outputs, inputs], bias [outputs] or NULL, residual [rows, outputs] or NULL
+ * (it may be y itself). */
+gart_status gart_linear(const gart_matrix* x, const gart_matrix* weight, const void* bias,
+                        const gart_matrix* residual, gart_activation act, gart_dtype dtype, const gart_matrix* y,
+                        void* scratch, size_t scratch_bytes, void* stream);
+
+size_t gart_linear_backward_scratch_bytes(int64_t rows, int64_t inputs, int64_t outputs, gart_dtype dtype,
+                                          gart_activation act);
+
+/* Gradients of gart_linear from its inputs and dl_dy (nothing of the forward
+ * is stored: z = x weight^T + bias is computed again where act needs it):
+ *   dz = dl_dy act'(z);  g_x = dz weight;  g_weight = dz^T x;  g_bias = sum of dz over rows.
+ * relu's derivative is 0 at z <= 0.  The residual's gradient is dl_dy.  Any of
+ * the three outputs may be NULL.  With 16-bit types dz enters the products
+ * rounded to that type; g_bias sums it unrounded. */
+gart_status gart_linear_backward(const gart_matrix* x, const gart_matrix* weight, const void* bias,
+                                 gart_activation act, const gart_matrix* dl_dy, gart_dtype dtype,
+                                 const gart_matrix* g_x, const gart_matrix* g_weight, void* g_bias, void* scratch,
+                                 size_t scratch_bytes, void* stream);
+
+/* y[r,c] = residual[r,c] + (kept ? x[r,c] / (1 - p) : 0), residual NULL for 0.
+ * p is taken as t / 2^16 with t = p 2^16 rounded to the nearest (0 <= p <= 1;
+ * at t = 2^16 everything is dropped).  The mask is never stored: element e =
+ * r * cols + c (whatever the strides) is kept iff its 16 random bits are >= t.
+ * They come from Philox-4x32-10 (Salmon, Moraes, Dror and Shaw, 2011) with key
+ * seed and counter (e / 8, offset), each low word first: element e uses half
+ * word e % 8 of the four output words, low halves first.  A dropped element
+ * contributes nothing, whatever it holds.  The same call on dL/dy, without a
+ * residual, is the gradient.  y may be x or the residual. */
+gart_status gart_dropout(const gart_matrix* x, const gart_matrix* residual, float p, uint64_t seed, uint64_t offset,
+                         gart_dtype dtype, const gart_matrix* y, void* stream);
+
 /* Human-readable name of a status code (static string). */
 const char* gart_status_string(gart_status status);
 

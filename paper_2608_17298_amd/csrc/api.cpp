@@ -11,6 +11,7 @@
 
 #include "../../include/gart.h"
 #include "ops.h"
+#include "status.h"
 
 using namespace gart;
 
@@ -18,8 +19,10 @@ using namespace gart;
 static __device__ __align__(256) unsigned char scratch[size_t(4) << 20];
 
 namespace {
-
 thread_local char g_err[512] = "";
+}  // namespace
+
+namespace gart {
 
 gart_status fail(gart_status s, const char* fmt, ...) {
   va_list ap;
@@ -29,16 +32,11 @@ gart_status fail(gart_status s, const char* fmt, ...) {
   return s;
 }
 
-#define GART_HIP(expr)                                                                   \
-  do {                                                                                   \
-    const hipError_t e_ = (expr);                                                        \
-    if (e_ != hipSuccess) return fail(GART_ERR_HIP, "%s: %s", #expr, hipGetErrorString(e_)); \
-  } while (0)
+void clear_error() { g_err[0] = 0; }
 
-#define GART_REQUIRE(cond, ...)                                   \
-  do {                                                            \
-    if (!(cond)) return fail(GART_ERR_INVALID_ARG, __VA_ARGS__); \
-  } while (0)
+}  // namespace gart
+
+namespace {
 
 size_t align_up(size_t v) { return (v + 255) & ~size_t(255); }
 

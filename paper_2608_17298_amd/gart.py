@@ -132,6 +132,24 @@ def lib():
         L.gart_l1_loss_grad.argtypes = [_P, _P, ctypes.c_int64, _P, _P, _P, _P]
         L.gart_adam_step.restype = ctypes.c_int
         L.gart_adam_step.argtypes = [_P, _P, _P, _P, ctypes.c_int64, _P, ctypes.c_int64, _P]
+        L.gart_embedding.restype = ctypes.c_int
+        L.gart_embedding.argtypes = [_P, _P, ctypes.c_int32, ctypes.c_float, ctypes.c_int, _P, _P]
+        L.gart_embedding_scratch_bytes.restype = ctypes.c_size_t
+        L.gart_embedding_scratch_bytes.argtypes = [ctypes.c_int64] * 3
+        L.gart_embedding_backward.restype = ctypes.c_int
+        L.gart_embedding_backward.argtypes = [_P, ctypes.c_int32, _P, ctypes.c_float, ctypes.c_int, _P, _P,
+                                              ctypes.c_size_t, _P]
+        L.gart_linear_scratch_bytes.restype = ctypes.c_size_t
+        L.gart_linear_scratch_bytes.argtypes = [ctypes.c_int64] * 3 + [ctypes.c_int]
+        L.gart_linear.restype = ctypes.c_int
+        L.gart_linear.argtypes = [_P, _P, _P, _P, ctypes.c_int, ctypes.c_int, _P, _P, ctypes.c_size_t, _P]
+        L.gart_linear_backward_scratch_bytes.restype = ctypes.c_size_t
+        L.gart_linear_backward_scratch_bytes.argtypes = [ctypes.c_int64] * 3 + [ctypes.c_int, ctypes.c_int]
+        L.gart_linear_backward.restype = ctypes.c_int
+        L.gart_linear_backward.argtypes = [_P, _P, _P, ctypes.c_int, _P, ctypes.c_int, _P, _P, _P, _P,
+                                           ctypes.c_size_t, _P]
+        L.gart_dropout.restype = ctypes.c_int
+        L.gart_dropout.argtypes = [_P, _P, ctypes.c_float, ctypes.c_uint64, ctypes.c_uint64, ctypes.c_int, _P, _P]
         _lib = L
     return _lib
 
@@ -480,6 +498,154 @@ def gart_adam_step(param: torch.Tensor, grad: torch.Tensor, m: torch.Tensor, v: 
             raise ValueError("param, grad, m and v must be float32 of one shape")
     _check(lib().gart_adam_step(_ptr(param), _ptr(grad), _ptr(m), _ptr(v), param.numel(), ctypes.byref(h),
                                 int(step), _stream(stream)), "gart_adam_step")
+
+
+# ---------------------------------------------------------------------------
+# Learned blocks in front of the parameters: embedding, linear layer, dropout
+# ---------------------------------------------------------------------------
+DTYPE_F32, DTYPE_BF16, DTYPE_F16 = 0, 1, 2
+DTYPES = {torch.float32: DTYPE_F32, torch.bfloat16: DTYPE_BF16, torch.float16: DTYPE_F16}
+ACT_NONE, ACT_RELU, ACT_SILU, ACT_GELU = 0, 1, 2, 3
+ACTIVATIONS = {"none": ACT_NONE, "relu": ACT_RELU, "silu": ACT_SILU, "gelu": ACT_GELU}
+
+
+class gart_matrix(ctypes.Structure):
+    _fields_ = [("data", _P), ("rows", ctypes.c_int64), ("cols", ctypes.c_int64), ("stride", ctypes.c_int64)]
+
+
+def _dtype(t: torch.Tensor) -> int:
+    d = DTYPES.get(t.dtype)
+    if d is None:
+        raise ValueError(f"GART blocks take float32, bfloat16 or float16, not {t.dtype}")
+    return d
+
+
+def _matrix(t: torch.Tensor, like: torch.Tensor, name: str) -> gart_matrix:
+    """A 2-D tensor whose rows are contiguous; rows may be strided, or one row repeated (stride 0)."""
+    if t.dim() != 2 or t.dtype != like.dtype or t.device != like.device or not t.is_cuda:
+        raise ValueError(f"{name} must be a 2-D {like.dtype} tensor on {like.device if like.is_cuda else 'a GPU'}")
+    rows, cols = t.shape
+    step, inner = t.stride()
+    if cols > 1 and inner != 1 and rows > 0:
+        raise ValueError(f"{name}'s rows must be contiguous")
+    return gart_matrix(t.data_ptr(), rows, cols, step if rows > 1 else cols)
+
+
+def _vector(t: torch.Tensor | None, like: torch.Tensor, n: int, name: str):
+    if t is None:
+        return None
+    if t.dim() != 1 or t.shape[0] != n or t.dtype != like.dtype or t.device != like.device or (n > 1 and t.stride(0) != 1):
+        raise ValueError(f"{name} must be a contiguous {like.dtype} tensor of {n} elements on {like.device}")
+    return t.data_ptr()
+
+
+def _ids(ids: torch.Tensor, like: torch.Tensor, n: int):
+    if ids.dim() != 1 or ids.shape[0] != n or ids.device != like.device or (n > 1 and ids.stride(0) != 1) \
+            or ids.dtype not in (torch.int32, torch.int64):
+        raise ValueError(f"ids must be a contiguous int32 or int64 tensor of {n} elements on {like.device}")
+    return ids.data_ptr(), int(ids.dtype == torch.int64)
+
+
+def _scratch(scratch: torch.Tensor | None, like: torch.Tensor):
+    if scratch is None:
+        return None, 0
+    if scratch.device != like.device or not scratch.is_contiguous():
+        raise ValueError(f"scratch must be a contiguous tensor on {like.device}")
+    return scratch.data_ptr(), scratch.numel() * scratch.element_size()
+
+
+def _stream_on(stream, like: torch.Tensor):
+    """The raw stream of the call: `stream`, or the current one of the tensors' GPU, which must be the current GPU."""
+    if like.device.index != torch.cuda.current_device():
+        raise ValueError(f"tensors are on {like.device}, the current GPU is {torch.cuda.current_device()}")
+    return (torch.cuda.current_stream() if stream is None else stream).cuda_stream
+
+
+def _act(act) -> int:
+    if isinstance(act, str):
+        if act not in ACTIVATIONS:
+            raise ValueError(f"unknown activation {act!r}")
+        return ACTIVATIONS[act]
+    return int(act)
+
+
+def gart_embedding(table: torch.Tensor, ids: torch.Tensor, out: torch.Tensor, scale: float = 1.0, stream=None):
+    """out[i] = scale * table[ids[i]]; a zero row where ids[i] is outside the table.  table [vocab, dim], ids [n]
+    int32 or int64, out [n, dim]."""
+    d = _dtype(table)
+    t, o = _matrix(table, table, "table"), _matrix(out, table, "out")
+    p, wide = _ids(ids, table, out.shape[0])
+    _check(lib().gart_embedding(ctypes.byref(t), p, wide, scale, d, ctypes.byref(o), _stream_on(stream, table)),
+           "gart_embedding")
+
+
+def gart_embedding_scratch_bytes(n: int, vocab: int, dim: int) -> int:
+    return int(lib().gart_embedding_scratch_bytes(int(n), int(vocab), int(dim)))
+
+
+def gart_embedding_backward(ids: torch.Tensor, dl_dout: torch.Tensor, g_table: torch.Tensor, scale: float = 1.0,
+                            scratch: torch.Tensor | None = None, stream=None):
+    """g_table[v] = scale * sum of dl_dout[i] over ids[i] = v (overwritten, zero for unused rows); scratch of
+    gart_embedding_scratch_bytes(n, vocab, dim) bytes."""
+    d = _dtype(g_table)
+    x, g = _matrix(dl_dout, g_table, "dl_dout"), _matrix(g_table, g_table, "g_table")
+    p, wide = _ids(ids, g_table, dl_dout.shape[0])
+    sp, sn = _scratch(scratch, g_table)
+    _check(lib().gart_embedding_backward(p, wide, ctypes.byref(x), scale, d, ctypes.byref(g), sp, sn,
+                                         _stream_on(stream, g_table)), "gart_embedding_backward")
+
+
+def gart_linear_scratch_bytes(rows: int, inputs: int, outputs: int, dtype: torch.dtype = torch.float32) -> int:
+    return int(lib().gart_linear_scratch_bytes(int(rows), int(inputs), int(outputs), DTYPES[dtype]))
+
+
+def gart_linear(x: torch.Tensor, weight: torch.Tensor, y: torch.Tensor, bias: torch.Tensor | None = None,
+                residual: torch.Tensor | None = None, act="none", scratch: torch.Tensor | None = None, stream=None):
+    """y = act(x weight^T + bias) + residual; x [rows, inputs], weight [outputs, inputs], bias [outputs], residual and
+    y [rows, outputs] (the residual may be y); act "none", "relu", "silu" or "gelu"; scratch of
+    gart_linear_scratch_bytes(rows, inputs, outputs, dtype) bytes."""
+    d = _dtype(x)
+    mx, mw, my = _matrix(x, x, "x"), _matrix(weight, x, "weight"), _matrix(y, x, "y")
+    mr = None if residual is None else ctypes.byref(_matrix(residual, x, "residual"))
+    sp, sn = _scratch(scratch, x)
+    _check(lib().gart_linear(ctypes.byref(mx), ctypes.byref(mw), _vector(bias, x, weight.shape[0], "bias"), mr,
+                             _act(act), d, ctypes.byref(my), sp, sn, _stream_on(stream, x)), "gart_linear")
+
+
+def gart_linear_backward_scratch_bytes(rows: int, inputs: int, outputs: int, dtype: torch.dtype = torch.float32,
+                                       act="none") -> int:
+    return int(lib().gart_linear_backward_scratch_bytes(int(rows), int(inputs), int(outputs), DTYPES[dtype],
+                                                        _act(act)))
+
+
+def gart_linear_backward(x: torch.Tensor, weight: torch.Tensor, dl_dy: torch.Tensor, g_x: torch.Tensor | None = None,
+                         g_weight: torch.Tensor | None = None, g_bias: torch.Tensor | None = None,
+                         bias: torch.Tensor | None = None, act="none", scratch: torch.Tensor | None = None,
+                         stream=None):
+    """Gradients of gart_linear (overwritten; None for those not wanted) from its inputs and dl_dy; scratch of
+    gart_linear_backward_scratch_bytes(rows, inputs, outputs, dtype, act) bytes."""
+    d = _dtype(x)
+    mx, mw, md = _matrix(x, x, "x"), _matrix(weight, x, "weight"), _matrix(dl_dy, x, "dl_dy")
+    gx = None if g_x is None else ctypes.byref(_matrix(g_x, x, "g_x"))
+    gw = None if g_weight is None else ctypes.byref(_matrix(g_weight, x, "g_weight"))
+    n = weight.shape[0]
+    sp, sn = _scratch(scratch, x)
+    _check(lib().gart_linear_backward(ctypes.byref(mx), ctypes.byref(mw), _vector(bias, x, n, "bias"), _act(act),
+                                      ctypes.byref(md), d, gx, gw, _vector(g_bias, x, n, "g_bias"), sp, sn,
+                                      _stream_on(stream, x)), "gart_linear_backward")
+
+
+def gart_dropout(x: torch.Tensor, y: torch.Tensor, p: float, seed: int, offset: int = 0,
+                 residual: torch.Tensor | None = None, stream=None):
+    """y = residual + x / (1 - p) where kept, with the mask of (seed, offset); y may be x or the residual.  Its
+    gradient is the same call on dL/dy without a residual."""
+    d = _dtype(x)
+    mx, my = _matrix(x, x, "x"), _matrix(y, x, "y")
+    mr = None if residual is None else ctypes.byref(_matrix(residual, x, "residual"))
+    if not (0 <= seed < 1 << 64 and 0 <= offset < 1 << 64):
+        raise ValueError("seed and offset are 64-bit unsigned")
+    _check(lib().gart_dropout(ctypes.byref(mx), mr, p, seed, offset, d, ctypes.byref(my), _stream_on(stream, x)),
+           "gart_dropout")
 
 
 def empty_grads(g: Gaussians) -> dict:

@@ -1,0 +1,513 @@
+"""The learned blocks (embedding, linear layer, dropout) on the GPU against plain 64-bit forms: sizes from nothing and
+one row up, odd and strided ones, every type, ids outside the table, non-finite values, offsets beyond 32 bits, other
+streams, graphs, repeatability.  Gradients also against central differences."""
+import numpy as np
+import pytest
+
+import blocks_ref as ref
+
+pytestmark = pytest.mark.gpu
+
+TYPES = ["f32", "bf16", "f16"]
+GUARD = 3.0  # fills what surrounds an output
+
+
+def _torch(dtype):
+    import torch
+    return dict(f32=torch.float32, bf16=torch.bfloat16, f16=torch.float16)[dtype]
+
+
+def _mat(rng, rows, cols, dtype, pad=0, scale=1.0):
+    """A device matrix of normal values (a view of a wider one if pad), and the same values in 64 bits."""
+    import torch
+    t = torch.from_numpy(rng.standard_normal((rows, cols + pad)) * scale).to(_torch(dtype)).cuda()[:, :cols]
+    return t, t.cpu().double().numpy()
+
+
+def _vec(rng, n, dtype, scale=1.0):
+    import torch
+    t = torch.from_numpy(rng.standard_normal(n) * scale).to(_torch(dtype)).cuda()
+    return t, t.cpu().double().numpy()
+
+
+class _Out:
+    """An output inside a larger buffer, whose surroundings must stay as they are."""
+
+    def __init__(self, rows, cols, dtype, pad):
+        import torch
+        self.buf = torch.full((rows + 2, cols + pad), GUARD, dtype=_torch(dtype), device="cuda")
+        self.rows, self.cols = rows, cols
+        self.t = self.buf[1:rows + 1, :cols]
+
+    def value(self):
+        b = self.buf.cpu().double().numpy()
+        assert (b[0] == GUARD).all() and (b[-1] == GUARD).all() and (b[:, self.cols:] == GUARD).all()
+        return b[1:self.rows + 1, :self.cols]
+
+
+def _scratch(nbytes):
+    import torch
+    return torch.full((nbytes,), 0xFF, dtype=torch.uint8, device="cuda")  # NaN in every float type
+
+
+def _within(got, want, tol):
+    assert got.shape == want.shape
+    bad = ~(np.abs(got - want) <= tol)
+    assert not bad.any(), f"{bad.sum()} of {bad.size} off, worst by {np.max(np.abs(got - want)[bad] / tol[bad])} tolerances"
+
+
+# ---- embedding -------------------------------------------------------------------
+def _ids(rng, n, vocab, kind):
+    if kind == "one":
+        ids = np.full(n, vocab // 2)
+    elif kind == "skew":
+        ids = np.minimum((vocab + 1.0) ** rng.random(n) - 1.0, vocab - 1).astype(np.int64)
+    else:
+        ids = rng.integers(0, max(vocab, 1), n)
+    ids = ids.astype(np.int64)
+    if kind == "absent":
+        ids[rng.random(n) < 0.5] = -1
+    if kind == "outside":
+        ids[::3] = vocab
+        ids[1::3] = -(2 ** 31)
+    return ids
+
+
+EMBED = [(0, 4, 5), (1, 1, 1), (1, 32, 4096), (5, 7, 3), (127, 48, 10), (129, 3, 200), (1000, 33, 17),
+         (4097, 64, 100), (9001, 8, 5000), (20000, 130, 3), (33, 1023, 40), (300, 2100, 9), (3, 0, 5), (4, 6, 0)]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n,dim,vocab", EMBED)
+@pytest.mark.parametrize("kind,wide,pad", [("uniform", True, 0), ("absent", False, 3), ("one", True, 8),
+                                           ("outside", False, 0)])
+def test_embedding(n, dim, vocab, dtype, kind, wide, pad):
+    import torch
+    from paper_2608_17298_amd import gart
+    rng = np.random.default_rng(n + dim)
+    table, t64 = _mat(rng, vocab, dim, dtype, pad)
+    ids = _ids(rng, n, vocab, kind)
+    out = _Out(n, dim, dtype, pad)
+    gart.gart_embedding(table, torch.from_numpy(ids).to(torch.int64 if wide else torch.int32).cuda(), out.t, 0.3)
+    want = ref.embedding(t64, ids, float(np.float32(0.3)))
+    _within(out.value(), want, 1.01 * ref.U[dtype] * np.abs(want) + 2 * ref.U32 * np.abs(want) + ref.TINY[dtype])
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n,dim,vocab", EMBED)
+@pytest.mark.parametrize("kind,wide,pad", [("uniform", True, 0), ("absent", False, 3), ("one", True, 8),
+                                           ("skew", True, 0), ("outside", False, 0)])
+def test_embedding_backward(n, dim, vocab, dtype, kind, wide, pad):
+    import torch
+    from paper_2608_17298_amd import gart
+    rng = np.random.default_rng(7 * n + dim)
+    dl, d64 = _mat(rng, n, dim, dtype, pad)
+    ids = _ids(rng, n, vocab, kind)
+    tid = torch.from_numpy(ids).to(torch.int64 if wide else torch.int32).cuda()
+    scratch = _scratch(gart.gart_embedding_scratch_bytes(n, vocab, dim))
+    got = []
+    for _ in range(2):
+        g = _Out(vocab, dim, dtype, pad)
+        gart.gart_embedding_backward(tid, dl, g.t, 0.3, scratch)
+        got.append(g.value())
+    assert np.array_equal(got[0], got[1])  # deterministic
+    want, size = ref.embedding_grad(ids, d64, vocab, float(np.float32(0.3)))
+    _within(got[0], want, 1.01 * ref.U[dtype] * np.abs(want) + 1.2 * ref.U32 * size + ref.TINY[dtype])
+
+
+def test_embedding_backward_sum_of_many_small_terms():
+    """65536 equal 16-bit terms: a sum held in 16 bits would stop growing at 256 of them."""
+    import torch
+    from paper_2608_17298_amd import gart
+    n = 65536
+    dl = torch.ones((n, 5), dtype=torch.bfloat16, device="cuda")
+    ids = torch.zeros(n, dtype=torch.int32, device="cuda")
+    g = torch.empty((2, 5), dtype=torch.bfloat16, device="cuda")
+    gart.gart_embedding_backward(ids, dl, g, 1.0, _scratch(gart.gart_embedding_scratch_bytes(n, 2, 5)))
+    assert (g[0] == 65536.0).all() and (g[1] == 0.0).all()
+
+
+def test_embedding_repeated_row_gradient():
+    """A broadcast dl_dout (row stride 0): each row of the table gets it once per id."""
+    import torch
+    from paper_2608_17298_amd import gart
+    row = torch.tensor([[1.0, -2.0, 0.5]], device="cuda")
+    ids = torch.tensor([1, 1, 3, 1, 0], device="cuda")
+    g = torch.empty((5, 3), device="cuda")
+    gart.gart_embedding_backward(ids, row.expand(5, 3), g, 2.0, _scratch(gart.gart_embedding_scratch_bytes(5, 5, 3)))
+    count = torch.tensor([1.0, 3.0, 0.0, 1.0, 0.0], device="cuda")
+    assert torch.equal(g, 2.0 * count[:, None] * row)
+
+
+# ---- linear ------------------------------------------------------------------------
+LINEAR = [(1, 1, 1), (1, 64, 48), (1, 1000, 130), (2, 257, 33), (3, 7, 5), (16, 32, 64), (17, 33, 130), (40, 300, 20),
+          (64, 1, 64), (65, 96, 1), (128, 64, 128), (129, 65, 63), (200, 128, 256), (257, 200, 131), (500, 16, 3),
+          (1000, 32, 64), (2051, 64, 48), (700, 520, 130), (3000, 256, 256)]
+EMPTY = [(0, 4, 6), (5, 0, 7), (5, 4, 0), (0, 0, 3)]
+ACTS = ["none", "relu", "silu", "gelu"]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("m,k,n", LINEAR + EMPTY)
+@pytest.mark.parametrize("act,bias,residual,pad", [("none", False, False, 0), ("silu", True, True, 3),
+                                                   ("gelu", True, False, 8), ("relu", False, True, 0)])
+def test_linear(m, k, n, dtype, act, bias, residual, pad):
+    from paper_2608_17298_amd import gart
+    rng = np.random.default_rng(m + 10 * k + 100 * n)
+    x, x64 = _mat(rng, m, k, dtype, pad)
+    w, w64 = _mat(rng, n, k, dtype, pad, max(k, 1) ** -0.5)
+    b, b64 = _vec(rng, n, dtype) if bias else (None, None)
+    r, r64 = _mat(rng, m, n, dtype, pad) if residual else (None, None)
+    y = _Out(m, n, dtype, pad)
+    scratch = _scratch(gart.gart_linear_scratch_bytes(m, k, n, _torch(dtype)))
+    gart.gart_linear(x, w, y.t, b, r, act, scratch)
+    _within(y.value(), ref.linear(x64, w64, b64, r64, act), ref.linear_tolerance(x64, w64, b64, r64, act, dtype))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("m,k,n", LINEAR + EMPTY)
+@pytest.mark.parametrize("act,bias,pad", [("none", True, 0), ("silu", True, 3), ("gelu", False, 8), ("relu", True, 0)])
+def test_linear_backward(m, k, n, dtype, act, bias, pad):
+    from paper_2608_17298_amd import gart
+    rng = np.random.default_rng(3 * m + 10 * k + 100 * n)
+    x, x64 = _mat(rng, m, k, dtype, pad)
+    w, w64 = _mat(rng, n, k, dtype, pad, max(k, 1) ** -0.5)
+    b, b64 = _vec(rng, n, dtype) if bias else (None, None)
+    dl, d64 = _mat(rng, m, n, dtype, pad)
+    if act == "relu" and m * n:
+        # the slope jumps at 0: no upstream gradient where rounding could fall on the other side
+        z = x64 @ w64.T + (0.0 if b64 is None else b64)
+        a = np.abs(x64) @ np.abs(w64).T + (0.0 if b64 is None else np.abs(b64))
+        near = np.abs(z) <= 1.2 * ref.U32 * (k + 4) * a
+        import torch
+        dl[torch.from_numpy(near).cuda()] = 0.0
+        d64 = np.where(near, 0.0, d64)
+    scratch = _scratch(gart.gart_linear_backward_scratch_bytes(m, k, n, _torch(dtype), act))
+    got = []
+    for _ in range(2):
+        gx, gw, gb = _Out(m, k, dtype, pad), _Out(n, k, dtype, pad), _Out(1, n, dtype, 0)
+        gart.gart_linear_backward(x, w, dl, gx.t, gw.t, gb.t.reshape(-1), b, act, scratch)
+        got.append((gx.value(), gw.value(), gb.value()[0]))
+    want = ref.linear_grads(x64, w64, b64, d64, act)
+    tol = ref.linear_grads_tolerance(x64, w64, b64, d64, act, dtype)
+    for q in range(3):
+        assert np.array_equal(got[0][q], got[1][q])  # deterministic
+        _within(got[0][q], want[q], tol[q])
+
+
+@pytest.mark.parametrize("want_x,want_w,want_b", [(1, 0, 0), (0, 1, 0), (0, 0, 1), (1, 0, 1)])
+@pytest.mark.parametrize("act", ["none", "gelu"])
+def test_linear_backward_some_outputs(want_x, want_w, want_b, act):
+    """Gradients that are not asked for change nothing in the others."""
+    import torch
+    from paper_2608_17298_amd import gart
+    rng = np.random.default_rng(5)
+    m, k, n = 300, 40, 24
+    (x, _), (w, _), (dl, _) = _mat(rng, m, k, "f32"), _mat(rng, n, k, "f32"), _mat(rng, m, n, "f32")
+    scratch = _scratch(gart.gart_linear_backward_scratch_bytes(m, k, n, torch.float32, act))
+    full = [torch.empty_like(x), torch.empty_like(w), torch.empty(n, device="cuda")]
+    gart.gart_linear_backward(x, w, dl, *full, None, act, scratch)
+    some = [torch.empty_like(t) if f else None for t, f in zip(full, (want_x, want_w, want_b))]
+    gart.gart_linear_backward(x, w, dl, *some, None, act, scratch)
+    for a, b in zip(full, some):
+        assert b is None or torch.equal(a, b)
+
+
+@pytest.mark.parametrize("act", ["none", "silu", "gelu"])
+@pytest.mark.parametrize("m,k,n", [(37, 9, 14), (300, 40, 70)])
+def test_linear_backward_against_differences(m, k, n, act):
+    """d(sum dl y) along random directions of x, weight and bias, by central differences in 64 bits."""
+    import torch
+    from paper_2608_17298_amd import gart
+    rng = np.random.default_rng(11)
+    x, x64 = _mat(rng, m, k, "f32")
+    w, w64 = _mat(rng, n, k, "f32", scale=k ** -0.5)
+    b, b64 = _vec(rng, n, "f32")
+    dl, d64 = _mat(rng, m, n, "f32")
+    gx, gw, gb = torch.empty_like(x), torch.empty_like(w), torch.empty_like(b)
+    gart.gart_linear_backward(x, w, dl, gx, gw, gb, b, act,
+                              _scratch(gart.gart_linear_backward_scratch_bytes(m, k, n, torch.float32, act)))
+    tol = ref.linear_grads_tolerance(x64, w64, b64, d64, act, "f32")
+    base, h = [x64, w64, b64], 1e-5
+    for q, g in enumerate((gx, gw, gb)):
+        v = rng.standard_normal(base[q].shape)
+        loss = []
+        for sign in (1.0, -1.0):
+            p = list(base)
+            p[q] = p[q] + sign * h * v
+            loss.append((d64 * ref.linear(p[0], p[1], p[2], None, act)).sum())
+        got = (g.cpu().double().numpy() * v).sum()
+        slope = (loss[0] - loss[1]) / (2 * h)
+        # the differences' own error: h^2 / 6 times a third derivative (act''' <= 3), and 64-bit rounding over 2 h
+        move = np.abs(v @ w64.T) if q == 0 else np.abs(x64 @ v.T) if q == 1 else np.abs(v)[None, :]
+        own = 0.5 * h * h * (np.abs(d64) * move ** 3).sum() + 1e-15 * np.abs(d64).sum() * 10 / h
+        assert abs(got - slope) <= (tol[q] * np.abs(v)).sum() + own
+
+
+@pytest.mark.parametrize("act", ["relu", "silu", "gelu"])
+@pytest.mark.parametrize("rows", [1, 70])
+def test_linear_nonfinite_and_large(act, rows):
+    """Pre-activations at the edges of float: both limits are reached without a NaN, and a NaN stays one."""
+    import torch
+    from paper_2608_17298_amd import gart
+    z = np.array([-np.inf, -3e38, -1e5, -90.0, -87.5, 0.0, 87.5, 90.0, 1e5, 3e38, np.inf, np.nan], dtype=np.float32)
+    b = torch.from_numpy(z).cuda()
+    x, w = torch.zeros((rows, 8), device="cuda"), torch.ones((len(z), 8), device="cuda")
+    y = torch.empty((rows, len(z)), device="cuda")
+    gart.gart_linear(x, w, y, b, None, act, _scratch(gart.gart_linear_scratch_bytes(rows, 8, len(z))))
+    want = np.maximum(z, 0.0)
+    want[2:5] = y[0, 2:5].cpu().numpy() if act != "relu" else 0.0
+    got = y.cpu().numpy()
+    assert np.array_equal(got, np.broadcast_to(want, got.shape), equal_nan=True)
+    assert (np.abs(got[:, 1:5]) <= 1e-30).all()
+    dl = torch.ones_like(y)
+    gb = torch.empty_like(b)
+    gart.gart_linear_backward(x, w, dl, None, None, gb, b, act,
+                              _scratch(gart.gart_linear_backward_scratch_bytes(rows, 8, len(z), torch.float32, act)))
+    g = gb.cpu().numpy() / rows
+    assert (np.abs(g[:5]) <= 1e-30).all() and (g[6:11] == 1.0).all()
+    assert np.isnan(g[11]) or act == "relu"
+
+
+def test_linear_nan_stays_in_its_row_and_column():
+    """A NaN in one row of x (or one row of weight) reaches that row (column) of y alone."""
+    import torch
+    from paper_2608_17298_amd import gart
+    for dtype in TYPES:
+        for m, k, n in [(3, 70, 20), (300, 70, 100)]:
+            x = torch.ones((m, k), dtype=_torch(dtype), device="cuda")
+            w = torch.ones((n, k), dtype=_torch(dtype), device="cuda")
+            x[1, k - 1] = float("nan")
+            w[n - 1, 0] = float("inf")
+            y = torch.empty((m, n), dtype=_torch(dtype), device="cuda")
+            gart.gart_linear(x, w, y, scratch=_scratch(gart.gart_linear_scratch_bytes(m, k, n, _torch(dtype))))
+            y = y.float().cpu().numpy()
+            assert np.isnan(y[1]).all()
+            rest = np.delete(y, 1, axis=0)
+            assert np.isposinf(rest[:, n - 1]).all() and (rest[:, :n - 1] == k).all()
+
+
+def test_linear_repeated_rows_and_in_place_residual():
+    """x and the residual as one row repeated (stride 0), and y written over the residual."""
+    import torch
+    from paper_2608_17298_amd import gart
+    rng = np.random.default_rng(2)
+    x, x64 = _mat(rng, 1, 24, "f32")
+    w, w64 = _mat(rng, 10, 24, "f32")
+    r, r64 = _mat(rng, 1, 10, "f32")
+    y = torch.empty((50, 10), device="cuda")
+    s = _scratch(gart.gart_linear_scratch_bytes(50, 24, 10))
+    gart.gart_linear(x.expand(50, 24), w, y, None, r.expand(50, 10), "silu", s)
+    want = np.repeat(ref.linear(x64, w64, None, r64, "silu"), 50, 0)
+    tol = np.repeat(ref.linear_tolerance(x64, w64, None, r64, "silu", "f32"), 50, 0)
+    _within(y.cpu().double().numpy(), want, tol)
+    z = r.expand(50, 10).contiguous()
+    gart.gart_linear(x.expand(50, 24), w, z, None, z, "silu", s)
+    assert torch.equal(z, y)
+
+
+# ---- dropout -------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,cols", [(0, 5), (5, 0), (1, 1), (1, 7), (3, 8), (9, 17), (100, 48), (33, 65), (7, 2050)])
+@pytest.mark.parametrize("p,residual,pad", [(0.1, True, 0), (0.5, False, 3), (0.0, True, 8), (1.0, True, 0)])
+def test_dropout(rows, cols, dtype, p, residual, pad):
+    from paper_2608_17298_amd import gart
+    rng = np.random.default_rng(rows + cols)
+    seed, offset = 0xDEADBEEF12345678, 0x123456789A
+    x, x64 = _mat(rng, rows, cols, dtype, pad)
+    r, r64 = _mat(rng, rows, cols, dtype, 2 * pad) if residual else (None, None)
+    y = _Out(rows, cols, dtype, pad)
+    gart.gart_dropout(x, y.t, p, seed, offset, r)
+    want = ref.dropout(x64, r64, p, seed, offset)
+    got = y.value()
+    _within(got, want, ref.dropout_tolerance(x64, r64, p, dtype, want))
+    if not residual:
+        assert np.array_equal(got != 0, ref.keep(rows * cols, p, seed, offset).reshape(rows, cols))
+
+
+def test_dropout_in_place_and_gradient():
+    """y over x, y over the residual; the gradient of sum dl y is dl under the same mask."""
+    import torch
+    from paper_2608_17298_amd import gart
+    rng = np.random.default_rng(1)
+    x, _ = _mat(rng, 37, 50, "f32")
+    r, _ = _mat(rng, 37, 50, "f32")
+    y = torch.empty_like(x)
+    gart.gart_dropout(x, y, 0.3, 5, 6, r)
+    a, b = x.clone(), r.clone()
+    gart.gart_dropout(a, a, 0.3, 5, 6, r)
+    gart.gart_dropout(x, b, 0.3, 5, 6, b)
+    assert torch.equal(a, y) and torch.equal(b, y)
+    dl, d64 = _mat(rng, 37, 50, "f32")
+    g = torch.empty_like(dl)
+    gart.gart_dropout(dl, g, 0.3, 5, 6)
+    h, v = 1e-3, rng.standard_normal((37, 50))
+    x64 = x.cpu().double().numpy()
+    loss = [(d64 * ref.dropout(x64 + s * h * v, None, 0.3, 5, 6)).sum() for s in (1.0, -1.0)]
+    got = (g.cpu().double().numpy() * v).sum()
+    # linear in x: the difference is exact but for 64-bit rounding; g for its own few roundings
+    assert abs(got - (loss[0] - loss[1]) / (2 * h)) <= 8 * ref.U32 * np.abs(d64 * v).sum() / 0.7 + 1e-9
+
+
+def test_dropout_discards_what_it_drops():
+    """NaN and infinities in dropped places leave zeros (or the residual)."""
+    import torch
+    from paper_2608_17298_amd import gart
+    k = ref.keep(200, 0.5, 9, 1).reshape(10, 20)
+    x = torch.full((10, 20), float("nan"), device="cuda")
+    x[torch.from_numpy(k).cuda()] = 2.0
+    y = torch.empty_like(x)
+    gart.gart_dropout(x, y, 0.5, 9, 1)
+    assert np.array_equal(y.cpu().numpy(), np.where(k, 4.0, 0.0).astype(np.float32))
+
+
+def test_dropout_rate_and_counters():
+    """Kept share within five standard deviations; another offset or seed is another mask; a long row's far elements
+    come from their own counters."""
+    import torch
+    from paper_2608_17298_amd import gart
+    n = 1 << 22
+    x = torch.ones((1, n), device="cuda")
+    y, z = torch.empty_like(x), torch.empty_like(x)
+    gart.gart_dropout(x, y, 0.1, 3, 0)
+    kept = int((y != 0).sum())
+    p = 6554 / 65536
+    assert abs(kept - n * (1 - p)) <= 5 * (n * p * (1 - p)) ** 0.5
+    for seed, offset in [(3, 1), (4, 0), (3, 1 << 32), (3 + (1 << 32), 0)]:
+        gart.gart_dropout(x, z, 0.1, seed, offset)
+        same = int(((y != 0) == (z != 0)).sum())
+        q = p * p + (1 - p) * (1 - p)
+        assert abs(same - n * q) <= 5 * (n * q * (1 - q)) ** 0.5
+    gart.gart_dropout(x, y, 0.1, 3, 0)
+    assert np.array_equal(y[0, -100:].cpu().numpy() != 0, ref.keep(100, 0.1, 3, 0, n - 100))
+
+
+# ---- all of them ---------------------------------------------------------------------
+def test_offsets_beyond_32_bits():
+    """Rows 2^22 elements apart, 1040 of them: element offsets pass 2^32.  The last rows are compared."""
+    import torch
+    from paper_2608_17298_amd import gart
+    rows, step, cols = 1040, 1 << 22, 24
+    rng = np.random.default_rng(3)
+    free, _ = torch.cuda.mem_get_info()
+    if free < 20 << 30:
+        pytest.skip("needs 18 GB of device memory")
+    far = [torch.empty((rows - 1) * step + cols, dtype=torch.bfloat16, device="cuda").as_strided((rows, cols), (step, 1))
+           for _ in range(2)]
+    x, _ = _mat(rng, rows, cols, "bf16")
+    w, _ = _mat(rng, cols, cols, "bf16")
+    far[0].copy_(x)
+    near, s = torch.empty_like(x), _scratch(gart.gart_linear_scratch_bytes(rows, cols, cols, torch.bfloat16))
+    print("[offsets] linear", flush=True)
+    gart.gart_linear(x, w, near, act="silu", scratch=s)
+    gart.gart_linear(far[0], w, far[1], act="silu", scratch=s)
+    assert torch.equal(far[1], near)
+    print("[offsets] linear_backward", flush=True)
+    s = _scratch(gart.gart_linear_backward_scratch_bytes(rows, cols, cols, torch.bfloat16, "silu"))
+    g = [[torch.empty_like(w), torch.empty(cols, dtype=torch.bfloat16, device="cuda")] for _ in range(2)]
+    gart.gart_linear_backward(x, w, near, x.new_empty(x.shape), *g[0], None, "silu", s)
+    gart.gart_linear_backward(far[0], w, far[1], None, *g[1], None, "silu", s)
+    assert torch.equal(g[0][0], g[1][0]) and torch.equal(g[0][1], g[1][1])
+    print("[offsets] dropout", flush=True)
+    gart.gart_dropout(x, near, 0.2, 1, 2)
+    gart.gart_dropout(far[0], far[1], 0.2, 1, 2)
+    assert torch.equal(far[1], near)
+    print("[offsets] embedding", flush=True)
+    ids = torch.randint(0, rows, (3000,), device="cuda")
+    out = [torch.empty((3000, cols), dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    gart.gart_embedding(x, ids, out[0])
+    gart.gart_embedding(far[0], ids, out[1])
+    assert torch.equal(out[0], out[1])
+    print("[offsets] embedding_backward", flush=True)
+    s = _scratch(gart.gart_embedding_scratch_bytes(rows, rows, cols))
+    gart.gart_embedding_backward(ids[:rows], x, near, 1.0, s)
+    gart.gart_embedding_backward(ids[:rows], far[0], far[1], 1.0, s)
+    assert torch.equal(far[1], near)
+
+
+def _calls(m=600, k=40, n=72, dtype="bf16"):
+    """One call of every operator, as functions of no argument, and the tensors they write."""
+    import torch
+    from paper_2608_17298_amd import gart
+    rng = np.random.default_rng(4)
+    t = _torch(dtype)
+    x, w, b = _mat(rng, m, k, dtype)[0], _mat(rng, n, k, dtype)[0], _vec(rng, n, dtype)[0]
+    dl = _mat(rng, m, n, dtype)[0]
+    ids = torch.randint(0, n, (m,), device="cuda")
+    y, d, e = torch.empty_like(dl), torch.empty_like(dl), torch.empty((m, k), dtype=t, device="cuda")
+    gx, gw, gb, gt = torch.empty_like(x), torch.empty_like(w), torch.empty_like(b), torch.empty_like(w)
+    s = [_scratch(v) for v in (gart.gart_linear_scratch_bytes(m, k, n, t),
+                               gart.gart_linear_backward_scratch_bytes(m, k, n, t, "gelu"),
+                               gart.gart_embedding_scratch_bytes(m, n, k))]
+
+    def run(stream=None):
+        gart.gart_embedding(w, ids, e, 0.5, stream=stream)
+        gart.gart_linear(e, w, y, b, dl, "gelu", s[0], stream=stream)
+        gart.gart_dropout(y, d, 0.25, 8, 1, y, stream=stream)
+        gart.gart_linear_backward(x, w, d, gx, gw, gb, b, "gelu", s[1], stream=stream)
+        gart.gart_embedding_backward(ids, gx, gt, 0.5, s[2], stream=stream)
+
+    return run, [e, y, d, gx, gw, gb, gt]
+
+
+def test_another_stream():
+    import torch
+    run, outs = _calls()
+    run()
+    want = [t.clone() for t in outs]
+    for t in outs:
+        t.zero_()
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    run(side)
+    side.synchronize()
+    for a, b in zip(outs, want):
+        assert torch.equal(a, b)
+
+
+def test_graph_replays():
+    """Captured once and replayed four times with other work between; every replay gives the eager result."""
+    import torch
+    run, outs = _calls()
+    run()
+    torch.cuda.synchronize()
+    want = [t.clone() for t in outs]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        run()
+    for _ in range(4):
+        for t in outs:
+            t.fill_(7.0)
+        other = torch.randn((512, 512), device="cuda")
+        (other * 2.0).sum().item()
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(outs, want):
+            assert torch.equal(a, b)
+
+
+def test_refusals_on_tensors():
+    """Tensors of the wrong kind are refused before the library is called, and nothing is written."""
+    import torch
+    from paper_2608_17298_amd import gart
+    x, w = torch.ones((4, 8), device="cuda"), torch.ones((6, 8), device="cuda")
+    y = torch.full((4, 6), 5.0, device="cuda")
+    bad = [lambda: gart.gart_linear(x.cpu(), w, y), lambda: gart.gart_linear(x, w.half(), y),
+           lambda: gart.gart_linear(x, w, y.t().contiguous().t()), lambda: gart.gart_linear(x, w, y, y[0, :5]),
+           lambda: gart.gart_linear(x, w, y, act="tanh"), lambda: gart.gart_linear(x.double(), w, y),
+           lambda: gart.gart_dropout(x, y[:, :4], 0.5, -1), lambda: gart.gart_dropout(x[0], x[0], 0.5, 1),
+           lambda: gart.gart_embedding(w, torch.zeros(3, device="cuda", dtype=torch.int64), x),
+           lambda: gart.gart_embedding(w, torch.zeros(4, device="cuda"), x)]
+    for f in bad:
+        with pytest.raises(ValueError):
+            f()
+    worse = [lambda: gart.gart_linear(x, w, y[:, :5]), lambda: gart.gart_linear(x, w[:, :7], y),
+             lambda: gart.gart_linear(x, w, x[:, :6]), lambda: gart.gart_dropout(x, x.clone(), 1.5, 1),
+             lambda: gart.gart_dropout(x[1:], x[:3], 0.5, 1),
+             lambda: gart.gart_linear_backward(x, w, y, x), lambda: gart.gart_linear(x, w, y[:1].expand(4, 6)),
+             lambda: gart.gart_embedding_backward(torch.zeros(4, device="cuda", dtype=torch.int32), x, w)]
+    for f in worse:
+        with pytest.raises(gart.GartError):
+            f()
+    torch.cuda.synchronize()
+    assert (y == 5.0).all() and (x == 1.0).all() and (w == 1.0).all()
