@@ -10,15 +10,23 @@ The paper trains with the 3DGS recipe (Adam over L1 plus SSIM for 30K
 iterations); here the loss is the L1 sum alone, whose gradient sign(C - C*)
 is the upstream gradient used throughout, and each parameter group has its
 own Adam learning rate (3DGS-style defaults below).
+
+With an appearance model (appearance.Appearance) the step renders the SH
+coefficients that the model gives for the view, and its weights and the
+view's codes are updated along with the scene.
 """
 from __future__ import annotations
+
+import dataclasses
 
 import torch
 
 from . import gart
+from .appearance import WEIGHTS
 
 # Per-group Adam learning rates (3DGS-style defaults; SH bands share one rate).
 DEFAULT_LR = dict(means=1.6e-4, log_scales=5e-3, quats=1e-3, logits=5e-2, sh=2.5e-3)
+APPEARANCE_LR = 1e-3  # weights and codes of an appearance model
 GROUPS = ("means", "log_scales", "quats", "logits", "sh")
 _PARAM_ATTR = dict(means="means", log_scales="log_scales", quats="quats", logits="opacity_logits", sh="sh")
 
@@ -27,7 +35,7 @@ class Trainer:
     """Adam on the Gaussians of `scene` over a set of views with target images."""
 
     def __init__(self, scene, cameras, targets, tile=None, mode="gather", lr=None, betas=(0.9, 0.999),
-                 eps=1e-15, stream=None):
+                 eps=1e-15, stream=None, appearance=None, appearance_lr=APPEARANCE_LR):
         if len(cameras) != len(targets) or not cameras:
             raise ValueError("one target image per camera")
         self.g = gart.Gaussians.from_scene(scene)
@@ -50,9 +58,27 @@ class Trainer:
         self.m = {k: torch.zeros_like(self.param(k)) for k in GROUPS}
         self.v = {k: torch.zeros_like(self.param(k)) for k in GROUPS}
         self.t = 0
+        self.appearance = appearance
+        if appearance is not None:
+            if appearance.codes.shape[0] != self.g.n or appearance.table.shape[0] < len(cameras):
+                raise ValueError("the appearance model is not of this scene's Gaussians and views")
+            self.appearance_adam = gart.gart_adam(appearance_lr, betas[0], betas[1], eps)
+            # moments of the weights, and of each view's codes, which step only when the view is used
+            self.am, self.av = ({k: torch.zeros_like(appearance.params[k]) for k in WEIGHTS} for _ in range(2))
+            self.tm, self.tv = torch.zeros_like(appearance.table), torch.zeros_like(appearance.table)
+            self.view_t = [0] * len(cameras)
 
     def param(self, k):
         return getattr(self.g, _PARAM_ATTR[k])
+
+    def _appearance_step(self, view):
+        """Gradients of the appearance model from that of the SH coefficients, and its Adam steps."""
+        a, h, s = self.appearance, self.appearance_adam, self.stream
+        a.backward(self.grads["sh"], self.t, stream=s)
+        for k in WEIGHTS:
+            gart.gart_adam_step(a.params[k], a.grads[k], self.am[k], self.av[k], h, self.t, stream=s)
+        self.view_t[view] += 1
+        gart.gart_adam_step(a.table[view], a.g_table, self.tm[view], self.tv[view], h, self.view_t[view], stream=s)
 
     def step(self, view: int, events=None):
         """One iteration on view `view`; returns the device fp64 loss.  With
@@ -64,15 +90,20 @@ class Trainer:
                 events[k].record(torch.cuda.current_stream() if s is None else s)
 
         mark(0)
-        self.frame = gart.prepare(self.g, cam, self.settings, self.frame, stream=s)
+        g = self.g
+        if self.appearance is not None:  # the step's number is t + 1, there and in the gradient
+            g = dataclasses.replace(g, sh=self.appearance.forward(view, g.sh, self.t + 1, stream=s))
+        self.frame = gart.prepare(g, cam, self.settings, self.frame, stream=s)
         mark(1)
-        gart.gart_forward(self.g, cam, self.settings, self.frame, self.image, stream=s)
+        gart.gart_forward(g, cam, self.settings, self.frame, self.image, stream=s)
         mark(2)
         gart.gart_l1_loss_grad(self.image, self.targets[view], self.dl, self.loss, self.partial, stream=s)
         mark(3)
-        gart.gart_backward(self.g, cam, self.settings, self.frame, self.dl, self.grads, stream=s)
+        gart.gart_backward(g, cam, self.settings, self.frame, self.dl, self.grads, stream=s)
         mark(4)
         self.t += 1
+        if self.appearance is not None:
+            self._appearance_step(view)
         for k in GROUPS:
             gart.gart_adam_step(self.param(k), self.grads[k], self.m[k], self.v[k], self.adam[k], self.t, stream=s)
         mark(5)
