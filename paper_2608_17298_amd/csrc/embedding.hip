@@ -6,7 +6,7 @@
 // Gradient: g[v] = scale * sum of the rows whose id is v.  The ids are sorted
 // (stable, with their positions), so equal ids stand side by side and a row's
 // sum needs no atomics: the order of its terms is their position, whatever the
-// schedule.  The sorted positions are cut into units of kUnit, which balances
+// schedule.  The sorted positions are cut into units of equal length, which balances
 // the work whatever the ids' distribution; a run of equal ids inside one unit
 // is summed and written there, a run that crosses units leaves one partial sum
 // a unit and is joined afterwards, in order.
@@ -20,7 +20,9 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kRowsPerThread = 4;
-constexpr int kUnit = 128;  // sorted positions per unit
+constexpr int kBatch = 8;            // rows in flight per thread of the gradient
+constexpr int kMinUnit = 8, kMaxUnit = 64;
+constexpr int64_t kUnitThreads = 131072;
 
 // ---- lookup ------------------------------------------------------------------
 // packs: 16-byte packs per row; lanes: threads per row (packs, at most 256);
@@ -89,18 +91,22 @@ __global__ __launch_bounds__(kThreads) void zero_rows_kernel(T* __restrict__ out
 
 // Partial sums: partial[2 u] is the part in unit u of a run that began before
 // u, partial[2 u + 1] the part in u of a run that begins in u and goes on.
+//
+// A thread owns 16 bytes of the rows of one unit.  kBatch rows are asked for
+// before any of them is added, whatever their keys: one row at a time left
+// the kernel waiting for memory (141 us at 1M rows of 64 bf16).
 template <typename T>
 __global__ __launch_bounds__(kThreads) void unit_sums_kernel(const EmbeddingArgs a, const uint32_t* __restrict__ keys,
                                                              const uint32_t* __restrict__ pos,
-                                                             float* __restrict__ partial, int packs, int lanes,
-                                                             int upb) {
+                                                             float* __restrict__ partial, int unit_rows, int packs,
+                                                             int lanes, int upb) {
   const T* __restrict__ rows = static_cast<const T*>(a.rows);
   T* __restrict__ out = static_cast<T*>(a.out);
   constexpr int V = Pack<T>::N;
   const int sub = threadIdx.x / lanes, lane = threadIdx.x - sub * lanes;
   if (sub >= upb) return;
   const int64_t unit = int64_t(blockIdx.x) * upb + sub;
-  const int64_t p0 = unit * kUnit, p1 = min(a.n, p0 + kUnit);
+  const int64_t p0 = unit * unit_rows, p1 = min(a.n, p0 + unit_rows);
   if (p0 >= a.n) return;
   const uint32_t none = uint32_t(a.vocab);
   const uint32_t before = p0 > 0 ? keys[p0 - 1] : none;
@@ -116,7 +122,13 @@ __global__ __launch_bounds__(kThreads) void unit_sums_kernel(const EmbeddingArgs
       const bool begun = first && cur == before, goes_on = last && cur == after;
       if (begun || goes_on) {
         float* q = partial + (2 * unit + (begun ? 0 : 1)) * a.dim + c;
-        for (int e = 0; e < count; ++e) q[e] = acc[e];
+#pragma unroll
+        for (int h = 0; h < V / 4; ++h) {
+          Pack<float> f;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) f.v[e] = acc[4 * h + e];
+          if (count > 4 * h) store_some(q + 4 * h, f, count - 4 * h);
+        }
       } else {
         Pack<T> v;
 #pragma unroll
@@ -124,40 +136,141 @@ __global__ __launch_bounds__(kThreads) void unit_sums_kernel(const EmbeddingArgs
         store_some(out + int64_t(cur) * a.out_ld + c, v, count);
       }
     };
-    for (int64_t i = p0; i < p1; ++i) {
-      const uint32_t k = keys[i];
-      if (k != cur) {
-        flush(false);
-        first = false;
-        cur = k;
+    for (int64_t i = p0; i < p1; i += kBatch) {
+      uint32_t k[kBatch];
+      Pack<T> v[kBatch];
 #pragma unroll
-        for (int e = 0; e < V; ++e) acc[e] = 0.0f;
+      for (int u = 0; u < kBatch; ++u) {
+        k[u] = i + u < p1 ? keys[i + u] : none;
+        v[u].v = T(0.0f);
+        if (k[u] != none) v[u] = load_some(rows + int64_t(pos[i + u]) * a.rows_ld + c, count);
       }
-      if (k == none) break;
-      const Pack<T> v = load_some(rows + int64_t(pos[i]) * a.rows_ld + c, count);
 #pragma unroll
-      for (int e = 0; e < V; ++e) acc[e] += float(v.v[e]);
+      for (int u = 0; u < kBatch; ++u) {
+        if (i + u < p1 && k[u] != cur) {
+          flush(false);
+          first = false;
+          cur = k[u];
+#pragma unroll
+          for (int e = 0; e < V; ++e) acc[e] = 0.0f;
+        }
+#pragma unroll
+        for (int e = 0; e < V; ++e) acc[e] += float(v[u].v[e]);
+      }
     }
     flush(true);
   }
 }
 
-// One block per unit whose last run begins there and goes on: adds up the
-// run's partial sums.
-template <typename T>
-__global__ __launch_bounds__(kThreads) void join_kernel(const EmbeddingArgs a, const uint32_t* __restrict__ keys,
-                                                        const float* __restrict__ partial) {
-  T* __restrict__ out = static_cast<T*>(a.out);
-  const int64_t unit = blockIdx.x, p0 = unit * kUnit, p1 = p0 + kUnit;
-  if (p1 >= a.n) return;
-  const uint32_t cur = keys[p1 - 1];
-  if (cur != keys[p1] || cur == uint32_t(a.vocab)) return;      // nothing goes on
-  if (p0 > 0 && keys[p0] == cur && keys[p0 - 1] == cur) return;  // began before
-  for (int64_t c = threadIdx.x; c < a.dim; c += kThreads) {
-    float acc = partial[(2 * unit + 1) * a.dim + c];
-    for (int64_t u = unit + 1; u * kUnit < a.n && keys[u * kUnit] == cur; ++u) acc += partial[2 * u * a.dim + c];
-    out[int64_t(cur) * a.out_ld + c] = T(acc * a.scale);
+// Joins the runs that cross units: unit u's last run begins there and goes on
+// if the key at its end equals the next unit's first, and that many further
+// units hold a part of it.  A wave takes one unit; a run over more than 64
+// units is left to the block's 16 waves together.  Lanes are spread over the
+// columns (four a lane) and, where those are few, over the run's units; the
+// shares are added in a fixed order.
+constexpr int kJoinThreads = 1024;
+constexpr int kJoinWaves = kJoinThreads / 64;
+
+// Sum of partial rows head(unit + 1 .. unit + more) and of unit's tail, by
+// `threads` threads of which this is `t`; column groups of 4, from c0 on.
+__device__ __forceinline__ float4 run_share(const float* __restrict__ partial, int64_t dim, int64_t unit, int64_t more,
+                                            int64_t c, int first, int step) {
+  float s[4] = {};
+  const int count = int(min(int64_t(4), dim - c));
+  for (int64_t u = first; u <= more; u += step) {
+    const Pack<float> q = load_some(partial + (u == 0 ? 2 * unit + 1 : 2 * (unit + u)) * dim + c, count);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) s[e] += q.v[e];
   }
+  return make_float4(s[0], s[1], s[2], s[3]);
+}
+
+template <typename T>
+__global__ __launch_bounds__(kJoinThreads) void join_kernel(const EmbeddingArgs a, const uint32_t* __restrict__ keys,
+                                                            const float* __restrict__ partial, int unit_rows,
+                                                            int64_t units) {
+  __shared__ uint32_t s_long[kJoinWaves];
+  __shared__ float4 s_sum[kJoinThreads];
+  T* __restrict__ out = static_cast<T*>(a.out);
+  const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
+  const int64_t base = int64_t(blockIdx.x) * kJoinWaves, unit = base + wave;
+  const int64_t p0 = unit * unit_rows, p1 = p0 + unit_rows;
+  const uint32_t none = uint32_t(a.vocab);
+  bool mine = unit < units && p1 < a.n;
+  uint32_t cur = none;
+  if (mine) {
+    cur = keys[p1 - 1];
+    mine = cur != none && cur == keys[p1] && !(p0 > 0 && keys[p0] == cur && keys[p0 - 1] == cur);
+  }
+  int more = 0;  // further units with a part of the run
+  if (mine) {
+    const int64_t q = p1 + int64_t(lane) * unit_rows;
+    const uint64_t same = __ballot(q < a.n && keys[q] == cur);
+    more = same == ~0ull ? 64 : __builtin_ctzll(~same);
+  }
+  if (lane == 0) s_long[wave] = more == 64 ? cur : none;
+  auto store = [&](uint32_t key, int64_t c, float4 s) {
+    const float v[4] = {s.x, s.y, s.z, s.w};
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (c + e < a.dim) out[int64_t(key) * a.out_ld + c + e] = T(v[e] * a.scale);
+  };
+  const int64_t quads = (a.dim + 3) / 4;
+  int w = 1;  // lanes over columns: a power of two, so that shares meet by shuffles
+  while (w < 64 && w < quads) w *= 2;
+  if (more > 0 && more < 64) {
+    for (int64_t c = int64_t(lane % w) * 4; c < quads * 4; c += 4 * w) {
+      float4 s = run_share(partial, a.dim, unit, more, c, lane / w, 64 / w);
+      for (int off = w; off < 64; off *= 2) {  // every lane of the wave that has this column is here
+        s.x += __shfl_xor(s.x, off);
+        s.y += __shfl_xor(s.y, off);
+        s.z += __shfl_xor(s.z, off);
+        s.w += __shfl_xor(s.w, off);
+      }
+      if (lane < w) store(cur, c, s);
+    }
+  }
+  __syncthreads();
+  for (int l = 0; l < kJoinWaves; ++l) {
+    const uint32_t key = s_long[l];
+    if (key == none) continue;  // the same for the block
+    const int64_t begin = base + l;
+    int64_t parts = 0;
+    for (;;) {
+      const int64_t q = (begin + 1 + parts + tid) * unit_rows;
+      const int here = __syncthreads_count(q < a.n && keys[q] == key);
+      parts += here;
+      if (here < kJoinThreads) break;
+    }
+    const int groups = kJoinThreads / w;
+    for (int64_t c0 = 0; c0 < quads * 4; c0 += 4 * w) {
+      const int64_t c = c0 + int64_t(tid % w) * 4;
+      s_sum[tid] = c < a.dim ? run_share(partial, a.dim, begin, parts, c, tid / w, groups) : make_float4(0, 0, 0, 0);
+      __syncthreads();
+      for (int g = groups / 2; g > 0; g /= 2) {
+        if (tid < g * w) {
+          float4 x = s_sum[tid];
+          const float4 y = s_sum[tid + g * w];
+          x.x += y.x;
+          x.y += y.y;
+          x.z += y.z;
+          x.w += y.w;
+          s_sum[tid] = x;
+        }
+        __syncthreads();
+      }
+      if (tid < w && c < a.dim) store(key, c, s_sum[tid]);
+      __syncthreads();
+    }
+  }
+}
+
+// Sorted positions per unit: enough threads (one per 16 bytes of a unit's
+// rows) to fill the card, units long enough that few runs cross them.
+int unit_rows_for(int64_t n, int64_t dim) {
+  int r = kMinUnit;
+  while (r < kMaxUnit && n * ceil_div64(dim, 8) / r > kUnitThreads) r *= 2;
+  return r;
 }
 
 int bits_for(int64_t v) {  // bits of the largest key v
@@ -183,7 +296,7 @@ GradLayout grad_layout(int64_t n, int64_t dim) {
   L.keys_alt = take(size_t(n) * 4);
   L.pos_alt = take(size_t(n) * 4);
   L.radix = take(radix_tmp_bytes(n));
-  L.partial = take(size_t(ceil_div64(n, kUnit)) * 2 * size_t(dim) * 4);
+  L.partial = take(size_t(ceil_div64(n, unit_rows_for(n, dim))) * 2 * size_t(dim) * 4);
   L.total = off;
   return L;
 }
@@ -221,10 +334,13 @@ hipError_t gradient(const EmbeddingArgs& a, hipStream_t s) {
   e = radix_sort_u32(keys, pos, words(L.keys_alt), words(L.pos_alt), a.n, bits_for(a.vocab), base + L.radix, s);
   if (e != hipSuccess) return e;
   float* partial = reinterpret_cast<float*>(base + L.partial);
-  const int64_t units = ceil_div64(a.n, kUnit);
-  unit_sums_kernel<T><<<uint32_t(ceil_div64(units, upb)), kThreads, 0, s>>>(a, keys, pos, partial, packs, lanes, upb);
+  const int unit_rows = unit_rows_for(a.n, a.dim);
+  const int64_t units = ceil_div64(a.n, unit_rows);
+  unit_sums_kernel<T><<<uint32_t(ceil_div64(units, upb)), kThreads, 0, s>>>(a, keys, pos, partial, unit_rows, packs,
+                                                                           lanes, upb);
   if ((e = hipGetLastError()) != hipSuccess) return e;
-  if (units > 1) join_kernel<T><<<uint32_t(units - 1), kThreads, 0, s>>>(a, keys, partial);
+  if (units > 1)
+    join_kernel<T><<<uint32_t(ceil_div64(units, kJoinWaves)), kJoinThreads, 0, s>>>(a, keys, partial, unit_rows, units);
   return hipGetLastError();
 }
 
