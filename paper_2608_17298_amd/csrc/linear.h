@@ -1,0 +1,163 @@
+// Device code shared by the linear layer's kernels: matrix instructions,
+// activations, fragments in LDS; and the launchers' sub-plans.
+#pragma once
+
+#include "blocks.h"
+
+namespace gart {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+template <typename T>
+struct Mfma;
+
+// 16 bits: 16x16x32, eight consecutive k a lane.
+template <>
+struct Mfma<bf16> {
+  static __device__ __forceinline__ f32x4 run(Pack<bf16>::V a, Pack<bf16>::V b, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+  }
+};
+template <>
+struct Mfma<f16> {
+  static __device__ __forceinline__ f32x4 run(Pack<f16>::V a, Pack<f16>::V b, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
+  }
+};
+// float: four 16x16x4, one k a lane each.  Which k a lane holds is free as
+// long as both operands agree, so it holds four consecutive ones, as one read.
+template <>
+struct Mfma<float> {
+  static __device__ __forceinline__ f32x4 run(Pack<float>::V a, Pack<float>::V b, f32x4 c) {
+#pragma unroll
+    for (int t = 0; t < 4; ++t) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[t], b[t], c, 0, 0, 0);
+    return c;
+  }
+};
+
+// ---- activations -----------------------------------------------------------
+// silu(z) = z g(z) and gelu(z) = z g(2 sqrt(2/pi) (z + 0.044715 z^3)) with the
+// logistic function g(u) = 1 / (1 + exp(-u)).  Beyond |u| = 87 g is 0 or 1 in
+// float and g' is 0.
+constexpr float kGelu = 1.5957691216057308f;  // 2 sqrt(2 / pi)
+
+struct Gate {
+  float g, slope;  // g(u), g'(u)
+};
+
+__device__ __forceinline__ Gate gate(float u) {
+  // exp(-u) = 2^h 2^l: h the rounded product, l what it lost and the low part
+  // of log2(e), so that float results keep their last bits for large |u|
+  const float c = fminf(fmaxf(-u, -87.0f), 87.0f);
+  const float h = c * 1.44269504f;
+  const float l = fmaf(c, 1.44269504f, -h) + c * 1.92596299e-8f;
+  float e = __builtin_amdgcn_exp2f(h);
+  e = fmaf(e, l * 0.693147181f, e);
+  Gate r;
+  r.g = __builtin_amdgcn_rcpf(1.0f + e);
+  r.slope = e * r.g * r.g;
+  if (u < -87.0f) r.g = 0.0f;
+  if (fabsf(u) > 87.0f) r.slope = 0.0f;
+  return r;
+}
+
+__device__ __forceinline__ float gate_argument(float z, gart_activation act) {
+  return act == GART_ACT_GELU ? kGelu * fmaf(0.044715f * z * z, z, z) : z;
+}
+
+// 16-bit results: one exponential of the plain product. z is held above the
+// point where the result is 0 in 32 bits, which keeps -infinity from meeting a
+// gate of 0; minimum and maximum let a NaN through.
+template <typename T>
+constexpr bool kShort = sizeof(T) == 2;
+
+__device__ __forceinline__ float edge_of(gart_activation act) { return act == GART_ACT_GELU ? 10.0f : 87.0f; }
+
+__device__ __forceinline__ float quick_gate(float z, gart_activation act) {
+  constexpr float kLog2e = 1.44269504f;
+  const float h = act == GART_ACT_GELU ? z * fmaf(z * z, -kGelu * 0.044715f * kLog2e, -kGelu * kLog2e) : z * -kLog2e;
+  return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(h));
+}
+
+template <typename T>
+__device__ __forceinline__ float activate(float z, gart_activation act) {
+  if (act == GART_ACT_NONE) return z;
+  if (act == GART_ACT_RELU) return z < 0.0f ? 0.0f : z;  // a NaN stays
+  if constexpr (kShort<T>) {
+    const float c = __builtin_elementwise_maximum(z, -edge_of(act));
+    return c * quick_gate(c, act);
+  }
+  const float g = gate(gate_argument(z, act)).g;
+  return g == 0.0f ? 0.0f : z * g;  // not inf * 0 at -infinity
+}
+
+// dl times act'(z)
+template <typename T>
+__device__ __forceinline__ float activate_grad(float z, float dl, gart_activation act) {
+  if (act == GART_ACT_NONE) return dl;
+  if (act == GART_ACT_RELU) return z <= 0.0f ? 0.0f : dl;
+  if constexpr (kShort<T>) {
+    const float c = __builtin_elementwise_minimum(__builtin_elementwise_maximum(z, -edge_of(act)), edge_of(act));
+    const float g = quick_gate(c, act);
+    const float s = act == GART_ACT_GELU ? c * fmaf(3.0f * 0.044715f * kGelu * c, c, kGelu) : c;
+    return dl * fmaf(s * g, 1.0f - g, g);
+  }
+  const Gate t = gate(gate_argument(z, act));
+  const float du = act == GART_ACT_GELU ? kGelu * fmaf(0.134145f * z, z, 1.0f) : 1.0f;
+  return dl * (t.slope == 0.0f && z == z ? t.g : fmaf(z * t.slope, du, t.g));
+}
+
+// ---- fragments ---------------------------------------------------------------
+// A 16-bit fragment holds eight consecutive k of a row, lanes r = lane % 16
+// over the rows and g = lane / 16 over the k (8 g ..); a float one four (4 g ..).
+template <typename T>
+constexpr int kDepth = sizeof(T) == 2 ? 32 : 16;  // k per fragment
+
+// Rows of a fragment of the products' first operand, which become a lane's
+// output columns.  16 bits: tiles 2q and 2q+1 together hold 32 columns, eight
+// consecutive ones a lane.  float: a lane's four are 16 bytes already.
+template <typename T>
+__device__ __forceinline__ int paired_row(int tile, int r) {
+  return sizeof(T) == 2 ? 32 * (tile / 2) + 8 * (r / 4) + 4 * (tile % 2) + r % 4 : 16 * tile + r;
+}
+
+// From LDS rows along k.
+template <typename T>
+__device__ __forceinline__ typename Pack<T>::V fragment_of_row(const T* lds, int pitch, int row, int k0, int g) {
+  return *reinterpret_cast<const typename Pack<T>::V*>(lds + row * pitch + k0 + Pack<T>::N * g);
+}
+
+// From LDS lines across k (line k holds the rows' elements side by side).  16
+// bits: the lanes of a group of 16 name four k times 16 columns, four a lane,
+// and the transposing load gives each the four k of its column.
+template <typename T, bool PAIRED>
+__device__ __forceinline__ typename Pack<T>::V fragment_of_columns(const T* lds, int pitch, int tile, int k0, int lane) {
+  const int r = lane % 16, g = lane / 16;
+  typename Pack<T>::V v;
+  if constexpr (sizeof(T) == 4) {
+    const T* q = lds + (k0 + 4 * g) * pitch + 16 * tile + r;
+#pragma unroll
+    for (int t = 0; t < 4; ++t) v[t] = q[t * pitch];
+  } else {
+    typedef short s16x4 __attribute__((ext_vector_type(4)));
+    typedef __attribute__((address_space(3))) s16x4* lds_ptr;
+    const int col = PAIRED ? paired_row<T>(tile, 4 * (r % 4)) : 16 * tile + 4 * (r % 4);
+    const T* q = lds + (k0 + 8 * g + r / 4) * pitch + col;
+    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(q));
+    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(q + 4 * pitch));
+    __builtin_memcpy(&v, &lo, 8);
+    __builtin_memcpy(reinterpret_cast<char*>(&v) + 8, &hi, 8);
+  }
+  return v;
+}
+
+// ---- linear_stream.hip ---------------------------------------------------------
+// Layers whose weight fits LDS: the rows stream past it once.
+bool stream_forward_fits(int64_t k, int64_t n, gart_dtype t);
+hipError_t launch_stream_forward(const LinearArgs& a, gart_dtype t, hipStream_t s);
+// Parts whose partial sums launch_stream_backward leaves: partial [parts, n, k]
+// and sums [parts, n] (0: the layer does not fit).
+int64_t stream_backward_parts(int64_t m, int64_t k, int64_t n, gart_dtype t);
+hipError_t launch_stream_backward(const LinearArgs& a, float* partial, float* sums, gart_dtype t, hipStream_t s);
+
+}  // namespace gart

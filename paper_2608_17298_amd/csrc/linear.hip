@@ -9,85 +9,10 @@
 // and 16-bit fragments of it are read with the transposing LDS load.
 #include <algorithm>
 
-#include "blocks.h"
+#include "linear.h"
 
 namespace gart {
 namespace {
-
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-
-template <typename T>
-struct Mfma;
-
-// 16 bits: 16x16x32, eight consecutive k a lane.
-template <>
-struct Mfma<bf16> {
-  static __device__ __forceinline__ f32x4 run(Pack<bf16>::V a, Pack<bf16>::V b, f32x4 c) {
-    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
-  }
-};
-template <>
-struct Mfma<f16> {
-  static __device__ __forceinline__ f32x4 run(Pack<f16>::V a, Pack<f16>::V b, f32x4 c) {
-    return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
-  }
-};
-// float: four 16x16x4, one k a lane each.  Which k a lane holds is free as
-// long as both operands agree, so it holds four consecutive ones, as one read.
-template <>
-struct Mfma<float> {
-  static __device__ __forceinline__ f32x4 run(Pack<float>::V a, Pack<float>::V b, f32x4 c) {
-#pragma unroll
-    for (int t = 0; t < 4; ++t) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[t], b[t], c, 0, 0, 0);
-    return c;
-  }
-};
-
-// ---- activations -----------------------------------------------------------
-// silu(z) = z g(z) and gelu(z) = z g(2 sqrt(2/pi) (z + 0.044715 z^3)) with the
-// logistic function g(u) = 1 / (1 + exp(-u)).  Beyond |u| = 87 g is 0 or 1 in
-// float and g' is 0.
-constexpr float kGelu = 1.5957691216057308f;  // 2 sqrt(2 / pi)
-
-struct Gate {
-  float g, slope;  // g(u), g'(u)
-};
-
-__device__ __forceinline__ Gate gate(float u) {
-  // exp(-u) = 2^h 2^l: h the rounded product, l what it lost and the low part
-  // of log2(e), so that float results keep their last bits for large |u|
-  const float c = fminf(fmaxf(-u, -87.0f), 87.0f);
-  const float h = c * 1.44269504f;
-  const float l = fmaf(c, 1.44269504f, -h) + c * 1.92596299e-8f;
-  float e = __builtin_amdgcn_exp2f(h);
-  e = fmaf(e, l * 0.693147181f, e);
-  Gate r;
-  r.g = __builtin_amdgcn_rcpf(1.0f + e);
-  r.slope = e * r.g * r.g;
-  if (u < -87.0f) r.g = 0.0f;
-  if (fabsf(u) > 87.0f) r.slope = 0.0f;
-  return r;
-}
-
-__device__ __forceinline__ float gate_argument(float z, gart_activation act) {
-  return act == GART_ACT_GELU ? kGelu * fmaf(0.044715f * z * z, z, z) : z;
-}
-
-__device__ __forceinline__ float activate(float z, gart_activation act) {
-  if (act == GART_ACT_NONE) return z;
-  if (act == GART_ACT_RELU) return z < 0.0f ? 0.0f : z;  // a NaN stays
-  const float g = gate(gate_argument(z, act)).g;
-  return g == 0.0f ? 0.0f : z * g;  // not inf * 0 at -infinity
-}
-
-// dl times act'(z)
-__device__ __forceinline__ float activate_grad(float z, float dl, gart_activation act) {
-  if (act == GART_ACT_NONE) return dl;
-  if (act == GART_ACT_RELU) return z <= 0.0f ? 0.0f : dl;
-  const Gate t = gate(gate_argument(z, act));
-  const float du = act == GART_ACT_GELU ? kGelu * fmaf(0.134145f * z, z, 1.0f) : 1.0f;
-  return dl * (t.slope == 0.0f && z == z ? t.g : fmaf(z * t.slope, du, t.g));
-}
 
 // ---- tiles -------------------------------------------------------------------
 constexpr int kLine = 128;  // bytes of k per step
@@ -107,12 +32,6 @@ struct Tile {
   static constexpr int PACKS = LINES * LINE_PACKS;
   static constexpr int PER_THREAD = (PACKS + THREADS - 1) / THREADS;
 
-  // 16 bits: tiles 2q and 2q+1 together hold 32 j, eight consecutive ones a
-  // lane.  float: a lane's four consecutive j are 16 bytes already.
-  static __device__ __forceinline__ int frag_row(int tile, int r) {
-    if (PERM && sizeof(T) == 2) return 32 * (tile / 2) + 8 * (r / 4) + 4 * (tile % 2) + r % 4;
-    return 16 * tile + r;
-  }
   // exchange of a row's 16-byte pieces: distinct for any eight lanes that read together
   static __device__ __forceinline__ int swizzle(int row) {
     return PERM && sizeof(T) == 2 ? (row & 3) | ((row >> 1) & 4) : row & 7;
@@ -145,30 +64,13 @@ struct Tile {
       *reinterpret_cast<typename Pack<T>::V*>(lds + line * PITCH + piece * V) = reg[u].v;
     }
   }
-  // fragment of 16 rows at tile `tile`, k step `s` (32 k of 16 bits, 16 of floats)
+  // fragment of 16 rows at tile `tile`, step `s` of the line's two
   static __device__ __forceinline__ typename Pack<T>::V fragment(const T* lds, int tile, int s, int lane) {
-    const int r = lane % 16, g = lane / 16;
     if constexpr (KC) {
-      const int row = frag_row(tile, r);
-      return *reinterpret_cast<const typename Pack<T>::V*>(lds + row * PITCH + ((4 * s + g) ^ swizzle(row)) * V);
-    } else if constexpr (sizeof(T) == 4) {
-      const T* q = lds + (16 * s + 4 * g) * PITCH + frag_row(tile, r);
-      typename Pack<T>::V v;
-#pragma unroll
-      for (int t = 0; t < 4; ++t) v[t] = q[t * PITCH];
-      return v;
+      const int r = lane % 16, g = lane / 16, row = PERM ? paired_row<T>(tile, r) : 16 * tile + r;
+      return fragment_of_row(lds, PITCH, row, 0, (4 * s + g) ^ swizzle(row));
     } else {
-      // the lanes of a group of 16 name four k times 16 columns, four a lane;
-      // each receives the four k of its column
-      typedef short s16x4 __attribute__((ext_vector_type(4)));
-      typedef __attribute__((address_space(3))) s16x4* lds_ptr;
-      const T* q = lds + (32 * s + 8 * g + r / 4) * PITCH + frag_row(tile, 4 * (r % 4));
-      const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(q));
-      const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(q + 4 * PITCH));
-      typename Pack<T>::V v;
-      __builtin_memcpy(&v, &lo, 8);
-      __builtin_memcpy(reinterpret_cast<char*>(&v) + 8, &hi, 8);
-      return v;
+      return fragment_of_columns<T, PERM>(lds, PITCH, tile, kDepth<T> * s, lane);
     }
   }
 };
@@ -289,14 +191,14 @@ __global__ __launch_bounds__(64 * WI * WJ) void gemm_kernel(const GemmArgs g) {
       } else {
         if constexpr (EPI == EPI_FORWARD) {
 #pragma unroll
-          for (int e = 0; e < V; ++e) c[e] = activate(c[e], g.act);
+          for (int e = 0; e < V; ++e) c[e] = activate<T>(c[e], g.act);
         }
         if (EPI == EPI_DZ || (EPI == EPI_FORWARD && g.extra)) {
           const Pack<T> p = load_some(static_cast<const T*>(g.extra) + row * g.extra_ld + j, count);
 #pragma unroll
           for (int e = 0; e < V; ++e) {
             if constexpr (EPI == EPI_DZ) {
-              c[e] = e < count ? activate_grad(c[e], float(p.v[e]), g.act) : 0.0f;
+              c[e] = e < count ? activate_grad<T>(c[e], float(p.v[e]), g.act) : 0.0f;
               sum[e] += c[e];
             } else {
               c[e] += float(p.v[e]);
@@ -346,16 +248,33 @@ __global__ __launch_bounds__(256) void column_sums_kernel(const T* __restrict__ 
   if (w == 0 && j < n) sums[int64_t(blockIdx.x) * n + j] = (s[0][lane] + s[1][lane]) + (s[2][lane] + s[3][lane]);
 }
 
-// out[i, j] = sum over parts of partial[part, i, j], in order of the parts
+// out[i, j] = sum over parts of partial[part, i, j].  A block takes 64
+// neighbouring elements; its 16 waves take every 16th part each and their sums
+// are added in order.
+constexpr int kJoinWaves = 16;
 template <typename T>
-__global__ __launch_bounds__(256) void join_parts_kernel(const float* __restrict__ partial, int64_t parts,
-                                                         int64_t rows, int64_t cols, T* __restrict__ out,
-                                                         int64_t out_ld) {
+__global__ __launch_bounds__(64 * kJoinWaves) void join_parts_kernel(const float* __restrict__ partial, int64_t parts,
+                                                                     int64_t rows, int64_t cols, T* __restrict__ out,
+                                                                     int64_t out_ld) {
+  __shared__ float s[kJoinWaves][64];
+  const int lane = threadIdx.x % 64, w = threadIdx.x / 64;
   const int64_t total = rows * cols;
-  for (int64_t e = int64_t(blockIdx.x) * 256 + threadIdx.x; e < total; e += int64_t(gridDim.x) * 256) {
+  for (int64_t b = int64_t(blockIdx.x) * 64; b < total; b += int64_t(gridDim.x) * 64) {
+    const int64_t e = b + lane;
     float t = 0.0f;
-    for (int64_t p = 0; p < parts; ++p) t += partial[p * total + e];
-    out[e / cols * out_ld + e % cols] = T(t);
+    if (e < total) {
+#pragma unroll 4
+      for (int64_t p = w; p < parts; p += kJoinWaves) t += partial[p * total + e];
+    }
+    s[w][lane] = t;
+    __syncthreads();
+    if (w == 0 && e < total) {
+      float sum = s[0][lane];
+#pragma unroll
+      for (int v = 1; v < kJoinWaves; ++v) sum += s[v][lane];
+      out[e / cols * out_ld + e % cols] = T(sum);
+    }
+    __syncthreads();
   }
 }
 
@@ -363,8 +282,8 @@ template <typename T>
 hipError_t join_parts(const float* partial, int64_t parts, int64_t rows, int64_t cols, void* out, int64_t ld,
                       hipStream_t s) {
   if (rows * cols <= 0) return hipSuccess;
-  const int64_t blocks = std::min<int64_t>(ceil_div64(rows * cols, 256), 1 << 16);
-  join_parts_kernel<T><<<uint32_t(blocks), 256, 0, s>>>(partial, parts, rows, cols, static_cast<T*>(out), ld);
+  const int64_t blocks = std::min<int64_t>(ceil_div64(rows * cols, 64), 1 << 16);
+  join_parts_kernel<T><<<uint32_t(blocks), 64 * kJoinWaves, 0, s>>>(partial, parts, rows, cols, static_cast<T*>(out), ld);
   return hipGetLastError();
 }
 
@@ -384,18 +303,28 @@ hipError_t gemm(GemmArgs g, hipStream_t s) {
 
 // ---- gradient ----------------------------------------------------------------
 struct BackwardPlan {
+  bool stream;
   int64_t dz_ld, part, parts, sum_parts;
   size_t dz, partial, sums, total;
 };
 
-BackwardPlan backward_plan(int64_t m, int64_t k, int64_t n, size_t es, gart_activation act) {
+BackwardPlan backward_plan(int64_t m, int64_t k, int64_t n, gart_dtype t, gart_activation act) {
   BackwardPlan p{};
+  const size_t es = dtype_bytes(t);
   size_t off = 0;
   auto take = [&](size_t bytes) {
     const size_t o = off;
     off += (bytes + 255) & ~size_t(255);
     return o;
   };
+  p.parts = p.sum_parts = stream_backward_parts(m, k, n, t);
+  if (p.parts > 0) {
+    p.stream = true;
+    p.partial = take(size_t(p.parts) * size_t(n) * size_t(k) * 4);
+    p.sums = take(size_t(p.parts) * size_t(n) * 4);
+    p.total = off;
+    return p;
+  }
   p.dz_ld = (n + 7) / 8 * 8;
   p.dz = take(act == GART_ACT_NONE ? 0 : size_t(m) * size_t(p.dz_ld) * es);
   // the weight's gradient sums over the rows: enough parts to fill the card
@@ -411,7 +340,8 @@ BackwardPlan backward_plan(int64_t m, int64_t k, int64_t n, size_t es, gart_acti
 }
 
 template <typename T>
-hipError_t forward(const LinearArgs& a, hipStream_t s) {
+hipError_t forward(const LinearArgs& a, gart_dtype t, hipStream_t s) {
+  if (stream_forward_fits(a.k, a.n, t)) return launch_stream_forward(a, t, s);
   GemmArgs g{};
   g.a = a.x;
   g.a_ld = a.x_ld;
@@ -430,13 +360,19 @@ hipError_t forward(const LinearArgs& a, hipStream_t s) {
 }
 
 template <typename T>
-hipError_t backward(const LinearArgs& a, hipStream_t s) {
-  const BackwardPlan p = backward_plan(a.m, a.k, a.n, sizeof(T), a.act);
+hipError_t backward(const LinearArgs& a, gart_dtype t, hipStream_t s) {
+  const BackwardPlan p = backward_plan(a.m, a.k, a.n, t, a.act);
   char* base = static_cast<char*>(a.scratch);
   const void* dz = a.dl;
   int64_t dz_ld = a.dl_ld;
   float* sums = reinterpret_cast<float*>(base + p.sums);
+  float* partial = reinterpret_cast<float*>(base + p.partial);
   hipError_t e;
+  if (p.stream) {
+    if ((e = launch_stream_backward(a, partial, sums, t, s)) != hipSuccess) return e;
+    if (a.g_w && (e = join_parts<T>(partial, p.parts, a.n, a.k, a.g_w, a.g_w_ld, s)) != hipSuccess) return e;
+    return a.g_bias ? join_parts<T>(sums, p.parts, 1, a.n, a.g_bias, a.n, s) : hipSuccess;
+  }
   if (a.act != GART_ACT_NONE) {
     GemmArgs g{};
     g.a = a.x;
@@ -486,10 +422,10 @@ hipError_t backward(const LinearArgs& a, hipStream_t s) {
     g.cols = a.k;
     g.depth = a.m;
     g.part = p.part;
-    g.out = base + p.partial;
+    g.out = partial;
     g.out_ld = a.k;
     if (a.m > 0 && (e = gemm<T, false, false, EPI_PARTIAL>(g, s)) != hipSuccess) return e;
-    return join_parts<T>(reinterpret_cast<float*>(base + p.partial), p.parts, a.n, a.k, a.g_w, a.g_w_ld, s);
+    return join_parts<T>(partial, p.parts, a.n, a.k, a.g_w, a.g_w_ld, s);
   }
   return hipSuccess;
 }
@@ -503,19 +439,19 @@ int64_t linear_scratch_bytes(int64_t m, int64_t, int64_t n, gart_dtype) {
 int64_t linear_backward_scratch_bytes(int64_t m, int64_t k, int64_t n, gart_dtype t, gart_activation act) {
   const int64_t mt = ceil_div64(m, kTile), nt = ceil_div64(n, kTile), kt = ceil_div64(k, kTile);
   if (mt * nt > kMaxTiles || mt * kt > kMaxTiles || nt * kt > kMaxTiles) return -1;
-  return int64_t(backward_plan(m, k, n, dtype_bytes(t), act).total);
+  return int64_t(backward_plan(m, k, n, t, act).total);
 }
 
 hipError_t launch_linear(const LinearArgs& a, gart_dtype t, hipStream_t s) {
-  if (t == GART_DTYPE_F32) return forward<float>(a, s);
-  if (t == GART_DTYPE_BF16) return forward<bf16>(a, s);
-  return forward<f16>(a, s);
+  if (t == GART_DTYPE_F32) return forward<float>(a, t, s);
+  if (t == GART_DTYPE_BF16) return forward<bf16>(a, t, s);
+  return forward<f16>(a, t, s);
 }
 
 hipError_t launch_linear_backward(const LinearArgs& a, gart_dtype t, hipStream_t s) {
-  if (t == GART_DTYPE_F32) return backward<float>(a, s);
-  if (t == GART_DTYPE_BF16) return backward<bf16>(a, s);
-  return backward<f16>(a, s);
+  if (t == GART_DTYPE_F32) return backward<float>(a, t, s);
+  if (t == GART_DTYPE_BF16) return backward<bf16>(a, t, s);
+  return backward<f16>(a, t, s);
 }
 
 }  // namespace gart

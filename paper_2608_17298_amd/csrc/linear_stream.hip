@@ -1,0 +1,433 @@
+// The linear layer where its weight fits LDS (a few hundred inputs and
+// outputs) and the rows are many: every row is read once and its results are
+// written once.
+//
+// Forward: a wave takes 32 rows.  x comes from memory straight into fragments
+// (a lane holds 16 consecutive bytes of a row), W stands in LDS, and the
+// outputs leave from registers, 16 bytes a lane.  Waves do not wait for each
+// other.
+//
+// Backward: a block takes a tile of rows at a time.  Each wave owns 32 outputs
+// (n): it computes z = W x^T for them again, dz = dl act'(z) in registers, and
+// puts dz into LDS, where the other two products meet it:
+//   g_weight (its 32 n, all k) += dz^T x over the tile's rows, kept in
+//   registers for all of the block's tiles;
+//   g_x (rows, k) = dz W, stored.
+// Each block leaves one partial sum of g_weight and g_bias.
+#include <algorithm>
+
+#include "linear.h"
+
+namespace gart {
+namespace {
+
+// ---- forward -----------------------------------------------------------------
+constexpr int kForwardWaves = 4;
+constexpr int kForwardBytes = 64 * 1024;  // of the weight in LDS
+constexpr int kForwardBlocks = 2048;
+
+// KP: inputs, rounded up.  LDS rows are 16 bytes longer, which spreads the
+// rows that lanes read together over the banks.
+template <typename T, int KP>
+__global__ __launch_bounds__(64 * kForwardWaves) void stream_forward_kernel(const LinearArgs a) {
+  constexpr int V = Pack<T>::N, S = KP / kDepth<T>, PITCH = KP + V, THREADS = 64 * kForwardWaves;
+  extern __shared__ __attribute__((aligned(16))) char lds_raw[];
+  T* w = reinterpret_cast<T*>(lds_raw);
+  const int tid = threadIdx.x, lane = tid % 64, r = lane % 16, g = lane / 16;
+  const int n_pad = int((a.n + 31) / 32 * 32);
+  for (int c = tid; c < n_pad * (KP / V); c += THREADS) {
+    const int row = c / (KP / V), at = c % (KP / V) * V;
+    Pack<T> p;
+    p.v = T(0.0f);
+    if (row < a.n && at < a.k) p = load_some(static_cast<const T*>(a.w) + row * a.w_ld + at, int(min(int64_t(V), a.k - at)));
+    *reinterpret_cast<typename Pack<T>::V*>(w + row * PITCH + at) = p.v;
+  }
+  __syncthreads();
+  const T* x = static_cast<const T*>(a.x);
+  const T* bias = static_cast<const T*>(a.bias);
+  const T* res = static_cast<const T*>(a.residual);
+  const int64_t tiles = (a.m + 31) / 32;
+  for (int64_t t = int64_t(blockIdx.x) * kForwardWaves + tid / 64; t < tiles; t += int64_t(gridDim.x) * kForwardWaves) {
+    typename Pack<T>::V fx[2][S];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int64_t row = t * 32 + 16 * i + r;
+#pragma unroll
+      for (int s = 0; s < S; ++s) {
+        const int64_t k = s * kDepth<T> + V * g;
+        fx[i][s] = T(0.0f);
+        if (row < a.m && k < a.k) fx[i][s] = load_some(x + row * a.x_ld + k, int(min(int64_t(V), a.k - k))).v;
+      }
+    }
+    for (int n0 = 0; n0 < n_pad; n0 += 32) {
+      f32x4 acc[2][2] = {};
+#pragma unroll
+      for (int s = 0; s < S; ++s) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const auto fw = fragment_of_row(w, PITCH, n0 + paired_row<T>(j, r), s * kDepth<T>, g);
+#pragma unroll
+          for (int i = 0; i < 2; ++i) acc[i][j] = Mfma<T>::run(fw, fx[i][s], acc[i][j]);
+        }
+      }
+      constexpr int Q = 8 / V;  // packs per lane: one of 8, or one of 4 from each tile
+#pragma unroll
+      for (int q = 0; q < Q; ++q) {
+        const int64_t n = n0 + (Q == 1 ? 8 * g : 16 * q + 4 * g);
+        const int count = int(min(int64_t(V), a.n - n));
+        if (count <= 0) continue;
+        float b[V] = {};
+        if (bias) {
+          const Pack<T> p = load_some(bias + n, count);
+#pragma unroll
+          for (int e = 0; e < V; ++e) b[e] = float(p.v[e]);
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const int64_t row = t * 32 + 16 * i + r;
+          if (row >= a.m) continue;
+          Pack<T> o, p;
+          if (res) p = load_some(res + row * a.residual_ld + n, count);
+#pragma unroll
+          for (int e = 0; e < V; ++e) {
+            float c = activate<T>(acc[i][Q == 1 ? e / 4 : q][e % 4] + b[e], a.act);
+            if (res) c += float(p.v[e]);
+            o.v[e] = T(c);
+          }
+          store_some(static_cast<T*>(a.y) + row * a.y_ld + n, o, count);
+        }
+      }
+    }
+  }
+}
+
+// ---- backward ------------------------------------------------------------------
+// NS: waves side by side over the outputs, 32 each.  With few of them, RG
+// groups of NS waves take rows of their own in a tile.
+template <typename T, int KP, int NS>
+struct BackwardShape {
+  static constexpr int RG = NS == 1 ? 4 : NS == 2 ? 2 : 1;
+  static constexpr int WAVES = NS * RG, THREADS = 64 * WAVES;
+  static constexpr int GROUP_ROWS = NS >= 4 ? 64 : 32, ROWS = GROUP_ROWS * RG;
+  static constexpr int NP = 32 * NS;
+  static constexpr int PAD = sizeof(T) == 2 ? 16 : 4;  // spreads rows (and columns' lines) over the banks
+  static constexpr int KPITCH = KP + PAD, NPITCH = NP + PAD;
+  static constexpr int W = NP * KPITCH, X = ROWS * KPITCH, Z = ROWS * NPITCH;
+  static constexpr size_t BYTES = size_t(W + X + Z) * sizeof(T);
+  static constexpr bool FITS = BYTES <= 160 * 1024 && KP * int(sizeof(T)) <= 512;
+};
+
+template <typename T, int KP, int NS>
+__global__ __launch_bounds__((BackwardShape<T, KP, NS>::THREADS)) void stream_backward_kernel(
+    const LinearArgs a, float* __restrict__ partial, float* __restrict__ sums, int64_t tiles) {
+  using B = BackwardShape<T, KP, NS>;
+  constexpr int V = Pack<T>::N, D = kDepth<T>, S = KP / D, KT = KP / 16, Q = 8 / V;
+  constexpr int MT = B::GROUP_ROWS / 16;
+  __shared__ __attribute__((aligned(16))) T lds[B::W + B::X + B::Z];
+  T *lw = lds, *lx = lds + B::W, *lz = lx + B::X;
+  const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64, r = lane % 16, g = lane / 16;
+  const int slice = wave % NS, group = wave / NS;
+  const T* x = static_cast<const T*>(a.x);
+  const T* dl = static_cast<const T*>(a.dl);
+
+  for (int c = tid; c < B::NP * (KP / V); c += B::THREADS) {
+    const int row = c / (KP / V), at = c % (KP / V) * V;
+    Pack<T> p;
+    p.v = T(0.0f);
+    if (row < a.n && at < a.k) p = load_some(static_cast<const T*>(a.w) + row * a.w_ld + at, int(min(int64_t(V), a.k - at)));
+    *reinterpret_cast<typename Pack<T>::V*>(lw + row * B::KPITCH + at) = p.v;
+  }
+
+  // a lane's outputs: n0(q) + 0 .. V-1
+  auto n0 = [&](int q) { return 32 * slice + (Q == 1 ? 8 * g : 16 * q + 4 * g); };
+  float b[8] = {}, sum_b[8] = {};
+  if (a.bias) {
+#pragma unroll
+    for (int q = 0; q < Q; ++q) {
+      if (n0(q) >= a.n) continue;
+      const Pack<T> p = load_some(static_cast<const T*>(a.bias) + n0(q), int(min(int64_t(V), a.n - n0(q))));
+#pragma unroll
+      for (int e = 0; e < V; ++e) b[q * V + e] = float(p.v[e]);
+    }
+  }
+  f32x4 acc_w[2][KT];
+#pragma unroll
+  for (int j = 0; j < 2; ++j)
+#pragma unroll
+    for (int k = 0; k < KT; ++k) acc_w[j][k] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+
+  constexpr int XALL = B::ROWS * (KP / V), XP = (XALL + B::THREADS - 1) / B::THREADS;  // x packs, per thread
+  constexpr bool XEVEN = XALL % B::THREADS == 0;
+  Pack<T> xr[XP], dr[MT][Q];
+  auto load_x = [&](int64_t t) {
+#pragma unroll
+    for (int u = 0; u < XP; ++u) {
+      const int c = u * B::THREADS + tid;
+      const int64_t row = t * B::ROWS + c / (KP / V);
+      const int at = c % (KP / V) * V;
+      xr[u].v = T(0.0f);
+      if ((XEVEN || c < XALL) && t < tiles && row < a.m && at < a.k)
+        xr[u] = load_some(x + row * a.x_ld + at, int(min(int64_t(V), a.k - at)));
+    }
+  };
+  auto load_dl = [&](int64_t t) {
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+      const int64_t row = t * B::ROWS + group * B::GROUP_ROWS + 16 * i + r;
+#pragma unroll
+      for (int q = 0; q < Q; ++q) {
+        dr[i][q].v = T(0.0f);
+        if (t < tiles && row < a.m && n0(q) < a.n)
+          dr[i][q] = load_some(dl + row * a.dl_ld + n0(q), int(min(int64_t(V), a.n - n0(q))));
+      }
+    }
+  };
+  load_x(blockIdx.x);
+  load_dl(blockIdx.x);
+  __syncthreads();  // W is there
+  typename Pack<T>::V fw[2][S];
+#pragma unroll
+  for (int j = 0; j < 2; ++j)
+#pragma unroll
+    for (int s = 0; s < S; ++s) fw[j][s] = fragment_of_row(lw, B::KPITCH, 32 * slice + paired_row<T>(j, r), s * D, g);
+
+  for (int64_t t = blockIdx.x; t < tiles; t += gridDim.x) {
+#pragma unroll
+    for (int u = 0; u < XP; ++u) {
+      const int c = u * B::THREADS + tid;
+      if (!XEVEN && c >= XALL) continue;
+      *reinterpret_cast<typename Pack<T>::V*>(lx + c / (KP / V) * B::KPITCH + c % (KP / V) * V) = xr[u].v;
+    }
+    __syncthreads();  // x is there; g_x of the last tile has read dz
+    load_x(t + gridDim.x);
+    // dz of this wave's rows and outputs
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+      const int lrow = group * B::GROUP_ROWS + 16 * i + r;
+      f32x4 z[2] = {};
+      if (a.act != GART_ACT_NONE) {
+#pragma unroll
+        for (int s = 0; s < S; ++s) {
+          const auto fx = fragment_of_row(lx, B::KPITCH, lrow, s * D, g);
+#pragma unroll
+          for (int j = 0; j < 2; ++j) z[j] = Mfma<T>::run(fw[j][s], fx, z[j]);
+        }
+      }
+      const bool real = t * B::ROWS + lrow < a.m;
+#pragma unroll
+      for (int q = 0; q < Q; ++q) {
+        Pack<T> o;
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          const float d = activate_grad<T>(z[Q == 1 ? e / 4 : q][e % 4] + b[q * V + e], float(dr[i][q].v[e]), a.act);
+          const float kept = real ? d : 0.0f;  // a row that is not there has a slope all the same
+          sum_b[q * V + e] += kept;
+          o.v[e] = T(kept);
+        }
+        *reinterpret_cast<typename Pack<T>::V*>(lz + lrow * B::NPITCH + n0(q)) = o.v;
+      }
+    }
+    load_dl(t + gridDim.x);
+    __syncthreads();  // dz is there
+    if (a.g_w) {
+#pragma unroll
+      for (int s = 0; s < B::GROUP_ROWS / D; ++s) {
+        const int k0 = group * B::GROUP_ROWS + s * D;
+        typename Pack<T>::V fz[2];
+#pragma unroll
+        for (int j = 0; j < 2; ++j) fz[j] = fragment_of_columns<T, false>(lz, B::NPITCH, 2 * slice + j, k0, lane);
+#pragma unroll
+        for (int k = 0; k < KT; ++k) {
+          const auto fx = fragment_of_columns<T, true>(lx, B::KPITCH, k, k0, lane);
+#pragma unroll
+          for (int j = 0; j < 2; ++j) acc_w[j][k] = Mfma<T>::run(fx, fz[j], acc_w[j][k]);
+        }
+      }
+    }
+    if (a.g_x) {
+      // 32 rows times 32 inputs at a time
+      for (int u = wave; u < B::ROWS / 32 * (KP / 32); u += B::WAVES) {
+        const int r0 = u / (KP / 32) * 32, kt = u % (KP / 32) * 2;
+        f32x4 acc[2][2] = {};
+#pragma unroll
+        for (int n = 0; n < B::NP; n += D) {
+          typename Pack<T>::V fz[2];
+#pragma unroll
+          for (int i = 0; i < 2; ++i) fz[i] = fragment_of_row(lz, B::NPITCH, r0 + 16 * i + r, n, g);
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            const auto fk = fragment_of_columns<T, true>(lw, B::KPITCH, kt + j, n, lane);
+#pragma unroll
+            for (int i = 0; i < 2; ++i) acc[i][j] = Mfma<T>::run(fk, fz[i], acc[i][j]);
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const int64_t row = t * B::ROWS + r0 + 16 * i + r;
+#pragma unroll
+          for (int q = 0; q < Q; ++q) {
+            const int64_t k = 16 * kt + (Q == 1 ? 8 * g : 16 * q + 4 * g);
+            if (row >= a.m || k >= a.k) continue;
+            Pack<T> o;
+#pragma unroll
+            for (int e = 0; e < V; ++e) o.v[e] = T(acc[i][Q == 1 ? e / 4 : q][e % 4]);
+            store_some(static_cast<T*>(a.g_x) + row * a.g_x_ld + k, o, int(min(int64_t(V), a.k - k)));
+          }
+        }
+      }
+    }
+    __syncthreads();  // x may be replaced
+  }
+
+  const int64_t part = int64_t(blockIdx.x) * B::RG + group;
+  if (a.g_w) {
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const int64_t n = 32 * slice + 16 * j + r;
+      if (n >= a.n) continue;
+      float* out = partial + (part * a.n + n) * a.k;
+#pragma unroll
+      for (int kt = 0; kt < KT; ++kt) {
+        const int64_t k = paired_row<T>(kt, 4 * g);
+        Pack<float> p;
+        p.v = acc_w[j][kt];
+        if (k < a.k) store_some(out + k, p, int(min(int64_t(4), a.k - k)));
+      }
+    }
+  }
+  if (a.g_bias) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+#pragma unroll
+      for (int off = 1; off < 16; off <<= 1) sum_b[e] += __shfl_xor(sum_b[e], off);
+      const int n = n0(e / V) + e % V;
+      if (r == 0 && n < a.n) sums[part * a.n + n] = sum_b[e];
+    }
+  }
+}
+
+// ---- launches --------------------------------------------------------------------
+int round_inputs(int64_t k) {
+  int p = 32;
+  while (p < k && p < 512) p *= 2;
+  return p;
+}
+
+int forward_lds(int kp, int64_t n, size_t es) { return int((n + 31) / 32 * 32 * (kp + 16 / int(es)) * int64_t(es)); }
+
+template <typename T, int KP>
+hipError_t forward_kp(const LinearArgs& a, hipStream_t s) {
+  const int64_t blocks = std::min<int64_t>(ceil_div64(ceil_div64(a.m, 32), kForwardWaves), kForwardBlocks);
+  stream_forward_kernel<T, KP><<<uint32_t(blocks), 64 * kForwardWaves, forward_lds(KP, a.n, sizeof(T)), s>>>(a);
+  return hipGetLastError();
+}
+
+template <typename T>
+hipError_t forward(const LinearArgs& a, hipStream_t s) {
+  switch (round_inputs(a.k)) {
+    case 32: return forward_kp<T, 32>(a, s);
+    case 64: return forward_kp<T, 64>(a, s);
+    case 128: return forward_kp<T, 128>(a, s);
+    default:
+      if constexpr (sizeof(T) == 2) return forward_kp<T, 256>(a, s);
+      return hipErrorInvalidValue;
+  }
+}
+
+// Blocks: about two of four waves for each of the 256 CUs; their partial sums
+// are then far fewer than the rows.
+constexpr int64_t kBackwardBlocks = 512;
+
+struct BackwardChoice {
+  int kp, ns, rows, groups;  // kp 0: none
+};
+
+template <typename T, int KP, int NS>
+bool offer(int64_t k, int64_t n, BackwardChoice* c) {
+  using B = BackwardShape<T, KP, NS>;
+  if constexpr (B::FITS) {
+    if (k <= KP && n <= 32 * NS) {
+      *c = BackwardChoice{KP, NS, B::ROWS, B::RG};
+      return true;
+    }
+  }
+  return false;
+}
+
+template <typename T, int KP>
+bool offer_ns(int64_t k, int64_t n, BackwardChoice* c) {
+  return offer<T, KP, 1>(k, n, c) || offer<T, KP, 2>(k, n, c) || offer<T, KP, 4>(k, n, c) || offer<T, KP, 8>(k, n, c);
+}
+
+template <typename T>
+BackwardChoice choose(int64_t k, int64_t n) {
+  BackwardChoice c{};
+  if (!(offer_ns<T, 32>(k, n, &c) || offer_ns<T, 64>(k, n, &c) || offer_ns<T, 128>(k, n, &c)))
+    offer_ns<T, 256>(k, n, &c);
+  return c;
+}
+
+BackwardChoice choose(int64_t k, int64_t n, gart_dtype t) {
+  return t == GART_DTYPE_F32 ? choose<float>(k, n) : choose<bf16>(k, n);
+}
+
+template <typename T, int KP, int NS>
+hipError_t backward_run(const LinearArgs& a, float* partial, float* sums, hipStream_t s) {
+  using B = BackwardShape<T, KP, NS>;
+  if constexpr (B::FITS) {
+    const int64_t tiles = ceil_div64(a.m, B::ROWS);
+    stream_backward_kernel<T, KP, NS>
+        <<<uint32_t(std::min(tiles, kBackwardBlocks)), B::THREADS, 0, s>>>(a, partial, sums, tiles);
+    return hipGetLastError();
+  }
+  return hipErrorInvalidValue;
+}
+
+template <typename T, int KP>
+hipError_t backward_kp(const LinearArgs& a, int ns, float* partial, float* sums, hipStream_t s) {
+  switch (ns) {
+    case 1: return backward_run<T, KP, 1>(a, partial, sums, s);
+    case 2: return backward_run<T, KP, 2>(a, partial, sums, s);
+    case 4: return backward_run<T, KP, 4>(a, partial, sums, s);
+    default: return backward_run<T, KP, 8>(a, partial, sums, s);
+  }
+}
+
+template <typename T>
+hipError_t backward(const LinearArgs& a, const BackwardChoice& c, float* partial, float* sums, hipStream_t s) {
+  switch (c.kp) {
+    case 32: return backward_kp<T, 32>(a, c.ns, partial, sums, s);
+    case 64: return backward_kp<T, 64>(a, c.ns, partial, sums, s);
+    case 128: return backward_kp<T, 128>(a, c.ns, partial, sums, s);
+    case 256: return backward_kp<T, 256>(a, c.ns, partial, sums, s);
+  }
+  return hipErrorInvalidValue;
+}
+
+}  // namespace
+
+bool stream_forward_fits(int64_t k, int64_t n, gart_dtype t) {
+  const size_t es = dtype_bytes(t);
+  return k <= 512 / int64_t(es) && n <= 2048 && forward_lds(round_inputs(k), n, es) <= kForwardBytes;
+}
+
+hipError_t launch_stream_forward(const LinearArgs& a, gart_dtype t, hipStream_t s) {
+  if (t == GART_DTYPE_F32) return forward<float>(a, s);
+  if (t == GART_DTYPE_BF16) return forward<bf16>(a, s);
+  return forward<f16>(a, s);
+}
+
+int64_t stream_backward_parts(int64_t m, int64_t k, int64_t n, gart_dtype t) {
+  if (m <= 0 || k <= 0 || n <= 0) return 0;
+  const BackwardChoice c = choose(k, n, t);
+  return c.kp == 0 ? 0 : std::min(ceil_div64(m, c.rows), kBackwardBlocks) * c.groups;
+}
+
+hipError_t launch_stream_backward(const LinearArgs& a, float* partial, float* sums, gart_dtype t, hipStream_t s) {
+  const BackwardChoice c = choose(a.k, a.n, t);
+  if (t == GART_DTYPE_F32) return backward<float>(a, c, partial, sums, s);
+  if (t == GART_DTYPE_BF16) return backward<bf16>(a, c, partial, sums, s);
+  return backward<f16>(a, c, partial, sums, s);
+}
+
+}  // namespace gart
