@@ -488,7 +488,8 @@ size_t gart_embedding_scratch_bytes(int64_t n, int64_t vocab, int64_t dim);
 /* Gradient of gart_embedding with respect to the table:
  *   g_table[v,:] = scale * sum over i with ids[i] = v of dl_dout[i,:]
  * for every v < g_table.rows (zero for rows no id names).  Rows are summed in
- * an order fixed by the ids alone, so the result is deterministic. */
+ * an order fixed by the ids alone, so the result is deterministic.
+ * UNSUPPORTED for more than 2^23 columns. */
 gart_status gart_embedding_backward(const void* ids, int32_t ids64, const gart_matrix* dl_dout, float scale,
                                     gart_dtype dtype, const gart_matrix* g_table, void* scratch,
                                     size_t scratch_bytes, void* stream);

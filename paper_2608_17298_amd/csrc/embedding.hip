@@ -14,9 +14,12 @@
 
 #include "blocks.h"
 #include "ops.h"
+#include "sort_small.h"
 
 namespace gart {
 namespace {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kThreads = 256;
 constexpr int kRowsPerThread = 4;
@@ -65,28 +68,46 @@ __global__ __launch_bounds__(kThreads) void lookup_kernel(const EmbeddingArgs a,
 }
 
 // ---- gradient ----------------------------------------------------------------
-// Keys of the sort: the id, or vocab (sorted last) where it names no row.
-template <typename Id>
-__global__ __launch_bounds__(kThreads) void keys_kernel(const Id* __restrict__ ids, int64_t n, int64_t vocab,
-                                                        uint32_t* __restrict__ keys, uint32_t* __restrict__ pos) {
-  const int64_t i = int64_t(blockIdx.x) * kThreads + threadIdx.x;
-  if (i >= n) return;
-  const int64_t id = int64_t(ids[i]);
-  keys[i] = uint32_t(id >= 0 && id < vocab ? id : vocab);
-  pos[i] = uint32_t(i);
-}
-
 template <typename T>
-__global__ __launch_bounds__(kThreads) void zero_rows_kernel(T* __restrict__ out, int64_t ld, int64_t rows,
-                                                             int64_t cols) {
+__device__ __forceinline__ void zero_rows(T* __restrict__ out, int64_t ld, int64_t rows, int64_t cols, int64_t first,
+                                          int64_t step) {
   constexpr int V = Pack<T>::N;
-  const int64_t packs = (cols + V - 1) / V, total = rows * packs;
+  const int64_t packs = (cols + V - 1) / V;
   Pack<T> z;
   z.v = T(0.0f);
-  for (int64_t i = int64_t(blockIdx.x) * kThreads + threadIdx.x; i < total; i += int64_t(gridDim.x) * kThreads) {
+  if (ld == cols) {  // one run of elements
+    const int64_t total = rows * cols;
+    for (int64_t i = first * V; i < total; i += step * V) store_some(out + i, z, int(min(int64_t(V), total - i)));
+    return;
+  }
+  for (int64_t i = first; i < rows * packs; i += step) {
     const int64_t r = i / packs, c = (i - r * packs) * V;
     store_some(out + r * ld + c, z, int(min(int64_t(V), cols - c)));
   }
+}
+
+template <typename T>
+__global__ __launch_bounds__(kThreads) void zero_rows_kernel(const EmbeddingArgs a) {
+  zero_rows(static_cast<T*>(a.out), a.out_ld, a.vocab, a.dim, int64_t(blockIdx.x) * kThreads + threadIdx.x,
+            int64_t(gridDim.x) * kThreads);
+}
+
+// Up to kSmallPairs ids: the first block sorts them while the others clear the
+// table's gradient (8191 ids into 50021 rows of 1023 f16: 17 and 16 us).
+template <typename T, typename Id>
+__global__ __launch_bounds__(kSmallThreads) void sort_and_zero_kernel(const EmbeddingArgs a,
+                                                                      uint32_t* __restrict__ keys,
+                                                                      uint32_t* __restrict__ pos, int bits) {
+  if (blockIdx.x > 0) {
+    zero_rows(static_cast<T*>(a.out), a.out_ld, a.vocab, a.dim, int64_t(blockIdx.x - 1) * kSmallThreads + threadIdx.x,
+              int64_t(gridDim.x - 1) * kSmallThreads);
+    return;
+  }
+  const IdSource<Id> source{static_cast<const Id*>(a.ids), a.vocab};
+  if (a.n <= kSmallThreads)
+    radix_small<1>(source, keys, pos, int(a.n), bits);
+  else
+    radix_small<8>(source, keys, pos, int(a.n), bits);
 }
 
 // Partial sums: partial[2 u] is the part in unit u of a run that began before
@@ -164,38 +185,41 @@ __global__ __launch_bounds__(kThreads) void unit_sums_kernel(const EmbeddingArgs
 
 // Joins the runs that cross units: unit u's last run begins there and goes on
 // if the key at its end equals the next unit's first, and that many further
-// units hold a part of it.  A wave takes one unit; a run over more than 64
-// units is left to the block's 16 waves together.  Lanes are spread over the
-// columns (four a lane) and, where those are few, over the run's units; the
-// shares are added in a fixed order.
+// units hold a part of it.  A wave takes one unit; a run that goes on over
+// kLongRun further units (at most one begins in a block's 16) is left to the
+// block's waves together.  Lanes are spread over a group of columns (four a
+// lane; blockIdx.y counts the groups) and, where columns are few, over the
+// run's units; the shares are added in a fixed order.
 constexpr int kJoinThreads = 1024;
 constexpr int kJoinWaves = kJoinThreads / 64;
+constexpr int kLongRun = kJoinWaves;
+constexpr int kJoinColumns = 256;
 
-// Sum of partial rows head(unit + 1 .. unit + more) and of unit's tail, by
-// `threads` threads of which this is `t`; column groups of 4, from c0 on.
-__device__ __forceinline__ float4 run_share(const float* __restrict__ partial, int64_t dim, int64_t unit, int64_t more,
-                                            int64_t c, int first, int step) {
-  float s[4] = {};
+// Sum over every step-th of a run's parts, from `first` on: part 0 is the tail
+// of `unit`, part u the head of unit + u.
+__device__ __forceinline__ f32x4 run_share(const float* __restrict__ partial, int64_t dim, int64_t unit, int64_t more,
+                                           int64_t c, int first, int step) {
+  f32x4 s = {0.0f, 0.0f, 0.0f, 0.0f};
   const int count = int(min(int64_t(4), dim - c));
-  for (int64_t u = first; u <= more; u += step) {
-    const Pack<float> q = load_some(partial + (u == 0 ? 2 * unit + 1 : 2 * (unit + u)) * dim + c, count);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) s[e] += q.v[e];
-  }
-  return make_float4(s[0], s[1], s[2], s[3]);
+#pragma unroll 4
+  for (int64_t u = first; u <= more; u += step)
+    s += load_some(partial + (u == 0 ? 2 * unit + 1 : 2 * (unit + u)) * dim + c, count).v;
+  return s;
 }
 
 template <typename T>
 __global__ __launch_bounds__(kJoinThreads) void join_kernel(const EmbeddingArgs a, const uint32_t* __restrict__ keys,
                                                             const float* __restrict__ partial, int unit_rows,
                                                             int64_t units) {
-  __shared__ uint32_t s_long[kJoinWaves];
-  __shared__ float4 s_sum[kJoinThreads];
+  __shared__ int s_long;  // the wave whose unit begins a long run, or -1
+  __shared__ f32x4 s_sum[kJoinThreads];
   T* __restrict__ out = static_cast<T*>(a.out);
   const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
   const int64_t base = int64_t(blockIdx.x) * kJoinWaves, unit = base + wave;
   const int64_t p0 = unit * unit_rows, p1 = p0 + unit_rows;
   const uint32_t none = uint32_t(a.vocab);
+  if (tid == 0) s_long = -1;
+  __syncthreads();
   bool mine = unit < units && p1 < a.n;
   uint32_t cur = none;
   if (mine) {
@@ -205,64 +229,48 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(const EmbeddingArgs 
   int more = 0;  // further units with a part of the run
   if (mine) {
     const int64_t q = p1 + int64_t(lane) * unit_rows;
-    const uint64_t same = __ballot(q < a.n && keys[q] == cur);
-    more = same == ~0ull ? 64 : __builtin_ctzll(~same);
+    const uint64_t other = ~__ballot(lane < kLongRun && q < a.n && keys[q] == cur);
+    more = __builtin_ctzll(other);
+    if (more == kLongRun && lane == 0) s_long = wave;
   }
-  if (lane == 0) s_long[wave] = more == 64 ? cur : none;
-  auto store = [&](uint32_t key, int64_t c, float4 s) {
-    const float v[4] = {s.x, s.y, s.z, s.w};
+  auto store = [&](uint32_t key, int64_t c, f32x4 s) {
 #pragma unroll
     for (int e = 0; e < 4; ++e)
-      if (c + e < a.dim) out[int64_t(key) * a.out_ld + c + e] = T(v[e] * a.scale);
+      if (c + e < a.dim) out[int64_t(key) * a.out_ld + c + e] = T(s[e] * a.scale);
   };
-  const int64_t quads = (a.dim + 3) / 4;
-  int w = 1;  // lanes over columns: a power of two, so that shares meet by shuffles
-  while (w < 64 && w < quads) w *= 2;
-  if (more > 0 && more < 64) {
-    for (int64_t c = int64_t(lane % w) * 4; c < quads * 4; c += 4 * w) {
-      float4 s = run_share(partial, a.dim, unit, more, c, lane / w, 64 / w);
-      for (int off = w; off < 64; off *= 2) {  // every lane of the wave that has this column is here
-        s.x += __shfl_xor(s.x, off);
-        s.y += __shfl_xor(s.y, off);
-        s.z += __shfl_xor(s.z, off);
-        s.w += __shfl_xor(s.w, off);
-      }
-      if (lane < w) store(cur, c, s);
-    }
+  // columns of this block, and lanes over them: a power of two
+  const int64_t c0 = int64_t(blockIdx.y) * kJoinColumns;
+  const int quads = int((min(int64_t(kJoinColumns), a.dim - c0) + 3) / 4);
+  int w = 1;
+  while (w < quads) w *= 2;
+  const int64_t c = c0 + int64_t(lane % w) * 4;
+  if (more > 0 && more < kLongRun) {
+    f32x4 s = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (c < a.dim) s = run_share(partial, a.dim, unit, more, c, lane / w, 64 / w);
+    for (int off = w; off < 64; off *= 2)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s[e] += __shfl_xor(s[e], off);
+    if (lane < w && c < a.dim) store(cur, c, s);
   }
   __syncthreads();
-  for (int l = 0; l < kJoinWaves; ++l) {
-    const uint32_t key = s_long[l];
-    if (key == none) continue;  // the same for the block
-    const int64_t begin = base + l;
-    int64_t parts = 0;
-    for (;;) {
-      const int64_t q = (begin + 1 + parts + tid) * unit_rows;
-      const int here = __syncthreads_count(q < a.n && keys[q] == key);
-      parts += here;
-      if (here < kJoinThreads) break;
-    }
-    const int groups = kJoinThreads / w;
-    for (int64_t c0 = 0; c0 < quads * 4; c0 += 4 * w) {
-      const int64_t c = c0 + int64_t(tid % w) * 4;
-      s_sum[tid] = c < a.dim ? run_share(partial, a.dim, begin, parts, c, tid / w, groups) : make_float4(0, 0, 0, 0);
-      __syncthreads();
-      for (int g = groups / 2; g > 0; g /= 2) {
-        if (tid < g * w) {
-          float4 x = s_sum[tid];
-          const float4 y = s_sum[tid + g * w];
-          x.x += y.x;
-          x.y += y.y;
-          x.z += y.z;
-          x.w += y.w;
-          s_sum[tid] = x;
-        }
-        __syncthreads();
-      }
-      if (tid < w && c < a.dim) store(key, c, s_sum[tid]);
-      __syncthreads();
-    }
+  if (s_long < 0) return;  // the same for the block
+  const int64_t begin = base + s_long;
+  const uint32_t key = keys[(begin + 1) * unit_rows];
+  int64_t parts = 0;
+  for (;;) {
+    const int64_t q = (begin + 1 + parts + tid) * unit_rows;
+    const int here = __syncthreads_count(q < a.n && keys[q] == key);
+    parts += here;
+    if (here < kJoinThreads) break;
   }
+  s_sum[tid] = c < a.dim ? run_share(partial, a.dim, begin, parts, c, tid / w, kJoinThreads / w)
+                         : f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  __syncthreads();
+  for (int g = kJoinThreads / w / 2; g > 0; g /= 2) {
+    if (tid < g * w) s_sum[tid] += s_sum[tid + g * w];
+    __syncthreads();
+  }
+  if (tid < w && c < a.dim) store(key, c, s_sum[tid]);
 }
 
 // Sorted positions per unit: enough threads (one per 16 bytes of a unit's
@@ -295,7 +303,7 @@ GradLayout grad_layout(int64_t n, int64_t dim) {
   L.pos = take(size_t(n) * 4);
   L.keys_alt = take(size_t(n) * 4);
   L.pos_alt = take(size_t(n) * 4);
-  L.radix = take(radix_tmp_bytes(n));
+  L.radix = take(radix_ids_tmp_bytes(n));
   L.partial = take(size_t(ceil_div64(n, unit_rows_for(n, dim))) * 2 * size_t(dim) * 4);
   L.total = off;
   return L;
@@ -317,21 +325,28 @@ template <typename T>
 hipError_t gradient(const EmbeddingArgs& a, hipStream_t s) {
   if (a.vocab <= 0 || a.dim <= 0) return hipSuccess;
   const int packs = int(ceil_div64(a.dim, Pack<T>::N)), lanes = std::min(packs, kThreads), upb = kThreads / lanes;
-  const int64_t zero_blocks = std::min<int64_t>(ceil_div64(a.vocab * packs, kThreads), 1 << 16);
-  zero_rows_kernel<T><<<uint32_t(zero_blocks), kThreads, 0, s>>>(static_cast<T*>(a.out), a.out_ld, a.vocab, a.dim);
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess || a.n <= 0) return e;
+  const int64_t table_packs = ceil_div64(a.vocab * ceil_div64(a.dim, Pack<T>::N), 4);  // four a thread
   const GradLayout L = grad_layout(a.n, a.dim);
   char* base = static_cast<char*>(a.scratch);
   auto words = [&](size_t off) { return reinterpret_cast<uint32_t*>(base + off); };
   uint32_t *keys = words(L.keys), *pos = words(L.pos);
-  const uint32_t blocks = uint32_t(ceil_div64(a.n, kThreads));
-  if (a.ids64)
-    keys_kernel<int64_t><<<blocks, kThreads, 0, s>>>(static_cast<const int64_t*>(a.ids), a.n, a.vocab, keys, pos);
-  else
-    keys_kernel<int32_t><<<blocks, kThreads, 0, s>>>(static_cast<const int32_t*>(a.ids), a.n, a.vocab, keys, pos);
-  if ((e = hipGetLastError()) != hipSuccess) return e;
-  e = radix_sort_u32(keys, pos, words(L.keys_alt), words(L.pos_alt), a.n, bits_for(a.vocab), base + L.radix, s);
+  const int bits = bits_for(a.vocab);
+  hipError_t e;
+  if (a.n > 0 && a.n <= kSmallPairs) {
+    const uint32_t blocks = uint32_t(1 + std::min<int64_t>(ceil_div64(table_packs, kSmallThreads), 2048));
+    if (a.ids64)
+      sort_and_zero_kernel<T, int64_t><<<blocks, kSmallThreads, 0, s>>>(a, keys, pos, bits);
+    else
+      sort_and_zero_kernel<T, int32_t><<<blocks, kSmallThreads, 0, s>>>(a, keys, pos, bits);
+    e = hipGetLastError();
+  } else {
+    const uint32_t blocks = uint32_t(std::min<int64_t>(ceil_div64(table_packs, kThreads), 8192));
+    zero_rows_kernel<T><<<blocks, kThreads, 0, s>>>(a);
+    e = hipGetLastError();
+    if (e != hipSuccess || a.n <= 0) return e;
+    e = radix_sort_ids(a.ids, a.ids64, a.vocab, keys, pos, words(L.keys_alt), words(L.pos_alt), a.n, bits,
+                       base + L.radix, s);
+  }
   if (e != hipSuccess) return e;
   float* partial = reinterpret_cast<float*>(base + L.partial);
   const int unit_rows = unit_rows_for(a.n, a.dim);
@@ -340,7 +355,8 @@ hipError_t gradient(const EmbeddingArgs& a, hipStream_t s) {
                                                                            lanes, upb);
   if ((e = hipGetLastError()) != hipSuccess) return e;
   if (units > 1)
-    join_kernel<T><<<uint32_t(ceil_div64(units, kJoinWaves)), kJoinThreads, 0, s>>>(a, keys, partial, unit_rows, units);
+    join_kernel<T><<<dim3(uint32_t(ceil_div64(units, kJoinWaves)), uint32_t(ceil_div64(a.dim, kJoinColumns))),
+                     kJoinThreads, 0, s>>>(a, keys, partial, unit_rows, units);
   return hipGetLastError();
 }
 

@@ -10,6 +10,7 @@
 #include <algorithm>
 
 #include "ops.h"
+#include "sort_small.h"
 
 namespace gart {
 namespace {
@@ -24,6 +25,7 @@ constexpr int kSortThreads = 256;
 #endif
 constexpr int kSortItems = GART_SORT_ITEMS;  // keys per thread and radix pass
 constexpr int kSortTile = kSortThreads * kSortItems;
+constexpr int kIdItems = 8;  // of a sort of ids: up to a few million, more blocks beat longer ones (1M: 16 items 147 us, 8 143)
 constexpr int kWaves = kSortThreads / 64;
 
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
@@ -136,21 +138,21 @@ hipError_t scan_impl(const Tin* in, T* out, int64_t n, T* total, char* tmp, hipS
 // the per-wave counts into offsets; the block's keys are staged in LDS in
 // digit order and written out as contiguous runs per digit.
 // ---------------------------------------------------------------------------
-__global__ __launch_bounds__(kSortThreads) void radix_hist_kernel(const uint32_t* __restrict__ keys, int64_t m,
-                                                                  int shift, uint32_t* __restrict__ counts,
-                                                                  int nblocks) {
+template <int ITEMS, typename Source>
+__global__ __launch_bounds__(kSortThreads) void radix_hist_kernel(const Source source, int64_t m, int shift,
+                                                                  uint32_t* __restrict__ counts, int nblocks) {
   __shared__ uint32_t h[256];
   h[threadIdx.x] = 0;
   __syncthreads();
-  const int64_t base = int64_t(blockIdx.x) * kSortTile;
-  uint32_t kv[kSortItems];
+  const int64_t base = int64_t(blockIdx.x) * (kSortThreads * ITEMS);
+  uint32_t kv[ITEMS];
 #pragma unroll
-  for (int r = 0; r < kSortItems; ++r) {
+  for (int r = 0; r < ITEMS; ++r) {
     const int64_t j = base + int64_t(r) * kSortThreads + threadIdx.x;
-    kv[r] = j < m ? keys[j] : 0u;
+    kv[r] = j < m ? source.key(j) : 0u;
   }
 #pragma unroll
-  for (int r = 0; r < kSortItems; ++r) {
+  for (int r = 0; r < ITEMS; ++r) {
     const int64_t j = base + int64_t(r) * kSortThreads + threadIdx.x;
     if (j < m) atomicAdd(&h[(kv[r] >> shift) & 255u], 1u);
   }
@@ -158,11 +160,11 @@ __global__ __launch_bounds__(kSortThreads) void radix_hist_kernel(const uint32_t
   counts[int64_t(threadIdx.x) * nblocks + blockIdx.x] = h[threadIdx.x];
 }
 
+template <int ITEMS, typename Source>
 __global__ __launch_bounds__(kSortThreads) void radix_scatter_kernel(
-    const uint32_t* __restrict__ kin, const uint32_t* __restrict__ vin, uint32_t* __restrict__ kout,
-    uint32_t* __restrict__ vout, int64_t m, int shift, const uint32_t* __restrict__ offsets, int nblocks) {
-  __shared__ uint32_t s_keys[kSortTile];
-  __shared__ uint32_t s_vals[kSortTile];
+    const Source source, uint32_t* __restrict__ kout, uint32_t* __restrict__ vout, int64_t m, int shift, const uint32_t* __restrict__ offsets, int nblocks) {
+  __shared__ uint32_t s_keys[(kSortThreads * ITEMS)];
+  __shared__ uint32_t s_vals[(kSortThreads * ITEMS)];
   __shared__ uint32_t s_wave[kWaves][256];  // per-wave digit counts, later per-wave digit bases
   __shared__ uint32_t s_start[256];
   __shared__ uint32_t s_gofs[256];
@@ -178,22 +180,22 @@ __global__ __launch_bounds__(kSortThreads) void radix_scatter_kernel(
   s_gofs[tid] = offsets[int64_t(tid) * nblocks + blockIdx.x];
   __syncthreads();
 
-  // Keys [wbase, wbase + 64 * kSortItems) belong to this wave, so block order
+  // Keys [wbase, wbase + 64 * ITEMS) belong to this wave, so block order
   // is wave, round, lane: the order of the input.
-  const int64_t wbase = int64_t(blockIdx.x) * kSortTile + int64_t(wave) * (64 * kSortItems);
-  uint32_t myk[kSortItems], myv[kSortItems], myr[kSortItems];
+  const int64_t wbase = int64_t(blockIdx.x) * (kSortThreads * ITEMS) + int64_t(wave) * (64 * ITEMS);
+  uint32_t myk[ITEMS], myv[ITEMS], myr[ITEMS];
 #pragma unroll
-  for (int r = 0; r < kSortItems; ++r) {
+  for (int r = 0; r < ITEMS; ++r) {
     const int64_t j = wbase + int64_t(r) * 64 + lane;
-    myk[r] = j < m ? kin[j] : 0u;
-    myv[r] = j < m ? vin[j] : 0u;
+    myk[r] = j < m ? source.key(j) : 0u;
+    myv[r] = j < m ? source.val(j) : 0u;
   }
   // The running counts are read and updated by different lanes of one wave;
   // LDS executes a wave's accesses in issue order, and volatile keeps the
   // compiler from reordering or caching them.
   volatile uint32_t* wcount = s_wave[wave];
 #pragma unroll
-  for (int r = 0; r < kSortItems; ++r) {
+  for (int r = 0; r < ITEMS; ++r) {
     const bool valid = wbase + int64_t(r) * 64 + lane < m;
     const uint32_t d = (myk[r] >> shift) & 255u;
     uint64_t peers = __ballot(valid);
@@ -239,7 +241,7 @@ __global__ __launch_bounds__(kSortThreads) void radix_scatter_kernel(
   __syncthreads();
 
 #pragma unroll
-  for (int r = 0; r < kSortItems; ++r) {
+  for (int r = 0; r < ITEMS; ++r) {
     if (wbase + int64_t(r) * 64 + lane < m) {
       const uint32_t d = (myk[r] >> shift) & 255u;
       const uint32_t pos = s_wave[wave][d] + myr[r];
@@ -249,8 +251,8 @@ __global__ __launch_bounds__(kSortThreads) void radix_scatter_kernel(
   }
   __syncthreads();
 
-  const int64_t base = int64_t(blockIdx.x) * kSortTile;
-  const int cnt = int(std::min<int64_t>(kSortTile, m - base));
+  const int64_t base = int64_t(blockIdx.x) * (kSortThreads * ITEMS);
+  const int cnt = int(std::min<int64_t>((kSortThreads * ITEMS), m - base));
   for (int q = tid; q < cnt; q += kSortThreads) {
     const uint32_t k = s_keys[q];
     const uint32_t d = (k >> shift) & 255u;
@@ -269,100 +271,10 @@ __global__ __launch_bounds__(kSortThreads) void radix_scatter_kernel(
 // with the pairs (13, 21 and 35 us) and with 16 per thread would reach their
 // time (16384: 66 us both).
 // ---------------------------------------------------------------------------
-constexpr int kSmallThreads = 1024;
-constexpr int kSmallWaves = kSmallThreads / 64;
-constexpr int64_t kSmallPairs = kSmallThreads * 8;
-
 template <int ITEMS>
 __global__ __launch_bounds__(kSmallThreads) void radix_small_kernel(uint32_t* __restrict__ keys,
                                                                     uint32_t* __restrict__ vals, int m, int bits) {
-  __shared__ uint32_t s_keys[kSmallThreads * ITEMS];
-  __shared__ uint32_t s_vals[kSmallThreads * ITEMS];
-  __shared__ uint32_t s_wave[kSmallWaves][256];
-  __shared__ uint32_t s_wsum[4];
-  const int tid = threadIdx.x, wave = tid / 64;
-  const unsigned lane = __lane_id();
-  const uint64_t lt_mask = (lane == 0) ? 0ull : (~0ull >> (64 - lane));
-  const int wbase = wave * 64 * ITEMS;  // this wave's keys: order is wave, round, lane
-  uint32_t myk[ITEMS], myv[ITEMS], myr[ITEMS];
-#pragma unroll
-  for (int r = 0; r < ITEMS; ++r) {
-    const int j = wbase + r * 64 + int(lane);
-    myk[r] = j < m ? keys[j] : 0u;
-    myv[r] = j < m ? vals[j] : 0u;
-  }
-  for (int shift = 0; shift < bits; shift += 8) {
-#pragma unroll
-    for (int w = 0; w < kSmallWaves / 4; ++w) s_wave[4 * w + tid / 256][tid % 256] = 0;
-    __syncthreads();
-    volatile uint32_t* wcount = s_wave[wave];
-#pragma unroll
-    for (int r = 0; r < ITEMS; ++r) {
-      if (wbase + r * 64 >= m) break;
-      const bool valid = wbase + r * 64 + int(lane) < m;
-      const uint32_t d = (myk[r] >> shift) & 255u;
-      uint64_t peers = __ballot(valid);
-#pragma unroll
-      for (int b = 0; b < 8; ++b) {
-        const bool bit = (d >> b) & 1u;
-        const uint64_t bal = __ballot(bit);
-        peers &= bit ? bal : ~bal;
-      }
-      const uint32_t below = __popcll(peers & lt_mask);
-      const uint32_t before = wcount[d];
-      myr[r] = before + below;
-      if (valid && below == 0) wcount[d] = before + uint32_t(__popcll(peers));
-    }
-    __syncthreads();
-    // digit tid (first 256 threads): start over digits, then each wave's base
-    uint32_t total = 0, inc = 0;
-    if (tid < 256) {
-#pragma unroll
-      for (int w = 0; w < kSmallWaves; ++w) total += s_wave[w][tid];
-      inc = total;
-#pragma unroll
-      for (int off = 1; off < 64; off <<= 1) {
-        const uint32_t u = __shfl_up(inc, off);
-        if (lane >= unsigned(off)) inc += u;
-      }
-      if (lane == 63) s_wsum[wave] = inc;
-    }
-    __syncthreads();
-    if (tid < 256) {
-      uint32_t run = inc - total;
-      for (int w = 0; w < wave; ++w) run += s_wsum[w];
-#pragma unroll
-      for (int w = 0; w < kSmallWaves; ++w) {
-        const uint32_t c = s_wave[w][tid];
-        s_wave[w][tid] = run;
-        run += c;
-      }
-    }
-    __syncthreads();
-#pragma unroll
-    for (int r = 0; r < ITEMS; ++r) {
-      if (wbase + r * 64 + int(lane) < m) {
-        const uint32_t pos = s_wave[wave][(myk[r] >> shift) & 255u] + myr[r];
-        s_keys[pos] = myk[r];
-        s_vals[pos] = myv[r];
-      }
-    }
-    __syncthreads();
-#pragma unroll
-    for (int r = 0; r < ITEMS; ++r) {
-      const int j = wbase + r * 64 + int(lane);
-      myk[r] = j < m ? s_keys[j] : 0u;
-      myv[r] = j < m ? s_vals[j] : 0u;
-    }
-  }
-#pragma unroll
-  for (int r = 0; r < ITEMS; ++r) {
-    const int j = wbase + r * 64 + int(lane);
-    if (j < m) {
-      keys[j] = myk[r];
-      vals[j] = myv[r];
-    }
-  }
+  radix_small<ITEMS>(PairSource{keys, vals}, keys, vals, m, bits);
 }
 
 __global__ void copy_pairs_kernel(const uint32_t* __restrict__ ka, const uint32_t* __restrict__ va,
@@ -425,6 +337,25 @@ size_t radix_tmp_bytes(int64_t m) {
   return counts + scan_tmp_bytes(nb * 256);
 }
 
+namespace {
+
+template <int ITEMS, typename Source>
+hipError_t radix_pass(const Source& source, uint32_t* kout, uint32_t* vout, int64_t m, int shift, void* tmp,
+                      hipStream_t s) {
+  const int64_t nb = ceil_div(m, kSortThreads * ITEMS);
+  uint32_t* counts = static_cast<uint32_t*>(tmp);
+  char* scan_tmp = static_cast<char*>(tmp) + ((size_t(nb) * 256 * sizeof(uint32_t) + 255) & ~size_t(255));
+  radix_hist_kernel<ITEMS><<<nb, kSortThreads, 0, s>>>(source, m, shift, counts, int(nb));
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  e = scan_exclusive_u32(counts, counts, nb * 256, nullptr, scan_tmp, s);
+  if (e != hipSuccess) return e;
+  radix_scatter_kernel<ITEMS><<<nb, kSortThreads, 0, s>>>(source, kout, vout, m, shift, counts, int(nb));
+  return hipGetLastError();
+}
+
+}  // namespace
+
 hipError_t radix_sort_u32(uint32_t* keys, uint32_t* vals, uint32_t* keys_alt, uint32_t* vals_alt, int64_t m, int bits,
                           void* tmp, hipStream_t s) {
   if (m <= 1 || bits <= 0) return hipSuccess;
@@ -435,19 +366,9 @@ hipError_t radix_sort_u32(uint32_t* keys, uint32_t* vals, uint32_t* keys_alt, ui
       radix_small_kernel<8><<<1, kSmallThreads, 0, s>>>(keys, vals, int(m), bits);
     return hipGetLastError();
   }
-  const int64_t nb = ceil_div(m, kSortTile);
-  uint32_t* counts = static_cast<uint32_t*>(tmp);
-  char* scan_tmp = static_cast<char*>(tmp) + ((size_t(nb) * 256 * sizeof(uint32_t) + 255) & ~size_t(255));
   uint32_t *ka = keys, *va = vals, *kb = keys_alt, *vb = vals_alt;
-  int passes = 0;
-  for (int shift = 0; shift < bits; shift += 8, ++passes) {
-    radix_hist_kernel<<<nb, kSortThreads, 0, s>>>(ka, m, shift, counts, int(nb));
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-    e = scan_exclusive_u32(counts, counts, nb * 256, nullptr, scan_tmp, s);
-    if (e != hipSuccess) return e;
-    radix_scatter_kernel<<<nb, kSortThreads, 0, s>>>(ka, va, kb, vb, m, shift, counts, int(nb));
-    e = hipGetLastError();
+  for (int shift = 0; shift < bits; shift += 8) {
+    const hipError_t e = radix_pass<kSortItems>(PairSource{ka, va}, kb, vb, m, shift, tmp, s);
     if (e != hipSuccess) return e;
     std::swap(ka, kb);
     std::swap(va, vb);
@@ -455,6 +376,30 @@ hipError_t radix_sort_u32(uint32_t* keys, uint32_t* vals, uint32_t* keys_alt, ui
   if (ka != keys) {
     copy_pairs_kernel<<<ceil_div(m, 256), 256, 0, s>>>(ka, va, keys, vals, m);
     return hipGetLastError();
+  }
+  return hipSuccess;
+}
+
+size_t radix_ids_tmp_bytes(int64_t m) { return radix_tmp_bytes(m * kSortItems / kIdItems); }
+
+hipError_t radix_sort_ids(const void* ids, bool ids64, int64_t limit, uint32_t* keys, uint32_t* pos,
+                          uint32_t* keys_alt, uint32_t* pos_alt, int64_t m, int bits, void* tmp, hipStream_t s) {
+  uint32_t *ka = keys, *va = pos, *kb = keys_alt, *vb = pos_alt;
+  if ((bits + 7) / 8 % 2 == 0) {  // the last pass ends in keys and pos
+    std::swap(ka, kb);
+    std::swap(va, vb);
+  }
+  for (int shift = 0; shift < bits; shift += 8) {
+    hipError_t e;
+    if (shift > 0)
+      e = radix_pass<kIdItems>(PairSource{kb, vb}, ka, va, m, shift, tmp, s);
+    else if (ids64)
+      e = radix_pass<kIdItems>(IdSource<int64_t>{static_cast<const int64_t*>(ids), limit}, ka, va, m, 0, tmp, s);
+    else
+      e = radix_pass<kIdItems>(IdSource<int32_t>{static_cast<const int32_t*>(ids), limit}, ka, va, m, 0, tmp, s);
+    if (e != hipSuccess) return e;
+    std::swap(ka, kb);
+    std::swap(va, vb);
   }
   return hipSuccess;
 }

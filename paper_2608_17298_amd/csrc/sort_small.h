@@ -1,0 +1,127 @@
+// Device code of the one-block sort, for kernels that sort beside other work.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+
+namespace gart {
+
+constexpr int kSmallThreads = 1024;
+constexpr int kSmallWaves = kSmallThreads / 64;
+constexpr int64_t kSmallPairs = kSmallThreads * 8;
+
+// Keys and values as they stand in memory.
+struct PairSource {
+  const uint32_t *keys, *vals;
+  __device__ __forceinline__ uint32_t key(int64_t j) const { return keys[j]; }
+  __device__ __forceinline__ uint32_t val(int64_t j) const { return vals[j]; }
+};
+
+// Ids and their positions; ids outside [0, limit) are sorted last, as limit.
+template <typename Id>
+struct IdSource {
+  const Id* ids;
+  int64_t limit;
+  __device__ __forceinline__ uint32_t key(int64_t j) const {
+    const int64_t id = int64_t(ids[j]);
+    return uint32_t(id >= 0 && id < limit ? id : limit);
+  }
+  __device__ __forceinline__ uint32_t val(int64_t j) const { return uint32_t(j); }
+};
+
+// source.key(j), source.val(j): the pairs to sort, j < m <= kSmallThreads *
+// ITEMS, by one block of kSmallThreads threads.
+template <int ITEMS, typename Source>
+__device__ __forceinline__ void radix_small(const Source& source, uint32_t* __restrict__ keys,
+                                            uint32_t* __restrict__ vals, int m, int bits) {
+  __shared__ uint32_t s_keys[kSmallThreads * ITEMS];
+  __shared__ uint32_t s_vals[kSmallThreads * ITEMS];
+  __shared__ uint32_t s_wave[kSmallWaves][256];
+  __shared__ uint32_t s_wsum[4];
+  const int tid = threadIdx.x, wave = tid / 64;
+  const unsigned lane = __lane_id();
+  const uint64_t lt_mask = (lane == 0) ? 0ull : (~0ull >> (64 - lane));
+  const int wbase = wave * 64 * ITEMS;  // this wave's keys: order is wave, round, lane
+  uint32_t myk[ITEMS], myv[ITEMS], myr[ITEMS];
+#pragma unroll
+  for (int r = 0; r < ITEMS; ++r) {
+    const int j = wbase + r * 64 + int(lane);
+    myk[r] = j < m ? source.key(j) : 0u;
+    myv[r] = j < m ? source.val(j) : 0u;
+  }
+  for (int shift = 0; shift < bits; shift += 8) {
+#pragma unroll
+    for (int w = 0; w < kSmallWaves / 4; ++w) s_wave[4 * w + tid / 256][tid % 256] = 0;
+    __syncthreads();
+    volatile uint32_t* wcount = s_wave[wave];
+#pragma unroll
+    for (int r = 0; r < ITEMS; ++r) {
+      if (wbase + r * 64 >= m) break;
+      const bool valid = wbase + r * 64 + int(lane) < m;
+      const uint32_t d = (myk[r] >> shift) & 255u;
+      uint64_t peers = __ballot(valid);
+#pragma unroll
+      for (int b = 0; b < 8; ++b) {
+        const bool bit = (d >> b) & 1u;
+        const uint64_t bal = __ballot(bit);
+        peers &= bit ? bal : ~bal;
+      }
+      const uint32_t below = __popcll(peers & lt_mask);
+      const uint32_t before = wcount[d];
+      myr[r] = before + below;
+      if (valid && below == 0) wcount[d] = before + uint32_t(__popcll(peers));
+    }
+    __syncthreads();
+    // digit tid (first 256 threads): start over digits, then each wave's base
+    uint32_t total = 0, inc = 0;
+    if (tid < 256) {
+#pragma unroll
+      for (int w = 0; w < kSmallWaves; ++w) total += s_wave[w][tid];
+      inc = total;
+#pragma unroll
+      for (int off = 1; off < 64; off <<= 1) {
+        const uint32_t u = __shfl_up(inc, off);
+        if (lane >= unsigned(off)) inc += u;
+      }
+      if (lane == 63) s_wsum[wave] = inc;
+    }
+    __syncthreads();
+    if (tid < 256) {
+      uint32_t run = inc - total;
+      for (int w = 0; w < wave; ++w) run += s_wsum[w];
+#pragma unroll
+      for (int w = 0; w < kSmallWaves; ++w) {
+        const uint32_t c = s_wave[w][tid];
+        s_wave[w][tid] = run;
+        run += c;
+      }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < ITEMS; ++r) {
+      if (wbase + r * 64 + int(lane) < m) {
+        const uint32_t pos = s_wave[wave][(myk[r] >> shift) & 255u] + myr[r];
+        s_keys[pos] = myk[r];
+        s_vals[pos] = myv[r];
+      }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < ITEMS; ++r) {
+      const int j = wbase + r * 64 + int(lane);
+      myk[r] = j < m ? s_keys[j] : 0u;
+      myv[r] = j < m ? s_vals[j] : 0u;
+    }
+  }
+#pragma unroll
+  for (int r = 0; r < ITEMS; ++r) {
+    const int j = wbase + r * 64 + int(lane);
+    if (j < m) {
+      keys[j] = myk[r];
+      vals[j] = myv[r];
+    }
+  }
+}
+
+}  // namespace gart
