@@ -2,6 +2,8 @@
 // activations, fragments in LDS; and the launchers' sub-plans.
 #pragma once
 
+#include <type_traits>
+
 #include "blocks.h"
 
 namespace gart {
@@ -37,74 +39,55 @@ struct Mfma<float> {
 
 // ---- activations -----------------------------------------------------------
 // silu(z) = z g(z) and gelu(z) = z g(2 sqrt(2/pi) (z + 0.044715 z^3)) with the
-// logistic function g(u) = 1 / (1 + exp(-u)).  Beyond |u| = 87 g is 0 or 1 in
-// float and g' is 0.
+// logistic function g(u) = 1 / (1 + exp(-u)) = 1 / (1 + 2^(-u log2 e)).  The
+// exponent is one rounded product: it is off by the size of z's own rounding.
+// z is held where g is exactly 0 or 1 in float, so that an infinite z meets no
+// infinity times 0; these minima and maxima let a NaN through.
 constexpr float kGelu = 1.5957691216057308f;  // 2 sqrt(2 / pi)
+constexpr float kCubic = 0.044715f;
+constexpr float kLog2e = 1.4426950408889634f;
 
-struct Gate {
-  float g, slope;  // g(u), g'(u)
-};
+template <gart_activation ACT>
+constexpr float kEdge = ACT == GART_ACT_GELU ? 12.0f : 104.0f;
 
-__device__ __forceinline__ Gate gate(float u) {
-  // exp(-u) = 2^h 2^l: h the rounded product, l what it lost and the low part
-  // of log2(e), so that float results keep their last bits for large |u|
-  const float c = fminf(fmaxf(-u, -87.0f), 87.0f);
-  const float h = c * 1.44269504f;
-  const float l = fmaf(c, 1.44269504f, -h) + c * 1.92596299e-8f;
-  float e = __builtin_amdgcn_exp2f(h);
-  e = fmaf(e, l * 0.693147181f, e);
-  Gate r;
-  r.g = __builtin_amdgcn_rcpf(1.0f + e);
-  r.slope = e * r.g * r.g;
-  if (u < -87.0f) r.g = 0.0f;
-  if (fabsf(u) > 87.0f) r.slope = 0.0f;
-  return r;
-}
-
-__device__ __forceinline__ float gate_argument(float z, gart_activation act) {
-  return act == GART_ACT_GELU ? kGelu * fmaf(0.044715f * z * z, z, z) : z;
-}
-
-// 16-bit results: one exponential of the plain product. z is held above the
-// point where the result is 0 in 32 bits, which keeps -infinity from meeting a
-// gate of 0; minimum and maximum let a NaN through.
-template <typename T>
-constexpr bool kShort = sizeof(T) == 2;
-
-__device__ __forceinline__ float edge_of(gart_activation act) { return act == GART_ACT_GELU ? 10.0f : 87.0f; }
-
-__device__ __forceinline__ float quick_gate(float z, gart_activation act) {
-  constexpr float kLog2e = 1.44269504f;
-  const float h = act == GART_ACT_GELU ? z * fmaf(z * z, -kGelu * 0.044715f * kLog2e, -kGelu * kLog2e) : z * -kLog2e;
+template <gart_activation ACT>
+__device__ __forceinline__ float gate(float z) {
+  float h;
+  if constexpr (ACT == GART_ACT_GELU)
+    h = z * fmaf(z * z, -kGelu * kCubic * kLog2e, -kGelu * kLog2e);
+  else
+    h = z * -kLog2e;
   return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(h));
 }
 
-template <typename T>
-__device__ __forceinline__ float activate(float z, gart_activation act) {
-  if (act == GART_ACT_NONE) return z;
-  if (act == GART_ACT_RELU) return z < 0.0f ? 0.0f : z;  // a NaN stays
-  if constexpr (kShort<T>) {
-    const float c = __builtin_elementwise_maximum(z, -edge_of(act));
-    return c * quick_gate(c, act);
-  }
-  const float g = gate(gate_argument(z, act)).g;
-  return g == 0.0f ? 0.0f : z * g;  // not inf * 0 at -infinity
+template <gart_activation ACT>
+__device__ __forceinline__ float activate(float z) {
+  if constexpr (ACT == GART_ACT_NONE) return z;
+  if constexpr (ACT == GART_ACT_RELU) return z < 0.0f ? 0.0f : z;  // a NaN stays
+  const float c = __builtin_elementwise_maximum(z, -kEdge<ACT>);
+  return c * gate<ACT>(c);
 }
 
 // dl times act'(z)
-template <typename T>
-__device__ __forceinline__ float activate_grad(float z, float dl, gart_activation act) {
-  if (act == GART_ACT_NONE) return dl;
-  if (act == GART_ACT_RELU) return z <= 0.0f ? 0.0f : dl;
-  if constexpr (kShort<T>) {
-    const float c = __builtin_elementwise_minimum(__builtin_elementwise_maximum(z, -edge_of(act)), edge_of(act));
-    const float g = quick_gate(c, act);
-    const float s = act == GART_ACT_GELU ? c * fmaf(3.0f * 0.044715f * kGelu * c, c, kGelu) : c;
-    return dl * fmaf(s * g, 1.0f - g, g);
+template <gart_activation ACT>
+__device__ __forceinline__ float activate_grad(float z, float dl) {
+  if constexpr (ACT == GART_ACT_NONE) return dl;
+  if constexpr (ACT == GART_ACT_RELU) return z <= 0.0f ? 0.0f : dl;
+  const float c = __builtin_elementwise_minimum(__builtin_elementwise_maximum(z, -kEdge<ACT>), kEdge<ACT>);
+  const float g = gate<ACT>(c);
+  const float s = ACT == GART_ACT_GELU ? c * fmaf(3.0f * kCubic * kGelu * c, c, kGelu) : c;
+  return dl * fmaf(s * g, 1.0f - g, g);
+}
+
+// f(integral constant of act): one branch a block of elements, none between them
+template <typename F>
+__device__ __forceinline__ void with_activation(gart_activation act, F&& f) {
+  switch (act) {
+    case GART_ACT_NONE: f(std::integral_constant<gart_activation, GART_ACT_NONE>{}); break;
+    case GART_ACT_RELU: f(std::integral_constant<gart_activation, GART_ACT_RELU>{}); break;
+    case GART_ACT_SILU: f(std::integral_constant<gart_activation, GART_ACT_SILU>{}); break;
+    case GART_ACT_GELU: f(std::integral_constant<gart_activation, GART_ACT_GELU>{}); break;
   }
-  const Gate t = gate(gate_argument(z, act));
-  const float du = act == GART_ACT_GELU ? kGelu * fmaf(0.134145f * z, z, 1.0f) : 1.0f;
-  return dl * (t.slope == 0.0f && z == z ? t.g : fmaf(z * t.slope, du, t.g));
 }
 
 // ---- fragments ---------------------------------------------------------------

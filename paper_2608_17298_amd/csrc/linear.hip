@@ -190,19 +190,24 @@ __global__ __launch_bounds__(64 * WI * WJ) void gemm_kernel(const GemmArgs g) {
           if (e < count) out[e] = c[e];
       } else {
         if constexpr (EPI == EPI_FORWARD) {
+          with_activation(g.act, [&](auto act) {
 #pragma unroll
-          for (int e = 0; e < V; ++e) c[e] = activate<T>(c[e], g.act);
+            for (int e = 0; e < V; ++e) c[e] = activate<decltype(act)::value>(c[e]);
+          });
         }
         if (EPI == EPI_DZ || (EPI == EPI_FORWARD && g.extra)) {
           const Pack<T> p = load_some(static_cast<const T*>(g.extra) + row * g.extra_ld + j, count);
+          if constexpr (EPI == EPI_DZ) {
+            with_activation(g.act, [&](auto act) {
 #pragma unroll
-          for (int e = 0; e < V; ++e) {
-            if constexpr (EPI == EPI_DZ) {
-              c[e] = e < count ? activate_grad<T>(c[e], float(p.v[e]), g.act) : 0.0f;
-              sum[e] += c[e];
-            } else {
-              c[e] += float(p.v[e]);
-            }
+              for (int e = 0; e < V; ++e) {
+                c[e] = activate_grad<decltype(act)::value>(c[e], float(p.v[e]));
+                if (e < count) sum[e] += c[e];
+              }
+            });
+          } else {
+#pragma unroll
+            for (int e = 0; e < V; ++e) c[e] += float(p.v[e]);
           }
         }
         Pack<T> o;

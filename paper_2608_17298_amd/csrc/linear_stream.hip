@@ -26,6 +26,9 @@ constexpr int kForwardWaves = 4;
 constexpr int kForwardBytes = 64 * 1024;  // of the weight in LDS
 constexpr int kForwardBlocks = 2048;
 
+// Row strides up to which offsets inside a tile of rows fit 32 bits.
+constexpr int64_t kNear = int64_t(1) << 22;
+
 // KP: inputs, rounded up.  LDS rows are 16 bytes longer, which spreads the
 // rows that lanes read together over the banks.
 template <typename T, int KP>
@@ -46,9 +49,28 @@ __global__ __launch_bounds__(64 * kForwardWaves) void stream_forward_kernel(cons
   const T* x = static_cast<const T*>(a.x);
   const T* bias = static_cast<const T*>(a.bias);
   const T* res = static_cast<const T*>(a.residual);
-  const int64_t tiles = (a.m + 31) / 32;
-  for (int64_t t = int64_t(blockIdx.x) * kForwardWaves + tid / 64; t < tiles; t += int64_t(gridDim.x) * kForwardWaves) {
-    typename Pack<T>::V fx[2][S];
+  T* y = static_cast<T*>(a.y);
+  constexpr int Q = 8 / V;  // packs of outputs per lane: one of 8, or one of 4 from each tile
+  const int64_t tiles = (a.m + 31) / 32, step = int64_t(gridDim.x) * kForwardWaves;
+  // Whole tiles of rows of whole packs need no counts, and lanes' offsets in a tile are the same for all of them.
+  const bool full_k = a.k % V == 0 && a.x_ld <= kNear;
+  const bool full_n = a.n % V == 0 && a.y_ld <= kNear && a.residual_ld <= kNear;
+  const uint32_t x_off = uint32_t(r * a.x_ld + V * g), y_off = uint32_t(r * a.y_ld + (Q == 1 ? 8 : 4) * g),
+                 res_off = uint32_t(r * a.residual_ld + (Q == 1 ? 8 : 4) * g);
+  auto load_x = [&](int64_t t, typename Pack<T>::V(&fx)[2][S]) {
+    if (t >= tiles) return;
+    if (full_k && (t + 1) * 32 <= a.m) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const T* p = x + (t * 32 + 16 * i) * a.x_ld;
+#pragma unroll
+        for (int s = 0; s < S; ++s) {
+          fx[i][s] = T(0.0f);
+          if (s * kDepth<T> + V * g < a.k) fx[i][s] = load_pack(p + s * kDepth<T> + x_off).v;
+        }
+      }
+      return;
+    }
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       const int64_t row = t * 32 + 16 * i + r;
@@ -59,7 +81,27 @@ __global__ __launch_bounds__(64 * kForwardWaves) void stream_forward_kernel(cons
         if (row < a.m && k < a.k) fx[i][s] = load_some(x + row * a.x_ld + k, int(min(int64_t(V), a.k - k))).v;
       }
     }
+  };
+  const int64_t first = int64_t(blockIdx.x) * kForwardWaves + __builtin_amdgcn_readfirstlane(tid / 64);
+  typename Pack<T>::V fx[2][S], next[2][S];
+  load_x(first, next);
+  for (int64_t t = first; t < tiles; t += step) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int s = 0; s < S; ++s) fx[i][s] = next[i][s];
+    load_x(t + step, next);
+    const bool whole = full_n && (t + 1) * 32 <= a.m;
     for (int n0 = 0; n0 < n_pad; n0 += 32) {
+      Pack<T> p[2][Q];
+      if (res && whole) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int q = 0; q < Q; ++q)
+            if (n0 + 16 * q + (Q == 1 ? 8 : 4) * g < a.n)
+              p[i][q] = load_pack(res + (t * 32 + 16 * i) * a.residual_ld + n0 + 16 * q + res_off);
+      }
       f32x4 acc[2][2] = {};
 #pragma unroll
       for (int s = 0; s < S; ++s) {
@@ -70,31 +112,44 @@ __global__ __launch_bounds__(64 * kForwardWaves) void stream_forward_kernel(cons
           for (int i = 0; i < 2; ++i) acc[i][j] = Mfma<T>::run(fw, fx[i][s], acc[i][j]);
         }
       }
-      constexpr int Q = 8 / V;  // packs per lane: one of 8, or one of 4 from each tile
 #pragma unroll
       for (int q = 0; q < Q; ++q) {
         const int64_t n = n0 + (Q == 1 ? 8 * g : 16 * q + 4 * g);
         const int count = int(min(int64_t(V), a.n - n));
-        if (count <= 0) continue;
-        float b[V] = {};
-        if (bias) {
-          const Pack<T> p = load_some(bias + n, count);
+        float c[2][V];
 #pragma unroll
-          for (int e = 0; e < V; ++e) b[e] = float(p.v[e]);
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int e = 0; e < V; ++e) c[i][e] = acc[i][Q == 1 ? e / 4 : q][e % 4];
+        if (bias && count > 0) {
+          const Pack<T> b = load_some(bias + n, count);
+#pragma unroll
+          for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int e = 0; e < V; ++e) c[i][e] += float(b.v[e]);
         }
+        with_activation(a.act, [&](auto act) {
+#pragma unroll
+          for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int e = 0; e < V; ++e) c[i][e] = activate<decltype(act)::value>(c[i][e]);
+        });
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
           const int64_t row = t * 32 + 16 * i + r;
-          if (row >= a.m) continue;
-          Pack<T> o, p;
-          if (res) p = load_some(res + row * a.residual_ld + n, count);
+          const bool here = row < a.m && count > 0;
+          if (res) {
+            if (!whole && here) p[i][q] = load_some(res + row * a.residual_ld + n, count);
 #pragma unroll
-          for (int e = 0; e < V; ++e) {
-            float c = activate<T>(acc[i][Q == 1 ? e / 4 : q][e % 4] + b[e], a.act);
-            if (res) c += float(p.v[e]);
-            o.v[e] = T(c);
+            for (int e = 0; e < V; ++e) c[i][e] += float(p[i][q].v[e]);
           }
-          store_some(static_cast<T*>(a.y) + row * a.y_ld + n, o, count);
+          Pack<T> o;
+#pragma unroll
+          for (int e = 0; e < V; ++e) o.v[e] = T(c[i][e]);
+          if (whole && count > 0)
+            store_pack(y + (t * 32 + 16 * i) * a.y_ld + n0 + 16 * q + y_off, o);
+          else if (!whole && here)
+            store_some(y + row * a.y_ld + n, o, count);
         }
       }
     }
@@ -118,14 +173,15 @@ struct BackwardShape {
 };
 
 template <typename T, int KP, int NS>
-__global__ __launch_bounds__((BackwardShape<T, KP, NS>::THREADS)) void stream_backward_kernel(
+__global__ __launch_bounds__((BackwardShape<T, KP, NS>::THREADS), (KP * sizeof(T) <= 128 && NS <= 4 ? 2 : 1)) void stream_backward_kernel(
     const LinearArgs a, float* __restrict__ partial, float* __restrict__ sums, int64_t tiles) {
   using B = BackwardShape<T, KP, NS>;
   constexpr int V = Pack<T>::N, D = kDepth<T>, S = KP / D, KT = KP / 16, Q = 8 / V;
   constexpr int MT = B::GROUP_ROWS / 16;
   __shared__ __attribute__((aligned(16))) T lds[B::W + B::X + B::Z];
   T *lw = lds, *lx = lds + B::W, *lz = lx + B::X;
-  const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64, r = lane % 16, g = lane / 16;
+  const int tid = threadIdx.x, lane = tid % 64, wave = __builtin_amdgcn_readfirstlane(tid / 64);
+  const int r = lane % 16, g = lane / 16;
   const int slice = wave % NS, group = wave / NS;
   const T* x = static_cast<const T*>(a.x);
   const T* dl = static_cast<const T*>(a.dl);
@@ -139,7 +195,7 @@ __global__ __launch_bounds__((BackwardShape<T, KP, NS>::THREADS)) void stream_ba
   }
 
   // a lane's outputs: n0(q) + 0 .. V-1
-  auto n0 = [&](int q) { return 32 * slice + (Q == 1 ? 8 * g : 16 * q + 4 * g); };
+  const auto n0 = [&](int q) { return 32 * slice + (Q == 1 ? 8 * g : 16 * q + 4 * g); };
   float b[8] = {}, sum_b[8] = {};
   if (a.bias) {
 #pragma unroll
@@ -158,8 +214,23 @@ __global__ __launch_bounds__((BackwardShape<T, KP, NS>::THREADS)) void stream_ba
 
   constexpr int XALL = B::ROWS * (KP / V), XP = (XALL + B::THREADS - 1) / B::THREADS;  // x packs, per thread
   constexpr bool XEVEN = XALL % B::THREADS == 0;
+  // Whole tiles of rows of whole packs need no counts, and lanes' offsets in a tile are the same for all of them.
+  const bool full = a.k % V == 0 && a.n % V == 0 && a.x_ld <= kNear && a.dl_ld <= kNear && a.g_x_ld <= kNear && XEVEN;
+  constexpr int XSTEP = B::THREADS / (KP / V);  // rows that one pack a thread covers
+  const uint32_t x_off = uint32_t(tid / (KP / V) * a.x_ld + tid % (KP / V) * V),
+                 dl_off = uint32_t((group * B::GROUP_ROWS + r) * a.dl_ld + n0(0)),
+                 gx_off = uint32_t(r * a.g_x_ld + (Q == 1 ? 8 : 4) * g);
   Pack<T> xr[XP], dr[MT][Q];
   auto load_x = [&](int64_t t) {
+    if (full && (t + 1) * B::ROWS <= a.m) {
+      const T* p = x + t * B::ROWS * a.x_ld;
+#pragma unroll
+      for (int u = 0; u < XP; ++u) {
+        xr[u].v = T(0.0f);
+        if (tid % (KP / V) * V < a.k) xr[u] = load_pack(p + u * XSTEP * a.x_ld + x_off);
+      }
+      return;
+    }
 #pragma unroll
     for (int u = 0; u < XP; ++u) {
       const int c = u * B::THREADS + tid;
@@ -171,6 +242,17 @@ __global__ __launch_bounds__((BackwardShape<T, KP, NS>::THREADS)) void stream_ba
     }
   };
   auto load_dl = [&](int64_t t) {
+    if (full && (t + 1) * B::ROWS <= a.m) {
+      const T* p = dl + t * B::ROWS * a.dl_ld;
+#pragma unroll
+      for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int q = 0; q < Q; ++q) {
+          dr[i][q].v = T(0.0f);
+          if (n0(q) < a.n) dr[i][q] = load_pack(p + 16 * i * a.dl_ld + 16 * q + dl_off);
+        }
+      return;
+    }
 #pragma unroll
     for (int i = 0; i < MT; ++i) {
       const int64_t row = t * B::ROWS + group * B::GROUP_ROWS + 16 * i + r;
@@ -200,6 +282,7 @@ __global__ __launch_bounds__((BackwardShape<T, KP, NS>::THREADS)) void stream_ba
     }
     __syncthreads();  // x is there; g_x of the last tile has read dz
     load_x(t + gridDim.x);
+    const bool whole = (t + 1) * B::ROWS <= a.m;
     // dz of this wave's rows and outputs
 #pragma unroll
     for (int i = 0; i < MT; ++i) {
@@ -213,16 +296,26 @@ __global__ __launch_bounds__((BackwardShape<T, KP, NS>::THREADS)) void stream_ba
           for (int j = 0; j < 2; ++j) z[j] = Mfma<T>::run(fw[j][s], fx, z[j]);
         }
       }
-      const bool real = t * B::ROWS + lrow < a.m;
+      float d[8];
+      with_activation(a.act, [&](auto act) {
+#pragma unroll
+        for (int q = 0; q < Q; ++q)
+#pragma unroll
+          for (int e = 0; e < V; ++e)
+            d[q * V + e] = activate_grad<decltype(act)::value>(z[Q == 1 ? e / 4 : q][e % 4] + b[q * V + e],
+                                                               float(dr[i][q].v[e]));
+      });
+      if (!whole && t * B::ROWS + lrow >= a.m) {  // a row that is not there has a slope all the same
+#pragma unroll
+        for (int e = 0; e < 8; ++e) d[e] = 0.0f;
+      }
 #pragma unroll
       for (int q = 0; q < Q; ++q) {
         Pack<T> o;
 #pragma unroll
         for (int e = 0; e < V; ++e) {
-          const float d = activate_grad<T>(z[Q == 1 ? e / 4 : q][e % 4] + b[q * V + e], float(dr[i][q].v[e]), a.act);
-          const float kept = real ? d : 0.0f;  // a row that is not there has a slope all the same
-          sum_b[q * V + e] += kept;
-          o.v[e] = T(kept);
+          sum_b[q * V + e] += d[q * V + e];
+          o.v[e] = T(d[q * V + e]);
         }
         *reinterpret_cast<typename Pack<T>::V*>(lz + lrow * B::NPITCH + n0(q)) = o.v;
       }
@@ -267,11 +360,13 @@ __global__ __launch_bounds__((BackwardShape<T, KP, NS>::THREADS)) void stream_ba
 #pragma unroll
           for (int q = 0; q < Q; ++q) {
             const int64_t k = 16 * kt + (Q == 1 ? 8 * g : 16 * q + 4 * g);
-            if (row >= a.m || k >= a.k) continue;
             Pack<T> o;
 #pragma unroll
             for (int e = 0; e < V; ++e) o.v[e] = T(acc[i][Q == 1 ? e / 4 : q][e % 4]);
-            store_some(static_cast<T*>(a.g_x) + row * a.g_x_ld + k, o, int(min(int64_t(V), a.k - k)));
+            if (full && whole && k < a.k)
+              store_pack(static_cast<T*>(a.g_x) + (t * B::ROWS + r0 + 16 * i) * a.g_x_ld + 16 * (kt + q) + gx_off, o);
+            else if (!(full && whole) && row < a.m && k < a.k)
+              store_some(static_cast<T*>(a.g_x) + row * a.g_x_ld + k, o, int(min(int64_t(V), a.k - k)));
           }
         }
       }
@@ -315,9 +410,14 @@ int round_inputs(int64_t k) {
 
 int forward_lds(int kp, int64_t n, size_t es) { return int((n + 31) / 32 * 32 * (kp + 16 / int(es)) * int64_t(es)); }
 
+// At most `most` blocks, all with the same number of turns (or one less).
+int64_t even_blocks(int64_t turns, int64_t most) {
+  return turns <= most ? turns : ceil_div64(turns, ceil_div64(turns, most));
+}
+
 template <typename T, int KP>
 hipError_t forward_kp(const LinearArgs& a, hipStream_t s) {
-  const int64_t blocks = std::min<int64_t>(ceil_div64(ceil_div64(a.m, 32), kForwardWaves), kForwardBlocks);
+  const int64_t blocks = even_blocks(ceil_div64(ceil_div64(a.m, 32), kForwardWaves), kForwardBlocks);
   stream_forward_kernel<T, KP><<<uint32_t(blocks), 64 * kForwardWaves, forward_lds(KP, a.n, sizeof(T)), s>>>(a);
   return hipGetLastError();
 }
@@ -377,7 +477,7 @@ hipError_t backward_run(const LinearArgs& a, float* partial, float* sums, hipStr
   if constexpr (B::FITS) {
     const int64_t tiles = ceil_div64(a.m, B::ROWS);
     stream_backward_kernel<T, KP, NS>
-        <<<uint32_t(std::min(tiles, kBackwardBlocks)), B::THREADS, 0, s>>>(a, partial, sums, tiles);
+        <<<uint32_t(even_blocks(tiles, kBackwardBlocks)), B::THREADS, 0, s>>>(a, partial, sums, tiles);
     return hipGetLastError();
   }
   return hipErrorInvalidValue;
@@ -420,7 +520,7 @@ hipError_t launch_stream_forward(const LinearArgs& a, gart_dtype t, hipStream_t 
 int64_t stream_backward_parts(int64_t m, int64_t k, int64_t n, gart_dtype t) {
   if (m <= 0 || k <= 0 || n <= 0) return 0;
   const BackwardChoice c = choose(k, n, t);
-  return c.kp == 0 ? 0 : std::min(ceil_div64(m, c.rows), kBackwardBlocks) * c.groups;
+  return c.kp == 0 ? 0 : even_blocks(ceil_div64(m, c.rows), kBackwardBlocks) * c.groups;
 }
 
 hipError_t launch_stream_backward(const LinearArgs& a, float* partial, float* sums, gart_dtype t, hipStream_t s) {

@@ -558,7 +558,9 @@ def _stream_on(stream, like: torch.Tensor):
     """The raw stream of the call: `stream`, or the current one of the tensors' GPU, which must be the current GPU."""
     if like.device.index != torch.cuda.current_device():
         raise ValueError(f"tensors are on {like.device}, the current GPU is {torch.cuda.current_device()}")
-    return (torch.cuda.current_stream() if stream is None else stream).cuda_stream
+    if stream is None:  # the raw handle: a Stream object costs as much as the launch
+        return torch._C._cuda_getCurrentRawStream(like.device.index)
+    return stream.cuda_stream
 
 
 def _act(act) -> int:
