@@ -110,9 +110,22 @@ __device__ __forceinline__ typename Pack<T>::V fragment_of_row(const T* lds, int
   return *reinterpret_cast<const typename Pack<T>::V*>(lds + row * pitch + k0 + Pack<T>::N * g);
 }
 
-// From LDS lines across k (line k holds the rows' elements side by side).  16
-// bits: the lanes of a group of 16 name four k times 16 columns, four a lane,
-// and the transposing load gives each the four k of its column.
+// 16 bits, from lines across k: the lanes of a group of 16 name four lines times
+// 16 columns, four columns a lane, and the transposing load gives each lane the
+// four k of its column; the other four k lie `down` elements on.
+template <typename T>
+__device__ __forceinline__ typename Pack<T>::V transposed_pair(const T* lds, int down) {
+  typedef short s16x4 __attribute__((ext_vector_type(4)));
+  typedef __attribute__((address_space(3))) s16x4* lds_ptr;
+  const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(lds));
+  const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(lds + down));
+  typename Pack<T>::V v;
+  __builtin_memcpy(&v, &lo, 8);
+  __builtin_memcpy(reinterpret_cast<char*>(&v) + 8, &hi, 8);
+  return v;
+}
+
+// From LDS lines across k (line k holds the rows' elements side by side).
 template <typename T, bool PAIRED>
 __device__ __forceinline__ typename Pack<T>::V fragment_of_columns(const T* lds, int pitch, int tile, int k0, int lane) {
   const int r = lane % 16, g = lane / 16;
@@ -122,25 +135,61 @@ __device__ __forceinline__ typename Pack<T>::V fragment_of_columns(const T* lds,
 #pragma unroll
     for (int t = 0; t < 4; ++t) v[t] = q[t * pitch];
   } else {
-    typedef short s16x4 __attribute__((ext_vector_type(4)));
-    typedef __attribute__((address_space(3))) s16x4* lds_ptr;
     const int col = PAIRED ? paired_row<T>(tile, 4 * (r % 4)) : 16 * tile + 4 * (r % 4);
-    const T* q = lds + (k0 + 8 * g + r / 4) * pitch + col;
-    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(q));
-    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(q + 4 * pitch));
-    __builtin_memcpy(&v, &lo, 8);
-    __builtin_memcpy(reinterpret_cast<char*>(&v) + 8, &hi, 8);
+    v = transposed_pair(lds + (k0 + 8 * g + r / 4) * pitch + col, 4 * pitch);
   }
   return v;
 }
 
-// ---- linear_stream.hip ---------------------------------------------------------
+// ---- how the work is cut (linear.hip) --------------------------------------------
+// Products that do not stream: tiles of 256 (one block of 8 waves a CU, straight
+// into LDS) where they fill the card, else of 128, else of 64; where even these
+// are few, the sums are cut into parts, which are joined afterwards.
+struct Cut {
+  int tile;
+  int64_t part, parts;
+};
+// most: parts at most; wide: alignment and sizes allow tiles of 256
+Cut cut_product(int64_t rows, int64_t cols, int64_t depth, int64_t most, bool wide);
+constexpr int64_t kJoinParts = 16;      // of y, dz and g_x, whose join has an epilogue
+constexpr int64_t kWeightParts = 1024;  // of g_weight
+constexpr int kJoinRows = 32;           // rows per column sum of a joined dz
+constexpr int kSumRows = 256;           // rows per column sum of dl
+constexpr int64_t kFewRows = 64;        // rows up to which every block takes all of them
+
+struct BackwardPlan {
+  bool stream;
+  int64_t parts, sum_parts;  // partial sums of g_weight and g_bias (stream)
+  int64_t dz_ld;
+  size_t dz, partial, sums, total;
+};
+BackwardPlan backward_plan(int64_t m, int64_t k, int64_t n, gart_dtype t, gart_activation act);
+
+template <typename T>
+constexpr gart_dtype kType = sizeof(T) == 4 ? GART_DTYPE_F32 : std::is_same<T, bf16>::value ? GART_DTYPE_BF16 : GART_DTYPE_F16;
+
+// ---- linear_rows.h, linear_stream.h, linear_gemm.h: one of each per type -----------
+inline bool few_rows(int64_t m, int64_t n) { return m <= kFewRows && n <= int64_t(1) << 24; }
+// y, or dz and g_bias's sum, of up to kFewRows rows
+template <typename T>
+hipError_t rows_forward(const LinearArgs& a, hipStream_t s);
+template <typename T>
+hipError_t rows_dz(const LinearArgs& a, void* dz, int64_t dz_ld, float* sums, hipStream_t s);
+
 // Layers whose weight fits LDS: the rows stream past it once.
-bool stream_forward_fits(int64_t k, int64_t n, gart_dtype t);
-hipError_t launch_stream_forward(const LinearArgs& a, gart_dtype t, hipStream_t s);
-// Parts whose partial sums launch_stream_backward leaves: partial [parts, n, k]
-// and sums [parts, n] (0: the layer does not fit).
-int64_t stream_backward_parts(int64_t m, int64_t k, int64_t n, gart_dtype t);
-hipError_t launch_stream_backward(const LinearArgs& a, float* partial, float* sums, gart_dtype t, hipStream_t s);
+bool stream_forward_fits(int64_t k, int64_t n, size_t es);
+// Parts whose partial sums the backward leaves: partial [parts, n, k], sums
+// [parts, n] (0: the layer does not fit).
+int64_t stream_backward_parts(int64_t m, int64_t k, int64_t n, size_t es);
+template <typename T>
+hipError_t stream_forward(const LinearArgs& a, hipStream_t s);
+template <typename T>
+hipError_t stream_backward(const LinearArgs& a, float* partial, float* sums, hipStream_t s);
+
+template <typename T>
+hipError_t gemm_forward(const LinearArgs& a, hipStream_t s);
+// everything after the plan, streams included
+template <typename T>
+hipError_t gemm_backward(const LinearArgs& a, hipStream_t s);
 
 }  // namespace gart

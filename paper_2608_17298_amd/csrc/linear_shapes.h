@@ -1,0 +1,77 @@
+// Sizes and block counts of the streaming forward and backward, shared by
+// their launchers and by the scratch they are given.
+#pragma once
+
+#include <algorithm>
+
+#include "linear.h"
+
+namespace gart {
+
+// ---- forward ---------------------------------------------------------------------
+constexpr int kForwardWaves = 4;
+constexpr int kForwardBytes = 64 * 1024;  // of the weight in LDS
+constexpr int kForwardBlocks = 2048;
+
+inline int round_inputs(int64_t k) {
+  int p = 32;
+  while (p < k && p < 512) p *= 2;
+  return p;
+}
+
+inline int64_t forward_lds(int kp, int64_t n, size_t es) { return (n + 31) / 32 * 32 * (kp + 16 / int64_t(es)) * int64_t(es); }
+
+// At most `most` blocks, all with the same number of turns (or one less).
+inline int64_t even_blocks(int64_t turns, int64_t most) {
+  return turns <= most ? turns : ceil_div64(turns, ceil_div64(turns, most));
+}
+
+// ---- backward --------------------------------------------------------------------
+// NS: waves side by side over the outputs, 32 each.  With few of them, RG
+// groups of NS waves take rows of their own in a tile.
+template <size_t ES, int KP, int NS>
+struct BackwardSizes {
+  static constexpr int RG = NS == 1 ? 4 : NS == 2 ? 2 : 1;
+  static constexpr int WAVES = NS * RG, THREADS = 64 * WAVES;
+  static constexpr int GROUP_ROWS = NS >= 4 ? 64 : 32, ROWS = GROUP_ROWS * RG;
+  static constexpr int NP = 32 * NS;
+  static constexpr int PAD = ES == 2 ? 16 : 4;  // spreads rows (and columns' lines) over the banks
+  static constexpr int KPITCH = KP + PAD, NPITCH = NP + PAD;
+  static constexpr int W = NP * KPITCH, X = ROWS * KPITCH, Z = ROWS * NPITCH;
+  static constexpr size_t BYTES = size_t(W + X + Z) * ES;
+  static constexpr bool FITS = BYTES <= 160 * 1024 && KP * int(ES) <= 512;
+};
+
+// Blocks: two of four waves for each of the 256 CUs; their partial sums are then
+// far fewer than the rows.
+constexpr int64_t kBackwardBlocks = 512;
+
+struct BackwardChoice {
+  int kp, ns, rows, groups;  // kp 0: none
+};
+
+template <size_t ES, int KP, int NS>
+bool offer(int64_t k, int64_t n, BackwardChoice* c) {
+  using B = BackwardSizes<ES, KP, NS>;
+  if (!B::FITS || k > KP || n > 32 * NS) return false;
+  *c = BackwardChoice{KP, NS, B::ROWS, B::RG};
+  return true;
+}
+
+template <size_t ES, int KP>
+bool offer_inputs(int64_t k, int64_t n, BackwardChoice* c) {
+  return offer<ES, KP, 1>(k, n, c) || offer<ES, KP, 2>(k, n, c) || offer<ES, KP, 4>(k, n, c) ||
+         offer<ES, KP, 8>(k, n, c);
+}
+
+template <size_t ES>
+BackwardChoice choose(int64_t k, int64_t n) {
+  BackwardChoice c{};
+  if (!(offer_inputs<ES, 32>(k, n, &c) || offer_inputs<ES, 64>(k, n, &c) || offer_inputs<ES, 128>(k, n, &c)))
+    offer_inputs<ES, 256>(k, n, &c);
+  return c;
+}
+
+inline BackwardChoice choose_backward(int64_t k, int64_t n, size_t es) { return es == 4 ? choose<4>(k, n) : choose<2>(k, n); }
+
+}  // namespace gart

@@ -14,18 +14,16 @@
 //   registers for all of the block's tiles;
 //   g_x (rows, k) = dz W, stored.
 // Each block leaves one partial sum of g_weight and g_bias.
+#pragma once
+
 #include <algorithm>
 
-#include "linear.h"
+#include "linear_shapes.h"
 
 namespace gart {
 namespace {
 
 // ---- forward -----------------------------------------------------------------
-constexpr int kForwardWaves = 4;
-constexpr int kForwardBytes = 64 * 1024;  // of the weight in LDS
-constexpr int kForwardBlocks = 2048;
-
 // Row strides up to which offsets inside a tile of rows fit 32 bits.
 constexpr int64_t kNear = int64_t(1) << 22;
 
@@ -157,20 +155,8 @@ __global__ __launch_bounds__(64 * kForwardWaves) void stream_forward_kernel(cons
 }
 
 // ---- backward ------------------------------------------------------------------
-// NS: waves side by side over the outputs, 32 each.  With few of them, RG
-// groups of NS waves take rows of their own in a tile.
 template <typename T, int KP, int NS>
-struct BackwardShape {
-  static constexpr int RG = NS == 1 ? 4 : NS == 2 ? 2 : 1;
-  static constexpr int WAVES = NS * RG, THREADS = 64 * WAVES;
-  static constexpr int GROUP_ROWS = NS >= 4 ? 64 : 32, ROWS = GROUP_ROWS * RG;
-  static constexpr int NP = 32 * NS;
-  static constexpr int PAD = sizeof(T) == 2 ? 16 : 4;  // spreads rows (and columns' lines) over the banks
-  static constexpr int KPITCH = KP + PAD, NPITCH = NP + PAD;
-  static constexpr int W = NP * KPITCH, X = ROWS * KPITCH, Z = ROWS * NPITCH;
-  static constexpr size_t BYTES = size_t(W + X + Z) * sizeof(T);
-  static constexpr bool FITS = BYTES <= 160 * 1024 && KP * int(sizeof(T)) <= 512;
-};
+using BackwardShape = BackwardSizes<sizeof(T), KP, NS>;
 
 template <typename T, int KP, int NS>
 __global__ __launch_bounds__((BackwardShape<T, KP, NS>::THREADS), (KP * sizeof(T) <= 128 && NS <= 4 ? 2 : 1)) void stream_backward_kernel(
@@ -402,73 +388,12 @@ __global__ __launch_bounds__((BackwardShape<T, KP, NS>::THREADS), (KP * sizeof(T
 }
 
 // ---- launches --------------------------------------------------------------------
-int round_inputs(int64_t k) {
-  int p = 32;
-  while (p < k && p < 512) p *= 2;
-  return p;
-}
-
-int forward_lds(int kp, int64_t n, size_t es) { return int((n + 31) / 32 * 32 * (kp + 16 / int(es)) * int64_t(es)); }
-
-// At most `most` blocks, all with the same number of turns (or one less).
-int64_t even_blocks(int64_t turns, int64_t most) {
-  return turns <= most ? turns : ceil_div64(turns, ceil_div64(turns, most));
-}
-
 template <typename T, int KP>
 hipError_t forward_kp(const LinearArgs& a, hipStream_t s) {
   const int64_t blocks = even_blocks(ceil_div64(ceil_div64(a.m, 32), kForwardWaves), kForwardBlocks);
-  stream_forward_kernel<T, KP><<<uint32_t(blocks), 64 * kForwardWaves, forward_lds(KP, a.n, sizeof(T)), s>>>(a);
+  stream_forward_kernel<T, KP>
+      <<<uint32_t(blocks), 64 * kForwardWaves, forward_lds(KP, a.n, sizeof(T)), s>>>(a);
   return hipGetLastError();
-}
-
-template <typename T>
-hipError_t forward(const LinearArgs& a, hipStream_t s) {
-  switch (round_inputs(a.k)) {
-    case 32: return forward_kp<T, 32>(a, s);
-    case 64: return forward_kp<T, 64>(a, s);
-    case 128: return forward_kp<T, 128>(a, s);
-    default:
-      if constexpr (sizeof(T) == 2) return forward_kp<T, 256>(a, s);
-      return hipErrorInvalidValue;
-  }
-}
-
-// Blocks: about two of four waves for each of the 256 CUs; their partial sums
-// are then far fewer than the rows.
-constexpr int64_t kBackwardBlocks = 512;
-
-struct BackwardChoice {
-  int kp, ns, rows, groups;  // kp 0: none
-};
-
-template <typename T, int KP, int NS>
-bool offer(int64_t k, int64_t n, BackwardChoice* c) {
-  using B = BackwardShape<T, KP, NS>;
-  if constexpr (B::FITS) {
-    if (k <= KP && n <= 32 * NS) {
-      *c = BackwardChoice{KP, NS, B::ROWS, B::RG};
-      return true;
-    }
-  }
-  return false;
-}
-
-template <typename T, int KP>
-bool offer_ns(int64_t k, int64_t n, BackwardChoice* c) {
-  return offer<T, KP, 1>(k, n, c) || offer<T, KP, 2>(k, n, c) || offer<T, KP, 4>(k, n, c) || offer<T, KP, 8>(k, n, c);
-}
-
-template <typename T>
-BackwardChoice choose(int64_t k, int64_t n) {
-  BackwardChoice c{};
-  if (!(offer_ns<T, 32>(k, n, &c) || offer_ns<T, 64>(k, n, &c) || offer_ns<T, 128>(k, n, &c)))
-    offer_ns<T, 256>(k, n, &c);
-  return c;
-}
-
-BackwardChoice choose(int64_t k, int64_t n, gart_dtype t) {
-  return t == GART_DTYPE_F32 ? choose<float>(k, n) : choose<bf16>(k, n);
 }
 
 template <typename T, int KP, int NS>
@@ -493,8 +418,23 @@ hipError_t backward_kp(const LinearArgs& a, int ns, float* partial, float* sums,
   }
 }
 
+}  // namespace
+
 template <typename T>
-hipError_t backward(const LinearArgs& a, const BackwardChoice& c, float* partial, float* sums, hipStream_t s) {
+hipError_t stream_forward(const LinearArgs& a, hipStream_t s) {
+  switch (round_inputs(a.k)) {
+    case 32: return forward_kp<T, 32>(a, s);
+    case 64: return forward_kp<T, 64>(a, s);
+    case 128: return forward_kp<T, 128>(a, s);
+    default:
+      if constexpr (sizeof(T) == 2) return forward_kp<T, 256>(a, s);
+      return hipErrorInvalidValue;
+  }
+}
+
+template <typename T>
+hipError_t stream_backward(const LinearArgs& a, float* partial, float* sums, hipStream_t s) {
+  const BackwardChoice c = choose_backward(a.k, a.n, sizeof(T));
   switch (c.kp) {
     case 32: return backward_kp<T, 32>(a, c.ns, partial, sums, s);
     case 64: return backward_kp<T, 64>(a, c.ns, partial, sums, s);
@@ -502,32 +442,6 @@ hipError_t backward(const LinearArgs& a, const BackwardChoice& c, float* partial
     case 256: return backward_kp<T, 256>(a, c.ns, partial, sums, s);
   }
   return hipErrorInvalidValue;
-}
-
-}  // namespace
-
-bool stream_forward_fits(int64_t k, int64_t n, gart_dtype t) {
-  const size_t es = dtype_bytes(t);
-  return k <= 512 / int64_t(es) && n <= 2048 && forward_lds(round_inputs(k), n, es) <= kForwardBytes;
-}
-
-hipError_t launch_stream_forward(const LinearArgs& a, gart_dtype t, hipStream_t s) {
-  if (t == GART_DTYPE_F32) return forward<float>(a, s);
-  if (t == GART_DTYPE_BF16) return forward<bf16>(a, s);
-  return forward<f16>(a, s);
-}
-
-int64_t stream_backward_parts(int64_t m, int64_t k, int64_t n, gart_dtype t) {
-  if (m <= 0 || k <= 0 || n <= 0) return 0;
-  const BackwardChoice c = choose(k, n, t);
-  return c.kp == 0 ? 0 : even_blocks(ceil_div64(m, c.rows), kBackwardBlocks) * c.groups;
-}
-
-hipError_t launch_stream_backward(const LinearArgs& a, float* partial, float* sums, gart_dtype t, hipStream_t s) {
-  const BackwardChoice c = choose(a.k, a.n, t);
-  if (t == GART_DTYPE_F32) return backward<float>(a, c, partial, sums, s);
-  if (t == GART_DTYPE_BF16) return backward<bf16>(a, c, partial, sums, s);
-  return backward<f16>(a, c, partial, sums, s);
 }
 
 }  // namespace gart

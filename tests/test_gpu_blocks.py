@@ -195,6 +195,32 @@ def test_linear_backward(m, k, n, dtype, act, bias, pad):
         _within(got[0][q], want[q], tol[q])
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("m,k,n,pad", [(3592, 64, 4040, 0), (3592, 4040, 64, 8), (64, 3592, 4040, 0), (100, 4040, 72, 0),
+                                       (70, 2000, 96, 3), (2000, 300, 500, 0), (90, 1000, 1000, 0), (40, 1500, 700, 8),
+                                       (20000, 272, 40, 0)])
+def test_linear_larger_sizes(m, k, n, pad, dtype):
+    """Tiles of every size, sums cut into parts, products that go straight into LDS: forward and gradients."""
+    from paper_2608_17298_amd import gart
+    rng = np.random.default_rng(m + k)
+    x, x64 = _mat(rng, m, k, dtype, pad)
+    w, w64 = _mat(rng, n, k, dtype, pad, k ** -0.5)
+    b, b64 = _vec(rng, n, dtype)
+    r, r64 = _mat(rng, m, n, dtype, pad)
+    t = _torch(dtype)
+    y = _Out(m, n, dtype, pad)
+    gart.gart_linear(x, w, y.t, b, r, "silu", _scratch(gart.gart_linear_scratch_bytes(m, k, n, t)))
+    _within(y.value(), ref.linear(x64, w64, b64, r64, "silu"), ref.linear_tolerance(x64, w64, b64, r64, "silu", dtype))
+    for act in ("gelu", "none"):
+        gx, gw, gb = _Out(m, k, dtype, pad), _Out(n, k, dtype, pad), _Out(1, n, dtype, 0)
+        scratch = _scratch(gart.gart_linear_backward_scratch_bytes(m, k, n, t, act))
+        gart.gart_linear_backward(x, w, r, gx.t, gw.t, gb.t.reshape(-1), b, act, scratch)
+        want = ref.linear_grads(x64, w64, b64, r64, act)
+        tol = ref.linear_grads_tolerance(x64, w64, b64, r64, act, dtype)
+        for got, a, c in zip((gx.value(), gw.value(), gb.value()[0]), want, tol):
+            _within(got, a, c)
+
+
 @pytest.mark.parametrize("want_x,want_w,want_b", [(1, 0, 0), (0, 1, 0), (0, 0, 1), (1, 0, 1)])
 @pytest.mark.parametrize("act", ["none", "gelu"])
 def test_linear_backward_some_outputs(want_x, want_w, want_b, act):
