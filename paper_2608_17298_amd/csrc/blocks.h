@@ -43,6 +43,13 @@ __device__ __forceinline__ void store_pack(T* p, const Pack<T>& r) {
   *reinterpret_cast<packed16*>(p) = q;
 }
 
+// A value the compiler takes for new, so that comparisons with it are made where
+// they are needed and not held through a loop (in scalar registers, which spill).
+__device__ __forceinline__ int fresh(int v) {
+  asm volatile("" : "+v"(v));
+  return v;
+}
+
 // The first `count` elements at p, the rest zero.
 template <typename T>
 __device__ __forceinline__ Pack<T> load_some(const T* p, int count) {
@@ -51,6 +58,37 @@ __device__ __forceinline__ Pack<T> load_some(const T* p, int count) {
 #pragma unroll
   for (int e = 0; e < Pack<T>::N; ++e) r.v[e] = e < count ? p[e] : T(0.0f);
   return r;
+}
+
+// Bits of a pack's first `count` elements: for packs that may be read whole in
+// any case (there are rows after them), without a branch.
+template <typename T>
+struct PackMask {
+  uint32_t w[4];
+};
+
+template <typename T>
+__device__ __forceinline__ PackMask<T> first_of_pack(int count) {
+  PackMask<T> m;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (sizeof(T) == 4)
+      m.w[i] = count > i ? ~0u : 0u;
+    else
+      m.w[i] = count > 2 * i + 1 ? ~0u : count == 2 * i + 1 ? 0xFFFFu : 0u;
+  }
+  return m;
+}
+
+template <typename T>
+__device__ __forceinline__ Pack<T> load_masked(const T* p, const PackMask<T>& m) {
+  const packed16 r = *reinterpret_cast<const packed16*>(p);
+  packed16 q;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) q.w[i] = r.w[i] & m.w[i];
+  Pack<T> v;
+  __builtin_memcpy(&v, &q, 16);
+  return v;
 }
 
 template <typename T>

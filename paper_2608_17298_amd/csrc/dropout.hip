@@ -99,6 +99,51 @@ __global__ __launch_bounds__(kThreads) void dropout_kernel(const DropoutArgs a) 
   }
 }
 
+// Short strided rows, where few draws stay inside one: a wave draws for 512
+// elements, its lanes hand the bits over through LDS and then take every 64th
+// element, so that neighbours in memory are neighbours in the wave.
+constexpr int kWaveElements = 64 * kDraw;
+template <typename T>
+__global__ __launch_bounds__(kThreads) void dropout_short_rows_kernel(const DropoutArgs a) {
+  __shared__ __attribute__((aligned(16))) uint16_t s_bits[kThreads / 64][kWaveElements];
+  const T* x = static_cast<const T*>(a.x);
+  const T* res = static_cast<const T*>(a.residual);
+  T* y = static_cast<T*>(a.y);
+  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+  const int64_t total = a.rows * a.cols;
+  const uint32_t cols = uint32_t(a.cols), down = 64 / cols, right = 64 % cols;
+  uint16_t* bits = s_bits[wave];
+  for (int64_t b = int64_t(blockIdx.x) * kThreads * kDraw; b < total; b += int64_t(gridDim.x) * kThreads * kDraw) {
+    const int64_t base = b + wave * kWaveElements;
+    const Words w = philox(uint64_t(base / kDraw + lane), a.offset, a.seed);
+    *reinterpret_cast<uint4*>(bits + lane * kDraw) = make_uint4(w.w[0], w.w[1], w.w[2], w.w[3]);
+    __syncthreads();
+    const int64_t brow = b / a.cols;  // the same for the block
+    const uint32_t c = uint32_t(b - brow * a.cols) + uint32_t(wave * kWaveElements + lane);
+    int64_t row = brow + c / cols;
+    uint32_t col = c % cols;
+#pragma unroll
+    for (int q = 0; q < kDraw; ++q) {
+      if (base + 64 * q + lane < total) {
+        float o = bits[64 * q + lane] >= a.threshold ? float(x[row * a.x_ld + col]) * a.scale : 0.0f;
+        if (res) o += float(res[row * a.residual_ld + col]);
+        y[row * a.y_ld + col] = T(o);
+      }
+      row += down;
+      col += right;
+      if (col >= cols) {
+        col -= cols;
+        ++row;
+      }
+    }
+    __syncthreads();
+  }
+}
+
+// Row lengths below which the kernel for short rows is faster (strided rows of 6:
+// 11 us against 37, of 33: 18 against 24, of 100: 24.6 against 20.7).
+constexpr int64_t kShortRow = 64;
+
 template <typename T>
 hipError_t launch(DropoutArgs a, hipStream_t s) {
   if (a.rows <= 0 || a.cols <= 0) return hipSuccess;
@@ -109,7 +154,9 @@ hipError_t launch(DropoutArgs a, hipStream_t s) {
   }
   const int64_t blocks = ceil_div64(ceil_div64(a.rows * a.cols, kDraw), kThreads);
   const dim3 grid(uint32_t(blocks < kMaxBlocks ? blocks : kMaxBlocks));
-  if (flat)
+  if (!flat && a.cols % kDraw != 0 && a.cols < kShortRow)
+    dropout_short_rows_kernel<T><<<grid, kThreads, 0, s>>>(a);
+  else if (flat)
     dropout_kernel<T, true><<<grid, kThreads, 0, s>>>(a);
   else
     dropout_kernel<T, false><<<grid, kThreads, 0, s>>>(a);

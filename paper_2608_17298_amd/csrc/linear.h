@@ -159,7 +159,7 @@ constexpr int64_t kFewRows = 64;        // rows up to which every block takes al
 
 struct BackwardPlan {
   bool stream;
-  int64_t parts, sum_parts;  // partial sums of g_weight and g_bias (stream)
+  int64_t parts;  // partial sums (stream)
   int64_t dz_ld;
   size_t dz, partial, sums, total;
 };
@@ -178,13 +178,13 @@ hipError_t rows_dz(const LinearArgs& a, void* dz, int64_t dz_ld, float* sums, hi
 
 // Layers whose weight fits LDS: the rows stream past it once.
 bool stream_forward_fits(int64_t k, int64_t n, size_t es);
-// Parts whose partial sums the backward leaves: partial [parts, n, k], sums
-// [parts, n] (0: the layer does not fit).
+// Parts whose partial sums the backward leaves in partial [parts, n k + n] if
+// they are more than one (0: the layer does not fit).
 int64_t stream_backward_parts(int64_t m, int64_t k, int64_t n, size_t es);
 template <typename T>
 hipError_t stream_forward(const LinearArgs& a, hipStream_t s);
 template <typename T>
-hipError_t stream_backward(const LinearArgs& a, float* partial, float* sums, hipStream_t s);
+hipError_t stream_backward(const LinearArgs& a, float* partial, hipStream_t s);
 
 template <typename T>
 hipError_t gemm_forward(const LinearArgs& a, hipStream_t s);

@@ -28,7 +28,7 @@ bool stream_forward_fits(int64_t k, int64_t n, size_t es) {
 int64_t stream_backward_parts(int64_t m, int64_t k, int64_t n, size_t es) {
   if (m <= 0 || k <= 0 || n <= 0) return 0;
   const BackwardChoice c = choose_backward(k, n, es);
-  return c.kp == 0 ? 0 : even_blocks(ceil_div64(m, c.rows), kBackwardBlocks) * c.groups;
+  return c.kp == 0 ? 0 : even_blocks(ceil_div64(m, c.rows), kBackwardBlocks);
 }
 
 BackwardPlan backward_plan(int64_t m, int64_t k, int64_t n, gart_dtype t, gart_activation act) {
@@ -41,11 +41,10 @@ BackwardPlan backward_plan(int64_t m, int64_t k, int64_t n, gart_dtype t, gart_a
     return o;
   };
   auto floats = [](int64_t parts, int64_t rows, int64_t cols) { return size_t(parts) * size_t(rows) * size_t(cols) * 4; };
-  p.parts = p.sum_parts = stream_backward_parts(m, k, n, es);
+  p.parts = stream_backward_parts(m, k, n, es);
   if (p.parts > 0) {
     p.stream = true;
-    p.partial = take(floats(p.parts, n, k));
-    p.sums = take(floats(p.sum_parts, 1, n));
+    p.partial = take(p.parts > 1 ? floats(p.parts, n, k + 1) : 0);
     p.total = off;
     return p;
   }

@@ -314,42 +314,48 @@ __global__ __launch_bounds__(256) void column_sums_kernel(const T* __restrict__ 
   if (w == 0 && j < n) sums[int64_t(blockIdx.x) * n + j] = (s[0][lane] + s[1][lane]) + (s[2][lane] + s[3][lane]);
 }
 
-// out[i, j] = sum over parts of partial[part, i, j].  A block takes 64
-// neighbouring elements; its 16 waves take every 16th part each and their sums
-// are added in order.
+// Sums over parts of partial[part, e], e < length: out (rows x cols) takes the
+// first rows * cols, tail the rest.  A block takes 64 neighbouring elements; its
+// 16 waves take every 16th part each and their sums are added in order.
 constexpr int kJoinWaves = 16;
 template <typename T>
 __global__ __launch_bounds__(64 * kJoinWaves) void join_parts_kernel(const float* __restrict__ partial, int64_t parts,
-                                                                     int64_t rows, int64_t cols, T* __restrict__ out,
-                                                                     int64_t out_ld) {
+                                                                     int64_t length, int64_t first, int64_t last,
+                                                                     int64_t cols, int64_t size, T* __restrict__ out,
+                                                                     int64_t out_ld, T* __restrict__ tail) {
   __shared__ float s[kJoinWaves][64];
   const int lane = threadIdx.x % 64, w = threadIdx.x / 64;
-  const int64_t total = rows * cols;
-  for (int64_t b = int64_t(blockIdx.x) * 64; b < total; b += int64_t(gridDim.x) * 64) {
+  for (int64_t b = first + int64_t(blockIdx.x) * 64; b < last; b += int64_t(gridDim.x) * 64) {
     const int64_t e = b + lane;
     float t = 0.0f;
-    if (e < total) {
-#pragma unroll 4
-      for (int64_t p = w; p < parts; p += kJoinWaves) t += partial[p * total + e];
+    if (e < last) {
+#pragma unroll 8
+      for (int64_t p = w; p < parts; p += kJoinWaves) t += partial[p * length + e];
     }
     s[w][lane] = t;
     __syncthreads();
-    if (w == 0 && e < total) {
+    if (w == 0 && e < last) {
       float sum = s[0][lane];
 #pragma unroll
       for (int v = 1; v < kJoinWaves; ++v) sum += s[v][lane];
-      out[e / cols * out_ld + e % cols] = T(sum);
+      if (e < size)
+        out[e / cols * out_ld + e % cols] = T(sum);
+      else
+        tail[e - size] = T(sum);
     }
     __syncthreads();
   }
 }
 
+// partial [parts, rows * cols + more]: out (may be NULL) and tail (may be NULL)
 template <typename T>
 hipError_t join_parts(const float* partial, int64_t parts, int64_t rows, int64_t cols, void* out, int64_t ld,
-                      hipStream_t s) {
-  if (rows * cols <= 0) return hipSuccess;
-  const int64_t blocks = std::min<int64_t>(ceil_div64(rows * cols, 64), 1 << 16);
-  join_parts_kernel<T><<<uint32_t(blocks), 64 * kJoinWaves, 0, s>>>(partial, parts, rows, cols, static_cast<T*>(out), ld);
+                      hipStream_t s, int64_t more = 0, void* tail = nullptr) {
+  const int64_t size = rows * cols, first = out ? 0 : size, last = tail ? size + more : size;
+  if (last <= first) return hipSuccess;
+  const int64_t blocks = std::min<int64_t>(ceil_div64(last - first, 64), 1 << 16);
+  join_parts_kernel<T><<<uint32_t(blocks), 64 * kJoinWaves, 0, s>>>(partial, parts, size + more, first, last, cols, size,
+                                                                    static_cast<T*>(out), ld, static_cast<T*>(tail));
   return hipGetLastError();
 }
 
@@ -473,9 +479,8 @@ hipError_t gemm_backward(const LinearArgs& a, hipStream_t s) {
   float* partial = reinterpret_cast<float*>(base + p.partial);
   hipError_t e = hipSuccess;
   if (p.stream) {
-    if ((e = stream_backward<T>(a, partial, sums, s)) != hipSuccess) return e;
-    if (a.g_w && (e = join_parts<T>(partial, p.parts, a.n, a.k, a.g_w, a.g_w_ld, s)) != hipSuccess) return e;
-    return a.g_bias ? join_parts<T>(sums, p.sum_parts, 1, a.n, a.g_bias, a.n, s) : hipSuccess;
+    if ((e = stream_backward<T>(a, partial, s)) != hipSuccess || p.parts == 1) return e;
+    return join_parts<T>(partial, p.parts, a.n, a.k, a.g_w, a.g_w_ld, s, a.n, a.g_bias);
   }
   const void* dz = a.dl;
   int64_t dz_ld = a.dl_ld, sum_parts = 0;

@@ -47,14 +47,14 @@ struct BackwardSizes {
 constexpr int64_t kBackwardBlocks = 512;
 
 struct BackwardChoice {
-  int kp, ns, rows, groups;  // kp 0: none
+  int kp, ns, rows;  // kp 0: none
 };
 
 template <size_t ES, int KP, int NS>
 bool offer(int64_t k, int64_t n, BackwardChoice* c) {
   using B = BackwardSizes<ES, KP, NS>;
   if (!B::FITS || k > KP || n > 32 * NS) return false;
-  *c = BackwardChoice{KP, NS, B::ROWS, B::RG};
+  *c = BackwardChoice{KP, NS, B::ROWS};
   return true;
 }
 

@@ -13,7 +13,8 @@
 //   g_weight (its 32 n, all k) += dz^T x over the tile's rows, kept in
 //   registers for all of the block's tiles;
 //   g_x (rows, k) = dz W, stored.
-// Each block leaves one partial sum of g_weight and g_bias.
+// Each block leaves one partial sum of g_weight and g_bias; a block that is
+// alone leaves the gradients.
 #pragma once
 
 #include <algorithm>
@@ -26,6 +27,7 @@ namespace {
 // ---- forward -----------------------------------------------------------------
 // Row strides up to which offsets inside a tile of rows fit 32 bits.
 constexpr int64_t kNear = int64_t(1) << 22;
+constexpr int kSpare = 8;  // rows of at least one element that hold a pack
 
 // KP: inputs, rounded up.  LDS rows are 16 bytes longer, which spreads the
 // rows that lanes read together over the banks.
@@ -50,21 +52,30 @@ __global__ __launch_bounds__(64 * kForwardWaves) void stream_forward_kernel(cons
   T* y = static_cast<T*>(a.y);
   constexpr int Q = 8 / V;  // packs of outputs per lane: one of 8, or one of 4 from each tile
   const int64_t tiles = (a.m + 31) / 32, step = int64_t(gridDim.x) * kForwardWaves;
-  // Whole tiles of rows of whole packs need no counts, and lanes' offsets in a tile are the same for all of them.
-  const bool full_k = a.k % V == 0 && a.x_ld <= kNear;
-  const bool full_n = a.n % V == 0 && a.y_ld <= kNear && a.residual_ld <= kNear;
+  // Away from the end, lanes' offsets in a tile are the same for all tiles, and
+  // a whole pack may be read at the end of a row: kSpare rows follow it.
+  const bool near_x = a.x_ld <= kNear && a.x_ld > 0, near_y = a.y_ld <= kNear && a.residual_ld <= kNear;
   const uint32_t x_off = uint32_t(r * a.x_ld + V * g), y_off = uint32_t(r * a.y_ld + (Q == 1 ? 8 : 4) * g),
                  res_off = uint32_t(r * a.residual_ld + (Q == 1 ? 8 : 4) * g);
+  // the last, partial step of k
+  const int k_last = int(a.k) / kDepth<T> * kDepth<T> + V * g;
+  const PackMask<T> k_mask = first_of_pack<T>(int(a.k) - k_last);
+  const uint32_t x_last = uint32_t(r * a.x_ld) + (k_last < a.k ? k_last : 0);
   auto load_x = [&](int64_t t, typename Pack<T>::V(&fx)[2][S]) {
     if (t >= tiles) return;
-    if (full_k && (t + 1) * 32 <= a.m) {
+    if (near_x && (t + 1) * 32 + kSpare <= a.m) {
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         const T* p = x + (t * 32 + 16 * i) * a.x_ld;
 #pragma unroll
         for (int s = 0; s < S; ++s) {
-          fx[i][s] = T(0.0f);
-          if (s * kDepth<T> + V * g < a.k) fx[i][s] = load_pack(p + s * kDepth<T> + x_off).v;
+          constexpr int D = kDepth<T>;
+          if (s * D + D <= int(a.k))
+            fx[i][s] = load_pack(p + (x_off + s * D)).v;
+          else if (s * D < int(a.k))
+            fx[i][s] = load_masked(p + x_last, k_mask).v;
+          else
+            fx[i][s] = T(0.0f);
         }
       }
       return;
@@ -76,7 +87,7 @@ __global__ __launch_bounds__(64 * kForwardWaves) void stream_forward_kernel(cons
       for (int s = 0; s < S; ++s) {
         const int64_t k = s * kDepth<T> + V * g;
         fx[i][s] = T(0.0f);
-        if (row < a.m && k < a.k) fx[i][s] = load_some(x + row * a.x_ld + k, int(min(int64_t(V), a.k - k))).v;
+        if (row < a.m && k < a.k) fx[i][s] = load_some(x + row * a.x_ld + k, fresh(int(a.k - k))).v;
       }
     }
   };
@@ -89,7 +100,7 @@ __global__ __launch_bounds__(64 * kForwardWaves) void stream_forward_kernel(cons
 #pragma unroll
       for (int s = 0; s < S; ++s) fx[i][s] = next[i][s];
     load_x(t + step, next);
-    const bool whole = full_n && (t + 1) * 32 <= a.m;
+    const bool whole = near_y && (t + 1) * 32 <= a.m;
     for (int n0 = 0; n0 < n_pad; n0 += 32) {
       Pack<T> p[2][Q];
       if (res && whole) {
@@ -97,8 +108,10 @@ __global__ __launch_bounds__(64 * kForwardWaves) void stream_forward_kernel(cons
         for (int i = 0; i < 2; ++i)
 #pragma unroll
           for (int q = 0; q < Q; ++q)
-            if (n0 + 16 * q + (Q == 1 ? 8 : 4) * g < a.n)
-              p[i][q] = load_pack(res + (t * 32 + 16 * i) * a.residual_ld + n0 + 16 * q + res_off);
+          {
+            const int count = fresh(int(a.n) - (n0 + 16 * q + (Q == 1 ? 8 : 4) * g));
+            if (count > 0) p[i][q] = load_some(res + (t * 32 + 16 * i) * a.residual_ld + n0 + 16 * q + res_off, count);
+          }
       }
       f32x4 acc[2][2] = {};
 #pragma unroll
@@ -113,7 +126,7 @@ __global__ __launch_bounds__(64 * kForwardWaves) void stream_forward_kernel(cons
 #pragma unroll
       for (int q = 0; q < Q; ++q) {
         const int64_t n = n0 + (Q == 1 ? 8 * g : 16 * q + 4 * g);
-        const int count = int(min(int64_t(V), a.n - n));
+        const int count = fresh(int(a.n - n));
         float c[2][V];
 #pragma unroll
         for (int i = 0; i < 2; ++i)
@@ -145,7 +158,7 @@ __global__ __launch_bounds__(64 * kForwardWaves) void stream_forward_kernel(cons
 #pragma unroll
           for (int e = 0; e < V; ++e) o.v[e] = T(c[i][e]);
           if (whole && count > 0)
-            store_pack(y + (t * 32 + 16 * i) * a.y_ld + n0 + 16 * q + y_off, o);
+            store_some(y + (t * 32 + 16 * i) * a.y_ld + n0 + 16 * q + y_off, o, count);
           else if (!whole && here)
             store_some(y + row * a.y_ld + n, o, count);
         }
@@ -160,7 +173,7 @@ using BackwardShape = BackwardSizes<sizeof(T), KP, NS>;
 
 template <typename T, int KP, int NS>
 __global__ __launch_bounds__((BackwardShape<T, KP, NS>::THREADS), (KP * sizeof(T) <= 128 && NS <= 4 ? 2 : 1)) void stream_backward_kernel(
-    const LinearArgs a, float* __restrict__ partial, float* __restrict__ sums, int64_t tiles) {
+    const LinearArgs a, float* __restrict__ partial, int64_t tiles) {
   using B = BackwardShape<T, KP, NS>;
   constexpr int V = Pack<T>::N, D = kDepth<T>, S = KP / D, KT = KP / 16, Q = 8 / V;
   constexpr int MT = B::GROUP_ROWS / 16;
@@ -200,20 +213,32 @@ __global__ __launch_bounds__((BackwardShape<T, KP, NS>::THREADS), (KP * sizeof(T
 
   constexpr int XALL = B::ROWS * (KP / V), XP = (XALL + B::THREADS - 1) / B::THREADS;  // x packs, per thread
   constexpr bool XEVEN = XALL % B::THREADS == 0;
-  // Whole tiles of rows of whole packs need no counts, and lanes' offsets in a tile are the same for all of them.
-  const bool full = a.k % V == 0 && a.n % V == 0 && a.x_ld <= kNear && a.dl_ld <= kNear && a.g_x_ld <= kNear && XEVEN;
+  // Away from the end, lanes' offsets in a tile are the same for all tiles, and
+  // a whole pack may be read at the end of a row: kSpare rows follow it.
+  const bool near = a.x_ld <= kNear && a.dl_ld <= kNear && a.g_x_ld <= kNear && a.x_ld > 0 && a.dl_ld > 0;
   constexpr int XSTEP = B::THREADS / (KP / V);  // rows that one pack a thread covers
-  const uint32_t x_off = uint32_t(tid / (KP / V) * a.x_ld + tid % (KP / V) * V),
-                 dl_off = uint32_t((group * B::GROUP_ROWS + r) * a.dl_ld + n0(0)),
+  const int x_at = tid % (KP / V) * V, x_count = XEVEN || tid < XALL ? int(a.k) - x_at : 0;
+  const uint32_t x_off = x_count > 0 ? uint32_t(tid / (KP / V) * a.x_ld + x_at) : 0u,
                  gx_off = uint32_t(r * a.g_x_ld + (Q == 1 ? 8 : 4) * g);
+  const uint32_t x_ld = uint32_t(a.x_ld), dl_ld = uint32_t(a.dl_ld), gx_ld = uint32_t(a.g_x_ld);  // if near
+  const PackMask<T> x_mask = first_of_pack<T>(x_count);
+  uint32_t dl_off[Q];
+  PackMask<T> dl_mask[Q];
+#pragma unroll
+  for (int q = 0; q < Q; ++q) {
+    dl_off[q] = uint32_t((group * B::GROUP_ROWS + r) * a.dl_ld + (n0(q) < a.n ? n0(q) : 0));
+    dl_mask[q] = first_of_pack<T>(int(a.n) - n0(q));
+  }
   Pack<T> xr[XP], dr[MT][Q];
   auto load_x = [&](int64_t t) {
-    if (full && (t + 1) * B::ROWS <= a.m) {
+    if (near && (t + 1) * B::ROWS + kSpare <= a.m) {
       const T* p = x + t * B::ROWS * a.x_ld;
 #pragma unroll
       for (int u = 0; u < XP; ++u) {
-        xr[u].v = T(0.0f);
-        if (tid % (KP / V) * V < a.k) xr[u] = load_pack(p + u * XSTEP * a.x_ld + x_off);
+        if (XEVEN && a.k == KP)
+          xr[u] = load_pack(p + (x_off + u * XSTEP * x_ld));
+        else
+          xr[u] = load_masked(p + (x_off + u * XSTEP * x_ld), x_mask);
       }
       return;
     }
@@ -224,18 +249,20 @@ __global__ __launch_bounds__((BackwardShape<T, KP, NS>::THREADS), (KP * sizeof(T
       const int at = c % (KP / V) * V;
       xr[u].v = T(0.0f);
       if ((XEVEN || c < XALL) && t < tiles && row < a.m && at < a.k)
-        xr[u] = load_some(x + row * a.x_ld + at, int(min(int64_t(V), a.k - at)));
+        xr[u] = load_some(x + row * a.x_ld + at, fresh(int(a.k) - at));
     }
   };
   auto load_dl = [&](int64_t t) {
-    if (full && (t + 1) * B::ROWS <= a.m) {
+    if (near && (t + 1) * B::ROWS + kSpare <= a.m) {
       const T* p = dl + t * B::ROWS * a.dl_ld;
 #pragma unroll
       for (int i = 0; i < MT; ++i)
 #pragma unroll
         for (int q = 0; q < Q; ++q) {
-          dr[i][q].v = T(0.0f);
-          if (n0(q) < a.n) dr[i][q] = load_pack(p + 16 * i * a.dl_ld + 16 * q + dl_off);
+          if (a.n == B::NP)
+            dr[i][q] = load_pack(p + (dl_off[q] + 16 * i * dl_ld));
+          else
+            dr[i][q] = load_masked(p + (dl_off[q] + 16 * i * dl_ld), dl_mask[q]);
         }
       return;
     }
@@ -246,7 +273,7 @@ __global__ __launch_bounds__((BackwardShape<T, KP, NS>::THREADS), (KP * sizeof(T
       for (int q = 0; q < Q; ++q) {
         dr[i][q].v = T(0.0f);
         if (t < tiles && row < a.m && n0(q) < a.n)
-          dr[i][q] = load_some(dl + row * a.dl_ld + n0(q), int(min(int64_t(V), a.n - n0(q))));
+          dr[i][q] = load_some(dl + row * a.dl_ld + n0(q), fresh(int(a.n) - n0(q)));
       }
     }
   };
@@ -349,10 +376,12 @@ __global__ __launch_bounds__((BackwardShape<T, KP, NS>::THREADS), (KP * sizeof(T
             Pack<T> o;
 #pragma unroll
             for (int e = 0; e < V; ++e) o.v[e] = T(acc[i][Q == 1 ? e / 4 : q][e % 4]);
-            if (full && whole && k < a.k)
-              store_pack(static_cast<T*>(a.g_x) + (t * B::ROWS + r0 + 16 * i) * a.g_x_ld + 16 * (kt + q) + gx_off, o);
-            else if (!(full && whole) && row < a.m && k < a.k)
-              store_some(static_cast<T*>(a.g_x) + row * a.g_x_ld + k, o, int(min(int64_t(V), a.k - k)));
+            if (near && whole) {
+              if (k < a.k)
+                store_some(static_cast<T*>(a.g_x) + t * B::ROWS * a.g_x_ld + ((r0 + 16 * i) * gx_ld + 16 * (kt + q) + gx_off),
+                           o, fresh(int(a.k - k)));
+            } else if (row < a.m && k < a.k)
+              store_some(static_cast<T*>(a.g_x) + row * a.g_x_ld + k, o, fresh(int(a.k - k)));
           }
         }
       }
@@ -360,29 +389,69 @@ __global__ __launch_bounds__((BackwardShape<T, KP, NS>::THREADS), (KP * sizeof(T
     __syncthreads();  // x may be replaced
   }
 
-  const int64_t part = int64_t(blockIdx.x) * B::RG + group;
+  // sums of the tile's columns, then those of the row groups, in order
+#pragma unroll
+  for (int e = 0; e < 8; ++e)
+#pragma unroll
+    for (int off = 1; off < 16; off <<= 1) sum_b[e] += __shfl_xor(sum_b[e], off);
+  if constexpr (B::RG > 1) {
+    f32x4* sw = reinterpret_cast<f32x4*>(lds);  // [slice][j][kt][lane]; the loop's last barrier has passed
+    float* sb = reinterpret_cast<float*>(lds) + B::NP * KP;
+    static_assert((B::NP * KP + B::NP) * 4 <= B::BYTES, "sums fit");
+#pragma unroll
+    for (int h = 0; h < B::RG; ++h) {
+      if (group == h) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+          for (int kt = 0; kt < KT; ++kt) {
+            f32x4* q = sw + ((slice * 2 + j) * KT + kt) * 64 + lane;
+            if (h > 0) acc_w[j][kt] += *q;
+            if (h < B::RG - 1) *q = acc_w[j][kt];
+          }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          float* q = sb + n0(e / V) + e % V;
+          if (h > 0) sum_b[e] += *q;
+          if (h < B::RG - 1 && r == 0) *q = sum_b[e];
+        }
+      }
+      __syncthreads();
+    }
+    if (group != B::RG - 1) return;
+  }
+  // One block: the results.  More: this block's part, weights, then bias.
+  const bool alone = gridDim.x == 1;
+  float* part = partial + int64_t(blockIdx.x) * a.n * (a.k + 1);
   if (a.g_w) {
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
       const int64_t n = 32 * slice + 16 * j + r;
       if (n >= a.n) continue;
-      float* out = partial + (part * a.n + n) * a.k;
 #pragma unroll
       for (int kt = 0; kt < KT; ++kt) {
         const int64_t k = paired_row<T>(kt, 4 * g);
+        const int count = int(min(int64_t(4), a.k - k));
         Pack<float> p;
         p.v = acc_w[j][kt];
-        if (k < a.k) store_some(out + k, p, int(min(int64_t(4), a.k - k)));
+        if (!alone && count > 0) store_some(part + n * a.k + k, p, count);
+        if (alone) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (e < count) static_cast<T*>(a.g_w)[n * a.g_w_ld + k + e] = T(p.v[e]);
+        }
       }
     }
   }
-  if (a.g_bias) {
+  if (a.g_bias && r == 0) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-#pragma unroll
-      for (int off = 1; off < 16; off <<= 1) sum_b[e] += __shfl_xor(sum_b[e], off);
       const int n = n0(e / V) + e % V;
-      if (r == 0 && n < a.n) sums[part * a.n + n] = sum_b[e];
+      if (n >= a.n) continue;
+      if (alone)
+        static_cast<T*>(a.g_bias)[n] = T(sum_b[e]);
+      else
+        part[a.n * a.k + n] = sum_b[e];
     }
   }
 }
@@ -397,24 +466,24 @@ hipError_t forward_kp(const LinearArgs& a, hipStream_t s) {
 }
 
 template <typename T, int KP, int NS>
-hipError_t backward_run(const LinearArgs& a, float* partial, float* sums, hipStream_t s) {
+hipError_t backward_run(const LinearArgs& a, float* partial, hipStream_t s) {
   using B = BackwardShape<T, KP, NS>;
   if constexpr (B::FITS) {
     const int64_t tiles = ceil_div64(a.m, B::ROWS);
     stream_backward_kernel<T, KP, NS>
-        <<<uint32_t(even_blocks(tiles, kBackwardBlocks)), B::THREADS, 0, s>>>(a, partial, sums, tiles);
+        <<<uint32_t(even_blocks(tiles, kBackwardBlocks)), B::THREADS, 0, s>>>(a, partial, tiles);
     return hipGetLastError();
   }
   return hipErrorInvalidValue;
 }
 
 template <typename T, int KP>
-hipError_t backward_kp(const LinearArgs& a, int ns, float* partial, float* sums, hipStream_t s) {
+hipError_t backward_kp(const LinearArgs& a, int ns, float* partial, hipStream_t s) {
   switch (ns) {
-    case 1: return backward_run<T, KP, 1>(a, partial, sums, s);
-    case 2: return backward_run<T, KP, 2>(a, partial, sums, s);
-    case 4: return backward_run<T, KP, 4>(a, partial, sums, s);
-    default: return backward_run<T, KP, 8>(a, partial, sums, s);
+    case 1: return backward_run<T, KP, 1>(a, partial, s);
+    case 2: return backward_run<T, KP, 2>(a, partial, s);
+    case 4: return backward_run<T, KP, 4>(a, partial, s);
+    default: return backward_run<T, KP, 8>(a, partial, s);
   }
 }
 
@@ -433,13 +502,13 @@ hipError_t stream_forward(const LinearArgs& a, hipStream_t s) {
 }
 
 template <typename T>
-hipError_t stream_backward(const LinearArgs& a, float* partial, float* sums, hipStream_t s) {
+hipError_t stream_backward(const LinearArgs& a, float* partial, hipStream_t s) {
   const BackwardChoice c = choose_backward(a.k, a.n, sizeof(T));
   switch (c.kp) {
-    case 32: return backward_kp<T, 32>(a, c.ns, partial, sums, s);
-    case 64: return backward_kp<T, 64>(a, c.ns, partial, sums, s);
-    case 128: return backward_kp<T, 128>(a, c.ns, partial, sums, s);
-    case 256: return backward_kp<T, 256>(a, c.ns, partial, sums, s);
+    case 32: return backward_kp<T, 32>(a, c.ns, partial, s);
+    case 64: return backward_kp<T, 64>(a, c.ns, partial, s);
+    case 128: return backward_kp<T, 128>(a, c.ns, partial, s);
+    case 256: return backward_kp<T, 256>(a, c.ns, partial, s);
   }
   return hipErrorInvalidValue;
 }

@@ -4,6 +4,6 @@
 namespace gart {
 
 template hipError_t stream_forward<bf16>(const LinearArgs&, hipStream_t);
-template hipError_t stream_backward<bf16>(const LinearArgs&, float*, float*, hipStream_t);
+template hipError_t stream_backward<bf16>(const LinearArgs&, float*, hipStream_t);
 
 }  // namespace gart

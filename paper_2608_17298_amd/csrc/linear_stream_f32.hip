@@ -4,6 +4,6 @@
 namespace gart {
 
 template hipError_t stream_forward<float>(const LinearArgs&, hipStream_t);
-template hipError_t stream_backward<float>(const LinearArgs&, float*, float*, hipStream_t);
+template hipError_t stream_backward<float>(const LinearArgs&, float*, hipStream_t);
 
 }  // namespace gart

@@ -25,7 +25,10 @@ constexpr int kSortThreads = 256;
 #endif
 constexpr int kSortItems = GART_SORT_ITEMS;  // keys per thread and radix pass
 constexpr int kSortTile = kSortThreads * kSortItems;
-constexpr int kIdItems = 8;  // of a sort of ids: up to a few million, more blocks beat longer ones (1M: 16 items 147 us, 8 143)
+// Of a sort of ids: up to a few million, more blocks beat longer ones (gradient
+// of 1M ids: 16 items 147 us, 8 143).
+constexpr int kIdItems = 8;
+constexpr int64_t kFewBlocks = 128;  // blocks up to which the scatter adds up counts itself
 constexpr int kWaves = kSortThreads / 64;
 
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
@@ -138,7 +141,9 @@ hipError_t scan_impl(const Tin* in, T* out, int64_t n, T* total, char* tmp, hipS
 // the per-wave counts into offsets; the block's keys are staged in LDS in
 // digit order and written out as contiguous runs per digit.
 // ---------------------------------------------------------------------------
-template <int ITEMS, typename Source>
+// COUNTS_BY_BLOCK: counts lie [block][digit] and are never scanned; the scatter
+// adds up what it needs of them.
+template <int ITEMS, bool COUNTS_BY_BLOCK, typename Source>
 __global__ __launch_bounds__(kSortThreads) void radix_hist_kernel(const Source source, int64_t m, int shift,
                                                                   uint32_t* __restrict__ counts, int nblocks) {
   __shared__ uint32_t h[256];
@@ -157,10 +162,13 @@ __global__ __launch_bounds__(kSortThreads) void radix_hist_kernel(const Source s
     if (j < m) atomicAdd(&h[(kv[r] >> shift) & 255u], 1u);
   }
   __syncthreads();
-  counts[int64_t(threadIdx.x) * nblocks + blockIdx.x] = h[threadIdx.x];
+  if (COUNTS_BY_BLOCK)
+    counts[int64_t(blockIdx.x) * 256 + threadIdx.x] = h[threadIdx.x];
+  else
+    counts[int64_t(threadIdx.x) * nblocks + blockIdx.x] = h[threadIdx.x];
 }
 
-template <int ITEMS, typename Source>
+template <int ITEMS, bool COUNTS_BY_BLOCK, typename Source>
 __global__ __launch_bounds__(kSortThreads) void radix_scatter_kernel(
     const Source source, uint32_t* __restrict__ kout, uint32_t* __restrict__ vout, int64_t m, int shift, const uint32_t* __restrict__ offsets, int nblocks) {
   __shared__ uint32_t s_keys[(kSortThreads * ITEMS)];
@@ -177,7 +185,19 @@ __global__ __launch_bounds__(kSortThreads) void radix_scatter_kernel(
 
 #pragma unroll
   for (int w = 0; w < kWaves; ++w) s_wave[w][tid] = 0;
-  s_gofs[tid] = offsets[int64_t(tid) * nblocks + blockIdx.x];
+  if (COUNTS_BY_BLOCK) {
+    uint32_t before = 0, all = 0;  // of this digit: in the blocks before, and in all
+#pragma unroll 16
+    for (int b = 0; b < nblocks; ++b) {
+      const uint32_t c = offsets[b * 256 + tid];
+      all += c;
+      before += b < int(blockIdx.x) ? c : 0u;
+    }
+    uint32_t total;
+    s_gofs[tid] = block_exclusive(all, &total) + before;
+  } else {
+    s_gofs[tid] = offsets[int64_t(tid) * nblocks + blockIdx.x];
+  }
   __syncthreads();
 
   // Keys [wbase, wbase + 64 * ITEMS) belong to this wave, so block order
@@ -339,19 +359,45 @@ size_t radix_tmp_bytes(int64_t m) {
 
 namespace {
 
-template <int ITEMS, typename Source>
+template <int ITEMS, bool COUNTS_BY_BLOCK, typename Source>
 hipError_t radix_pass(const Source& source, uint32_t* kout, uint32_t* vout, int64_t m, int shift, void* tmp,
                       hipStream_t s) {
   const int64_t nb = ceil_div(m, kSortThreads * ITEMS);
   uint32_t* counts = static_cast<uint32_t*>(tmp);
   char* scan_tmp = static_cast<char*>(tmp) + ((size_t(nb) * 256 * sizeof(uint32_t) + 255) & ~size_t(255));
-  radix_hist_kernel<ITEMS><<<nb, kSortThreads, 0, s>>>(source, m, shift, counts, int(nb));
+  radix_hist_kernel<ITEMS, COUNTS_BY_BLOCK><<<nb, kSortThreads, 0, s>>>(source, m, shift, counts, int(nb));
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  e = scan_exclusive_u32(counts, counts, nb * 256, nullptr, scan_tmp, s);
+  if (!COUNTS_BY_BLOCK) e = scan_exclusive_u32(counts, counts, nb * 256, nullptr, scan_tmp, s);
   if (e != hipSuccess) return e;
-  radix_scatter_kernel<ITEMS><<<nb, kSortThreads, 0, s>>>(source, kout, vout, m, shift, counts, int(nb));
+  radix_scatter_kernel<ITEMS, COUNTS_BY_BLOCK>
+      <<<nb, kSortThreads, 0, s>>>(source, kout, vout, m, shift, counts, int(nb));
   return hipGetLastError();
+}
+
+template <bool COUNTS_BY_BLOCK>
+hipError_t sort_ids(const void* ids, bool ids64, int64_t limit, uint32_t* keys, uint32_t* pos, uint32_t* keys_alt,
+                    uint32_t* pos_alt, int64_t m, int bits, void* tmp, hipStream_t s) {
+  uint32_t *ka = keys, *va = pos, *kb = keys_alt, *vb = pos_alt;
+  if ((bits + 7) / 8 % 2 == 0) {  // the last pass ends in keys and pos
+    std::swap(ka, kb);
+    std::swap(va, vb);
+  }
+  for (int shift = 0; shift < bits; shift += 8) {
+    hipError_t e;
+    if (shift > 0)
+      e = radix_pass<kIdItems, COUNTS_BY_BLOCK>(PairSource{kb, vb}, ka, va, m, shift, tmp, s);
+    else if (ids64)
+      e = radix_pass<kIdItems, COUNTS_BY_BLOCK>(IdSource<int64_t>{static_cast<const int64_t*>(ids), limit}, ka, va, m,
+                                                0, tmp, s);
+    else
+      e = radix_pass<kIdItems, COUNTS_BY_BLOCK>(IdSource<int32_t>{static_cast<const int32_t*>(ids), limit}, ka, va, m,
+                                                0, tmp, s);
+    if (e != hipSuccess) return e;
+    std::swap(ka, kb);
+    std::swap(va, vb);
+  }
+  return hipSuccess;
 }
 
 }  // namespace
@@ -368,7 +414,7 @@ hipError_t radix_sort_u32(uint32_t* keys, uint32_t* vals, uint32_t* keys_alt, ui
   }
   uint32_t *ka = keys, *va = vals, *kb = keys_alt, *vb = vals_alt;
   for (int shift = 0; shift < bits; shift += 8) {
-    const hipError_t e = radix_pass<kSortItems>(PairSource{ka, va}, kb, vb, m, shift, tmp, s);
+    const hipError_t e = radix_pass<kSortItems, false>(PairSource{ka, va}, kb, vb, m, shift, tmp, s);
     if (e != hipSuccess) return e;
     std::swap(ka, kb);
     std::swap(va, vb);
@@ -384,24 +430,9 @@ size_t radix_ids_tmp_bytes(int64_t m) { return radix_tmp_bytes(m * kSortItems / 
 
 hipError_t radix_sort_ids(const void* ids, bool ids64, int64_t limit, uint32_t* keys, uint32_t* pos,
                           uint32_t* keys_alt, uint32_t* pos_alt, int64_t m, int bits, void* tmp, hipStream_t s) {
-  uint32_t *ka = keys, *va = pos, *kb = keys_alt, *vb = pos_alt;
-  if ((bits + 7) / 8 % 2 == 0) {  // the last pass ends in keys and pos
-    std::swap(ka, kb);
-    std::swap(va, vb);
-  }
-  for (int shift = 0; shift < bits; shift += 8) {
-    hipError_t e;
-    if (shift > 0)
-      e = radix_pass<kIdItems>(PairSource{kb, vb}, ka, va, m, shift, tmp, s);
-    else if (ids64)
-      e = radix_pass<kIdItems>(IdSource<int64_t>{static_cast<const int64_t*>(ids), limit}, ka, va, m, 0, tmp, s);
-    else
-      e = radix_pass<kIdItems>(IdSource<int32_t>{static_cast<const int32_t*>(ids), limit}, ka, va, m, 0, tmp, s);
-    if (e != hipSuccess) return e;
-    std::swap(ka, kb);
-    std::swap(va, vb);
-  }
-  return hipSuccess;
+  return ceil_div(m, kSortThreads * kIdItems) <= kFewBlocks
+             ? sort_ids<true>(ids, ids64, limit, keys, pos, keys_alt, pos_alt, m, bits, tmp, s)
+             : sort_ids<false>(ids, ids64, limit, keys, pos, keys_alt, pos_alt, m, bits, tmp, s);
 }
 
 hipError_t fill_u32(uint32_t* p, uint32_t v, int64_t n, hipStream_t s) { return fill_any<uint32_t>(p, v, n, s); }
