@@ -7,9 +7,9 @@
 // (stable, with their positions), so equal ids stand side by side and a row's
 // sum needs no atomics: the order of its terms is their position, whatever the
 // schedule.  The sorted positions are cut into units of equal length, which balances
-// the work whatever the ids' distribution; a run of equal ids inside one unit
-// is summed and written there, a run that crosses units leaves one partial sum
-// a unit and is joined afterwards, in order.
+// the work whatever the ids' distribution; a run of equal ids is summed in its
+// units, joined in the block's LDS and, where it crosses blocks, afterwards
+// from their partial sums, always in order.
 #include <algorithm>
 
 #include "blocks.h"
@@ -22,10 +22,10 @@ namespace {
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kThreads = 256;
-constexpr int kRowsPerThread = 4;
+constexpr int kRowsPerThread = 2;
 constexpr int kBatch = 8;            // rows in flight per thread of the gradient
 constexpr int kMinUnit = 8, kMaxUnit = 64;
-constexpr int64_t kUnitThreads = 131072;
+constexpr int64_t kUnitThreads = 262144;
 
 // ---- lookup ------------------------------------------------------------------
 // packs: 16-byte packs per row; lanes: threads per row (packs, at most 256);
@@ -110,82 +110,120 @@ __global__ __launch_bounds__(kSmallThreads) void sort_and_zero_kernel(const Embe
     radix_small<8>(source, keys, pos, int(a.n), bits);
 }
 
-// Partial sums: partial[2 u] is the part in unit u of a run that began before
-// u, partial[2 u + 1] the part in u of a run that begins in u and goes on.
-//
-// A thread owns 16 bytes of the rows of one unit.  kBatch rows are asked for
-// before any of them is added, whatever their keys: one row at a time left
-// the kernel waiting for memory (141 us at 1M rows of 64 bf16).
+// Sums of a block's units.  A thread owns 16 bytes of the rows of one unit.
+// kBatch rows are asked for before any of them is added, whatever their keys
+// (one row at a time left the kernel waiting for memory: 141 us at 1M rows of
+// 64 bf16).  Runs that cross units meet in LDS, in order; what crosses blocks
+// leaves partial sums: partial[2 b] is the part in block b of a run that began
+// before b, partial[2 b + 1] the part of a run that begins in b and goes on.
 template <typename T>
 __global__ __launch_bounds__(kThreads) void unit_sums_kernel(const EmbeddingArgs a, const uint32_t* __restrict__ keys,
                                                              const uint32_t* __restrict__ pos,
                                                              float* __restrict__ partial, int unit_rows, int packs,
                                                              int lanes, int upb) {
+  constexpr int V = Pack<T>::N;
+  __shared__ __attribute__((aligned(16))) float s_head[kThreads][V];  // of the unit's first run, if it began before
+  __shared__ bool s_whole[kThreads];  // the unit is one run that began before and goes on
   const T* __restrict__ rows = static_cast<const T*>(a.rows);
   T* __restrict__ out = static_cast<T*>(a.out);
-  constexpr int V = Pack<T>::N;
   const int sub = threadIdx.x / lanes, lane = threadIdx.x - sub * lanes;
-  if (sub >= upb) return;
-  const int64_t unit = int64_t(blockIdx.x) * upb + sub;
-  const int64_t p0 = unit * unit_rows, p1 = min(a.n, p0 + unit_rows);
-  if (p0 >= a.n) return;
+  const int64_t block_p0 = int64_t(blockIdx.x) * upb * unit_rows, p0 = block_p0 + int64_t(sub) * unit_rows;
+  const int64_t p1 = min(a.n, p0 + unit_rows);
+  const int units = int(min(int64_t(upb), (a.n - block_p0 + unit_rows - 1) / unit_rows));
+  const bool active = sub < units;
   const uint32_t none = uint32_t(a.vocab);
-  const uint32_t before = p0 > 0 ? keys[p0 - 1] : none;
-  const uint32_t after = p1 < a.n ? keys[p1] : none;
-  for (int p = lane; p < packs; p += lanes) {
+  const uint32_t before = active && p0 > 0 ? keys[p0 - 1] : none;
+  const uint32_t after = active && p1 < a.n ? keys[p1] : none;
+  for (int base = 0; base < packs; base += lanes) {
+    const int p = base + lane;
+    const bool mine = active && p < packs;
     const int64_t c = int64_t(p) * V;
     const int count = int(min(int64_t(V), a.dim - c));
     float acc[V] = {};
-    uint32_t cur = keys[p0];
+    uint32_t cur = mine ? keys[p0] : none;
     bool first = true;
-    auto flush = [&](bool last) {
-      if (cur == none) return;
-      const bool begun = first && cur == before, goes_on = last && cur == after;
-      if (begun || goes_on) {
-        float* q = partial + (2 * unit + (begun ? 0 : 1)) * a.dim + c;
+    auto put = [&](uint32_t key, const float* sum) {
+      Pack<T> v;
 #pragma unroll
-        for (int h = 0; h < V / 4; ++h) {
-          Pack<float> f;
+      for (int e = 0; e < V; ++e) v.v[e] = T(sum[e] * a.scale);
+      store_some(out + int64_t(key) * a.out_ld + c, v, count);
+    };
+    auto put_partial = [&](int which, const float* sum) {
+      float* q = partial + (2 * int64_t(blockIdx.x) + which) * a.dim + c;
 #pragma unroll
-          for (int e = 0; e < 4; ++e) f.v[e] = acc[4 * h + e];
-          if (count > 4 * h) store_some(q + 4 * h, f, count - 4 * h);
-        }
-      } else {
-        Pack<T> v;
+      for (int h = 0; h < V / 4; ++h) {
+        Pack<float> f;
 #pragma unroll
-        for (int e = 0; e < V; ++e) v.v[e] = T(acc[e] * a.scale);
-        store_some(out + int64_t(cur) * a.out_ld + c, v, count);
+        for (int e = 0; e < 4; ++e) f.v[e] = sum[4 * h + e];
+        if (count > 4 * h) store_some(q + 4 * h, f, count - 4 * h);
       }
     };
-    for (int64_t i = p0; i < p1; i += kBatch) {
-      uint32_t k[kBatch];
-      Pack<T> v[kBatch];
+    auto keep_head = [&] {
 #pragma unroll
-      for (int u = 0; u < kBatch; ++u) {
-        k[u] = i + u < p1 ? keys[i + u] : none;
-        v[u].v = T(0.0f);
-        if (k[u] != none) v[u] = load_some(rows + int64_t(pos[i + u]) * a.rows_ld + c, count);
-      }
+      for (int e = 0; e < V; ++e) s_head[threadIdx.x][e] = acc[e];
+    };
+    if (mine) {
+      for (int64_t i = p0; i < p1; i += kBatch) {
+        uint32_t k[kBatch];
+        Pack<T> v[kBatch];
 #pragma unroll
-      for (int u = 0; u < kBatch; ++u) {
-        if (i + u < p1 && k[u] != cur) {
-          flush(false);
-          first = false;
-          cur = k[u];
-#pragma unroll
-          for (int e = 0; e < V; ++e) acc[e] = 0.0f;
+        for (int u = 0; u < kBatch; ++u) {
+          k[u] = i + u < p1 ? keys[i + u] : none;
+          v[u].v = T(0.0f);
+          if (k[u] != none) v[u] = load_some(rows + int64_t(pos[i + u]) * a.rows_ld + c, count);
         }
 #pragma unroll
-        for (int e = 0; e < V; ++e) acc[e] += float(v[u].v[e]);
+        for (int u = 0; u < kBatch; ++u) {
+          if (i + u < p1 && k[u] != cur) {  // the run ends inside the unit
+            if (first && cur == before)
+              keep_head();
+            else
+              put(cur, acc);
+            first = false;
+            cur = k[u];
+#pragma unroll
+            for (int e = 0; e < V; ++e) acc[e] = 0.0f;
+          }
+#pragma unroll
+          for (int e = 0; e < V; ++e) acc[e] += float(v[u].v[e]);
+        }
       }
     }
-    flush(true);
+    // the unit's last run: acc, key cur
+    const bool there = mine && cur != none, begun = there && first && cur == before, goes_on = there && cur == after;
+    if (begun) keep_head();
+    if (there && !begun && !goes_on) put(cur, acc);
+    if (mine) s_whole[threadIdx.x] = begun && goes_on;
+    __syncthreads();
+    // adds the units after sub to acc while their first run is the one before's; true if it leaves the block
+    auto follow = [&](bool open) {
+      for (int u = sub + 1; open && u < units; ++u) {
+        const int t = u * lanes + lane;
+#pragma unroll
+        for (int e = 0; e < V; ++e) acc[e] += s_head[t][e];
+        open = s_whole[t];
+      }
+      return open;
+    };
+    if (there && !begun && goes_on) {
+      if (follow(true))
+        put_partial(1, acc);
+      else
+        put(cur, acc);
+    }
+    if (mine && sub == 0 && before != none && keys[p0] == before) {  // began before the block
+#pragma unroll
+      for (int e = 0; e < V; ++e) acc[e] = s_head[threadIdx.x][e];
+      follow(s_whole[threadIdx.x]);
+      put_partial(0, acc);
+    }
+    __syncthreads();
   }
 }
 
-// Joins the runs that cross units: unit u's last run begins there and goes on
-// if the key at its end equals the next unit's first, and that many further
-// units hold a part of it.  A wave takes one unit; a run that goes on over
+// Joins the runs that cross the blocks above, its units here: unit u's last run
+// begins there and goes on if the key at its end equals the next unit's first,
+// and that many further units hold a part of it.  A wave takes one unit; a run that goes on over
 // kLongRun further units (at most one begins in a block's 16) is left to the
 // block's waves together.  Lanes are spread over a group of columns (four a
 // lane; blockIdx.y counts the groups) and, where columns are few, over the
@@ -287,6 +325,9 @@ int bits_for(int64_t v) {  // bits of the largest key v
   return b;
 }
 
+int lanes_per_unit(int64_t dim, int elements) { return int(std::min<int64_t>(ceil_div64(dim, elements), kThreads)); }
+int units_per_block(int64_t dim, int elements) { return kThreads / lanes_per_unit(dim, elements); }
+
 struct GradLayout {
   size_t keys, pos, keys_alt, pos_alt, radix, partial, total;
 };
@@ -304,7 +345,8 @@ GradLayout grad_layout(int64_t n, int64_t dim) {
   L.keys_alt = take(size_t(n) * 4);
   L.pos_alt = take(size_t(n) * 4);
   L.radix = take(radix_ids_tmp_bytes(n));
-  L.partial = take(size_t(ceil_div64(n, unit_rows_for(n, dim))) * 2 * size_t(dim) * 4);
+  // blocks hold the fewest units with the fewest elements per thread, a float's four
+  L.partial = take(size_t(ceil_div64(n, int64_t(unit_rows_for(n, dim)) * units_per_block(dim, 4))) * 2 * size_t(dim) * 4);
   L.total = off;
   return L;
 }
@@ -324,7 +366,8 @@ hipError_t lookup(const EmbeddingArgs& a, hipStream_t s) {
 template <typename T>
 hipError_t gradient(const EmbeddingArgs& a, hipStream_t s) {
   if (a.vocab <= 0 || a.dim <= 0) return hipSuccess;
-  const int packs = int(ceil_div64(a.dim, Pack<T>::N)), lanes = std::min(packs, kThreads), upb = kThreads / lanes;
+  const int packs = int(ceil_div64(a.dim, Pack<T>::N)), lanes = lanes_per_unit(a.dim, Pack<T>::N);
+  const int upb = units_per_block(a.dim, Pack<T>::N);
   const int64_t table_packs = ceil_div64(a.vocab * ceil_div64(a.dim, Pack<T>::N), 4);  // four a thread
   const GradLayout L = grad_layout(a.n, a.dim);
   char* base = static_cast<char*>(a.scratch);
@@ -350,19 +393,21 @@ hipError_t gradient(const EmbeddingArgs& a, hipStream_t s) {
   if (e != hipSuccess) return e;
   float* partial = reinterpret_cast<float*>(base + L.partial);
   const int unit_rows = unit_rows_for(a.n, a.dim);
-  const int64_t units = ceil_div64(a.n, unit_rows);
-  unit_sums_kernel<T><<<uint32_t(ceil_div64(units, upb)), kThreads, 0, s>>>(a, keys, pos, partial, unit_rows, packs,
-                                                                           lanes, upb);
+  const int block_rows = unit_rows * upb;
+  const int64_t blocks = ceil_div64(a.n, block_rows);
+  unit_sums_kernel<T><<<uint32_t(blocks), kThreads, 0, s>>>(a, keys, pos, partial, unit_rows, packs, lanes, upb);
   if ((e = hipGetLastError()) != hipSuccess) return e;
-  if (units > 1)
-    join_kernel<T><<<dim3(uint32_t(ceil_div64(units, kJoinWaves)), uint32_t(ceil_div64(a.dim, kJoinColumns))),
-                     kJoinThreads, 0, s>>>(a, keys, partial, unit_rows, units);
+  if (blocks > 1)
+    join_kernel<T><<<dim3(uint32_t(ceil_div64(blocks, kJoinWaves)), uint32_t(ceil_div64(a.dim, kJoinColumns))),
+                     kJoinThreads, 0, s>>>(a, keys, partial, block_rows, blocks);
   return hipGetLastError();
 }
 
 }  // namespace
 
-size_t embedding_scratch_bytes(int64_t n, int64_t, int64_t dim) { return n > 0 ? grad_layout(n, dim).total : 0; }
+size_t embedding_scratch_bytes(int64_t n, int64_t vocab, int64_t dim) {
+  return n > 0 && vocab > 0 && dim > 0 ? grad_layout(n, dim).total : 0;
+}
 
 hipError_t launch_embedding(const EmbeddingArgs& a, gart_dtype t, hipStream_t s) {
   if (t == GART_DTYPE_F32) return lookup<float>(a, s);

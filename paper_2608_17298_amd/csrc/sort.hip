@@ -141,9 +141,12 @@ hipError_t scan_impl(const Tin* in, T* out, int64_t n, T* total, char* tmp, hipS
 // the per-wave counts into offsets; the block's keys are staged in LDS in
 // digit order and written out as contiguous runs per digit.
 // ---------------------------------------------------------------------------
-// COUNTS_BY_BLOCK: counts lie [block][digit] and are never scanned; the scatter
-// adds up what it needs of them.
-template <int ITEMS, bool COUNTS_BY_BLOCK, typename Source>
+// How the counts of a pass become positions: by a scan over all of them, by a
+// scan per digit whose totals the scatter scans, or (counts [block][digit]) by
+// sums in the scatter itself.
+enum Positions { SCAN_ALL, SCAN_DIGITS, SUM_BLOCKS };
+
+template <int ITEMS, Positions HOW, typename Source>
 __global__ __launch_bounds__(kSortThreads) void radix_hist_kernel(const Source source, int64_t m, int shift,
                                                                   uint32_t* __restrict__ counts, int nblocks) {
   __shared__ uint32_t h[256];
@@ -162,13 +165,13 @@ __global__ __launch_bounds__(kSortThreads) void radix_hist_kernel(const Source s
     if (j < m) atomicAdd(&h[(kv[r] >> shift) & 255u], 1u);
   }
   __syncthreads();
-  if (COUNTS_BY_BLOCK)
+  if (HOW == SUM_BLOCKS)
     counts[int64_t(blockIdx.x) * 256 + threadIdx.x] = h[threadIdx.x];
   else
     counts[int64_t(threadIdx.x) * nblocks + blockIdx.x] = h[threadIdx.x];
 }
 
-template <int ITEMS, bool COUNTS_BY_BLOCK, typename Source>
+template <int ITEMS, Positions HOW, typename Source>
 __global__ __launch_bounds__(kSortThreads) void radix_scatter_kernel(
     const Source source, uint32_t* __restrict__ kout, uint32_t* __restrict__ vout, int64_t m, int shift, const uint32_t* __restrict__ offsets, int nblocks) {
   __shared__ uint32_t s_keys[(kSortThreads * ITEMS)];
@@ -185,7 +188,11 @@ __global__ __launch_bounds__(kSortThreads) void radix_scatter_kernel(
 
 #pragma unroll
   for (int w = 0; w < kWaves; ++w) s_wave[w][tid] = 0;
-  if (COUNTS_BY_BLOCK) {
+  if (HOW == SCAN_DIGITS) {
+    uint32_t total;
+    s_gofs[tid] = block_exclusive(offsets[int64_t(256) * nblocks + tid], &total) +
+                  offsets[int64_t(tid) * nblocks + blockIdx.x];
+  } else if (HOW == SUM_BLOCKS) {
     uint32_t before = 0, all = 0;  // of this digit: in the blocks before, and in all
 #pragma unroll 16
     for (int b = 0; b < nblocks; ++b) {
@@ -359,23 +366,52 @@ size_t radix_tmp_bytes(int64_t m) {
 
 namespace {
 
-template <int ITEMS, bool COUNTS_BY_BLOCK, typename Source>
+// Counts [digit][block] to positions: a block per digit scans its blocks'
+// counts and leaves the digit's total, which the scatter's blocks scan over
+// the digits.
+constexpr int kDigitThreads = 1024;
+__global__ __launch_bounds__(kDigitThreads) void digit_scan_kernel(uint32_t* __restrict__ counts, int nblocks,
+                                                                   uint32_t* __restrict__ totals) {
+  __shared__ uint32_t s_wave[kDigitThreads / 64];
+  uint32_t* row = counts + int64_t(blockIdx.x) * nblocks;
+  const int wave = threadIdx.x / 64;
+  uint32_t carry = 0;
+  for (int b0 = 0; b0 < nblocks; b0 += kDigitThreads) {
+    const int b = b0 + int(threadIdx.x);
+    const uint32_t v = b < nblocks ? row[b] : 0u, inc = wave_inclusive(v);
+    if (__lane_id() == 63) s_wave[wave] = inc;
+    __syncthreads();
+    uint32_t before = carry, all = 0;
+#pragma unroll
+    for (int w = 0; w < kDigitThreads / 64; ++w) {
+      if (w < wave) before += s_wave[w];
+      all += s_wave[w];
+    }
+    if (b < nblocks) row[b] = before + inc - v;
+    carry += all;
+    __syncthreads();
+  }
+  if (threadIdx.x == 0) totals[blockIdx.x] = carry;
+}
+
+template <int ITEMS, Positions HOW, typename Source>
 hipError_t radix_pass(const Source& source, uint32_t* kout, uint32_t* vout, int64_t m, int shift, void* tmp,
                       hipStream_t s) {
   const int64_t nb = ceil_div(m, kSortThreads * ITEMS);
   uint32_t* counts = static_cast<uint32_t*>(tmp);
   char* scan_tmp = static_cast<char*>(tmp) + ((size_t(nb) * 256 * sizeof(uint32_t) + 255) & ~size_t(255));
-  radix_hist_kernel<ITEMS, COUNTS_BY_BLOCK><<<nb, kSortThreads, 0, s>>>(source, m, shift, counts, int(nb));
+  radix_hist_kernel<ITEMS, HOW><<<nb, kSortThreads, 0, s>>>(source, m, shift, counts, int(nb));
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  if (!COUNTS_BY_BLOCK) e = scan_exclusive_u32(counts, counts, nb * 256, nullptr, scan_tmp, s);
+  if (HOW == SCAN_ALL) e = scan_exclusive_u32(counts, counts, nb * 256, nullptr, scan_tmp, s);
   if (e != hipSuccess) return e;
-  radix_scatter_kernel<ITEMS, COUNTS_BY_BLOCK>
-      <<<nb, kSortThreads, 0, s>>>(source, kout, vout, m, shift, counts, int(nb));
+  if (HOW == SCAN_DIGITS) digit_scan_kernel<<<256, kDigitThreads, 0, s>>>(counts, int(nb), counts + nb * 256);
+  if ((e = hipGetLastError()) != hipSuccess) return e;
+  radix_scatter_kernel<ITEMS, HOW><<<nb, kSortThreads, 0, s>>>(source, kout, vout, m, shift, counts, int(nb));
   return hipGetLastError();
 }
 
-template <bool COUNTS_BY_BLOCK>
+template <Positions HOW>
 hipError_t sort_ids(const void* ids, bool ids64, int64_t limit, uint32_t* keys, uint32_t* pos, uint32_t* keys_alt,
                     uint32_t* pos_alt, int64_t m, int bits, void* tmp, hipStream_t s) {
   uint32_t *ka = keys, *va = pos, *kb = keys_alt, *vb = pos_alt;
@@ -386,12 +422,12 @@ hipError_t sort_ids(const void* ids, bool ids64, int64_t limit, uint32_t* keys, 
   for (int shift = 0; shift < bits; shift += 8) {
     hipError_t e;
     if (shift > 0)
-      e = radix_pass<kIdItems, COUNTS_BY_BLOCK>(PairSource{kb, vb}, ka, va, m, shift, tmp, s);
+      e = radix_pass<kIdItems, HOW>(PairSource{kb, vb}, ka, va, m, shift, tmp, s);
     else if (ids64)
-      e = radix_pass<kIdItems, COUNTS_BY_BLOCK>(IdSource<int64_t>{static_cast<const int64_t*>(ids), limit}, ka, va, m,
+      e = radix_pass<kIdItems, HOW>(IdSource<int64_t>{static_cast<const int64_t*>(ids), limit}, ka, va, m,
                                                 0, tmp, s);
     else
-      e = radix_pass<kIdItems, COUNTS_BY_BLOCK>(IdSource<int32_t>{static_cast<const int32_t*>(ids), limit}, ka, va, m,
+      e = radix_pass<kIdItems, HOW>(IdSource<int32_t>{static_cast<const int32_t*>(ids), limit}, ka, va, m,
                                                 0, tmp, s);
     if (e != hipSuccess) return e;
     std::swap(ka, kb);
@@ -414,7 +450,7 @@ hipError_t radix_sort_u32(uint32_t* keys, uint32_t* vals, uint32_t* keys_alt, ui
   }
   uint32_t *ka = keys, *va = vals, *kb = keys_alt, *vb = vals_alt;
   for (int shift = 0; shift < bits; shift += 8) {
-    const hipError_t e = radix_pass<kSortItems, false>(PairSource{ka, va}, kb, vb, m, shift, tmp, s);
+    const hipError_t e = radix_pass<kSortItems, SCAN_ALL>(PairSource{ka, va}, kb, vb, m, shift, tmp, s);
     if (e != hipSuccess) return e;
     std::swap(ka, kb);
     std::swap(va, vb);
@@ -426,13 +462,14 @@ hipError_t radix_sort_u32(uint32_t* keys, uint32_t* vals, uint32_t* keys_alt, ui
   return hipSuccess;
 }
 
-size_t radix_ids_tmp_bytes(int64_t m) { return radix_tmp_bytes(m * kSortItems / kIdItems); }
+// counts, then (SCAN_DIGITS) 256 totals
+size_t radix_ids_tmp_bytes(int64_t m) { return radix_tmp_bytes(m * kSortItems / kIdItems) + 256 * sizeof(uint32_t); }
 
 hipError_t radix_sort_ids(const void* ids, bool ids64, int64_t limit, uint32_t* keys, uint32_t* pos,
                           uint32_t* keys_alt, uint32_t* pos_alt, int64_t m, int bits, void* tmp, hipStream_t s) {
   return ceil_div(m, kSortThreads * kIdItems) <= kFewBlocks
-             ? sort_ids<true>(ids, ids64, limit, keys, pos, keys_alt, pos_alt, m, bits, tmp, s)
-             : sort_ids<false>(ids, ids64, limit, keys, pos, keys_alt, pos_alt, m, bits, tmp, s);
+             ? sort_ids<SUM_BLOCKS>(ids, ids64, limit, keys, pos, keys_alt, pos_alt, m, bits, tmp, s)
+             : sort_ids<SCAN_DIGITS>(ids, ids64, limit, keys, pos, keys_alt, pos_alt, m, bits, tmp, s);
 }
 
 hipError_t fill_u32(uint32_t* p, uint32_t v, int64_t n, hipStream_t s) { return fill_any<uint32_t>(p, v, n, s); }

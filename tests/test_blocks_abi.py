@@ -96,6 +96,10 @@ def test_scratch_refused():
 def test_scratch_sizes():
     from paper_2608_17298_amd import gart
     lib = gart.lib()
+    for empty in ((0, 5, 5), (5, 0, 5), (5, 5, 0), (0, 0, 0)):
+        assert lib.gart_embedding_scratch_bytes(*empty) == 0
+        lib.gart_linear_scratch_bytes(*empty, 0)
+        lib.gart_linear_backward_scratch_bytes(*empty, 1, 2)
     assert lib.gart_embedding_scratch_bytes(0, 5, 5) == 0 and lib.gart_embedding_scratch_bytes(-1, 5, 5) == 0
     assert lib.gart_linear_backward_scratch_bytes(-1, 5, 5, 0, 0) == 0
     assert lib.gart_linear_backward_scratch_bytes(10, 5, 5, 7, 0) == 0
