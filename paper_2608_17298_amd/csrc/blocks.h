@@ -50,6 +50,17 @@ __device__ __forceinline__ int fresh(int v) {
   return v;
 }
 
+// Loaded values are waited for here.  Loads and stores retire in order, so a
+// wait placed after younger stores would wait for those as well.
+template <typename V>
+__device__ __forceinline__ void arrive(V& v) {
+  typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+  u32x4 w;
+  __builtin_memcpy(&w, &v, 16);
+  asm volatile("" : "+v"(w));
+  __builtin_memcpy(&v, &w, 16);
+}
+
 // The first `count` elements at p, the rest zero.
 template <typename T>
 __device__ __forceinline__ Pack<T> load_some(const T* p, int count) {
@@ -81,14 +92,12 @@ __device__ __forceinline__ PackMask<T> first_of_pack(int count) {
 }
 
 template <typename T>
-__device__ __forceinline__ Pack<T> load_masked(const T* p, const PackMask<T>& m) {
-  const packed16 r = *reinterpret_cast<const packed16*>(p);
-  packed16 q;
+__device__ __forceinline__ void mask_pack(Pack<T>& v, const PackMask<T>& m) {
+  uint32_t w[4];
+  __builtin_memcpy(w, &v, 16);
 #pragma unroll
-  for (int i = 0; i < 4; ++i) q.w[i] = r.w[i] & m.w[i];
-  Pack<T> v;
-  __builtin_memcpy(&v, &q, 16);
-  return v;
+  for (int i = 0; i < 4; ++i) w[i] &= m.w[i];
+  __builtin_memcpy(&v, w, 16);
 }
 
 template <typename T>

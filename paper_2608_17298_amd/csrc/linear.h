@@ -141,6 +141,14 @@ __device__ __forceinline__ typename Pack<T>::V fragment_of_columns(const T* lds,
   return v;
 }
 
+// A barrier that orders the block's LDS accesses alone: loads and stores of
+// global memory stay in flight across it (__syncthreads waits for them all).
+__device__ __forceinline__ void lds_barrier() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+  __builtin_amdgcn_s_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+}
+
 // ---- how the work is cut (linear.hip) --------------------------------------------
 // Products that do not stream: tiles of 256 (one block of 8 waves a CU, straight
 // into LDS) where they fill the card, else of 128, else of 64; where even these

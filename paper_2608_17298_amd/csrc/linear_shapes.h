@@ -19,7 +19,8 @@ inline int round_inputs(int64_t k) {
   return p;
 }
 
-inline int64_t forward_lds(int kp, int64_t n, size_t es) { return (n + 31) / 32 * 32 * (kp + 16 / int64_t(es)) * int64_t(es); }
+// the weight's rows, 16 bytes longer, and the bias as floats
+inline int64_t forward_lds(int kp, int64_t n, size_t es) { return (n + 31) / 32 * 32 * (kp * int64_t(es) + 16 + 4); }
 
 // At most `most` blocks, all with the same number of turns (or one less).
 inline int64_t even_blocks(int64_t turns, int64_t most) {

@@ -31,7 +31,8 @@ constexpr int kSpare = 8;  // rows of at least one element that hold a pack
 
 // KP: inputs, rounded up.  LDS rows are 16 bytes longer, which spreads the
 // rows that lanes read together over the banks.
-template <typename T, int KP>
+// TAIL: fewer inputs than KP.
+template <typename T, int KP, bool TAIL>
 __global__ __launch_bounds__(64 * kForwardWaves) void stream_forward_kernel(const LinearArgs a) {
   constexpr int V = Pack<T>::N, S = KP / kDepth<T>, PITCH = KP + V, THREADS = 64 * kForwardWaves;
   extern __shared__ __attribute__((aligned(16))) char lds_raw[];
@@ -45,74 +46,73 @@ __global__ __launch_bounds__(64 * kForwardWaves) void stream_forward_kernel(cons
     if (row < a.n && at < a.k) p = load_some(static_cast<const T*>(a.w) + row * a.w_ld + at, int(min(int64_t(V), a.k - at)));
     *reinterpret_cast<typename Pack<T>::V*>(w + row * PITCH + at) = p.v;
   }
+  // the bias too: a load from memory would be waited for behind the stores
+  float* s_bias = reinterpret_cast<float*>(w + n_pad * PITCH);
+  for (int n = tid; n < n_pad; n += THREADS) s_bias[n] = a.bias && n < a.n ? float(static_cast<const T*>(a.bias)[n]) : 0.0f;
   __syncthreads();
   const T* x = static_cast<const T*>(a.x);
-  const T* bias = static_cast<const T*>(a.bias);
   const T* res = static_cast<const T*>(a.residual);
   T* y = static_cast<T*>(a.y);
   constexpr int Q = 8 / V;  // packs of outputs per lane: one of 8, or one of 4 from each tile
   const int64_t tiles = (a.m + 31) / 32, step = int64_t(gridDim.x) * kForwardWaves;
-  // Away from the end, lanes' offsets in a tile are the same for all tiles, and
-  // a whole pack may be read at the end of a row: kSpare rows follow it.
-  const bool near_x = a.x_ld <= kNear && a.x_ld > 0, near_y = a.y_ld <= kNear && a.residual_ld <= kNear;
+  // Inside, away from the last rows, lanes' offsets in a tile are the same for
+  // all tiles, and a whole pack may be read at the end of a row: kSpare rows
+  // follow it.  The edge has a loop of its own, so that nothing but the loads
+  // themselves writes the registers they are on the way to.
+  const bool near = a.x_ld <= kNear && a.x_ld > 0 && a.y_ld <= kNear && a.residual_ld <= kNear;
+  const int64_t inside = near && a.m > kSpare ? (a.m - kSpare) / 32 : 0;
   const uint32_t x_off = uint32_t(r * a.x_ld + V * g), y_off = uint32_t(r * a.y_ld + (Q == 1 ? 8 : 4) * g),
                  res_off = uint32_t(r * a.residual_ld + (Q == 1 ? 8 : 4) * g);
-  // the last, partial step of k
-  const int k_last = int(a.k) / kDepth<T> * kDepth<T> + V * g;
-  const PackMask<T> k_mask = first_of_pack<T>(int(a.k) - k_last);
-  const uint32_t x_last = uint32_t(r * a.x_ld) + (k_last < a.k ? k_last : 0);
-  auto load_x = [&](int64_t t, typename Pack<T>::V(&fx)[2][S]) {
-    if (t >= tiles) return;
-    if (near_x && (t + 1) * 32 + kSpare <= a.m) {
+  uint32_t x_at[S];
+  PackMask<T> x_mask[S];
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const T* p = x + (t * 32 + 16 * i) * a.x_ld;
+  for (int s = 0; s < S; ++s) {
+    const int count = int(a.k) - (s * kDepth<T> + V * g);
+    x_at[s] = TAIL && count <= 0 ? x_off - V * g : x_off + s * kDepth<T>;
+    x_mask[s] = first_of_pack<T>(count);
+  }
+  typedef typename Pack<T>::V Rows[2][S];
+  auto load_inside = [&](int64_t t, Rows& f) {
 #pragma unroll
-        for (int s = 0; s < S; ++s) {
-          constexpr int D = kDepth<T>;
-          if (s * D + D <= int(a.k))
-            fx[i][s] = load_pack(p + (x_off + s * D)).v;
-          else if (s * D < int(a.k))
-            fx[i][s] = load_masked(p + x_last, k_mask).v;
-          else
-            fx[i][s] = T(0.0f);
-        }
-      }
-      return;
+    for (int i = 0; i < 2; ++i) {
+      const T* p = x + (t * 32 + 16 * i) * a.x_ld;
+#pragma unroll
+      for (int s = 0; s < S; ++s) f[i][s] = load_pack(p + x_at[s]).v;  // masked where it is used: not a wait here
     }
+  };
+  auto load_edge = [&](int64_t t, Rows& f) {
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       const int64_t row = t * 32 + 16 * i + r;
 #pragma unroll
       for (int s = 0; s < S; ++s) {
         const int64_t k = s * kDepth<T> + V * g;
-        fx[i][s] = T(0.0f);
-        if (row < a.m && k < a.k) fx[i][s] = load_some(x + row * a.x_ld + k, fresh(int(a.k - k))).v;
+        f[i][s] = T(0.0f);
+        if (row < a.m && k < a.k) f[i][s] = load_some(x + row * a.x_ld + k, fresh(int(a.k - k))).v;
       }
     }
   };
-  const int64_t first = int64_t(blockIdx.x) * kForwardWaves + __builtin_amdgcn_readfirstlane(tid / 64);
-  typename Pack<T>::V fx[2][S], next[2][S];
-  load_x(first, next);
-  for (int64_t t = first; t < tiles; t += step) {
+  // The outputs of a tile's rows fx; before_stores(): between the first ones' sums and their stores.
+  auto outputs = [&](auto whole_tile, int64_t t, const Rows& fx, auto&& before_stores) {
+    constexpr bool whole = decltype(whole_tile)::value;
+    Pack<T> p[2][Q];
+    auto load_residual = [&](int n0) {
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+      for (int i = 0; i < 2; ++i) {
+        const int64_t row = t * 32 + 16 * i + r;
 #pragma unroll
-      for (int s = 0; s < S; ++s) fx[i][s] = next[i][s];
-    load_x(t + step, next);
-    const bool whole = near_y && (t + 1) * 32 <= a.m;
-    for (int n0 = 0; n0 < n_pad; n0 += 32) {
-      Pack<T> p[2][Q];
-      if (res && whole) {
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-#pragma unroll
-          for (int q = 0; q < Q; ++q)
-          {
-            const int count = fresh(int(a.n) - (n0 + 16 * q + (Q == 1 ? 8 : 4) * g));
-            if (count > 0) p[i][q] = load_some(res + (t * 32 + 16 * i) * a.residual_ld + n0 + 16 * q + res_off, count);
-          }
+        for (int q = 0; q < Q; ++q) {
+          const int n = n0 + 16 * q + (Q == 1 ? 8 : 4) * g, count = fresh(int(a.n) - n);
+          if (count <= 0) continue;
+          if (whole)
+            p[i][q] = load_some(res + (t * 32 + 16 * i) * a.residual_ld + (n0 + 16 * q + res_off), count);
+          else if (row < a.m)
+            p[i][q] = load_some(res + row * a.residual_ld + n, count);
+        }
       }
+    };
+    if (res) load_residual(0);
+    for (int n0 = 0; n0 < n_pad; n0 += 32) {
       f32x4 acc[2][2] = {};
 #pragma unroll
       for (int s = 0; s < S; ++s) {
@@ -123,22 +123,15 @@ __global__ __launch_bounds__(64 * kForwardWaves) void stream_forward_kernel(cons
           for (int i = 0; i < 2; ++i) acc[i][j] = Mfma<T>::run(fw, fx[i][s], acc[i][j]);
         }
       }
+      Pack<T> o[2][Q];
 #pragma unroll
       for (int q = 0; q < Q; ++q) {
-        const int64_t n = n0 + (Q == 1 ? 8 * g : 16 * q + 4 * g);
-        const int count = fresh(int(a.n - n));
+        const float* b = s_bias + n0 + (Q == 1 ? 8 * g : 16 * q + 4 * g);
         float c[2][V];
 #pragma unroll
         for (int i = 0; i < 2; ++i)
 #pragma unroll
-          for (int e = 0; e < V; ++e) c[i][e] = acc[i][Q == 1 ? e / 4 : q][e % 4];
-        if (bias && count > 0) {
-          const Pack<T> b = load_some(bias + n, count);
-#pragma unroll
-          for (int i = 0; i < 2; ++i)
-#pragma unroll
-            for (int e = 0; e < V; ++e) c[i][e] += float(b.v[e]);
-        }
+          for (int e = 0; e < V; ++e) c[i][e] = acc[i][Q == 1 ? e / 4 : q][e % 4] + b[e];
         with_activation(a.act, [&](auto act) {
 #pragma unroll
           for (int i = 0; i < 2; ++i)
@@ -147,23 +140,60 @@ __global__ __launch_bounds__(64 * kForwardWaves) void stream_forward_kernel(cons
         });
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-          const int64_t row = t * 32 + 16 * i + r;
-          const bool here = row < a.m && count > 0;
           if (res) {
-            if (!whole && here) p[i][q] = load_some(res + row * a.residual_ld + n, count);
 #pragma unroll
             for (int e = 0; e < V; ++e) c[i][e] += float(p[i][q].v[e]);
           }
-          Pack<T> o;
 #pragma unroll
-          for (int e = 0; e < V; ++e) o.v[e] = T(c[i][e]);
-          if (whole && count > 0)
-            store_some(y + (t * 32 + 16 * i) * a.y_ld + n0 + 16 * q + y_off, o, count);
-          else if (!whole && here)
-            store_some(y + row * a.y_ld + n, o, count);
+          for (int e = 0; e < V; ++e) o[i][q].v[e] = T(c[i][e]);
+        }
+      }
+      // what the next steps need is asked for, and the next rows are here, before this step's stores
+      if (res && n0 + 32 < n_pad) load_residual(n0 + 32);
+      if (n0 == 0) before_stores();
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int64_t row = t * 32 + 16 * i + r;
+#pragma unroll
+        for (int q = 0; q < Q; ++q) {
+          const int n = n0 + (Q == 1 ? 8 * g : 16 * q + 4 * g), count = fresh(int(a.n) - n);
+          if (count <= 0) continue;
+          if (whole)
+            store_some(y + (t * 32 + 16 * i) * a.y_ld + (n0 + 16 * q + y_off), o[i][q], count);
+          else if (row < a.m)
+            store_some(y + row * a.y_ld + n, o[i][q], count);
         }
       }
     }
+  };
+  const int64_t first = int64_t(blockIdx.x) * kForwardWaves + __builtin_amdgcn_readfirstlane(tid / 64);
+  int64_t t = first;
+  Rows fx;
+  if (t < inside) {
+    Rows next;
+    load_inside(t, next);
+    for (; t < inside; t += step) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int s = 0; s < S; ++s) {
+          Pack<T> v;
+          v.v = next[i][s];
+          if (TAIL) mask_pack(v, x_mask[s]);
+          fx[i][s] = v.v;
+        }
+      load_inside(min(t + step, inside - 1), next);
+      outputs(std::true_type{}, t, fx, [&] {  // the next rows are here before this tile's stores are on the way
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int s = 0; s < S; ++s) arrive(next[i][s]);
+      });
+    }
+  }
+  for (; t < tiles; t += step) {
+    load_edge(t, fx);
+    outputs(std::false_type{}, t, fx, [] {});
   }
 }
 
@@ -213,13 +243,14 @@ __global__ __launch_bounds__((BackwardShape<T, KP, NS>::THREADS), (KP * sizeof(T
 
   constexpr int XALL = B::ROWS * (KP / V), XP = (XALL + B::THREADS - 1) / B::THREADS;  // x packs, per thread
   constexpr bool XEVEN = XALL % B::THREADS == 0;
-  // Away from the end, lanes' offsets in a tile are the same for all tiles, and
-  // a whole pack may be read at the end of a row: kSpare rows follow it.
+  // Inside and edge as in the forward.
   const bool near = a.x_ld <= kNear && a.dl_ld <= kNear && a.g_x_ld <= kNear && a.x_ld > 0 && a.dl_ld > 0;
+  const int64_t inside = near && a.m > kSpare ? (a.m - kSpare) / B::ROWS : 0;
   constexpr int XSTEP = B::THREADS / (KP / V);  // rows that one pack a thread covers
   const int x_at = tid % (KP / V) * V, x_count = XEVEN || tid < XALL ? int(a.k) - x_at : 0;
   const uint32_t x_off = x_count > 0 ? uint32_t(tid / (KP / V) * a.x_ld + x_at) : 0u,
                  gx_off = uint32_t(r * a.g_x_ld + (Q == 1 ? 8 : 4) * g);
+  const bool tail = a.k != KP || a.n != B::NP;  // packs are masked where they are used: not a wait for the load
   const uint32_t x_ld = uint32_t(a.x_ld), dl_ld = uint32_t(a.dl_ld), gx_ld = uint32_t(a.g_x_ld);  // if near
   const PackMask<T> x_mask = first_of_pack<T>(x_count);
   uint32_t dl_off[Q];
@@ -230,41 +261,26 @@ __global__ __launch_bounds__((BackwardShape<T, KP, NS>::THREADS), (KP * sizeof(T
     dl_mask[q] = first_of_pack<T>(int(a.n) - n0(q));
   }
   Pack<T> xr[XP], dr[MT][Q];
-  auto load_x = [&](int64_t t) {
-    if (near && (t + 1) * B::ROWS + kSpare <= a.m) {
-      const T* p = x + t * B::ROWS * a.x_ld;
+  auto load_x_inside = [&](int64_t t) {
+    const T* p = x + t * B::ROWS * a.x_ld;
 #pragma unroll
-      for (int u = 0; u < XP; ++u) {
-        if (XEVEN && a.k == KP)
-          xr[u] = load_pack(p + (x_off + u * XSTEP * x_ld));
-        else
-          xr[u] = load_masked(p + (x_off + u * XSTEP * x_ld), x_mask);
-      }
-      return;
-    }
+    for (int u = 0; u < XP; ++u) xr[u] = load_pack(p + (x_off + u * XSTEP * x_ld));
+  };
+  auto load_dl_inside = [&](int64_t t) {
+    const T* p = dl + t * B::ROWS * a.dl_ld;
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+      for (int q = 0; q < Q; ++q) dr[i][q] = load_pack(p + (dl_off[q] + 16 * i * dl_ld));
+  };
+  auto load_edge = [&](int64_t t) {
 #pragma unroll
     for (int u = 0; u < XP; ++u) {
       const int c = u * B::THREADS + tid;
       const int64_t row = t * B::ROWS + c / (KP / V);
       const int at = c % (KP / V) * V;
       xr[u].v = T(0.0f);
-      if ((XEVEN || c < XALL) && t < tiles && row < a.m && at < a.k)
-        xr[u] = load_some(x + row * a.x_ld + at, fresh(int(a.k) - at));
-    }
-  };
-  auto load_dl = [&](int64_t t) {
-    if (near && (t + 1) * B::ROWS + kSpare <= a.m) {
-      const T* p = dl + t * B::ROWS * a.dl_ld;
-#pragma unroll
-      for (int i = 0; i < MT; ++i)
-#pragma unroll
-        for (int q = 0; q < Q; ++q) {
-          if (a.n == B::NP)
-            dr[i][q] = load_pack(p + (dl_off[q] + 16 * i * dl_ld));
-          else
-            dr[i][q] = load_masked(p + (dl_off[q] + 16 * i * dl_ld), dl_mask[q]);
-        }
-      return;
+      if ((XEVEN || c < XALL) && row < a.m && at < a.k) xr[u] = load_some(x + row * a.x_ld + at, fresh(int(a.k) - at));
     }
 #pragma unroll
     for (int i = 0; i < MT; ++i) {
@@ -272,13 +288,10 @@ __global__ __launch_bounds__((BackwardShape<T, KP, NS>::THREADS), (KP * sizeof(T
 #pragma unroll
       for (int q = 0; q < Q; ++q) {
         dr[i][q].v = T(0.0f);
-        if (t < tiles && row < a.m && n0(q) < a.n)
-          dr[i][q] = load_some(dl + row * a.dl_ld + n0(q), fresh(int(a.n) - n0(q)));
+        if (row < a.m && n0(q) < a.n) dr[i][q] = load_some(dl + row * a.dl_ld + n0(q), fresh(int(a.n) - n0(q)));
       }
     }
   };
-  load_x(blockIdx.x);
-  load_dl(blockIdx.x);
   __syncthreads();  // W is there
   typename Pack<T>::V fw[2][S];
 #pragma unroll
@@ -286,16 +299,18 @@ __global__ __launch_bounds__((BackwardShape<T, KP, NS>::THREADS), (KP * sizeof(T
 #pragma unroll
     for (int s = 0; s < S; ++s) fw[j][s] = fragment_of_row(lw, B::KPITCH, 32 * slice + paired_row<T>(j, r), s * D, g);
 
-  for (int64_t t = blockIdx.x; t < tiles; t += gridDim.x) {
+  // One tile, whose rows are in (or on the way to) xr and dr; next: the tile to ask for meanwhile.
+  auto work = [&](auto whole_tile, int64_t t, int64_t next) {
+    constexpr bool whole = decltype(whole_tile)::value;
 #pragma unroll
     for (int u = 0; u < XP; ++u) {
       const int c = u * B::THREADS + tid;
       if (!XEVEN && c >= XALL) continue;
+      if (tail) mask_pack(xr[u], x_mask);
       *reinterpret_cast<typename Pack<T>::V*>(lx + c / (KP / V) * B::KPITCH + c % (KP / V) * V) = xr[u].v;
     }
-    __syncthreads();  // x is there; g_x of the last tile has read dz
-    load_x(t + gridDim.x);
-    const bool whole = (t + 1) * B::ROWS <= a.m;
+    lds_barrier();  // x is there; g_x of the last tile has read dz
+    if (whole) load_x_inside(next);
     // dz of this wave's rows and outputs
 #pragma unroll
     for (int i = 0; i < MT; ++i) {
@@ -308,6 +323,10 @@ __global__ __launch_bounds__((BackwardShape<T, KP, NS>::THREADS), (KP * sizeof(T
 #pragma unroll
           for (int j = 0; j < 2; ++j) z[j] = Mfma<T>::run(fw[j][s], fx, z[j]);
         }
+      }
+      if (tail) {
+#pragma unroll
+        for (int q = 0; q < Q; ++q) mask_pack(dr[i][q], dl_mask[q]);
       }
       float d[8];
       with_activation(a.act, [&](auto act) {
@@ -333,8 +352,8 @@ __global__ __launch_bounds__((BackwardShape<T, KP, NS>::THREADS), (KP * sizeof(T
         *reinterpret_cast<typename Pack<T>::V*>(lz + lrow * B::NPITCH + n0(q)) = o.v;
       }
     }
-    load_dl(t + gridDim.x);
-    __syncthreads();  // dz is there
+    if (whole) load_dl_inside(next);
+    lds_barrier();  // dz is there
     if (a.g_w) {
 #pragma unroll
       for (int s = 0; s < B::GROUP_ROWS / D; ++s) {
@@ -351,24 +370,32 @@ __global__ __launch_bounds__((BackwardShape<T, KP, NS>::THREADS), (KP * sizeof(T
       }
     }
     if (a.g_x) {
-      // 32 rows times 32 inputs at a time
-      for (int u = wave; u < B::ROWS / 32 * (KP / 32); u += B::WAVES) {
-        const int r0 = u / (KP / 32) * 32, kt = u % (KP / 32) * 2;
-        f32x4 acc[2][2] = {};
+      // 32 rows, or 16 where that leaves waves without, times 32 inputs at a time
+      constexpr int IT = B::ROWS / 32 * (KP / 32) >= B::WAVES ? 2 : 1;
+      for (int u = wave; u < B::ROWS / (16 * IT) * (KP / 32); u += B::WAVES) {
+        const int r0 = u / (KP / 32) * 16 * IT, kt = u % (KP / 32) * 2;
+        f32x4 acc[IT][2] = {};
 #pragma unroll
         for (int n = 0; n < B::NP; n += D) {
-          typename Pack<T>::V fz[2];
+          typename Pack<T>::V fz[IT];
 #pragma unroll
-          for (int i = 0; i < 2; ++i) fz[i] = fragment_of_row(lz, B::NPITCH, r0 + 16 * i + r, n, g);
+          for (int i = 0; i < IT; ++i) fz[i] = fragment_of_row(lz, B::NPITCH, r0 + 16 * i + r, n, g);
 #pragma unroll
           for (int j = 0; j < 2; ++j) {
             const auto fk = fragment_of_columns<T, true>(lw, B::KPITCH, kt + j, n, lane);
 #pragma unroll
-            for (int i = 0; i < 2; ++i) acc[i][j] = Mfma<T>::run(fk, fz[i], acc[i][j]);
+            for (int i = 0; i < IT; ++i) acc[i][j] = Mfma<T>::run(fk, fz[i], acc[i][j]);
           }
         }
+        // the next tile's loads are waited for before these stores
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
+        for (int i = 0; i < XP; ++i) arrive(xr[i]);
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+          for (int q = 0; q < Q; ++q) arrive(dr[i][q]);
+#pragma unroll
+        for (int i = 0; i < IT; ++i) {
           const int64_t row = t * B::ROWS + r0 + 16 * i + r;
 #pragma unroll
           for (int q = 0; q < Q; ++q) {
@@ -376,7 +403,7 @@ __global__ __launch_bounds__((BackwardShape<T, KP, NS>::THREADS), (KP * sizeof(T
             Pack<T> o;
 #pragma unroll
             for (int e = 0; e < V; ++e) o.v[e] = T(acc[i][Q == 1 ? e / 4 : q][e % 4]);
-            if (near && whole) {
+            if (whole) {
               if (k < a.k)
                 store_some(static_cast<T*>(a.g_x) + t * B::ROWS * a.g_x_ld + ((r0 + 16 * i) * gx_ld + 16 * (kt + q) + gx_off),
                            o, fresh(int(a.k - k)));
@@ -386,7 +413,17 @@ __global__ __launch_bounds__((BackwardShape<T, KP, NS>::THREADS), (KP * sizeof(T
         }
       }
     }
-    __syncthreads();  // x may be replaced
+    lds_barrier();  // x may be replaced
+  };
+  int64_t t = blockIdx.x;
+  if (t < inside) {
+    load_x_inside(t);
+    load_dl_inside(t);
+    for (; t < inside; t += gridDim.x) work(std::true_type{}, t, min(t + int64_t(gridDim.x), inside - 1));
+  }
+  for (; t < tiles; t += gridDim.x) {
+    load_edge(t);
+    work(std::false_type{}, t, 0);
   }
 
   // sums of the tile's columns, then those of the row groups, in order
@@ -460,8 +497,11 @@ __global__ __launch_bounds__((BackwardShape<T, KP, NS>::THREADS), (KP * sizeof(T
 template <typename T, int KP>
 hipError_t forward_kp(const LinearArgs& a, hipStream_t s) {
   const int64_t blocks = even_blocks(ceil_div64(ceil_div64(a.m, 32), kForwardWaves), kForwardBlocks);
-  stream_forward_kernel<T, KP>
-      <<<uint32_t(blocks), 64 * kForwardWaves, forward_lds(KP, a.n, sizeof(T)), s>>>(a);
+  const size_t lds = forward_lds(KP, a.n, sizeof(T));
+  if (a.k == KP)
+    stream_forward_kernel<T, KP, false><<<uint32_t(blocks), 64 * kForwardWaves, lds, s>>>(a);
+  else
+    stream_forward_kernel<T, KP, true><<<uint32_t(blocks), 64 * kForwardWaves, lds, s>>>(a);
   return hipGetLastError();
 }
 
