@@ -110,6 +110,24 @@ __device__ __forceinline__ typename Pack<T>::V fragment_of_row(const T* lds, int
   return *reinterpret_cast<const typename Pack<T>::V*>(lds + row * pitch + k0 + Pack<T>::N * g);
 }
 
+// A pack of a row (columns at ..) into LDS so that the rows a paired tile takes
+// stand side by side: of 16 bits, the first halves of a block of 32 columns come
+// before the second halves.  fragment_of_columns, unpaired, of such rows yields
+// the paired columns without bank conflicts (paired from plain rows: two-way);
+// along rows, two operands stored alike still agree on k.
+template <typename T>
+__device__ __forceinline__ void store_paired(T* row, int at, const Pack<T>& p) {
+  if constexpr (sizeof(T) == 4) {
+    *reinterpret_cast<typename Pack<T>::V*>(row + at) = p.v;
+  } else {
+    uint2 h[2];
+    __builtin_memcpy(h, &p, 16);
+    T* q = row + at / 32 * 32 + at % 32 / 2;
+    *reinterpret_cast<uint2*>(q) = h[0];
+    *reinterpret_cast<uint2*>(q + 16) = h[1];
+  }
+}
+
 // 16 bits, from lines across k: the lanes of a group of 16 name four lines times
 // 16 columns, four columns a lane, and the transposing load gives each lane the
 // four k of its column; the other four k lie `down` elements on.
@@ -126,7 +144,7 @@ __device__ __forceinline__ typename Pack<T>::V transposed_pair(const T* lds, int
 }
 
 // From LDS lines across k (line k holds the rows' elements side by side).
-template <typename T, bool PAIRED>
+template <typename T>
 __device__ __forceinline__ typename Pack<T>::V fragment_of_columns(const T* lds, int pitch, int tile, int k0, int lane) {
   const int r = lane % 16, g = lane / 16;
   typename Pack<T>::V v;
@@ -135,8 +153,7 @@ __device__ __forceinline__ typename Pack<T>::V fragment_of_columns(const T* lds,
 #pragma unroll
     for (int t = 0; t < 4; ++t) v[t] = q[t * pitch];
   } else {
-    const int col = PAIRED ? paired_row<T>(tile, 4 * (r % 4)) : 16 * tile + 4 * (r % 4);
-    v = transposed_pair(lds + (k0 + 8 * g + r / 4) * pitch + col, 4 * pitch);
+    v = transposed_pair(lds + (k0 + 8 * g + r / 4) * pitch + 16 * tile + 4 * (r % 4), 4 * pitch);
   }
   return v;
 }

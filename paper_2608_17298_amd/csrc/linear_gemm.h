@@ -101,7 +101,7 @@ struct Tile {
       const int row = PERM ? paired_row<T>(tile, r) : 16 * tile + r;
       return fragment_of_row(lds, PITCH, row, 0, (4 * s + g) ^ swizzle(row));
     } else if constexpr (!SHORT) {
-      return fragment_of_columns<T, PERM>(lds, PITCH, tile, kDepth<T> * s, lane);
+      return fragment_of_columns(lds, PITCH, tile, kDepth<T> * s, lane);
     } else {
       const int line = kDepth<T> * s + 8 * g + r / 4;  // line + 4 has the same exchange
       const int col = PERM ? paired_row<T>(tile, 4 * (r % 4)) : 16 * tile + 4 * (r % 4);

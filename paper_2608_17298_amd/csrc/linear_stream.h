@@ -113,7 +113,10 @@ __global__ __launch_bounds__(64 * kForwardWaves) void stream_forward_kernel(cons
     };
     if (res) load_residual(0);
     for (int n0 = 0; n0 < n_pad; n0 += 32) {
-      f32x4 acc[2][2] = {};
+      f32x4 acc[2][2];
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+        acc[0][j] = acc[1][j] = *reinterpret_cast<const f32x4*>(s_bias + n0 + paired_row<T>(j, 4 * g));
 #pragma unroll
       for (int s = 0; s < S; ++s) {
 #pragma unroll
@@ -126,12 +129,11 @@ __global__ __launch_bounds__(64 * kForwardWaves) void stream_forward_kernel(cons
       Pack<T> o[2][Q];
 #pragma unroll
       for (int q = 0; q < Q; ++q) {
-        const float* b = s_bias + n0 + (Q == 1 ? 8 * g : 16 * q + 4 * g);
         float c[2][V];
 #pragma unroll
         for (int i = 0; i < 2; ++i)
 #pragma unroll
-          for (int e = 0; e < V; ++e) c[i][e] = acc[i][Q == 1 ? e / 4 : q][e % 4] + b[e];
+          for (int e = 0; e < V; ++e) c[i][e] = acc[i][Q == 1 ? e / 4 : q][e % 4];
         with_activation(a.act, [&](auto act) {
 #pragma unroll
           for (int i = 0; i < 2; ++i)
@@ -220,7 +222,7 @@ __global__ __launch_bounds__((BackwardShape<T, KP, NS>::THREADS), (KP * sizeof(T
     Pack<T> p;
     p.v = T(0.0f);
     if (row < a.n && at < a.k) p = load_some(static_cast<const T*>(a.w) + row * a.w_ld + at, int(min(int64_t(V), a.k - at)));
-    *reinterpret_cast<typename Pack<T>::V*>(lw + row * B::KPITCH + at) = p.v;
+    store_paired(lw + row * B::KPITCH, at, p);
   }
 
   // a lane's outputs: n0(q) + 0 .. V-1
@@ -307,7 +309,7 @@ __global__ __launch_bounds__((BackwardShape<T, KP, NS>::THREADS), (KP * sizeof(T
       const int c = u * B::THREADS + tid;
       if (!XEVEN && c >= XALL) continue;
       if (tail) mask_pack(xr[u], x_mask);
-      *reinterpret_cast<typename Pack<T>::V*>(lx + c / (KP / V) * B::KPITCH + c % (KP / V) * V) = xr[u].v;
+      store_paired(lx + c / (KP / V) * B::KPITCH, c % (KP / V) * V, xr[u]);
     }
     lds_barrier();  // x is there; g_x of the last tile has read dz
     if (whole) load_x_inside(next);
@@ -315,7 +317,7 @@ __global__ __launch_bounds__((BackwardShape<T, KP, NS>::THREADS), (KP * sizeof(T
 #pragma unroll
     for (int i = 0; i < MT; ++i) {
       const int lrow = group * B::GROUP_ROWS + 16 * i + r;
-      f32x4 z[2] = {};
+      f32x4 z[2] = {f32x4{b[0], b[1], b[2], b[3]}, f32x4{b[4], b[5], b[6], b[7]}};
       if (a.act != GART_ACT_NONE) {
 #pragma unroll
         for (int s = 0; s < S; ++s) {
@@ -334,8 +336,7 @@ __global__ __launch_bounds__((BackwardShape<T, KP, NS>::THREADS), (KP * sizeof(T
         for (int q = 0; q < Q; ++q)
 #pragma unroll
           for (int e = 0; e < V; ++e)
-            d[q * V + e] = activate_grad<decltype(act)::value>(z[Q == 1 ? e / 4 : q][e % 4] + b[q * V + e],
-                                                               float(dr[i][q].v[e]));
+            d[q * V + e] = activate_grad<decltype(act)::value>(z[Q == 1 ? e / 4 : q][e % 4], float(dr[i][q].v[e]));
       });
       if (!whole && t * B::ROWS + lrow >= a.m) {  // a row that is not there has a slope all the same
 #pragma unroll
@@ -360,10 +361,10 @@ __global__ __launch_bounds__((BackwardShape<T, KP, NS>::THREADS), (KP * sizeof(T
         const int k0 = group * B::GROUP_ROWS + s * D;
         typename Pack<T>::V fz[2];
 #pragma unroll
-        for (int j = 0; j < 2; ++j) fz[j] = fragment_of_columns<T, false>(lz, B::NPITCH, 2 * slice + j, k0, lane);
+        for (int j = 0; j < 2; ++j) fz[j] = fragment_of_columns<T>(lz, B::NPITCH, 2 * slice + j, k0, lane);
 #pragma unroll
         for (int k = 0; k < KT; ++k) {
-          const auto fx = fragment_of_columns<T, true>(lx, B::KPITCH, k, k0, lane);
+          const auto fx = fragment_of_columns<T>(lx, B::KPITCH, k, k0, lane);
 #pragma unroll
           for (int j = 0; j < 2; ++j) acc_w[j][k] = Mfma<T>::run(fx, fz[j], acc_w[j][k]);
         }
@@ -382,7 +383,7 @@ __global__ __launch_bounds__((BackwardShape<T, KP, NS>::THREADS), (KP * sizeof(T
           for (int i = 0; i < IT; ++i) fz[i] = fragment_of_row(lz, B::NPITCH, r0 + 16 * i + r, n, g);
 #pragma unroll
           for (int j = 0; j < 2; ++j) {
-            const auto fk = fragment_of_columns<T, true>(lw, B::KPITCH, kt + j, n, lane);
+            const auto fk = fragment_of_columns<T>(lw, B::KPITCH, kt + j, n, lane);
 #pragma unroll
             for (int i = 0; i < IT; ++i) acc[i][j] = Mfma<T>::run(fk, fz[i], acc[i][j]);
           }
