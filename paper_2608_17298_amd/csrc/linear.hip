@@ -16,9 +16,17 @@ Cut cut_product(int64_t rows, int64_t cols, int64_t depth, int64_t most, bool wi
     const int64_t part = std::max<int64_t>(64, ceil_div64(ceil_div64(depth, n), 64) * 64);
     return Cut{t, part, std::max<int64_t>(1, ceil_div64(depth, part))};
   };
+  // Short sums are bound by their outputs: many small blocks overlap more of
+  // them (20000 x 256 -> 1024 f16: 49 us with 128, 44 with 64; 20000 x 200 -> 500
+  // f32: 99 and 62; 8000 x 512 -> 1000 f16: 22 and 25).
+  if (depth <= 256) return with(64, 1);
   if (wide && tiles(256) >= kCus * 7 / 8) return with(256, 1);
+  if (tiles(128) >= kCus * 3 / 2) return with(128, 1);
+  // Fewer of 128 leave CUs with one block and nothing to overlap (2000 x 2048 ->
+  // 2000 f16: 45 us, in two parts 43, with 64 38); long sums are worth the parts.
+  if (tiles(64) >= kCus * 2 && depth <= 4096) return with(64, 1);
   const int64_t p = parts(128, 512);
-  return tiles(128) * p >= kCus ? with(128, p) : with(64, parts(64, 256));
+  return tiles(128) * p >= kCus * 3 / 2 ? with(128, p) : with(64, parts(64, 256));
 }
 
 bool stream_forward_fits(int64_t k, int64_t n, size_t es) {

@@ -517,16 +517,21 @@ def _dtype(t: torch.Tensor) -> int:
     d = DTYPES.get(t.dtype)
     if d is None:
         raise ValueError(f"GART blocks take float32, bfloat16 or float16, not {t.dtype}")
+    if not t.is_cuda:
+        raise ValueError("GART takes device tensors only")
     return d
 
 
 def _matrix(t: torch.Tensor, like: torch.Tensor, name: str) -> gart_matrix:
     """A 2-D tensor whose rows are contiguous; rows may be strided, or one row repeated (stride 0)."""
-    if t.dim() != 2 or t.dtype != like.dtype or t.device != like.device or not t.is_cuda:
-        raise ValueError(f"{name} must be a 2-D {like.dtype} tensor on {like.device if like.is_cuda else 'a GPU'}")
-    rows, cols = t.shape
+    if t is not like and (t.dtype is not like.dtype or t.get_device() != like.get_device()):
+        raise ValueError(f"{name} must be a {like.dtype} tensor on {like.device}")
+    shape = t.shape
+    if len(shape) != 2:
+        raise ValueError(f"{name} must be a matrix")
+    rows, cols = shape
     step, inner = t.stride()
-    if cols > 1 and inner != 1 and rows > 0:
+    if inner != 1 and cols > 1 and rows > 0:
         raise ValueError(f"{name}'s rows must be contiguous")
     return gart_matrix(t.data_ptr(), rows, cols, step if rows > 1 else cols)
 
@@ -534,14 +539,15 @@ def _matrix(t: torch.Tensor, like: torch.Tensor, name: str) -> gart_matrix:
 def _vector(t: torch.Tensor | None, like: torch.Tensor, n: int, name: str):
     if t is None:
         return None
-    if t.dim() != 1 or t.shape[0] != n or t.dtype != like.dtype or t.device != like.device or (n > 1 and t.stride(0) != 1):
+    if t.dim() != 1 or t.shape[0] != n or t.dtype is not like.dtype \
+            or t.get_device() != like.get_device() or (n > 1 and t.stride(0) != 1):
         raise ValueError(f"{name} must be a contiguous {like.dtype} tensor of {n} elements on {like.device}")
     return t.data_ptr()
 
 
 def _ids(ids: torch.Tensor, like: torch.Tensor, n: int):
-    if ids.dim() != 1 or ids.shape[0] != n or ids.device != like.device or (n > 1 and ids.stride(0) != 1) \
-            or ids.dtype not in (torch.int32, torch.int64):
+    if ids.dim() != 1 or ids.shape[0] != n or ids.get_device() != like.get_device() \
+            or (n > 1 and ids.stride(0) != 1) or ids.dtype not in (torch.int32, torch.int64):
         raise ValueError(f"ids must be a contiguous int32 or int64 tensor of {n} elements on {like.device}")
     return ids.data_ptr(), int(ids.dtype == torch.int64)
 
@@ -549,17 +555,18 @@ def _ids(ids: torch.Tensor, like: torch.Tensor, n: int):
 def _scratch(scratch: torch.Tensor | None, like: torch.Tensor):
     if scratch is None:
         return None, 0
-    if scratch.device != like.device or not scratch.is_contiguous():
+    if scratch.get_device() != like.get_device() or not scratch.is_contiguous():
         raise ValueError(f"scratch must be a contiguous tensor on {like.device}")
     return scratch.data_ptr(), scratch.numel() * scratch.element_size()
 
 
 def _stream_on(stream, like: torch.Tensor):
     """The raw stream of the call: `stream`, or the current one of the tensors' GPU, which must be the current GPU."""
-    if like.device.index != torch.cuda.current_device():
+    device = like.get_device()
+    if device != torch.cuda.current_device():
         raise ValueError(f"tensors are on {like.device}, the current GPU is {torch.cuda.current_device()}")
     if stream is None:  # the raw handle: a Stream object costs as much as the launch
-        return torch._C._cuda_getCurrentRawStream(like.device.index)
+        return torch._C._cuda_getCurrentRawStream(device)
     return stream.cuda_stream
 
 
