@@ -455,7 +455,7 @@ gart_status gart_frame_status(const gart_frame* frame, uint32_t* flags_host, voi
  *  - An output may not overlap another output or an input, except where a
  *    call names one it may be equal to (the same data and stride).
  *  - The calls only enqueue kernels (they may be captured in a HIP graph) and
- *    give the same bits for the same inputs.  scratch is caller-owned device
+ *    give the same bits for the same inputs laid out alike.  scratch is caller-owned device
  *    memory, 16-byte aligned, used by one stream at a time, with nothing kept
  *    in it between calls.  INVALID_ARG for NULL, mismatched or overlapping
  *    arguments, before anything is launched. */

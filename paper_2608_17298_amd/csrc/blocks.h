@@ -43,6 +43,15 @@ __device__ __forceinline__ void store_pack(T* p, const Pack<T>& r) {
   *reinterpret_cast<packed16*>(p) = q;
 }
 
+// The same past the caches, for full lines that nothing is going to read soon.
+template <typename T>
+__device__ __forceinline__ void store_past(T* p, const Pack<T>& r) {
+  typedef uint32_t u32x4 __attribute__((ext_vector_type(4), aligned(2)));
+  u32x4 q;
+  __builtin_memcpy(&q, &r, 16);
+  __builtin_nontemporal_store(q, reinterpret_cast<u32x4*>(p));
+}
+
 // A value the compiler takes for new, so that comparisons with it are made where
 // they are needed and not held through a loop (in scalar registers, which spill).
 __device__ __forceinline__ int fresh(int v) {

@@ -275,7 +275,11 @@ __global__ __launch_bounds__(64 * WI * WJ) void gemm_kernel(const GemmArgs g) {
         Pack<T> o;
 #pragma unroll
         for (int e = 0; e < V; ++e) o.v[e] = T(c[e]);
-        store_some(static_cast<T*>(g.out) + row * g.out_ld + j, o, count);
+        T* out = static_cast<T*>(g.out) + row * g.out_ld + j;
+        if (DIRECT && count == V)
+          store_past(out, o);  // large: it would push the operands out (4096 x 1024 -> 4096 f16: 50 us, past 44)
+        else
+          store_some(out, o, count);
       }
     }
     if constexpr (EPI == EPI_DZ) {
