@@ -47,11 +47,9 @@ struct Tile {
   }
 
   // ---- through registers: any size and alignment ----
-  Pack<T> reg[PER_THREAD];
-
   // rows x ks elements are there; i0, k0: where the tile begins
-  __device__ __forceinline__ void load(const T* __restrict__ p, int64_t ld, int64_t i0, int64_t rows, int64_t k0,
-                                       int64_t ks, int tid) {
+  static __device__ __forceinline__ void load_edge(Pack<T> (&reg)[PER_THREAD], const T* __restrict__ p, int64_t ld,
+                                                   int64_t i0, int64_t rows, int64_t k0, int64_t ks, int tid) {
 #pragma unroll
     for (int u = 0; u < PER_THREAD; ++u) {
       const int c = u * THREADS + tid;
@@ -62,7 +60,7 @@ struct Tile {
       if (l < lines && o < length) reg[u] = load_some(p + l * ld + o, int(min(int64_t(V), length - o)));
     }
   }
-  __device__ __forceinline__ void store(T* lds, int tid) const {
+  static __device__ __forceinline__ void store(T* lds, const Pack<T> (&reg)[PER_THREAD], int tid) {
 #pragma unroll
     for (int u = 0; u < PER_THREAD; ++u) {
       const int c = u * THREADS + tid;
@@ -71,27 +69,37 @@ struct Tile {
     }
   }
 
-  // ---- straight into LDS: a wave's 64 packs land side by side, so the
-  // exchange is made on the memory side.  Rows past the end repeat the last
-  // (pack of) rows; their products are not stored.
+  // ---- whole steps of k, without checks ----
+  // Rows past the end repeat the last one (pack of them, for lines across k);
+  // their products are not stored.  Needs whole packs of rows at the end.
+  static __device__ __forceinline__ bool regular(int64_t i0, int64_t rows) {
+    return KC || i0 + ROWS <= rows || rows % V == 0;
+  }
   const T* from[PER_THREAD];
 
+  // DIRECT: in the order of LDS, where a wave's 64 packs land side by side
+  template <bool DIRECT>
   __device__ __forceinline__ void aim(const T* p, int64_t ld, int64_t i0, int64_t rows, int64_t k0, int tid) {
 #pragma unroll
     for (int u = 0; u < PER_THREAD; ++u) {
       const int c = u * THREADS + tid;
-      const int line = c / LINE_PACKS, at = (c % LINE_PACKS ^ swizzle(line)) * V;
+      const int line = c / LINE_PACKS, at = (DIRECT ? c % LINE_PACKS ^ swizzle(line) : c % LINE_PACKS) * V;
       from[u] = KC ? p + min(i0 + line, rows - 1) * ld + k0 + at : p + (k0 + line) * ld + min(i0 + at, rows - V);
     }
   }
-  __device__ __forceinline__ void fetch(T* lds, int64_t ld, int wave) {
+  static __device__ __forceinline__ int64_t stride(int64_t ld) { return KC ? int64_t(kStep<T>) : kStep<T> * ld; }
+
+  __device__ __forceinline__ void load(Pack<T> (&reg)[PER_THREAD], int64_t offset) const {
+#pragma unroll
+    for (int u = 0; u < PER_THREAD; ++u) reg[u] = load_pack(from[u] + offset);
+  }
+  __device__ __forceinline__ void fetch(T* lds, int64_t offset, int wave) const {
     typedef const __attribute__((address_space(1))) uint32_t* global_ptr;
     typedef __attribute__((address_space(3))) uint32_t* lds_ptr;
 #pragma unroll
-    for (int u = 0; u < PER_THREAD; ++u) {
-      __builtin_amdgcn_global_load_lds((global_ptr)(from[u]), (lds_ptr)(lds + (u * THREADS + 64 * wave) * V), 16, 0, 0);
-      from[u] += KC ? int64_t(kStep<T>) : kStep<T> * ld;
-    }
+    for (int u = 0; u < PER_THREAD; ++u)
+      __builtin_amdgcn_global_load_lds((global_ptr)(from[u] + offset), (lds_ptr)(lds + (u * THREADS + 64 * wave) * V), 16,
+                                       0, 0);
   }
 
   // fragment of 16 rows at tile `tile`, step `s` of the line's two
@@ -180,39 +188,68 @@ __global__ __launch_bounds__(64 * WI * WJ) void gemm_kernel(const GemmArgs g) {
         for (int j = 0; j < TJ; ++j) acc[i][j] = Mfma<T>::run(fb[j], fa[i], acc[i][j]);
     }
   };
+  const int64_t a_step = TA::stride(g.a_ld), b_step = TB::stride(g.b_ld), whole = (k1 - k0) / kStep<T>;
   TA ta;
   TB tb;
-  int buf = 0;
   if constexpr (DIRECT) {
-    ta.aim(pa, g.a_ld, i0, g.rows, k0, tid);
-    tb.aim(pb, g.b_ld, j0, g.cols, k0, tid);
-    if (k0 < k1) {
-      ta.fetch(lds[0], g.a_ld, wave);
-      tb.fetch(lds[0] + TA::ELEMS, g.b_ld, wave);
-    }
-    for (int64_t k = k0; k < k1; k += kStep<T>) {
+    ta.template aim<true>(pa, g.a_ld, i0, g.rows, k0, tid);
+    tb.template aim<true>(pb, g.b_ld, j0, g.cols, k0, tid);
+    auto fetch = [&](int h, int64_t n) {
+      ta.fetch(lds[h], n * a_step, wave);
+      tb.fetch(lds[h] + TA::ELEMS, n * b_step, wave);
+    };
+    if (whole > 0) fetch(0, 0);
+    for (int64_t n = 0; n < whole; ++n) {
       asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // this wave's part of the buffer has landed
       __syncthreads();                                  // everyone's has, and the other buffer has been read
-      if (k + kStep<T> < k1) {
-        ta.fetch(lds[buf ^ 1], g.a_ld, wave);
-        tb.fetch(lds[buf ^ 1] + TA::ELEMS, g.b_ld, wave);
-      }
-      multiply(lds[buf], lds[buf] + TA::ELEMS);
-      buf ^= 1;
+      if (n + 1 < whole) fetch((n + 1) & 1, n + 1);
+      multiply(lds[n & 1], lds[n & 1] + TA::ELEMS);
     }
   } else {
-    ta.load(pa, g.a_ld, i0, g.rows, k0, k1, tid);
-    tb.load(pb, g.b_ld, j0, g.cols, k0, k1, tid);
-    for (int64_t k = k0; k < k1; k += kStep<T>) {
-      ta.store(lds[buf], tid);
-      tb.store(lds[buf] + TA::ELEMS, tid);
-      __syncthreads();  // also: the other buffer's readers are past it once all threads are here
-      if (k + kStep<T> < k1) {
-        ta.load(pa, g.a_ld, i0, g.rows, k + kStep<T>, k1, tid);
-        tb.load(pb, g.b_ld, j0, g.cols, k + kStep<T>, k1, tid);
+    int64_t k = k0;
+    if (whole > 0 && TA::regular(i0, g.rows) && TB::regular(j0, g.cols)) {
+      // Two steps are on the way while one is multiplied: with few blocks a CU a
+      // step is much shorter than the way from memory.
+      ta.template aim<false>(pa, g.a_ld, i0, g.rows, k0, tid);
+      tb.template aim<false>(pb, g.b_ld, j0, g.cols, k0, tid);
+      Pack<T> ra[2][TA::PER_THREAD], rb[2][TB::PER_THREAD];
+      auto load = [&](int h, int64_t n) {
+        n = min(n, whole - 1);
+        ta.load(ra[h], n * a_step);
+        tb.load(rb[h], n * b_step);
+      };
+      auto step = [&](int h, int64_t n) {
+        TA::store(lds[h], ra[h], tid);
+        TB::store(lds[h] + TA::ELEMS, rb[h], tid);
+        lds_barrier();  // also: the other buffer's readers are past it once all threads are here
+        load(h, n + 2);
+        multiply(lds[h], lds[h] + TA::ELEMS);
+      };
+      load(0, 0);
+      load(1, 1);
+      int64_t n = 0;
+      for (; n + 1 < whole; n += 2) {
+        step(0, n);
+        step(1, n + 1);
       }
-      multiply(lds[buf], lds[buf] + TA::ELEMS);
-      buf ^= 1;
+      if (n < whole) step(0, n);
+      k += whole * kStep<T>;
+      lds_barrier();
+    }
+    if (k < k1) {  // the last, partial step; or all of them
+      Pack<T> ra[TA::PER_THREAD], rb[TB::PER_THREAD];
+      auto load = [&](int64_t at) {
+        TA::load_edge(ra, pa, g.a_ld, i0, g.rows, at, k1, tid);
+        TB::load_edge(rb, pb, g.b_ld, j0, g.cols, at, k1, tid);
+      };
+      load(k);
+      for (int h = 0; k < k1; k += kStep<T>, h ^= 1) {
+        TA::store(lds[h], ra, tid);
+        TB::store(lds[h] + TA::ELEMS, rb, tid);
+        lds_barrier();
+        if (k + kStep<T> < k1) load(k + kStep<T>);
+        multiply(lds[h], lds[h] + TA::ELEMS);
+      }
     }
   }
 
