@@ -55,15 +55,16 @@ class Appearance:
         gart.gart_embedding(self.table[view], self.codes, self.e, self.scale, stream=stream)
         gart.gart_linear(self.e, p["w1"], self.h, p["b1"], None, self.act, self.scratch, stream=stream)
         gart.gart_dropout(self.h, self.d, self.p if train else 0.0, self.seed, step, stream=stream)
-        gart.gart_linear(self.d, p["w2"], self.sh, p["b2"], sh_base.view(n, self.sh.shape[1]), "none", self.scratch, stream=stream)
+        gart.gart_linear(self.d, p["w2"], self.sh, p["b2"], sh_base.view(n, self.sh.shape[1]), "none", self.scratch,
+                         stream=stream)
         return self.sh.view(sh_base.shape)
 
     def backward(self, g_sh: torch.Tensor, step: int = 0, stream=None):
         """Gradients (self.grads, self.g_table) of the training forward that ran last, with the same step, from that
         of its SH coefficients, which is also sh_base's."""
         p, g, n = self.params, self.grads, self.codes.shape[0]
-        gart.gart_linear_backward(self.d, p["w2"], g_sh.view(n, self.sh.shape[1]), self.g_d, g["w2"], g["b2"], p["b2"], "none",
-                                  self.scratch, stream=stream)
+        gart.gart_linear_backward(self.d, p["w2"], g_sh.view(n, self.sh.shape[1]), self.g_d, g["w2"], g["b2"], p["b2"],
+                                  "none", self.scratch, stream=stream)
         gart.gart_dropout(self.g_d, self.g_d, self.p, self.seed, step, stream=stream)
         gart.gart_linear_backward(self.e, p["w1"], self.g_d, self.g_e, g["w1"], g["b1"], p["b1"], self.act,
                                   self.scratch, stream=stream)

@@ -86,7 +86,10 @@ def linear_grads_tolerance(x, w, bias, dl, name, dtype):
         e = np.abs(dl) * U32 * (1.2 * (k + 4) * a + 16.0 * (1.0 + np.abs(z)) ** 2)
     er = e + (0.0 if name == "none" else 1.01 * U[dtype] * np.abs(dz) + TINY[dtype])
     gx, gw, gb = linear_grads(x, w, bias, dl, name)
-    one = lambda g, terms, size, err: 1.01 * U[dtype] * np.abs(g) + 1.2 * U32 * (terms + 4) * size + err + TINY[dtype]  # noqa: E731
+
+    def one(g, terms, size, err):
+        return 1.01 * U[dtype] * np.abs(g) + 1.2 * U32 * (terms + 4) * size + err + TINY[dtype]
+
     ax, aw, ad = np.abs(x), np.abs(w), np.abs(dz) + er
     return (one(gx, n, ad @ aw, er @ aw), one(gw, m, ad.T @ ax, er.T @ ax),
             one(gb, m, (np.abs(dz) + e).sum(axis=0), e.sum(axis=0)))

@@ -116,8 +116,8 @@ def test_interleaved_columns_are_no_overlap():
     from paper_2608_17298_amd import gart
     lib = gart.lib()
     x, w, y = _m(gart, 1 << 20, 4, 8, 20), _m(gart, 2 << 20, 6, 8), _m(gart, (1 << 20) + 36, 4, 6, 20)
-    r = lib.gart_linear(ctypes.byref(x), ctypes.byref(w), None, None, 0, 0, ctypes.byref(_m(gart, (1 << 20) + 28, 4, 6, 20)),
-                        None, 0, None)
+    inside = _m(gart, (1 << 20) + 28, 4, 6, 20)
+    r = lib.gart_linear(ctypes.byref(x), ctypes.byref(w), None, None, 0, 0, ctypes.byref(inside), None, 0, None)
     assert r == INVALID and "overlaps" in _err(lib)  # begins inside x's eight columns
     r = lib.gart_linear(ctypes.byref(x), ctypes.byref(w), None, ctypes.byref(_m(gart, 5 << 20, 4, 5)), 0, 0,
                         ctypes.byref(y), None, 0, None)
@@ -128,7 +128,8 @@ def test_empty_calls_need_nothing():
     from paper_2608_17298_amd import gart
     lib = gart.lib()
     e = lambda r, c: ctypes.byref(_m(gart, 0, r, c))  # noqa: E731
-    assert lib.gart_linear(e(0, 8), ctypes.byref(_m(gart, 1 << 20, 6, 8)), None, None, 1, 1, e(0, 6), None, 0, None) == 0
+    w = ctypes.byref(_m(gart, 1 << 20, 6, 8))
+    assert lib.gart_linear(e(0, 8), w, None, None, 1, 1, e(0, 6), None, 0, None) == 0
     assert lib.gart_embedding(ctypes.byref(_m(gart, 1 << 20, 6, 8)), None, 1, 1.0, 0, e(0, 8), None) == 0
     assert lib.gart_dropout(e(0, 3), None, 0.5, 0, 0, 2, e(0, 3), None) == 0
     assert lib.gart_embedding_backward(None, 0, e(0, 0), 1.0, 0, e(5, 0), None, 0, None) == 0
@@ -140,13 +141,14 @@ def test_matrix_struct_matches_header(tmp_path):
     fields = [f[0] for f in gart.gart_matrix._fields_]
     src.write_text('#include <stdio.h>\n#include <stddef.h>\n#include "gart.h"\nint main(void) {\n'
                    + "".join(f'  printf("%zu ", offsetof(gart_matrix, {f}));\n' for f in fields)
-                   + '  printf("%zu %d %d %d %d\\n", sizeof(gart_matrix), GART_DTYPE_BF16, GART_DTYPE_F16, GART_ACT_SILU,'
-                     ' GART_ACT_GELU);\n  return 0;\n}\n')
+                   + '  printf("%zu %d %d %d %d\\n", sizeof(gart_matrix), GART_DTYPE_BF16, GART_DTYPE_F16,'
+                     ' GART_ACT_SILU, GART_ACT_GELU);\n  return 0;\n}\n')
     exe = tmp_path / "m"
     subprocess.run(["gcc", "-std=c11", "-I", os.path.join(ROOT, "include"), str(src), "-o", str(exe)], check=True)
     got = [int(v) for v in subprocess.run([str(exe)], check=True, capture_output=True, text=True).stdout.split()]
     want = [getattr(gart.gart_matrix, f).offset for f in fields]
-    assert got == want + [ctypes.sizeof(gart.gart_matrix), gart.DTYPE_BF16, gart.DTYPE_F16, gart.ACT_SILU, gart.ACT_GELU]
+    assert got == want + [ctypes.sizeof(gart.gart_matrix), gart.DTYPE_BF16, gart.DTYPE_F16, gart.ACT_SILU,
+                          gart.ACT_GELU]
 
 
 def test_generator_known_answers():
@@ -163,7 +165,7 @@ def test_reference_gradients_by_differences(name):
     h = 1e-5
     d = (ref.act(z + h, name) - ref.act(z - h, name)) / (2 * h)
     assert np.abs(d - ref.act_grad(z, name)).max() <= 1e-9
-    x, w, b, dl = rng.standard_normal((5, 3)), rng.standard_normal((4, 3)), rng.standard_normal(4), rng.standard_normal((5, 4))
+    x, w, b, dl = (rng.standard_normal(s) for s in ((5, 3), (4, 3), 4, (5, 4)))
     gx, gw, gb = ref.linear_grads(x, w, b, dl, name)
     f = lambda x, w, b: (dl * ref.linear(x, w, b, None, name)).sum()  # noqa: E731
     for q, g in enumerate((gx, gw, gb)):

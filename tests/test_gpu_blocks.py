@@ -53,7 +53,7 @@ def _scratch(nbytes):
 def _within(got, want, tol):
     assert got.shape == want.shape
     bad = ~(np.abs(got - want) <= tol)
-    assert not bad.any(), f"{bad.sum()} of {bad.size} off, worst by {np.max(np.abs(got - want)[bad] / tol[bad])} tolerances"
+    assert not bad.any(), f"{bad.sum()} of {bad.size} off, worst {np.max(np.abs(got - want)[bad] / tol[bad])} tolerances"
 
 
 # ---- embedding -------------------------------------------------------------------
@@ -196,9 +196,9 @@ def test_linear_backward(m, k, n, dtype, act, bias, pad):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
-@pytest.mark.parametrize("m,k,n,pad", [(3592, 64, 4040, 0), (3592, 4040, 64, 8), (64, 3592, 4040, 0), (100, 4040, 72, 0),
-                                       (70, 2000, 96, 3), (2000, 300, 500, 0), (90, 1000, 1000, 0), (40, 1500, 700, 8),
-                                       (20000, 272, 40, 0)])
+@pytest.mark.parametrize("m,k,n,pad", [(3592, 64, 4040, 0), (3592, 4040, 64, 8), (64, 3592, 4040, 0),
+                                       (100, 4040, 72, 0), (70, 2000, 96, 3), (2000, 300, 500, 0), (90, 1000, 1000, 0),
+                                       (40, 1500, 700, 8), (20000, 272, 40, 0)])
 def test_linear_larger_sizes(m, k, n, pad, dtype):
     """Tiles of every size, sums cut into parts, products that go straight into LDS: forward and gradients."""
     from paper_2608_17298_amd import gart
@@ -219,6 +219,69 @@ def test_linear_larger_sizes(m, k, n, pad, dtype):
         tol = ref.linear_grads_tolerance(x64, w64, b64, r64, act, dtype)
         for got, a, c in zip((gx.value(), gw.value(), gb.value()[0]), want, tol):
             _within(got, a, c)
+
+
+def _integers(rng, rows, cols, dtype, pad, hi):
+    """A device matrix of whole numbers in -hi .. hi (exact in every type), and the same in 64 bits."""
+    import torch
+    v = rng.integers(-hi, hi + 1, (rows, cols + pad)).astype(np.float32)
+    return torch.from_numpy(v).to(_torch(dtype)).cuda()[:, :cols], v[:, :cols].astype(np.float64)
+
+
+def _rounded(a, dtype):
+    import torch
+    return torch.from_numpy(a).to(_torch(dtype)).double().numpy()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("m,k,n,pad", [(70001, 24, 40, 0), (300007, 9, 17, 3), (40000, 64, 128, 0),
+                                       (70016, 130, 20, 1), (33333, 40, 200, 8), (20011, 300, 9, 0)])
+def test_linear_many_rows_is_exact_in_whole_numbers(m, k, n, pad, dtype):
+    """Whole numbers whose sums stay below 2^24: every product and sum is exact in float, so each result is the exact
+    one rounded once, over many turns of every block.  relu with half-integer biases decides every slope exactly."""
+    from paper_2608_17298_amd import gart
+    rng = np.random.default_rng(m)
+    x, x64 = _integers(rng, m, k, dtype, pad, 1)
+    w, w64 = _integers(rng, n, k, dtype, pad, 2)
+    dl, d64 = _integers(rng, m, n, dtype, pad, 2)
+    b, b64 = _integers(rng, 1, n, dtype, 0, 3)
+    b, b64 = (b[0] + 0.5).contiguous(), b64[0] + 0.5
+    t = _torch(dtype)
+    y = _Out(m, n, dtype, pad)
+    gart.gart_linear(x, w, y.t, b, None, "relu", _scratch(gart.gart_linear_scratch_bytes(m, k, n, t)))
+    z = x64 @ w64.T + b64
+    assert np.array_equal(y.value(), _rounded(np.maximum(z, 0.0), dtype))
+    for act in ("relu", "none"):
+        dz = np.where(z > 0, d64, 0.0) if act == "relu" else d64
+        gx, gw, gb = _Out(m, k, dtype, pad), _Out(n, k, dtype, pad), _Out(1, n, dtype, 0)
+        s = _scratch(gart.gart_linear_backward_scratch_bytes(m, k, n, t, act))
+        gart.gart_linear_backward(x, w, dl, gx.t, gw.t, gb.t.reshape(-1), b, act, s)
+        for got, want in ((gx.value(), dz @ w64), (gw.value(), dz.T @ x64), (gb.value()[0], dz.sum(axis=0))):
+            assert np.abs(want).max() < 60000  # float16 holds it
+            assert np.array_equal(got, _rounded(want, dtype))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n,dim,vocab,kind", [(300000, 7, 100, "skew"), (300000, 64, 5000, "skew"),
+                                              (262145, 5, 70000, "uniform"), (100000, 33, 3, "uniform"),
+                                              (40000, 2100, 50, "absent"), (8193, 16, 9, "one")])
+def test_embedding_backward_is_exact_in_whole_numbers(n, dim, vocab, kind, dtype):
+    """As above: runs inside units, across units and across blocks, in sorts of one and several passes."""
+    import torch
+    from paper_2608_17298_amd import gart
+    rng = np.random.default_rng(n + vocab)
+    dl, d64 = _integers(rng, n, dim, dtype, 0, 1)
+    ids = _ids(rng, n, vocab, kind)
+    g = _Out(vocab, dim, dtype, 0)
+    gart.gart_embedding_backward(torch.from_numpy(ids).cuda(), dl, g.t, 2.0,
+                                 _scratch(gart.gart_embedding_scratch_bytes(n, vocab, dim)))
+    order = np.argsort(ids, kind="stable")
+    order = order[(ids[order] >= 0) & (ids[order] < vocab)]
+    which, first = np.unique(ids[order], return_index=True)
+    want = np.zeros((vocab, dim))
+    want[which] = 2.0 * np.add.reduceat(d64[order], first, axis=0)
+    assert np.abs(want).max() < 60000
+    assert np.array_equal(g.value(), _rounded(want, dtype))
 
 
 @pytest.mark.parametrize("want_x,want_w,want_b", [(1, 0, 0), (0, 1, 0), (0, 0, 1), (1, 0, 1)])
@@ -408,6 +471,21 @@ def test_dropout_rate_and_counters():
     assert np.array_equal(y[0, -100:].cpu().numpy() != 0, ref.keep(100, 0.1, 3, 0, n - 100))
 
 
+def test_dropout_beyond_2_to_31_elements():
+    """More elements than one round of the grid: the last ones come from their own counters."""
+    import torch
+    from paper_2608_17298_amd import gart
+    rows, cols = 2, (1 << 30) + 24
+    if torch.cuda.mem_get_info()[0] < 12 << 30:
+        pytest.skip("needs 9 GB of device memory")
+    x = torch.ones((rows, cols), dtype=torch.bfloat16, device="cuda")
+    y = torch.empty_like(x)
+    gart.gart_dropout(x, y, 0.5, 77, 5)
+    for first in (0, (1 << 31) - 64, rows * cols - 128):
+        got = y.view(-1)[first:first + 128].cpu().float().numpy() != 0
+        assert np.array_equal(got, ref.keep(len(got), 0.5, 77, 5, first))  # the middle window ends with the matrix
+
+
 # ---- all of them ---------------------------------------------------------------------
 def test_offsets_beyond_32_bits():
     """Rows 2^22 elements apart, 1040 of them: element offsets pass 2^32.  The last rows are compared."""
@@ -418,8 +496,8 @@ def test_offsets_beyond_32_bits():
     free, _ = torch.cuda.mem_get_info()
     if free < 20 << 30:
         pytest.skip("needs 18 GB of device memory")
-    far = [torch.empty((rows - 1) * step + cols, dtype=torch.bfloat16, device="cuda").as_strided((rows, cols), (step, 1))
-           for _ in range(2)]
+    buffers = [torch.empty((rows - 1) * step + cols, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    far = [b.as_strided((rows, cols), (step, 1)) for b in buffers]
     x, _ = _mat(rng, rows, cols, "bf16")
     w, _ = _mat(rng, cols, cols, "bf16")
     far[0].copy_(x)
