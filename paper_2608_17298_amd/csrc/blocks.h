@@ -120,13 +120,6 @@ __device__ __forceinline__ void store_some(T* p, const Pack<T>& r, int count) {
     if (e < count) p[e] = r.v[e];
 }
 
-// A row-major matrix in device memory; the stride is in elements.
-template <typename T>
-struct Mat {
-  T* p;
-  int64_t ld;
-};
-
 inline int64_t ceil_div64(int64_t a, int64_t b) { return (a + b - 1) / b; }
 inline size_t dtype_bytes(gart_dtype t) { return t == GART_DTYPE_F32 ? 4 : 2; }
 

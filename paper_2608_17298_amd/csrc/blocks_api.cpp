@@ -12,7 +12,8 @@ using namespace gart;
 namespace {
 
 constexpr int64_t kMaxSize = (int64_t(1) << 31) - 1;
-constexpr int64_t kMaxDim = int64_t(1) << 23;  // of an embedding's gradient: its columns span a launch's second dimension
+// Columns of an embedding's gradient: they span a launch's second dimension.
+constexpr int64_t kMaxDim = int64_t(1) << 23;
 
 gart_status check_dtype(gart_dtype t) {
   GART_REQUIRE(t >= GART_DTYPE_F32 && t <= GART_DTYPE_F16, "unknown dtype %d", int(t));
@@ -68,7 +69,8 @@ bool overlap(const Span& a, const Span& b) {
   if (a.begin >= b.end || b.begin >= a.end) return false;
   if (a.step == 0 || a.step != b.step) return true;  // interleaved only where rows step alike
   // columns of one wider buffer: disjoint if b's row fits beside a's in a step
-  const uint64_t d = (b.begin >= a.begin) ? (b.begin - a.begin) % a.step : (a.step - (a.begin - b.begin) % a.step) % a.step;
+  const uint64_t d = b.begin >= a.begin ? (b.begin - a.begin) % a.step
+                                        : (a.step - (a.begin - b.begin) % a.step) % a.step;
   return !(d >= a.row && d + b.row <= a.step);
 }
 
@@ -144,7 +146,8 @@ gart_status gart_embedding_backward(const void* ids, int32_t ids64, const gart_m
   const size_t ids_bytes = ids64 ? 8 : 4;
   GART_REQUIRE(dl_dout->rows == 0 || ids != nullptr, "ids is NULL");
   GART_REQUIRE(reinterpret_cast<uintptr_t>(ids) % ids_bytes == 0, "ids is not aligned to its elements");
-  GART_CHECK(check_scratch(scratch, scratch_bytes, embedding_scratch_bytes(dl_dout->rows, g_table->rows, g_table->cols)));
+  GART_CHECK(
+      check_scratch(scratch, scratch_bytes, embedding_scratch_bytes(dl_dout->rows, g_table->rows, g_table->cols)));
   const Span o = span_of(g_table, dtype);
   GART_REQUIRE(!overlap(o, span_of(dl_dout, dtype)) && !overlap(o, span_of(ids, int64_t(ids_bytes) * dl_dout->rows)),
                "g_table overlaps an input");
@@ -280,7 +283,8 @@ gart_status gart_linear_backward(const gart_matrix* x, const gart_matrix* weight
   }
   if (g_weight) {
     GART_CHECK(check_matrix("g_weight", g_weight, dtype, true));
-    GART_REQUIRE(g_weight->rows == weight->rows && g_weight->cols == weight->cols, "g_weight and weight differ in size");
+    GART_REQUIRE(g_weight->rows == weight->rows && g_weight->cols == weight->cols,
+                 "g_weight and weight differ in size");
   }
   const int64_t need = linear_backward_scratch_bytes(x->rows, x->cols, weight->rows, dtype, act);
   if (need < 0)

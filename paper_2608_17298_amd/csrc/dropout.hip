@@ -8,7 +8,8 @@
 //
 // One thread owns one call of the generator, that is 8 consecutive elements:
 // 16 bits an element halve the generator's work against a word each (two
-// 32x32->64 products and a few adds and xors per round, 10 rounds).
+// 32x32->64 products and a few adds and xors per round, 10 rounds).  Bound by
+// bytes: 1M x 128 bf16 with a residual take 128 us, 6.0 TB/s.
 #include "blocks.h"
 
 namespace gart {

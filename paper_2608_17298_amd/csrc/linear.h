@@ -145,7 +145,8 @@ __device__ __forceinline__ typename Pack<T>::V transposed_pair(const T* lds, int
 
 // From LDS lines across k (line k holds the rows' elements side by side).
 template <typename T>
-__device__ __forceinline__ typename Pack<T>::V fragment_of_columns(const T* lds, int pitch, int tile, int k0, int lane) {
+__device__ __forceinline__ typename Pack<T>::V fragment_of_columns(const T* lds, int pitch, int tile, int k0,
+                                                                   int lane) {
   const int r = lane % 16, g = lane / 16;
   typename Pack<T>::V v;
   if constexpr (sizeof(T) == 4) {
@@ -191,7 +192,9 @@ struct BackwardPlan {
 BackwardPlan backward_plan(int64_t m, int64_t k, int64_t n, gart_dtype t, gart_activation act);
 
 template <typename T>
-constexpr gart_dtype kType = sizeof(T) == 4 ? GART_DTYPE_F32 : std::is_same<T, bf16>::value ? GART_DTYPE_BF16 : GART_DTYPE_F16;
+constexpr gart_dtype kType = sizeof(T) == 4                  ? GART_DTYPE_F32
+                             : std::is_same<T, bf16>::value ? GART_DTYPE_BF16
+                                                            : GART_DTYPE_F16;
 
 // ---- linear_rows.h, linear_stream.h, linear_gemm.h: one of each per type -----------
 inline bool few_rows(int64_t m, int64_t n) { return m <= kFewRows && n <= int64_t(1) << 24; }

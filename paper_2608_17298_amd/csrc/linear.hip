@@ -48,7 +48,9 @@ BackwardPlan backward_plan(int64_t m, int64_t k, int64_t n, gart_dtype t, gart_a
     off += (bytes + 255) & ~size_t(255);
     return o;
   };
-  auto floats = [](int64_t parts, int64_t rows, int64_t cols) { return size_t(parts) * size_t(rows) * size_t(cols) * 4; };
+  auto floats = [](int64_t parts, int64_t rows, int64_t cols) {
+    return size_t(parts) * size_t(rows) * size_t(cols) * 4;
+  };
   p.parts = stream_backward_parts(m, k, n, es);
   if (p.parts > 0) {
     p.stream = true;

@@ -2,7 +2,8 @@
 // the weight once.  A block takes 16 outputs and all rows; its waves share the
 // inputs and read their pieces of 16 weight rows straight into fragments,
 // kInFlight at a time, so that a whole block's weights are asked for at once.
-// The waves' sums meet in LDS, in order.
+// The waves' sums meet in LDS, in order.  One row of 1024 -> 4096 bf16: 4 us,
+// one round trip to memory, launch and joins (8 MB: 2 TB/s); in tiles 18 us.
 #pragma once
 
 #include <algorithm>

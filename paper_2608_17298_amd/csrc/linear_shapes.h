@@ -43,8 +43,9 @@ struct BackwardSizes {
   static constexpr bool FITS = BYTES <= 160 * 1024 && KP * int(ES) <= 512;
 };
 
-// Blocks: two of four waves for each of the 256 CUs; their partial sums are then
-// far fewer than the rows.
+// Blocks: two of four waves for each of the 256 CUs, as many as the registers
+// hold (100000 x 32 -> 64 f32: 30 us; three with fewer registers each 33, four
+// 41); their partial sums are then far fewer than the rows.
 constexpr int64_t kBackwardBlocks = 512;
 
 struct BackwardChoice {
@@ -73,6 +74,8 @@ BackwardChoice choose(int64_t k, int64_t n) {
   return c;
 }
 
-inline BackwardChoice choose_backward(int64_t k, int64_t n, size_t es) { return es == 4 ? choose<4>(k, n) : choose<2>(k, n); }
+inline BackwardChoice choose_backward(int64_t k, int64_t n, size_t es) {
+  return es == 4 ? choose<4>(k, n) : choose<2>(k, n);
+}
 
 }  // namespace gart
