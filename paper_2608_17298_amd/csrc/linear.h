@@ -169,10 +169,11 @@ __device__ __forceinline__ void lds_barrier() {
 
 // ---- how the work is cut (linear.hip) --------------------------------------------
 // Products that do not stream: tiles of 256 (one block of 8 waves a CU, straight
-// into LDS) where they fill the card, else of 128, else of 64; where even these
-// are few, the sums are cut into parts, which are joined afterwards.
+// into LDS) where they fill the card, else of 128, else of 64, and 128 x 32 or 32
+// x 128 for narrow ones; where tiles are few, the sums are cut into parts, which
+// are joined afterwards.
 struct Cut {
-  int tile;
+  int rows, cols;  // of a tile
   int64_t part, parts;
 };
 // most: parts at most; wide: alignment and sizes allow tiles of 256

@@ -8,25 +8,28 @@ namespace gart {
 
 Cut cut_product(int64_t rows, int64_t cols, int64_t depth, int64_t most, bool wide) {
   constexpr int64_t kCus = 256;
-  auto tiles = [&](int t) { return ceil_div64(rows, t) * ceil_div64(cols, t); };
-  auto parts = [&](int t, int64_t least) {  // two blocks a CU, `least` terms a part
-    return std::max<int64_t>(1, std::min({most, 2 * kCus / tiles(t), depth / least}));
+  auto tiles = [&](int i, int j) { return ceil_div64(rows, i) * ceil_div64(cols, j); };
+  auto parts = [&](int i, int j, int64_t least) {  // two blocks a CU, `least` terms a part
+    return std::max<int64_t>(1, std::min({most, 2 * kCus / tiles(i, j), depth / least}));
   };
-  auto with = [&](int t, int64_t n) {
+  auto with = [&](int i, int j, int64_t n) {
     const int64_t part = std::max<int64_t>(64, ceil_div64(ceil_div64(depth, n), 64) * 64);
-    return Cut{t, part, std::max<int64_t>(1, ceil_div64(depth, part))};
+    return Cut{i, j, part, std::max<int64_t>(1, ceil_div64(depth, part))};
   };
+  if (wide && tiles(256, 256) >= kCus * 7 / 8) return with(256, 256, 1);
+  // Narrow products are bound by their one large operand.
+  if (cols <= 32 && rows > 64) return with(128, 32, parts(128, 32, 256));
+  if (rows <= 32 && cols > 64) return with(32, 128, parts(32, 128, 256));
   // Short sums are bound by their outputs: many small blocks overlap more of
   // them (20000 x 256 -> 1024 f16: 49 us with 128, 44 with 64; 20000 x 200 -> 500
   // f32: 99 and 62; 8000 x 512 -> 1000 f16: 22 and 25).
-  if (depth <= 256) return with(64, 1);
-  if (wide && tiles(256) >= kCus * 7 / 8) return with(256, 1);
-  if (tiles(128) >= kCus * 3 / 2) return with(128, 1);
+  if (depth <= 256) return with(64, 64, 1);
+  if (tiles(128, 128) >= kCus * 3 / 2) return with(128, 128, 1);
   // Fewer of 128 leave CUs with one block and nothing to overlap (2000 x 2048 ->
   // 2000 f16: 45 us, in two parts 43, with 64 38); long sums are worth the parts.
-  if (tiles(64) >= kCus * 2 && depth <= 4096) return with(64, 1);
-  const int64_t p = parts(128, 512);
-  return tiles(128) * p >= kCus * 3 / 2 ? with(128, p) : with(64, parts(64, 256));
+  if (tiles(64, 64) >= kCus * 2 && depth <= 4096) return with(64, 64, 1);
+  const int64_t p = parts(128, 128, 512);
+  return tiles(128, 128) * p >= kCus * 3 / 2 ? with(128, 128, p) : with(64, 64, parts(64, 64, 256));
 }
 
 bool stream_forward_fits(int64_t k, int64_t n, size_t es) {
@@ -81,10 +84,7 @@ namespace {
 
 constexpr int64_t kMaxTiles = int64_t(1) << 23;  // blocks of a launch
 
-bool launchable(int64_t rows, int64_t cols) {
-  const int64_t i = ceil_div64(rows, 64), j = ceil_div64(cols, 64);
-  return i * j <= kMaxTiles || ceil_div64(rows, 128) * ceil_div64(cols, 128) <= kMaxTiles;
-}
+bool launchable(int64_t rows, int64_t cols) { return ceil_div64(rows, 64) * ceil_div64(cols, 64) <= kMaxTiles; }
 
 }  // namespace
 

@@ -49,7 +49,9 @@ struct Tile {
   static __device__ __forceinline__ int swizzle(int line) {
     if (KC) return PERM && SHORT ? (line & 3) | ((line >> 1) & 4) : line & 7;
     if (!SHORT) return 0;
-    return 2 * (ROWS >= 128 ? (line & 3) | ((line >> 1) & 4) : ((line >> 1) & 1) | ((line >> 2) & 2));
+    return 2 * (ROWS >= 128  ? (line & 3) | ((line >> 1) & 4)
+                : ROWS >= 64 ? ((line >> 1) & 1) | ((line >> 2) & 2)
+                             : (line >> 3) & 1);
   }
 
   // ---- through registers: any size and alignment ----
@@ -445,13 +447,17 @@ __global__ __launch_bounds__(256) void join_rows_kernel(const GemmArgs g, const 
 
 template <typename T, bool AKC, bool BKC, Epilogue EPI>
 hipError_t run_tiles(GemmArgs g, const Cut& c, hipStream_t s) {
-  g.tiles_i = ceil_div64(g.rows, c.tile);
-  g.tiles_j = ceil_div64(g.cols, c.tile);
+  g.tiles_i = ceil_div64(g.rows, c.rows);
+  g.tiles_j = ceil_div64(g.cols, c.cols);
   g.part = c.part;
   const dim3 grid(uint32_t(g.tiles_i * g.tiles_j), 1, uint32_t(EPI == EPI_PARTIAL ? c.parts : 1));
-  if (c.tile == 64) {
+  if (c.rows == 64) {
     gemm_kernel<T, AKC, BKC, 2, 2, 2, 2, false, EPI><<<grid, 256, 0, s>>>(g);
-  } else if (c.tile == 128) {
+  } else if (c.cols == 32) {
+    gemm_kernel<T, AKC, BKC, 2, 2, 4, 1, false, EPI><<<grid, 256, 0, s>>>(g);
+  } else if (c.rows == 32) {
+    gemm_kernel<T, AKC, BKC, 2, 2, 1, 4, false, EPI><<<grid, 256, 0, s>>>(g);
+  } else if (c.rows == 128) {
     gemm_kernel<T, AKC, BKC, 4, 4, 2, 2, false, EPI><<<grid, 256, 0, s>>>(g);
   } else {
     if constexpr (sizeof(T) == 2 && EPI != EPI_PARTIAL)
@@ -477,7 +483,7 @@ hipError_t product(GemmArgs g, int64_t most, float* partial, hipStream_t s, int6
   const bool wide = g.depth % 64 == 0 && wide_operand<T>(g.a, g.a_ld, g.rows, AKC) &&
                     wide_operand<T>(g.b, g.b_ld, g.cols, BKC);
   const Cut c = cut_product(g.rows, g.cols, g.depth, most, wide);
-  if (sum_parts) *sum_parts = ceil_div64(g.rows, c.parts == 1 ? c.tile : kJoinRows);
+  if (sum_parts) *sum_parts = ceil_div64(g.rows, c.parts == 1 ? c.rows : kJoinRows);
   if (c.parts == 1) return run_tiles<T, AKC, BKC, EPI>(g, c, s);
   GemmArgs p = g;
   p.out = partial;
