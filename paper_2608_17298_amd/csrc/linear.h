@@ -199,11 +199,11 @@ constexpr gart_dtype kType = sizeof(T) == 4                  ? GART_DTYPE_F32
 
 // ---- linear_rows.h, linear_stream.h, linear_gemm.h: one of each per type -----------
 inline bool few_rows(int64_t m, int64_t n) { return m <= kFewRows && n <= int64_t(1) << 24; }
-// y, or dz and g_bias's sum, of up to kFewRows rows
+// y, or dz and g_bias (may be NULL), of up to kFewRows rows
 template <typename T>
 hipError_t rows_forward(const LinearArgs& a, hipStream_t s);
 template <typename T>
-hipError_t rows_dz(const LinearArgs& a, void* dz, int64_t dz_ld, float* sums, hipStream_t s);
+hipError_t rows_dz(const LinearArgs& a, void* dz, int64_t dz_ld, hipStream_t s);
 
 // Layers whose weight fits LDS: the rows stream past it once.
 bool stream_forward_fits(int64_t k, int64_t n, size_t es);

@@ -348,10 +348,11 @@ __global__ __launch_bounds__(64 * WI * WJ) void gemm_kernel(const GemmArgs g) {
   }
 }
 
-// Column sums of m rows, one part of kSumRows rows a block: sums[part, n].
+// Column sums of m rows, one part of kSumRows rows a block: sums[part, n], or
+// the result itself if there is one part.
 template <typename T>
 __global__ __launch_bounds__(256) void column_sums_kernel(const T* __restrict__ p, int64_t ld, int64_t m, int64_t n,
-                                                          float* __restrict__ sums) {
+                                                          float* __restrict__ sums, T* __restrict__ out) {
   __shared__ float s[4][64];
   const int lane = threadIdx.x % 64, w = threadIdx.x / 64;
   const int64_t j = int64_t(blockIdx.y) * 64 + lane, r0 = int64_t(blockIdx.x) * kSumRows;
@@ -360,7 +361,12 @@ __global__ __launch_bounds__(256) void column_sums_kernel(const T* __restrict__ 
     for (int64_t r = r0 + w; r < min(m, r0 + kSumRows); r += 4) t += float(p[r * ld + j]);
   s[w][lane] = t;
   __syncthreads();
-  if (w == 0 && j < n) sums[int64_t(blockIdx.x) * n + j] = (s[0][lane] + s[1][lane]) + (s[2][lane] + s[3][lane]);
+  if (w > 0 || j >= n) return;
+  t = (s[0][lane] + s[1][lane]) + (s[2][lane] + s[3][lane]);
+  if (gridDim.x == 1)
+    out[j] = T(t);
+  else
+    sums[int64_t(blockIdx.x) * n + j] = t;
 }
 
 // Sums over parts of partial[part, e], e < length: out (rows x cols) takes the
@@ -537,13 +543,14 @@ hipError_t gemm_backward(const LinearArgs& a, hipStream_t s) {
   }
   const void* dz = a.dl;
   int64_t dz_ld = a.dl_ld, sum_parts = 0;
+  bool bias_done = false;
   if (a.act != GART_ACT_NONE) {
     // dz is rounded to the type: it is the products' operand
     dz = base + p.dz;
     dz_ld = p.dz_ld;
     if (few_rows(a.m, a.n)) {
-      sum_parts = a.m > 0 ? 1 : 0;
-      e = rows_dz<T>(a, base + p.dz, dz_ld, a.g_bias ? sums : nullptr, s);
+      e = rows_dz<T>(a, base + p.dz, dz_ld, s);
+      bias_done = a.m > 0;
     } else {
       GemmArgs g = layer_product<T>(a);
       g.extra = a.dl;
@@ -556,11 +563,12 @@ hipError_t gemm_backward(const LinearArgs& a, hipStream_t s) {
   } else if (a.g_bias && a.m > 0 && a.n > 0) {
     sum_parts = ceil_div64(a.m, kSumRows);
     column_sums_kernel<T><<<dim3(uint32_t(sum_parts), uint32_t(ceil_div64(a.n, 64))), 256, 0, s>>>(
-        static_cast<const T*>(a.dl), a.dl_ld, a.m, a.n, sums);
+        static_cast<const T*>(a.dl), a.dl_ld, a.m, a.n, sums, static_cast<T*>(a.g_bias));
     e = hipGetLastError();
+    bias_done = sum_parts == 1;
   }
   if (e != hipSuccess) return e;
-  if (a.g_bias && (e = join_parts<T>(sums, sum_parts, 1, a.n, a.g_bias, a.n, s)) != hipSuccess) return e;
+  if (a.g_bias && !bias_done && (e = join_parts<T>(sums, sum_parts, 1, a.n, a.g_bias, a.n, s)) != hipSuccess) return e;
   GemmArgs g{};
   g.a = dz;
   g.a_ld = dz_ld;

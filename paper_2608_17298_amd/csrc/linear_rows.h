@@ -16,10 +16,9 @@ namespace {
 constexpr int kInFlight = 4;
 constexpr int kRowsWaves = 16;
 
-// DZ: dz = dl act'(z) in place of y, and its sum over the rows.
+// DZ: dz = dl act'(z) in place of y, and g_bias, its sum over the rows.
 template <typename T, int MT, bool DZ>
-__global__ __launch_bounds__(64 * kRowsWaves) void rows_kernel(const LinearArgs a, T* out, int64_t out_ld,
-                                                               float* __restrict__ sums) {
+__global__ __launch_bounds__(64 * kRowsWaves) void rows_kernel(const LinearArgs a, T* out, int64_t out_ld) {
   constexpr int V = Pack<T>::N, D = kDepth<T>, SIZE = 16 * MT * 16;
   extern __shared__ __attribute__((aligned(16))) float s_acc[];  // [waves][SIZE]
   const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64, waves = blockDim.x / 64;
@@ -70,19 +69,19 @@ __global__ __launch_bounds__(64 * kRowsWaves) void rows_kernel(const LinearArgs 
     out[m * out_ld + j] = T(c);
     if (DZ) s_acc[o] = c;  // this thread alone has read it (every wave's share of o)
   }
-  if (DZ && sums) {
+  if (DZ && a.g_bias) {
     __syncthreads();
     const int64_t j = int64_t(blockIdx.x) * 16 + tid;
     if (tid < 16 && j < a.n) {
       float t = 0.0f;
       for (int m = 0; m < a.m; ++m) t += s_acc[m * 16 + tid];
-      sums[j] = t;
+      static_cast<T*>(a.g_bias)[j] = T(t);
     }
   }
 }
 
 template <typename T, bool DZ>
-hipError_t rows_launch(const LinearArgs& a, void* out, int64_t out_ld, float* sums, hipStream_t s) {
+hipError_t rows_launch(const LinearArgs& a, void* out, int64_t out_ld, hipStream_t s) {
   if (a.m <= 0 || a.n <= 0) return hipSuccess;
   const int64_t steps = ceil_div64(std::max<int64_t>(a.k, 1), kDepth<T>);
   const int waves = int(std::min<int64_t>(kRowsWaves, ceil_div64(steps, kInFlight)));
@@ -91,11 +90,11 @@ hipError_t rows_launch(const LinearArgs& a, void* out, int64_t out_ld, float* su
   const size_t bytes = size_t(waves) * mt * 256 * 4;
   T* p = static_cast<T*>(out);
   if (mt == 1)
-    rows_kernel<T, 1, DZ><<<blocks, 64 * waves, bytes, s>>>(a, p, out_ld, sums);
+    rows_kernel<T, 1, DZ><<<blocks, 64 * waves, bytes, s>>>(a, p, out_ld);
   else if (mt == 2)
-    rows_kernel<T, 2, DZ><<<blocks, 64 * waves, bytes, s>>>(a, p, out_ld, sums);
+    rows_kernel<T, 2, DZ><<<blocks, 64 * waves, bytes, s>>>(a, p, out_ld);
   else
-    rows_kernel<T, 4, DZ><<<blocks, 64 * waves, bytes, s>>>(a, p, out_ld, sums);
+    rows_kernel<T, 4, DZ><<<blocks, 64 * waves, bytes, s>>>(a, p, out_ld);
   return hipGetLastError();
 }
 
@@ -103,12 +102,12 @@ hipError_t rows_launch(const LinearArgs& a, void* out, int64_t out_ld, float* su
 
 template <typename T>
 hipError_t rows_forward(const LinearArgs& a, hipStream_t s) {
-  return rows_launch<T, false>(a, a.y, a.y_ld, nullptr, s);
+  return rows_launch<T, false>(a, a.y, a.y_ld, s);
 }
 
 template <typename T>
-hipError_t rows_dz(const LinearArgs& a, void* dz, int64_t dz_ld, float* sums, hipStream_t s) {
-  return rows_launch<T, true>(a, dz, dz_ld, sums, s);
+hipError_t rows_dz(const LinearArgs& a, void* dz, int64_t dz_ld, hipStream_t s) {
+  return rows_launch<T, true>(a, dz, dz_ld, s);
 }
 
 }  // namespace gart
