@@ -11,13 +11,13 @@
 // units, joined in the block's LDS and, where it crosses blocks, afterwards
 // from their partial sums, always in order.
 //
-// 1M rows of 64 bf16 into 4096 take 98 us: the sort's two passes 48, the sums 34
+// 1M rows of 64 bf16 into 4096 take 97 us: the sort's two passes 48, the sums 34
 // to 38 (rows of 128 bytes at random, 3.7 TB/s), the rest clearing and joins.
 #include <algorithm>
 
 #include "blocks.h"
 #include "ops.h"
-#include "sort_small.h"
+#include "sort_device.h"
 
 namespace gart {
 namespace {
@@ -102,10 +102,18 @@ __device__ __forceinline__ void zero_rows(T* __restrict__ out, int64_t ld, int64
   }
 }
 
-template <typename T>
-__global__ __launch_bounds__(kThreads) void zero_rows_kernel(const EmbeddingArgs a) {
-  zero_rows(static_cast<T*>(a.out), a.out_ld, a.vocab, a.dim, int64_t(blockIdx.x) * kThreads + threadIdx.x,
-            int64_t(gridDim.x) * kThreads);
+// The first `counting` blocks count the ids' first digits, the others clear the
+// table's gradient (with no ids, all of them do).
+template <typename T, typename Id>
+__global__ __launch_bounds__(kThreads) void count_and_zero_kernel(const EmbeddingArgs a, uint32_t* __restrict__ counts,
+                                                                  int counting, bool by_block) {
+  static_assert(kThreads == kSortThreads, "a block counts as one of the sort's");
+  if (int(blockIdx.x) < counting) {
+    radix_count<kIdItems>(IdSource<Id>{static_cast<const Id*>(a.ids), a.vocab}, a.n, 0, counts, counting, by_block);
+    return;
+  }
+  zero_rows(static_cast<T*>(a.out), a.out_ld, a.vocab, a.dim,
+            int64_t(blockIdx.x - counting) * kThreads + threadIdx.x, int64_t(gridDim.x - counting) * kThreads);
 }
 
 // Up to kSmallPairs ids: the first block sorts them while the others clear the
@@ -410,8 +418,13 @@ hipError_t gradient(const EmbeddingArgs& a, hipStream_t s) {
       sort_and_zero_kernel<T, int32_t><<<blocks, kSmallThreads, 0, s>>>(a, keys, pos, bits);
     e = hipGetLastError();
   } else {
-    const uint32_t blocks = uint32_t(std::min<int64_t>(ceil_div64(table_packs, kThreads), 8192));
-    zero_rows_kernel<T><<<blocks, kThreads, 0, s>>>(a);
+    const int counting = int(id_sort_blocks(a.n));
+    const uint32_t blocks = uint32_t(counting + std::min<int64_t>(ceil_div64(table_packs, kThreads), 8192));
+    uint32_t* counts = a.n > 0 ? words(L.radix) : nullptr;
+    if (a.ids64)
+      count_and_zero_kernel<T, int64_t><<<blocks, kThreads, 0, s>>>(a, counts, counting, id_counts_by_block(a.n));
+    else
+      count_and_zero_kernel<T, int32_t><<<blocks, kThreads, 0, s>>>(a, counts, counting, id_counts_by_block(a.n));
     e = hipGetLastError();
     if (e != hipSuccess || a.n <= 0) return e;
     e = radix_sort_ids(a.ids, a.ids64, a.vocab, keys, pos, words(L.keys_alt), words(L.pos_alt), a.n, bits,

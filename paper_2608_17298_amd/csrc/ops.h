@@ -30,8 +30,9 @@ hipError_t radix_sort_u32(uint32_t* keys, uint32_t* vals, uint32_t* keys_alt, ui
                           void* tmp, hipStream_t s);
 
 // Stable sort of ids (int32, or int64 if ids64) with their positions 0 .. m-1
-// on bits [0, bits), more than one block's worth of them; ids outside
-// [0, limit) become limit.  The pairs end in (keys, pos).  tmp must hold
+// on bits [0, bits), whose first pass has been counted into tmp (radix_count of
+// id_sort_blocks blocks, by block if id_counts_by_block); ids outside [0, limit)
+// become limit.  The pairs end in (keys, pos).  tmp must hold
 // radix_ids_tmp_bytes(m) bytes.
 size_t radix_ids_tmp_bytes(int64_t m);
 hipError_t radix_sort_ids(const void* ids, bool ids64, int64_t limit, uint32_t* keys, uint32_t* pos,

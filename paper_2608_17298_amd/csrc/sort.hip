@@ -10,7 +10,7 @@
 #include <algorithm>
 
 #include "ops.h"
-#include "sort_small.h"
+#include "sort_device.h"
 
 namespace gart {
 namespace {
@@ -19,16 +19,11 @@ constexpr int kScanThreads = 256;
 constexpr int kScanItems = 8;
 constexpr int kScanTile = kScanThreads * kScanItems;
 
-constexpr int kSortThreads = 256;
 #ifndef GART_SORT_ITEMS
 #define GART_SORT_ITEMS 16
 #endif
 constexpr int kSortItems = GART_SORT_ITEMS;  // keys per thread and radix pass
 constexpr int kSortTile = kSortThreads * kSortItems;
-// Of a sort of ids: up to a few million, more blocks beat longer ones (gradient
-// of 1M ids: 16 items 147 us, 8 143).
-constexpr int kIdItems = 8;
-constexpr int64_t kFewBlocks = 128;  // blocks up to which the scatter adds up counts itself
 constexpr int kWaves = kSortThreads / 64;
 
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
@@ -149,26 +144,7 @@ enum Positions { SCAN_ALL, SCAN_DIGITS, SUM_BLOCKS };
 template <int ITEMS, Positions HOW, typename Source>
 __global__ __launch_bounds__(kSortThreads) void radix_hist_kernel(const Source source, int64_t m, int shift,
                                                                   uint32_t* __restrict__ counts, int nblocks) {
-  __shared__ uint32_t h[256];
-  h[threadIdx.x] = 0;
-  __syncthreads();
-  const int64_t base = int64_t(blockIdx.x) * (kSortThreads * ITEMS);
-  uint32_t kv[ITEMS];
-#pragma unroll
-  for (int r = 0; r < ITEMS; ++r) {
-    const int64_t j = base + int64_t(r) * kSortThreads + threadIdx.x;
-    kv[r] = j < m ? source.key(j) : 0u;
-  }
-#pragma unroll
-  for (int r = 0; r < ITEMS; ++r) {
-    const int64_t j = base + int64_t(r) * kSortThreads + threadIdx.x;
-    if (j < m) atomicAdd(&h[(kv[r] >> shift) & 255u], 1u);
-  }
-  __syncthreads();
-  if (HOW == SUM_BLOCKS)
-    counts[int64_t(blockIdx.x) * 256 + threadIdx.x] = h[threadIdx.x];
-  else
-    counts[int64_t(threadIdx.x) * nblocks + blockIdx.x] = h[threadIdx.x];
+  radix_count<ITEMS>(source, m, shift, counts, nblocks, HOW == SUM_BLOCKS);
 }
 
 template <int ITEMS, Positions HOW, typename Source>
@@ -396,11 +372,11 @@ __global__ __launch_bounds__(kDigitThreads) void digit_scan_kernel(uint32_t* __r
 
 template <int ITEMS, Positions HOW, typename Source>
 hipError_t radix_pass(const Source& source, uint32_t* kout, uint32_t* vout, int64_t m, int shift, void* tmp,
-                      hipStream_t s) {
+                      hipStream_t s, bool counted = false) {
   const int64_t nb = ceil_div(m, kSortThreads * ITEMS);
   uint32_t* counts = static_cast<uint32_t*>(tmp);
   char* scan_tmp = static_cast<char*>(tmp) + ((size_t(nb) * 256 * sizeof(uint32_t) + 255) & ~size_t(255));
-  radix_hist_kernel<ITEMS, HOW><<<nb, kSortThreads, 0, s>>>(source, m, shift, counts, int(nb));
+  if (!counted) radix_hist_kernel<ITEMS, HOW><<<nb, kSortThreads, 0, s>>>(source, m, shift, counts, int(nb));
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   if (HOW == SCAN_ALL) e = scan_exclusive_u32(counts, counts, nb * 256, nullptr, scan_tmp, s);
@@ -425,10 +401,10 @@ hipError_t sort_ids(const void* ids, bool ids64, int64_t limit, uint32_t* keys, 
       e = radix_pass<kIdItems, HOW>(PairSource{kb, vb}, ka, va, m, shift, tmp, s);
     else if (ids64)
       e = radix_pass<kIdItems, HOW>(IdSource<int64_t>{static_cast<const int64_t*>(ids), limit}, ka, va, m,
-                                                0, tmp, s);
+                                                0, tmp, s, true);
     else
       e = radix_pass<kIdItems, HOW>(IdSource<int32_t>{static_cast<const int32_t*>(ids), limit}, ka, va, m,
-                                                0, tmp, s);
+                                                0, tmp, s, true);
     if (e != hipSuccess) return e;
     std::swap(ka, kb);
     std::swap(va, vb);
@@ -467,7 +443,7 @@ size_t radix_ids_tmp_bytes(int64_t m) { return radix_tmp_bytes(m * kSortItems / 
 
 hipError_t radix_sort_ids(const void* ids, bool ids64, int64_t limit, uint32_t* keys, uint32_t* pos,
                           uint32_t* keys_alt, uint32_t* pos_alt, int64_t m, int bits, void* tmp, hipStream_t s) {
-  return ceil_div(m, kSortThreads * kIdItems) <= kFewBlocks
+  return id_counts_by_block(m)
              ? sort_ids<SUM_BLOCKS>(ids, ids64, limit, keys, pos, keys_alt, pos_alt, m, bits, tmp, s)
              : sort_ids<SCAN_DIGITS>(ids, ids64, limit, keys, pos, keys_alt, pos_alt, m, bits, tmp, s);
 }
