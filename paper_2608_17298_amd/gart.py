@@ -560,13 +560,18 @@ def _scratch(scratch: torch.Tensor | None, like: torch.Tensor):
     return scratch.data_ptr(), scratch.numel() * scratch.element_size()
 
 
+# The raw handle of a GPU's current stream: making a Stream object costs as much as a launch.
+_current_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) \
+    or (lambda device: torch.cuda.current_stream(device).cuda_stream)
+
+
 def _stream_on(stream, like: torch.Tensor):
     """The raw stream of the call: `stream`, or the current one of the tensors' GPU, which must be the current GPU."""
     device = like.get_device()
     if device != torch.cuda.current_device():
         raise ValueError(f"tensors are on {like.device}, the current GPU is {torch.cuda.current_device()}")
-    if stream is None:  # the raw handle: a Stream object costs as much as the launch
-        return torch._C._cuda_getCurrentRawStream(device)
+    if stream is None:
+        return _current_raw_stream(device)
     return stream.cuda_stream
 
 
