@@ -146,11 +146,15 @@ gart_status gart_embedding_backward(const void* ids, int32_t ids64, const gart_m
   const size_t ids_bytes = ids64 ? 8 : 4;
   GART_REQUIRE(dl_dout->rows == 0 || ids != nullptr, "ids is NULL");
   GART_REQUIRE(reinterpret_cast<uintptr_t>(ids) % ids_bytes == 0, "ids is not aligned to its elements");
-  GART_CHECK(
-      check_scratch(scratch, scratch_bytes, embedding_scratch_bytes(dl_dout->rows, g_table->rows, g_table->cols)));
+  const size_t need = embedding_scratch_bytes(dl_dout->rows, g_table->rows, g_table->cols);
+  GART_CHECK(check_scratch(scratch, scratch_bytes, need));
   const Span o = span_of(g_table, dtype);
   GART_REQUIRE(!overlap(o, span_of(dl_dout, dtype)) && !overlap(o, span_of(ids, int64_t(ids_bytes) * dl_dout->rows)),
                "g_table overlaps an input");
+  const Span w = span_of(scratch, int64_t(need));
+  GART_REQUIRE(!overlap(w, o) && !overlap(w, span_of(dl_dout, dtype)) &&
+                   !overlap(w, span_of(ids, int64_t(ids_bytes) * dl_dout->rows)),
+               "scratch overlaps an argument");
   EmbeddingArgs a{};
   a.ids = ids;
   a.ids64 = ids64 != 0;
@@ -243,6 +247,11 @@ gart_status gart_linear(const gart_matrix* x, const gart_matrix* weight, const v
                    !overlap(o, span_of(bias, y->cols * int64_t(dtype_bytes(dtype)))),
                "y overlaps an input");
   GART_REQUIRE(!residual || same(residual, y) || !overlap(o, span_of(residual, dtype)), "y overlaps the residual");
+  const Span s = span_of(scratch, need);
+  GART_REQUIRE(!overlap(s, o) && !overlap(s, span_of(x, dtype)) && !overlap(s, span_of(weight, dtype)) &&
+                   !overlap(s, span_of(bias, y->cols * int64_t(dtype_bytes(dtype)))) &&
+                   !overlap(s, span_of(residual, dtype)),
+               "scratch overlaps an argument");
   LinearArgs a{};
   a.m = x->rows;
   a.k = x->cols;
@@ -294,7 +303,10 @@ gart_status gart_linear_backward(const gart_matrix* x, const gart_matrix* weight
   const int64_t vec = weight->rows * int64_t(dtype_bytes(dtype));
   const Span out[3] = {span_of(g_x, dtype), span_of(g_weight, dtype), span_of(g_bias, vec)};
   const Span in[4] = {span_of(x, dtype), span_of(weight, dtype), span_of(dl_dy, dtype), span_of(bias, vec)};
+  const Span s = span_of(scratch, need);
+  for (int j = 0; j < 4; ++j) GART_REQUIRE(!overlap(s, in[j]), "scratch overlaps an input");
   for (int i = 0; i < 3; ++i) {
+    GART_REQUIRE(!overlap(s, out[i]), "scratch overlaps a gradient");
     for (int j = 0; j < 4; ++j) GART_REQUIRE(!overlap(out[i], in[j]), "a gradient overlaps an input");
     for (int j = 0; j < i; ++j) GART_REQUIRE(!overlap(out[i], out[j]), "gradients overlap");
   }

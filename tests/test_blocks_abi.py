@@ -93,6 +93,29 @@ def test_scratch_refused():
         assert r == INVALID and "scratch" in _err(lib)
 
 
+def test_scratch_overlaps_refused():
+    """Scratch on an input or an output: refused, whichever it is."""
+    from paper_2608_17298_amd import gart
+    lib = gart.lib()
+    m = lambda mb, r, c: ctypes.byref(_m(gart, mb << 20, r, c))  # noqa: E731
+    need = lib.gart_embedding_scratch_bytes(100, 9, 8)
+    for mb in (1, 2, 4):
+        r = lib.gart_embedding_backward(4 << 20, 0, m(1, 100, 8), 1.0, 0, m(2, 9, 8), (mb << 20) + 16, need, None)
+        assert r == INVALID and "scratch overlaps" in _err(lib)
+    need = lib.gart_linear_scratch_bytes(300, 2000, 200, 0)
+    assert 0 < need < 16 << 20
+    for mb in (32, 64, 96, 128, 160):
+        r = lib.gart_linear(m(32, 300, 2000), m(64, 200, 2000), 96 << 20, m(128, 300, 200), 0, 0, m(160, 300, 200),
+                            (mb << 20) + 16, need, None)
+        assert r == INVALID and "scratch overlaps" in _err(lib)
+    need = lib.gart_linear_backward_scratch_bytes(300, 8, 6, 0, 2)
+    assert 0 < need < 16 << 20
+    for mb in range(32, 32 * 8, 32):
+        r = lib.gart_linear_backward(m(32, 300, 8), m(64, 6, 8), 96 << 20, 2, m(128, 300, 6), 0, m(160, 300, 8),
+                                     m(192, 6, 8), 224 << 20, (mb << 20) + 16, need, None)
+        assert r == INVALID and "scratch overlaps" in _err(lib)
+
+
 def test_scratch_sizes():
     from paper_2608_17298_amd import gart
     lib = gart.lib()
