@@ -395,6 +395,118 @@ def test_linear_repeated_rows_and_in_place_residual():
     assert torch.equal(z, y)
 
 
+def _inside(values, dtype, pad, around):
+    """A matrix of these values inside a larger buffer that holds `around` everywhere else."""
+    import torch
+    v = torch.from_numpy(values).to(_torch(dtype))
+    buf = torch.full((v.shape[0] + 4, v.shape[1] + pad), around, dtype=v.dtype)
+    buf[2:-2, :v.shape[1]] = v
+    return buf.cuda()[2:-2, :v.shape[1]]
+
+
+AROUND = [(1, 1000, 130, 1), (40, 300, 20, 3), (1, 7, 5, 8), (65, 96, 1, 1), (129, 65, 63, 3), (1000, 32, 64, 8),
+          (2051, 9, 17, 0), (700, 520, 130, 1), (100, 4040, 72, 8), (70, 2000, 96, 3), (3592, 64, 4040, 8),
+          (3592, 4040, 64, 0), (20000, 272, 40, 1), (300, 1100, 24, 5), (24, 900, 1100, 5)]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("m,k,n,pad", AROUND)
+@pytest.mark.parametrize("act", ["none", "silu"])
+def test_linear_uses_nothing_around_its_inputs(m, k, n, pad, act, dtype):
+    """NaN before, behind and between the rows of every input: the results are those with zeros there, bit for bit."""
+    import torch
+    from paper_2608_17298_amd import gart
+    rng = np.random.default_rng(7 * m + k + n)
+    x, w, r = (rng.standard_normal(q) for q in ((m, k), (n, k), (m, n)))
+    w, b, t = w * k ** -0.5, rng.standard_normal((1, n)), _torch(dtype)
+    got = []
+    for around in (0.0, float("nan")):
+        dx, dw, dr = (_inside(v, dtype, pad, around) for v in (x, w, r))
+        db = _inside(b, dtype, 0, around).reshape(-1)
+        y = torch.empty((m, n), dtype=t, device="cuda")
+        gart.gart_linear(dx, dw, y, db, dr, act, _scratch(gart.gart_linear_scratch_bytes(m, k, n, t)))
+        g = [torch.empty(q, dtype=t, device="cuda") for q in ((m, k), (n, k), (n,))]
+        gart.gart_linear_backward(dx, dw, dr, *g, db, act,
+                                  _scratch(gart.gart_linear_backward_scratch_bytes(m, k, n, t, act)))
+        got.append([y, *g])
+    for zeros, nans in zip(*got):
+        assert torch.isfinite(zeros).all() and torch.equal(zeros, nans)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("m,k,n,pad", AROUND)
+def test_linear_gradient_of_nan_stays_in_its_rows_and_columns(m, k, n, pad, dtype):
+    """A NaN in dl_dy[r, j] reaches g_x[r], g_weight[j] and g_bias[j]; one in x[r, c] reaches g_weight[:, c]."""
+    import torch
+    from paper_2608_17298_amd import gart
+    t, r, j, c = _torch(dtype), m // 2, n - 1, k // 3
+    for where in ("dl", "x"):
+        x, w, d = (_inside(np.ones(q), dtype, pad, 0.0) for q in ((m, k), (n, k), (m, n)))
+        if where == "dl":
+            d[r, j] = float("nan")
+        else:
+            x[r, c] = float("nan")
+        gx, gw, gb = (torch.empty(q, dtype=t, device="cuda") for q in ((m, k), (n, k), (n,)))
+        gart.gart_linear_backward(x, w, d, gx, gw, gb, None, "none",
+                                  _scratch(gart.gart_linear_backward_scratch_bytes(m, k, n, t, "none")))
+        want = [torch.zeros_like(q, dtype=torch.bool) for q in (gx, gw, gb)]
+        if where == "dl":
+            want[0][r] = want[1][j] = True
+            want[2][j] = True
+        else:
+            want[1][:, c] = True
+        for got, nan in zip((gx, gw, gb), want):
+            assert torch.equal(torch.isnan(got), nan) and torch.isfinite(got[~nan]).all()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n,dim,vocab,pad", [(1, 5, 3, 3), (200, 48, 30, 1), (5000, 33, 900, 8), (9001, 64, 40, 0),
+                                             (20000, 130, 3000, 5), (300, 1023, 40, 1)])
+def test_embedding_uses_nothing_else(n, dim, vocab, pad, dtype):
+    """NaN around the rows, in table rows that no id names and in gradient rows without an id: none is used; a NaN in
+    a gradient row reaches its id's row alone."""
+    import torch
+    from paper_2608_17298_amd import gart
+    rng = np.random.default_rng(n + dim)
+    t, ids = _torch(dtype), rng.integers(0, vocab, n)
+    ids[ids % 3 == 1] -= 1  # unused: 1, 4, 7 ..
+    where = rng.random(n) < 0.1
+    table, rows = rng.standard_normal((vocab, dim)), rng.standard_normal((n, dim))
+    di = torch.from_numpy(np.where(where, -1, ids)).cuda()
+    scratch = _scratch(gart.gart_embedding_scratch_bytes(n, vocab, dim))
+    got = []
+    for around in (0.0, float("nan")):
+        table[1::3], rows[where] = around, around
+        out = torch.empty((n, dim), dtype=t, device="cuda")
+        gart.gart_embedding(_inside(table, dtype, pad, around), di, out, 0.5)
+        g = torch.empty((vocab, dim), dtype=t, device="cuda")
+        gart.gart_embedding_backward(di, _inside(rows, dtype, pad, around), g, 0.5, scratch)
+        got.append([out, g])
+    for zeros, nans in zip(*got):
+        assert torch.isfinite(zeros).all() and torch.equal(zeros, nans)
+    if not where[n // 2]:
+        rows[n // 2] = float("nan")
+        gart.gart_embedding_backward(di, _inside(rows, dtype, pad, 0.0), g, 0.5, scratch)
+        nan = torch.zeros_like(g, dtype=torch.bool)
+        nan[int(ids[n // 2])] = True
+        assert torch.equal(torch.isnan(g), nan) and torch.equal(g[~nan], got[0][1][~nan])
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,cols,pad", [(1, 5, 3), (100, 48, 1), (33, 65, 8), (5000, 7, 1), (2000, 130, 0)])
+def test_dropout_uses_nothing_around_its_inputs(rows, cols, pad, dtype):
+    import torch
+    from paper_2608_17298_amd import gart
+    rng = np.random.default_rng(rows)
+    x, r = rng.standard_normal((rows, cols)), rng.standard_normal((rows, cols))
+    got = []
+    for around in (0.0, float("nan")):
+        y = torch.empty((rows, cols), dtype=_torch(dtype), device="cuda")
+        gart.gart_dropout(_inside(x, dtype, pad, around), y, 0.3, 5, 6, _inside(r, dtype, pad, around))
+        got.append(y)
+    assert torch.isfinite(got[0]).all() and torch.equal(*got)
+
+
 # ---- dropout -------------------------------------------------------------------------
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("rows,cols", [(0, 5), (5, 0), (1, 1), (1, 7), (3, 8), (9, 17), (100, 48), (33, 65), (7, 2050)])
