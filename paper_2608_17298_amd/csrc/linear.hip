@@ -32,8 +32,9 @@ Cut cut_product(int64_t rows, int64_t cols, int64_t depth, int64_t most, bool wi
   return tiles(128, 128) * p >= kCus * 3 / 2 ? with(128, 128, p) : with(64, 64, parts(64, 64, 256));
 }
 
+// Without inputs there is nothing that a stream could read a pack of.
 bool stream_forward_fits(int64_t k, int64_t n, size_t es) {
-  return k <= 512 / int64_t(es) && n <= 2048 && forward_lds(round_inputs(k), n, es) <= kForwardBytes;
+  return k > 0 && k <= 512 / int64_t(es) && n <= 2048 && forward_lds(round_inputs(k), n, es) <= kForwardBytes;
 }
 
 int64_t stream_backward_parts(int64_t m, int64_t k, int64_t n, size_t es) {

@@ -196,6 +196,24 @@ def test_linear_backward(m, k, n, dtype, act, bias, pad):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("m", [41, 65, 300, 60000])
+def test_linear_without_inputs(m, dtype):
+    """No inputs (k = 0), few and many rows: y = act(bias) + residual, g_bias = sum of dl act'(bias)."""
+    from paper_2608_17298_amd import gart
+    rng = np.random.default_rng(m)
+    n, t = 7, _torch(dtype)
+    (x, x64), (w, w64) = _mat(rng, m, 0, dtype), _mat(rng, n, 0, dtype)
+    (b, b64), (r, r64) = _vec(rng, n, dtype), _mat(rng, m, n, dtype)
+    y, gb = _Out(m, n, dtype, 3), _Out(1, n, dtype, 0)
+    gart.gart_linear(x, w, y.t, b, r, "silu", _scratch(gart.gart_linear_scratch_bytes(m, 0, n, t)))
+    _within(y.value(), ref.linear(x64, w64, b64, r64, "silu"), ref.linear_tolerance(x64, w64, b64, r64, "silu", dtype))
+    gart.gart_linear_backward(x, w, r, None, None, gb.t.reshape(-1), b, "silu",
+                              _scratch(gart.gart_linear_backward_scratch_bytes(m, 0, n, t, "silu")))
+    _within(gb.value()[0], ref.linear_grads(x64, w64, b64, r64, "silu")[2],
+            ref.linear_grads_tolerance(x64, w64, b64, r64, "silu", dtype)[2])
+
+
+@pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("m,k,n,pad", [(3592, 64, 4040, 0), (3592, 4040, 64, 8), (64, 3592, 4040, 0),
                                        (100, 4040, 72, 0), (70, 2000, 96, 3), (2000, 300, 500, 0), (90, 1000, 1000, 0),
                                        (40, 1500, 700, 8), (20000, 272, 40, 0)])
