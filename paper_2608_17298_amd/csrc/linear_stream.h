@@ -261,15 +261,15 @@ __global__ __launch_bounds__((BackwardShape<T, KP, NS>::THREADS), (kResident<T, 
   const int x_at = tid % (KP / V) * V, x_count = XEVEN || tid < XALL ? int(a.k) - x_at : 0;
   const uint32_t x_off = x_count > 0 ? uint32_t(tid / (KP / V) * a.x_ld + x_at) : 0u,
                  gx_off = uint32_t(r * a.g_x_ld + (Q == 1 ? 8 : 4) * g);
-  const bool tail = a.k != KP || a.n != B::NP;  // packs are masked where they are used: not a wait for the load
+  const bool tail = a.k != KP || a.n != B::NP;  // packs are masked after the loads have been waited for
   const uint32_t x_ld = uint32_t(a.x_ld), dl_ld = uint32_t(a.dl_ld), gx_ld = uint32_t(a.g_x_ld);  // if near
   const PackMask<T> x_mask = first_of_pack<T>(x_count);
   uint32_t dl_off[Q];
-  PackMask<T> dl_mask[Q];
+  PackMask<T> dz_mask[Q];
 #pragma unroll
   for (int q = 0; q < Q; ++q) {
     dl_off[q] = uint32_t((group * B::GROUP_ROWS + r) * a.dl_ld + (n0(q) < a.n ? n0(q) : 0));
-    dl_mask[q] = first_of_pack<T>(int(a.n) - n0(q));
+    dz_mask[q] = first_of_pack<T>(int(a.n) - n0(q));
   }
   Pack<T> xr[XP], dr[MT][Q];
   auto load_x_inside = [&](int64_t t) {
@@ -335,10 +335,6 @@ __global__ __launch_bounds__((BackwardShape<T, KP, NS>::THREADS), (kResident<T, 
           for (int j = 0; j < 2; ++j) z[j] = Mfma<T>::run(fw[j][s], fx, z[j]);
         }
       }
-      if (tail) {
-#pragma unroll
-        for (int q = 0; q < Q; ++q) mask_pack(dr[i][q], dl_mask[q]);
-      }
       float d[8];
       with_activation(a.act, [&](auto act) {
 #pragma unroll
@@ -359,6 +355,7 @@ __global__ __launch_bounds__((BackwardShape<T, KP, NS>::THREADS), (kResident<T, 
           sum_b[q * V + e] += d[q * V + e];
           o.v[e] = T(d[q * V + e]);
         }
+        if (tail) mask_pack(o, dz_mask[q]);  // outputs that are not there: their z is a NaN where x is infinite
         *reinterpret_cast<typename Pack<T>::V*>(lz + lrow * B::NPITCH + n0(q)) = o.v;
       }
     }

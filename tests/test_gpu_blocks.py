@@ -478,6 +478,33 @@ def test_linear_gradient_of_nan_stays_in_its_rows_and_columns(m, k, n, pad, dtyp
 
 
 @pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("act", ["silu", "gelu"])
+@pytest.mark.parametrize("m,k,n", [(3, 9, 5), (70, 9, 5), (300, 24, 20), (700, 70, 33), (300, 300, 40), (2000, 32, 64)])
+def test_linear_gradient_of_infinite_inputs(m, k, n, act, dtype):
+    """An infinity in x[r] drives every z of the row to a limit, where the slope is 0 or 1: g_x[r] is the sum of dl W
+    over the outputs at the upper one, and the row's part of g_bias that of dl."""
+    import torch
+    from paper_2608_17298_amd import gart
+    rng = np.random.default_rng(m + n)
+    x, _ = _integers(rng, m, k, dtype, 0, 1)
+    w, w64 = _integers(rng, n, k, dtype, 0, 2)
+    d, d64 = _integers(rng, m, n, dtype, 0, 2)
+    r, c, t = m // 2, k - 1, _torch(dtype)
+    w[:, c] = torch.where(torch.arange(n) % 3 == 0, 1.0, -1.0).to(t).cuda()
+    w64[:, c] = w[:, c].cpu().double().numpy()
+    d[:] = 0.0  # the other rows add nothing to g_bias
+    d[r] = torch.from_numpy(d64[r]).to(t).cuda()
+    x[r, c] = float("inf")
+    gx, gb = torch.empty((m, k), dtype=t, device="cuda"), torch.empty(n, dtype=t, device="cuda")
+    gart.gart_linear_backward(x, w, d, gx, None, gb, None, act,
+                              _scratch(gart.gart_linear_backward_scratch_bytes(m, k, n, t, act)))
+    dz = np.where(w64[:, c] > 0, d64[r], 0.0)
+    got = gx.cpu().double().numpy()
+    assert np.array_equal(got[r], _rounded(dz @ w64, dtype)) and (np.delete(got, r, 0) == 0.0).all()
+    assert np.array_equal(gb.cpu().double().numpy(), _rounded(dz, dtype))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("n,dim,vocab,pad", [(1, 5, 3, 3), (200, 48, 30, 1), (5000, 33, 900, 8), (9001, 64, 40, 0),
                                              (20000, 130, 3000, 5), (300, 1023, 40, 1)])
 def test_embedding_uses_nothing_else(n, dim, vocab, pad, dtype):
