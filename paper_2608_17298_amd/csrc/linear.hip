@@ -16,10 +16,12 @@ Cut cut_product(int64_t rows, int64_t cols, int64_t depth, int64_t most, bool wi
     const int64_t part = std::max<int64_t>(64, ceil_div64(ceil_div64(depth, n), 64) * 64);
     return Cut{i, j, part, std::max<int64_t>(1, ceil_div64(depth, part))};
   };
-  if (wide && tiles(256, 256) >= kCus * 7 / 8) return with(256, 256, 1);
   // Narrow products are bound by their one large operand.
   if (cols <= 32 && rows > 64) return with(128, 32, parts(128, 32, 256));
   if (rows <= 32 && cols > 64) return with(32, 128, parts(32, 128, 256));
+  // Up to 128 rows or columns leave half of a tile of 256 empty (60000 x 1024 ->
+  // 128 bf16: 37 us, with 128 33; 100000 x 512 -> 16: 38 and, in narrow tiles, 20).
+  if (wide && std::min(rows, cols) > 128 && tiles(256, 256) >= kCus * 7 / 8) return with(256, 256, 1);
   // Short sums are bound by their outputs: many small blocks overlap more of
   // them (20000 x 256 -> 1024 f16: 49 us with 128, 44 with 64; 20000 x 200 -> 500
   // f32: 99 and 62; 8000 x 512 -> 1000 f16: 22 and 25).
