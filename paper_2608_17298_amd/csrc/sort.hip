@@ -201,13 +201,7 @@ __global__ __launch_bounds__(kSortThreads) void radix_scatter_kernel(
   for (int r = 0; r < ITEMS; ++r) {
     const bool valid = wbase + int64_t(r) * 64 + lane < m;
     const uint32_t d = (myk[r] >> shift) & 255u;
-    uint64_t peers = __ballot(valid);
-#pragma unroll
-    for (int b = 0; b < 8; ++b) {
-      const bool bit = (d >> b) & 1u;
-      const uint64_t bal = __ballot(bit);
-      peers &= bit ? bal : ~bal;
-    }
+    const uint64_t peers = same_digit(valid, d);
     const uint32_t below = __popcll(peers & lt_mask);
     const uint32_t before = wcount[d];
     myr[r] = before + below;

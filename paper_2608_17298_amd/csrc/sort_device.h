@@ -64,6 +64,21 @@ __device__ __forceinline__ void radix_count(const Source& source, int64_t m, int
       h[threadIdx.x];
 }
 
+// The valid lanes of the wave whose 8-bit digit is this lane's.  Each bit's
+// ballot is matched as ballot == bit in both halves, three operands an instruction.
+__device__ __forceinline__ uint64_t same_digit(bool valid, uint32_t d) {
+  const uint64_t all = __ballot(valid);
+  uint32_t lo = uint32_t(all), hi = uint32_t(all >> 32);
+#pragma unroll
+  for (int b = 0; b < 8; ++b) {
+    const uint32_t bit = uint32_t(int32_t(d << (31 - b)) >> 31);  // all ones or none
+    const uint64_t set = __ballot(bit != 0u);
+    lo &= ~(uint32_t(set) ^ bit);
+    hi &= ~(uint32_t(set >> 32) ^ bit);
+  }
+  return uint64_t(hi) << 32 | lo;
+}
+
 // source.key(j), source.val(j): the pairs to sort, j < m <= kSmallThreads *
 // ITEMS, by one block of kSmallThreads threads.
 template <int ITEMS, typename Source>
@@ -94,13 +109,7 @@ __device__ __forceinline__ void radix_small(const Source& source, uint32_t* __re
       if (wbase + r * 64 >= m) break;
       const bool valid = wbase + r * 64 + int(lane) < m;
       const uint32_t d = (myk[r] >> shift) & 255u;
-      uint64_t peers = __ballot(valid);
-#pragma unroll
-      for (int b = 0; b < 8; ++b) {
-        const bool bit = (d >> b) & 1u;
-        const uint64_t bal = __ballot(bit);
-        peers &= bit ? bal : ~bal;
-      }
+      const uint64_t peers = same_digit(valid, d);
       const uint32_t below = __popcll(peers & lt_mask);
       const uint32_t before = wcount[d];
       myr[r] = before + below;
