@@ -42,7 +42,7 @@ bool stream_forward_fits(int64_t k, int64_t n, size_t es) {
 int64_t stream_backward_parts(int64_t m, int64_t k, int64_t n, size_t es) {
   if (m <= 0 || k <= 0 || n <= 0) return 0;
   const BackwardChoice c = choose_backward(k, n, es);
-  return c.kp == 0 ? 0 : even_blocks(ceil_div64(m, c.rows), kBackwardBlocks);
+  return c.kp == 0 ? 0 : backward_blocks(ceil_div64(m, c.rows));
 }
 
 BackwardPlan backward_plan(int64_t m, int64_t k, int64_t n, gart_dtype t, gart_activation act) {

@@ -519,7 +519,7 @@ hipError_t backward_run(const LinearArgs& a, float* partial, hipStream_t s) {
   if constexpr (B::FITS) {
     const int64_t tiles = ceil_div64(a.m, B::ROWS);
     stream_backward_kernel<T, KP, NS>
-        <<<uint32_t(even_blocks(tiles, kBackwardBlocks)), B::THREADS, 0, s>>>(a, partial, tiles);
+        <<<uint32_t(backward_blocks(tiles)), B::THREADS, 0, s>>>(a, partial, tiles);
     return hipGetLastError();
   }
   return hipErrorInvalidValue;
