@@ -184,8 +184,13 @@ constexpr int kJoinRows = 32;           // rows per column sum of a joined dz
 constexpr int kSumRows = 256;           // rows per column sum of dl
 constexpr int64_t kFewRows = 64;        // rows up to which every block takes all of them
 
+// 16-bit gradients whose dz stays float: elements of dz, and inputs, up to which
+// (linear_small.h).  Beyond, dz's roundings average out.
+constexpr int64_t kSmallElements = 1024;
+constexpr int64_t kSmallInputs = 16384;
+
 struct BackwardPlan {
-  bool stream;
+  bool small, stream;
   int64_t parts;  // partial sums (stream)
   int64_t dz_ld;
   size_t dz, partial, sums, total;

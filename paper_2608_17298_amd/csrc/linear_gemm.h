@@ -19,6 +19,7 @@
 #include <algorithm>
 
 #include "linear.h"
+#include "linear_small.h"
 
 namespace gart {
 namespace {
@@ -537,6 +538,9 @@ hipError_t gemm_backward(const LinearArgs& a, hipStream_t s) {
   float* sums = reinterpret_cast<float*>(base + p.sums);
   float* partial = reinterpret_cast<float*>(base + p.partial);
   hipError_t e = hipSuccess;
+  if constexpr (sizeof(T) == 2) {
+    if (p.small) return small_backward<T>(a, reinterpret_cast<float*>(base + p.dz), s);
+  }
   if (p.stream) {
     if ((e = stream_backward<T>(a, partial, s)) != hipSuccess || p.parts == 1) return e;
     return join_parts<T>(partial, p.parts, a.n, a.k, a.g_w, a.g_w_ld, s, a.n, a.g_bias);

@@ -195,6 +195,26 @@ def test_linear_backward(m, k, n, dtype, act, bias, pad):
         _within(got[0][q], want[q], tol[q])
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("m,k,n,pad", [(1, 2, 3, 0), (29, 52, 1, 3), (1, 1, 1024, 0), (64, 1000, 16, 8), (1, 4097, 64, 1),
+                                       (1000, 100, 1, 0), (9, 16, 4, 0), (300, 2000, 3, 3), (1, 16384, 2, 0)])
+@pytest.mark.parametrize("act", ["silu", "gelu"])
+def test_linear_gradient_of_few_elements_rounds_once(m, k, n, pad, act, dtype):
+    """Up to 1024 elements of dz: it is not rounded to 16 bits, so the results are as exact as float's, rounded once."""
+    from paper_2608_17298_amd import gart
+    rng = np.random.default_rng(m + k + n)
+    x, x64 = _mat(rng, m, k, dtype, pad)
+    w, w64 = _mat(rng, n, k, dtype, pad, k ** -0.5)
+    (b, b64), (dl, d64) = _vec(rng, n, dtype), _mat(rng, m, n, dtype, pad)
+    gx, gw, gb = _Out(m, k, dtype, pad), _Out(n, k, dtype, pad), _Out(1, n, dtype, 0)
+    gart.gart_linear_backward(x, w, dl, gx.t, gw.t, gb.t.reshape(-1), b, act,
+                              _scratch(gart.gart_linear_backward_scratch_bytes(m, k, n, _torch(dtype), act)))
+    want = ref.linear_grads(x64, w64, b64, d64, act)
+    tol = ref.linear_grads_tolerance(x64, w64, b64, d64, act, "f32")
+    for got, a, t in zip((gx.value(), gw.value(), gb.value()[0]), want, tol):
+        _within(got, a, t + 1.01 * ref.U[dtype] * np.abs(a) + ref.TINY[dtype])
+
+
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("m", [41, 65, 300, 60000])
 def test_linear_without_inputs(m, dtype):
