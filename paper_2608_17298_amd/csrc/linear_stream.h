@@ -5,7 +5,7 @@
 // Forward: a wave takes 32 rows.  x comes from memory straight into fragments
 // (a lane holds 16 consecutive bytes of a row), W stands in LDS, and the
 // outputs leave from registers, 16 bytes a lane.  Waves do not wait for each
-// other.  Bound by bytes: 1M x 32 -> 64 f32 with gelu 85 us, 4.5 TB/s; 1016814 x
+// other.  Bound by bytes: 1M x 32 -> 64 f32 with gelu 88 us, 4.4 TB/s; 1016814 x
 // 64 -> 48 bf16 with a residual 72 us, 4.5 TB/s.
 //
 // Backward: a block takes a tile of rows at a time.  Each wave owns 32 outputs
