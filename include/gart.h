@@ -511,9 +511,9 @@ size_t gart_linear_backward_scratch_bytes(int64_t rows, int64_t inputs, int64_t 
  * is stored: z = x weight^T + bias is computed again where act needs it):
  *   dz = dl_dy act'(z);  g_x = dz weight;  g_weight = dz^T x;  g_bias = sum of dz over rows.
  * relu's derivative is 0 at z <= 0.  The residual's gradient is dl_dy.  Any of
- * the three outputs may be NULL.  With 16-bit types dz enters the products
- * rounded to that type, unless it has 1024 elements or fewer (and up to 16384
- * inputs); g_bias sums it unrounded. */
+ * the three outputs may be NULL.  With 16-bit types dz enters the products as
+ * the sum of two numbers of that type, off by 2^-15 (bf16) or 2^-20 (f16, and
+ * 2^-33) of itself at most, so the results are float32's, rounded once. */
 gart_status gart_linear_backward(const gart_matrix* x, const gart_matrix* weight, const void* bias,
                                  gart_activation act, const gart_matrix* dl_dy, gart_dtype dtype,
                                  const gart_matrix* g_x, const gart_matrix* g_weight, void* g_bias, void* scratch,

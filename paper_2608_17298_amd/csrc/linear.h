@@ -90,6 +90,80 @@ __device__ __forceinline__ void with_activation(gart_activation act, F&& f) {
   }
 }
 
+// ---- dz in two parts -----------------------------------------------------------
+// 16 bits: dz = dl act'(z), the operand of two products, is more exact than its
+// inputs, so it enters them as the sum of two numbers of the type, high + low,
+// with one matrix instruction each: off by 2^-15 (bf16) or 2^-20 (f16) of itself.
+// Where act' is 0 or 1 (none, relu) dz is of the type anyway.
+//
+// The high part is dz, less one unit of its last place as a float, cut off to the
+// type.  So both parts have dz's sign and neither is 0 unless dz is (or is as small
+// as the type's smallest number): an infinite operand gives dz's infinity, not
+// the NaN of infinity times 0 or of two signs; and an infinite dz leaves a finite
+// high and an infinite low part.  float16 holds dz times kDzUnit, as |act'| passes
+// 1, and the low part times kDzLow, as small ones would be lost below 2^-24.
+template <typename T>
+constexpr float kDzUnit = std::is_same<T, f16>::value ? 0.5f : 1.0f;
+template <typename T>
+constexpr float kDzLow = std::is_same<T, f16>::value ? 1024.0f : 1.0f;
+
+inline bool dz_in_parts(gart_activation act, size_t es) {
+  return es == 2 && (act == GART_ACT_SILU || act == GART_ACT_GELU);
+}
+
+// Two elements: their high parts, the first one's in the low bits, and their low parts.
+template <typename T>
+__device__ __forceinline__ void split_dz(float d0, float d1, uint32_t& high, uint32_t& low) {
+  float h[2] = {fmaf(d0, kDzUnit<T>, 0.0f), fmaf(d1, kDzUnit<T>, 0.0f)};  // -0 becomes 0
+  uint32_t u[2];
+#pragma unroll
+  for (int e = 0; e < 2; ++e) u[e] = __builtin_elementwise_sub_sat(__builtin_bit_cast(uint32_t, h[e]), 1u);
+  if constexpr (std::is_same<T, bf16>::value) {
+    high = __builtin_amdgcn_perm(u[1], u[0], 0x07060302u);
+    bf16 l[2];
+#pragma unroll
+    for (int e = 0; e < 2; ++e) l[e] = bf16(h[e] - __builtin_bit_cast(float, u[e] & 0xFFFF0000u));
+    __builtin_memcpy(&low, l, 4);
+  } else {
+    const auto t = __builtin_amdgcn_cvt_pkrtz(__builtin_bit_cast(float, u[0]), __builtin_bit_cast(float, u[1]));
+    const auto l = __builtin_amdgcn_cvt_pkrtz((h[0] - float(t[0])) * kDzLow<T>, (h[1] - float(t[1])) * kDzLow<T>);
+    __builtin_memcpy(&high, &t, 4);
+    __builtin_memcpy(&low, &l, 4);
+  }
+}
+
+template <typename T>
+__device__ __forceinline__ void split_dz(float d, T& high, T& low) {
+  uint32_t h, l;
+  split_dz<T>(d, 0.0f, h, l);
+  __builtin_memcpy(&high, &h, 2);
+  __builtin_memcpy(&low, &l, 2);
+}
+
+template <typename T>
+__device__ __forceinline__ void split_dz(const float* d, Pack<T>& high, Pack<T>& low) {
+  uint32_t h[4], l[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) split_dz<T>(d[2 * e], d[2 * e + 1], h[e], l[e]);
+  __builtin_memcpy(&high, h, 16);
+  __builtin_memcpy(&low, l, 16);
+}
+
+// c + kDzUnit a dz
+template <typename T>
+__device__ __forceinline__ f32x4 mfma_dz(typename Pack<T>::V a, typename Pack<T>::V high, typename Pack<T>::V low,
+                                         f32x4 c) {
+  if constexpr (kDzLow<T> == 1.0f) {
+    return Mfma<T>::run(a, high, Mfma<T>::run(a, low, c));
+  } else {
+    const f32x4 t = Mfma<T>::run(a, low, f32x4{0.0f, 0.0f, 0.0f, 0.0f});
+    c = Mfma<T>::run(a, high, c);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) c[e] = fmaf(t[e], 1.0f / kDzLow<T>, c[e]);
+    return c;
+  }
+}
+
 // ---- fragments ---------------------------------------------------------------
 // A 16-bit fragment holds eight consecutive k of a row, lanes r = lane % 16
 // over the rows and g = lane / 16 over the k (8 g ..); a float one four (4 g ..).
@@ -192,7 +266,7 @@ constexpr int64_t kSmallInputs = 16384;
 struct BackwardPlan {
   bool small, stream;
   int64_t parts;  // partial sums (stream)
-  int64_t dz_ld;
+  int64_t dz_ld, dz_low;  // dz_low: elements from dz's high parts to the low ones, or 0
   size_t dz, partial, sums, total;
 };
 BackwardPlan backward_plan(int64_t m, int64_t k, int64_t n, gart_dtype t, gart_activation act);
@@ -204,11 +278,12 @@ constexpr gart_dtype kType = sizeof(T) == 4                  ? GART_DTYPE_F32
 
 // ---- linear_rows.h, linear_stream.h, linear_gemm.h: one of each per type -----------
 inline bool few_rows(int64_t m, int64_t n) { return m <= kFewRows && n <= int64_t(1) << 24; }
-// y, or dz and g_bias (may be NULL), of up to kFewRows rows
+// y, or dz and g_bias (may be NULL), of up to kFewRows rows; dz_low: elements from
+// dz's high parts to the low ones, 0 if it is not in parts
 template <typename T>
 hipError_t rows_forward(const LinearArgs& a, hipStream_t s);
 template <typename T>
-hipError_t rows_dz(const LinearArgs& a, void* dz, int64_t dz_ld, hipStream_t s);
+hipError_t rows_dz(const LinearArgs& a, void* dz, int64_t dz_ld, int64_t dz_low, hipStream_t s);
 
 // Layers whose weight fits LDS: the rows stream past it once.
 bool stream_forward_fits(int64_t k, int64_t n, size_t es);

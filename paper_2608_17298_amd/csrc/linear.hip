@@ -72,7 +72,8 @@ BackwardPlan backward_plan(int64_t m, int64_t k, int64_t n, gart_dtype t, gart_a
     return p;
   }
   p.dz_ld = (n + 7) / 8 * 8;
-  p.dz = take(act == GART_ACT_NONE ? 0 : size_t(m) * size_t(p.dz_ld) * es);
+  p.dz_low = dz_in_parts(act, es) ? m * p.dz_ld : 0;
+  p.dz = take(act == GART_ACT_NONE ? 0 : size_t(m * p.dz_ld + p.dz_low) * es);
   // Products that are cut leave their parts here, one after the other; tiles of
   // 256 are never cut, and where they could be taken those of 128 are not either.
   size_t parts = 0;

@@ -138,6 +138,7 @@ enum Epilogue {
 struct GemmArgs {
   const void *a, *b;
   int64_t a_ld, b_ld;
+  int64_t a_low;  // A is dz: elements from its high parts to the low ones, or 0
   int64_t rows, cols, depth;  // of C, and the length of the sums
   int64_t part;               // length of one part of the sums (EPI_PARTIAL: blockIdx.z)
   int64_t tiles_i, tiles_j;
@@ -145,7 +146,7 @@ struct GemmArgs {
   const void *bias, *extra;  // extra: residual or dl
   int64_t extra_ld;
   void* out;
-  int64_t out_ld;
+  int64_t out_ld, out_low;  // out_low: EPI_DZ, as a_low
   float* sums;  // EPI_DZ: [tiles_i, cols] column sums, or NULL
 };
 
@@ -158,14 +159,20 @@ __device__ __forceinline__ int64_t xcd_tile(int64_t b, int64_t total) {
 
 // TI x TJ tiles a wave, WI x WJ waves a block.  DIRECT: both operands go
 // straight from memory into LDS, which needs 16-byte aligned rows and whole
-// steps of k; otherwise they pass through registers.
-template <typename T, bool AKC, bool BKC, int TI, int TJ, int WI, int WJ, bool DIRECT, Epilogue EPI>
-__global__ __launch_bounds__(64 * WI * WJ) void gemm_kernel(const GemmArgs g) {
+// steps of k; otherwise they pass through registers.  PARTS: A is dz in two
+// parts (split_dz), the low ones g.a_low elements behind the high ones.
+template <typename T, bool AKC, bool BKC, int TI, int TJ, int WI, int WJ, bool DIRECT, Epilogue EPI, bool PARTS>
+__global__ __launch_bounds__(64 * WI * WJ, PARTS ? 2 : 1) void gemm_kernel(const GemmArgs g) {
   constexpr int THREADS = 64 * WI * WJ;
   using TA = Tile<T, AKC, 16 * TI * WI, WI * WJ, false>;
   using TB = Tile<T, BKC, 16 * TJ * WJ, WI * WJ, true>;
   constexpr int BI = 16 * TI * WI, BJ = 16 * TJ * WJ, V = Pack<T>::N;
-  __shared__ __attribute__((aligned(16))) T lds[2][TA::ELEMS + TB::ELEMS];
+  // Both parts of a step meet B's fragments at a time, in one LDS buffer, so that two blocks still fit a CU (one part
+  // after the other, in two buffers: gradient of 60000 x 300 -> 400 bf16 381 us, so 294).  With the second launch bound
+  // the sums stay out of the accumulation registers, which no fma reaches (f16: 405 us, so 304).
+  constexpr bool BOTH = PARTS && !DIRECT;
+  constexpr int A_LOW = TA::ELEMS + TB::ELEMS, ELEMS = A_LOW + (BOTH ? TA::ELEMS : 0);
+  __shared__ __attribute__((aligned(16))) T lds[BOTH ? 1 : 2][ELEMS];
   __shared__ float s_sum[EPI == EPI_DZ ? WI : 1][EPI == EPI_DZ ? BJ : 1];
 
   const int tid = threadIdx.x, lane = tid % 64, wave = __builtin_amdgcn_readfirstlane(tid / 64);
@@ -186,15 +193,19 @@ __global__ __launch_bounds__(64 * WI * WJ) void gemm_kernel(const GemmArgs g) {
   auto multiply = [&](const T* la, const T* lb) {
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
-      typename Pack<T>::V fa[TI], fb[TJ];
+      typename Pack<T>::V fa[TI], fa_low[TI], fb[TJ];
 #pragma unroll
       for (int j = 0; j < TJ; ++j) fb[j] = TB::fragment(lb, wj * TJ + j, s, lane);
 #pragma unroll
-      for (int i = 0; i < TI; ++i) fa[i] = TA::fragment(la, wi * TI + i, s, lane);
+      for (int i = 0; i < TI; ++i) {
+        fa[i] = TA::fragment(la, wi * TI + i, s, lane);
+        if (BOTH) fa_low[i] = TA::fragment(la + A_LOW, wi * TI + i, s, lane);
+      }
 #pragma unroll
       for (int i = 0; i < TI; ++i)
 #pragma unroll
-        for (int j = 0; j < TJ; ++j) acc[i][j] = Mfma<T>::run(fb[j], fa[i], acc[i][j]);
+        for (int j = 0; j < TJ; ++j)
+          acc[i][j] = BOTH ? mfma_dz<T>(fb[j], fa[i], fa_low[i], acc[i][j]) : Mfma<T>::run(fb[j], fa[i], acc[i][j]);
     }
   };
   const int64_t a_step = TA::stride(g.a_ld), b_step = TB::stride(g.b_ld), whole = (k1 - k0) / kStep<T>;
@@ -203,16 +214,57 @@ __global__ __launch_bounds__(64 * WI * WJ) void gemm_kernel(const GemmArgs g) {
   if constexpr (DIRECT) {
     ta.template aim<true>(pa, g.a_ld, i0, g.rows, k0, tid);
     tb.template aim<true>(pb, g.b_ld, j0, g.cols, k0, tid);
+    // PARTS: the sums run over dz's low parts first, whose scale is then taken back, and then over the high ones
+    const int64_t steps = PARTS ? 2 * whole : whole;
     auto fetch = [&](int h, int64_t n) {
-      ta.fetch(lds[h], n * a_step, wave);
-      tb.fetch(lds[h] + TA::ELEMS, n * b_step, wave);
+      const int64_t at = PARTS && n >= whole ? n - whole : n;
+      ta.fetch(lds[h], at * a_step + (PARTS && n < whole ? g.a_low : 0), wave);
+      tb.fetch(lds[h] + TA::ELEMS, at * b_step, wave);
     };
-    if (whole > 0) fetch(0, 0);
-    for (int64_t n = 0; n < whole; ++n) {
+    if (steps > 0) fetch(0, 0);
+    for (int64_t n = 0; n < steps; ++n) {
       asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // this wave's part of the buffer has landed
       __syncthreads();                                  // everyone's has, and the other buffer has been read
-      if (n + 1 < whole) fetch((n + 1) & 1, n + 1);
+      if (n + 1 < steps) fetch((n + 1) & 1, n + 1);
+      if constexpr (PARTS && kDzLow<T> != 1.0f) {
+        if (n == whole) {
+#pragma unroll
+          for (int i = 0; i < TI; ++i)
+#pragma unroll
+            for (int j = 0; j < TJ; ++j) acc[i][j] *= 1.0f / kDzLow<T>;
+        }
+      }
       multiply(lds[n & 1], lds[n & 1] + TA::ELEMS);
+    }
+  } else if constexpr (PARTS) {
+    const int64_t inner = TA::regular(i0, g.rows) && TB::regular(j0, g.cols) ? whole : 0;
+    const int64_t steps = (k1 - k0 + kStep<T> - 1) / kStep<T>;
+    if (inner > 0) {
+      ta.template aim<false>(pa, g.a_ld, i0, g.rows, k0, tid);
+      tb.template aim<false>(pb, g.b_ld, j0, g.cols, k0, tid);
+    }
+    Pack<T> ra[TA::PER_THREAD], ra_low[TA::PER_THREAD], rb[TB::PER_THREAD];
+    auto load = [&](int64_t n) {
+      if (n < inner) {
+        ta.load(ra, n * a_step);
+        ta.load(ra_low, n * a_step + g.a_low);
+        tb.load(rb, n * b_step);
+      } else if (n < steps) {
+        const int64_t at = k0 + n * kStep<T>;
+        TA::load_edge(ra, pa, g.a_ld, i0, g.rows, at, k1, tid);
+        TA::load_edge(ra_low, pa + g.a_low, g.a_ld, i0, g.rows, at, k1, tid);
+        TB::load_edge(rb, pb, g.b_ld, j0, g.cols, at, k1, tid);
+      }
+    };
+    load(0);
+    for (int64_t n = 0; n < steps; ++n) {
+      TA::store(lds[0], ra, tid);
+      TA::store(lds[0] + A_LOW, ra_low, tid);
+      TB::store(lds[0] + TA::ELEMS, rb, tid);
+      lds_barrier();
+      load(n + 1);
+      multiply(lds[0], lds[0] + TA::ELEMS);
+      lds_barrier();  // the buffer has been read
     }
   } else {
     int64_t k = k0;
@@ -286,7 +338,11 @@ __global__ __launch_bounds__(64 * WI * WJ) void gemm_kernel(const GemmArgs g) {
       if (row >= g.rows || count == 0) continue;
       float c[V];
 #pragma unroll
-      for (int e = 0; e < V; ++e) c[e] = acc[i][jq * JQ + e / 4][e % 4] + b[e];
+      for (int e = 0; e < V; ++e) {
+        c[e] = acc[i][jq * JQ + e / 4][e % 4];
+        if (PARTS) c[e] *= 1.0f / kDzUnit<T>;
+        c[e] += b[e];
+      }
       if constexpr (EPI == EPI_PARTIAL) {
         float* out = static_cast<float*>(g.out) + (int64_t(blockIdx.z) * g.rows + row) * g.cols + j;
 #pragma unroll
@@ -318,14 +374,26 @@ __global__ __launch_bounds__(64 * WI * WJ) void gemm_kernel(const GemmArgs g) {
             for (int e = 0; e < V; ++e) c[e] += float(p.v[e]);
           }
         }
+        T* out = static_cast<T*>(g.out) + row * g.out_ld + j;
+        auto put = [&](T* to, const Pack<T>& o) {
+          if (DIRECT && count == V)
+            store_past(to, o);  // large: it would push the operands out (4096 x 1024 -> 4096 f16: 50 us, past 44)
+          else
+            store_some(to, o, count);
+        };
         Pack<T> o;
+        if constexpr (EPI == EPI_DZ && sizeof(T) == 2) {
+          if (g.out_low) {
+            Pack<T> low;
+            split_dz<T>(c, o, low);
+            put(out, o);
+            put(out + g.out_low, low);
+            continue;
+          }
+        }
 #pragma unroll
         for (int e = 0; e < V; ++e) o.v[e] = T(c[e]);
-        T* out = static_cast<T*>(g.out) + row * g.out_ld + j;
-        if (DIRECT && count == V)
-          store_past(out, o);  // large: it would push the operands out (4096 x 1024 -> 4096 f16: 50 us, past 44)
-        else
-          store_some(out, o, count);
+        put(out, o);
       }
     }
     if constexpr (EPI == EPI_DZ) {
@@ -440,7 +508,14 @@ __global__ __launch_bounds__(256) void join_rows_kernel(const GemmArgs g, const 
           c = activate_grad<decltype(act)::value>(c + b, float(*extra));
           sum += c;
         }
-        static_cast<T*>(g.out)[r * g.out_ld + j] = T(c);
+        T* out = static_cast<T*>(g.out) + r * g.out_ld + j;
+        if constexpr (EPI == EPI_DZ && sizeof(T) == 2) {
+          if (g.out_low) {
+            split_dz<T>(c, *out, out[g.out_low]);
+            continue;
+          }
+        }
+        *out = T(c);
       }
     });
   }
@@ -452,23 +527,23 @@ __global__ __launch_bounds__(256) void join_rows_kernel(const GemmArgs g, const 
   }
 }
 
-template <typename T, bool AKC, bool BKC, Epilogue EPI>
+template <typename T, bool AKC, bool BKC, Epilogue EPI, bool PARTS>
 hipError_t run_tiles(GemmArgs g, const Cut& c, hipStream_t s) {
   g.tiles_i = ceil_div64(g.rows, c.rows);
   g.tiles_j = ceil_div64(g.cols, c.cols);
   g.part = c.part;
   const dim3 grid(uint32_t(g.tiles_i * g.tiles_j), 1, uint32_t(EPI == EPI_PARTIAL ? c.parts : 1));
   if (c.rows == 64) {
-    gemm_kernel<T, AKC, BKC, 2, 2, 2, 2, false, EPI><<<grid, 256, 0, s>>>(g);
+    gemm_kernel<T, AKC, BKC, 2, 2, 2, 2, false, EPI, PARTS><<<grid, 256, 0, s>>>(g);
   } else if (c.cols == 32) {
-    gemm_kernel<T, AKC, BKC, 2, 2, 4, 1, false, EPI><<<grid, 256, 0, s>>>(g);
+    gemm_kernel<T, AKC, BKC, 2, 2, 4, 1, false, EPI, PARTS><<<grid, 256, 0, s>>>(g);
   } else if (c.rows == 32) {
-    gemm_kernel<T, AKC, BKC, 2, 2, 1, 4, false, EPI><<<grid, 256, 0, s>>>(g);
+    gemm_kernel<T, AKC, BKC, 2, 2, 1, 4, false, EPI, PARTS><<<grid, 256, 0, s>>>(g);
   } else if (c.rows == 128) {
-    gemm_kernel<T, AKC, BKC, 4, 4, 2, 2, false, EPI><<<grid, 256, 0, s>>>(g);
+    gemm_kernel<T, AKC, BKC, 4, 4, 2, 2, false, EPI, PARTS><<<grid, 256, 0, s>>>(g);
   } else {
     if constexpr (sizeof(T) == 2 && EPI != EPI_PARTIAL)
-      gemm_kernel<T, AKC, BKC, 8, 4, 2, 4, true, EPI><<<grid, 512, 0, s>>>(g);
+      gemm_kernel<T, AKC, BKC, 8, 4, 2, 4, true, EPI, PARTS><<<grid, 512, 0, s>>>(g);
     else
       return hipErrorInvalidValue;
   }
@@ -484,17 +559,17 @@ bool wide_operand(const void* p, int64_t ld, int64_t rows, bool kc) {
 
 // The product with its epilogue; partial holds parts * rows * cols floats where
 // it is cut.  *sum_parts: the column sums that EPI_DZ leaves.
-template <typename T, bool AKC, bool BKC, Epilogue EPI>
+template <typename T, bool AKC, bool BKC, Epilogue EPI, bool PARTS = false>
 hipError_t product(GemmArgs g, int64_t most, float* partial, hipStream_t s, int64_t* sum_parts = nullptr) {
   if (g.rows <= 0 || g.cols <= 0) return hipSuccess;
   const bool wide = g.depth % 64 == 0 && wide_operand<T>(g.a, g.a_ld, g.rows, AKC) &&
                     wide_operand<T>(g.b, g.b_ld, g.cols, BKC);
   const Cut c = cut_product(g.rows, g.cols, g.depth, most, wide);
   if (sum_parts) *sum_parts = ceil_div64(g.rows, c.parts == 1 ? c.rows : kJoinRows);
-  if (c.parts == 1) return run_tiles<T, AKC, BKC, EPI>(g, c, s);
+  if (c.parts == 1) return run_tiles<T, AKC, BKC, EPI, PARTS>(g, c, s);
   GemmArgs p = g;
   p.out = partial;
-  const hipError_t e = run_tiles<T, AKC, BKC, EPI_PARTIAL>(p, c, s);
+  const hipError_t e = run_tiles<T, AKC, BKC, EPI_PARTIAL, PARTS>(p, c, s);
   if (e != hipSuccess) return e;
   if constexpr (EPI == EPI_STORE) {
     if (c.parts > kJoinParts) return join_parts<T>(partial, c.parts, g.rows, g.cols, g.out, g.out_ld, s);
@@ -502,6 +577,15 @@ hipError_t product(GemmArgs g, int64_t most, float* partial, hipStream_t s, int6
   const dim3 grid(uint32_t(ceil_div64(g.cols, 64)), uint32_t(ceil_div64(g.rows, kJoinRows)));
   join_rows_kernel<T, EPI><<<grid, 256, 0, s>>>(g, partial, c.parts);
   return hipGetLastError();
+}
+
+// A product of dz, which is in two parts where g.a_low says so.
+template <typename T, bool AKC>
+hipError_t dz_product(const GemmArgs& g, int64_t most, float* partial, hipStream_t s) {
+  if constexpr (sizeof(T) == 2) {
+    if (g.a_low) return product<T, AKC, false, EPI_STORE, true>(g, most, partial, s);
+  }
+  return product<T, AKC, false, EPI_STORE>(g, most, partial, s);
 }
 
 template <typename T>
@@ -546,14 +630,14 @@ hipError_t gemm_backward(const LinearArgs& a, hipStream_t s) {
     return join_parts<T>(partial, p.parts, a.n, a.k, a.g_w, a.g_w_ld, s, a.n, a.g_bias);
   }
   const void* dz = a.dl;
-  int64_t dz_ld = a.dl_ld, sum_parts = 0;
+  int64_t dz_ld = a.dl_ld, dz_low = 0, sum_parts = 0;
   bool bias_done = false;
   if (a.act != GART_ACT_NONE) {
-    // dz is rounded to the type: it is the products' operand
     dz = base + p.dz;
     dz_ld = p.dz_ld;
+    dz_low = p.dz_low;
     if (few_rows(a.m, a.n)) {
-      e = rows_dz<T>(a, base + p.dz, dz_ld, s);
+      e = rows_dz<T>(a, base + p.dz, dz_ld, dz_low, s);
       bias_done = a.m > 0;
     } else {
       GemmArgs g = layer_product<T>(a);
@@ -561,6 +645,7 @@ hipError_t gemm_backward(const LinearArgs& a, hipStream_t s) {
       g.extra_ld = a.dl_ld;
       g.out = base + p.dz;
       g.out_ld = dz_ld;
+      g.out_low = dz_low;
       g.sums = a.g_bias ? sums : nullptr;
       e = product<T, true, true, EPI_DZ>(g, kJoinParts, partial, s, &sum_parts);
     }
@@ -576,6 +661,7 @@ hipError_t gemm_backward(const LinearArgs& a, hipStream_t s) {
   GemmArgs g{};
   g.a = dz;
   g.a_ld = dz_ld;
+  g.a_low = dz_low;
   if (a.g_x) {
     g.b = a.w;
     g.b_ld = a.w_ld;
@@ -584,7 +670,7 @@ hipError_t gemm_backward(const LinearArgs& a, hipStream_t s) {
     g.depth = a.n;
     g.out = a.g_x;
     g.out_ld = a.g_x_ld;
-    if ((e = product<T, true, false, EPI_STORE>(g, kJoinParts, partial, s)) != hipSuccess) return e;
+    if ((e = dz_product<T, true>(g, kJoinParts, partial, s)) != hipSuccess) return e;
   }
   if (a.g_w) {
     g.b = a.x;
@@ -594,7 +680,7 @@ hipError_t gemm_backward(const LinearArgs& a, hipStream_t s) {
     g.depth = a.m;
     g.out = a.g_w;
     g.out_ld = a.g_w_ld;
-    return product<T, false, false, EPI_STORE>(g, kWeightParts, partial, s);
+    return dz_product<T, false>(g, kWeightParts, partial, s);
   }
   return hipSuccess;
 }

@@ -18,7 +18,8 @@ constexpr int kRowsWaves = 16;
 
 // DZ: dz = dl act'(z) in place of y, and g_bias, its sum over the rows.
 template <typename T, int MT, bool DZ>
-__global__ __launch_bounds__(64 * kRowsWaves) void rows_kernel(const LinearArgs a, T* out, int64_t out_ld) {
+__global__ __launch_bounds__(64 * kRowsWaves) void rows_kernel(const LinearArgs a, T* out, int64_t out_ld,
+                                                                 int64_t out_low) {
   constexpr int V = Pack<T>::N, D = kDepth<T>, SIZE = 16 * MT * 16;
   extern __shared__ __attribute__((aligned(16))) float s_acc[];  // [waves][SIZE]
   const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64, waves = blockDim.x / 64;
@@ -66,7 +67,12 @@ __global__ __launch_bounds__(64 * kRowsWaves) void rows_kernel(const LinearArgs 
       else
         c = activate<decltype(act)::value>(c) + e;
     });
-    out[m * out_ld + j] = T(c);
+    T* to = out + m * out_ld + j;
+    if (DZ && out_low) {
+      if constexpr (sizeof(T) == 2) split_dz<T>(c, *to, to[out_low]);
+    } else {
+      *to = T(c);
+    }
     if (DZ) s_acc[o] = c;  // this thread alone has read it (every wave's share of o)
   }
   if (DZ && a.g_bias) {
@@ -81,7 +87,7 @@ __global__ __launch_bounds__(64 * kRowsWaves) void rows_kernel(const LinearArgs 
 }
 
 template <typename T, bool DZ>
-hipError_t rows_launch(const LinearArgs& a, void* out, int64_t out_ld, hipStream_t s) {
+hipError_t rows_launch(const LinearArgs& a, void* out, int64_t out_ld, int64_t out_low, hipStream_t s) {
   if (a.m <= 0 || a.n <= 0) return hipSuccess;
   const int64_t steps = ceil_div64(std::max<int64_t>(a.k, 1), kDepth<T>);
   const int waves = int(std::min<int64_t>(kRowsWaves, ceil_div64(steps, kInFlight)));
@@ -90,11 +96,11 @@ hipError_t rows_launch(const LinearArgs& a, void* out, int64_t out_ld, hipStream
   const size_t bytes = size_t(waves) * mt * 256 * 4;
   T* p = static_cast<T*>(out);
   if (mt == 1)
-    rows_kernel<T, 1, DZ><<<blocks, 64 * waves, bytes, s>>>(a, p, out_ld);
+    rows_kernel<T, 1, DZ><<<blocks, 64 * waves, bytes, s>>>(a, p, out_ld, out_low);
   else if (mt == 2)
-    rows_kernel<T, 2, DZ><<<blocks, 64 * waves, bytes, s>>>(a, p, out_ld);
+    rows_kernel<T, 2, DZ><<<blocks, 64 * waves, bytes, s>>>(a, p, out_ld, out_low);
   else
-    rows_kernel<T, 4, DZ><<<blocks, 64 * waves, bytes, s>>>(a, p, out_ld);
+    rows_kernel<T, 4, DZ><<<blocks, 64 * waves, bytes, s>>>(a, p, out_ld, out_low);
   return hipGetLastError();
 }
 
@@ -102,12 +108,12 @@ hipError_t rows_launch(const LinearArgs& a, void* out, int64_t out_ld, hipStream
 
 template <typename T>
 hipError_t rows_forward(const LinearArgs& a, hipStream_t s) {
-  return rows_launch<T, false>(a, a.y, a.y_ld, s);
+  return rows_launch<T, false>(a, a.y, a.y_ld, 0, s);
 }
 
 template <typename T>
-hipError_t rows_dz(const LinearArgs& a, void* dz, int64_t dz_ld, hipStream_t s) {
-  return rows_launch<T, true>(a, dz, dz_ld, s);
+hipError_t rows_dz(const LinearArgs& a, void* dz, int64_t dz_ld, int64_t dz_low, hipStream_t s) {
+  return rows_launch<T, true>(a, dz, dz_ld, dz_low, s);
 }
 
 }  // namespace gart

@@ -29,8 +29,9 @@ inline int64_t even_blocks(int64_t turns, int64_t most) {
 
 // ---- backward --------------------------------------------------------------------
 // NS: waves side by side over the outputs, 32 each.  With few of them, RG
-// groups of NS waves take rows of their own in a tile.
-template <size_t ES, int KP, int NS>
+// groups of NS waves take rows of their own in a tile.  PARTS: dz is in two
+// parts (split_dz); what fits LDS with one fits it with two.
+template <size_t ES, int KP, int NS, bool PARTS>
 struct BackwardSizes {
   static constexpr int RG = NS == 1 ? 4 : NS == 2 ? 2 : 1;
   static constexpr int WAVES = NS * RG, THREADS = 64 * WAVES;
@@ -39,7 +40,8 @@ struct BackwardSizes {
   static constexpr int PAD = ES == 2 ? 16 : 4;  // spreads rows (and columns' lines) over the banks
   static constexpr int KPITCH = KP + PAD, NPITCH = NP + PAD;
   static constexpr int W = NP * KPITCH, X = ROWS * KPITCH, Z = ROWS * NPITCH;
-  static constexpr size_t BYTES = size_t(W + X + Z) * ES;
+  static constexpr int Z_LOW = PARTS ? Z : 0;
+  static constexpr size_t BYTES = size_t(W + X + Z + Z_LOW) * ES;
   static constexpr bool FITS = BYTES <= 160 * 1024 && KP * int(ES) <= 512;
 };
 
@@ -64,7 +66,8 @@ struct BackwardChoice {
 
 template <size_t ES, int KP, int NS>
 bool offer(int64_t k, int64_t n, BackwardChoice* c) {
-  using B = BackwardSizes<ES, KP, NS>;
+  using B = BackwardSizes<ES, KP, NS, false>;
+  static_assert(!B::FITS || ES == 4 || BackwardSizes<ES, KP, NS, true>::FITS, "dz in two parts fits");
   if (!B::FITS || k > KP || n > 32 * NS) return false;
   *c = BackwardChoice{KP, NS, B::ROWS};
   return true;

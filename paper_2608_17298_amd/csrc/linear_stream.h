@@ -15,9 +15,10 @@
 //   registers for all of the block's tiles;
 //   g_x (rows, k) = dz W, stored.
 // Each block leaves one partial sum of g_weight and g_bias; a block that is
-// alone leaves the gradients.  1M x 64 -> 128 bf16 with silu takes 132 us (3.9
-// TB/s, 370 TFLOP/s; product by product it took 3094): vector instructions,
-// mostly the activation's slope, fill 46 % of the time, LDS and bytes the rest.
+// alone leaves the gradients.  1M x 64 -> 128 bf16 with silu takes 157 us (3.3
+// TB/s; product by product it took 3094), f16 172; with dz rounded to the type
+// it was 132, in error by 1.4 times a rounding of the results.  Bound by vector
+// instructions, mostly the activation's slope and dz's parts, beside LDS and bytes.
 #pragma once
 
 #include <algorithm>
@@ -204,22 +205,24 @@ __global__ __launch_bounds__(64 * kForwardWaves) void stream_forward_kernel(cons
 }
 
 // ---- backward ------------------------------------------------------------------
-template <typename T, int KP, int NS>
-using BackwardShape = BackwardSizes<sizeof(T), KP, NS>;
+template <typename T, int KP, int NS, bool PARTS>
+using BackwardShape = BackwardSizes<sizeof(T), KP, NS, PARTS>;
 
 // Blocks a CU that the registers have to hold: two for small weights (one
 // cost 204 us where two took 140, 1M x 64 -> 128 bf16), else what they hold.
 template <typename T, int KP, int NS>
 constexpr int kResident = KP * sizeof(T) <= 128 && NS <= 4 ? 2 : 1;
 
-template <typename T, int KP, int NS>
-__global__ __launch_bounds__((BackwardShape<T, KP, NS>::THREADS), (kResident<T, KP, NS>)) void stream_backward_kernel(
-    const LinearArgs a, float* __restrict__ partial, int64_t tiles) {
-  using B = BackwardShape<T, KP, NS>;
+template <typename T, int KP, int NS, bool PARTS>
+__global__ __launch_bounds__((BackwardShape<T, KP, NS, PARTS>::THREADS),
+                             (kResident<T, KP, NS>)) void stream_backward_kernel(const LinearArgs a,
+                                                                                 float* __restrict__ partial,
+                                                                                 int64_t tiles) {
+  using B = BackwardShape<T, KP, NS, PARTS>;
   constexpr int V = Pack<T>::N, D = kDepth<T>, S = KP / D, KT = KP / 16, Q = 8 / V;
   constexpr int MT = B::GROUP_ROWS / 16;
-  __shared__ __attribute__((aligned(16))) T lds[B::W + B::X + B::Z];
-  T *lw = lds, *lx = lds + B::W, *lz = lx + B::X;
+  __shared__ __attribute__((aligned(16))) T lds[B::W + B::X + B::Z + B::Z_LOW];
+  T *lw = lds, *lx = lds + B::W, *lz = lx + B::X, *lz_low = lz + B::Z;  // lz_low: PARTS
   const int tid = threadIdx.x, lane = tid % 64, wave = __builtin_amdgcn_readfirstlane(tid / 64);
   const int r = lane % 16, g = lane / 16;
   const int slice = wave % NS, group = wave / NS;
@@ -349,14 +352,22 @@ __global__ __launch_bounds__((BackwardShape<T, KP, NS>::THREADS), (kResident<T, 
       }
 #pragma unroll
       for (int q = 0; q < Q; ++q) {
-        Pack<T> o;
+        Pack<T> o, low;
 #pragma unroll
-        for (int e = 0; e < V; ++e) {
-          sum_b[q * V + e] += d[q * V + e];
-          o.v[e] = T(d[q * V + e]);
+        for (int e = 0; e < V; ++e) sum_b[q * V + e] += d[q * V + e];
+        if constexpr (PARTS) {
+          split_dz<T>(d, o, low);
+        } else {
+#pragma unroll
+          for (int e = 0; e < V; ++e) o.v[e] = T(d[q * V + e]);
         }
-        if (tail) mask_pack(o, dz_mask[q]);  // outputs that are not there: their z is a NaN where x is infinite
+        // outputs that are not there are masked: their z is a NaN where x is infinite
+        if (tail) mask_pack(o, dz_mask[q]);
         *reinterpret_cast<typename Pack<T>::V*>(lz + lrow * B::NPITCH + n0(q)) = o.v;
+        if constexpr (PARTS) {
+          if (tail) mask_pack(low, dz_mask[q]);
+          *reinterpret_cast<typename Pack<T>::V*>(lz_low + lrow * B::NPITCH + n0(q)) = low.v;
+        }
       }
     }
     if (whole) load_dl_inside(next);
@@ -365,14 +376,18 @@ __global__ __launch_bounds__((BackwardShape<T, KP, NS>::THREADS), (kResident<T, 
 #pragma unroll
       for (int s = 0; s < B::GROUP_ROWS / D; ++s) {
         const int k0 = group * B::GROUP_ROWS + s * D;
-        typename Pack<T>::V fz[2];
+        typename Pack<T>::V fz[2], fz_low[2];
 #pragma unroll
-        for (int j = 0; j < 2; ++j) fz[j] = fragment_of_columns<T>(lz, B::NPITCH, 2 * slice + j, k0, lane);
+        for (int j = 0; j < 2; ++j) {
+          fz[j] = fragment_of_columns<T>(lz, B::NPITCH, 2 * slice + j, k0, lane);
+          if (PARTS) fz_low[j] = fragment_of_columns<T>(lz_low, B::NPITCH, 2 * slice + j, k0, lane);
+        }
 #pragma unroll
         for (int k = 0; k < KT; ++k) {
           const auto fx = fragment_of_columns<T>(lx, B::KPITCH, k, k0, lane);
 #pragma unroll
-          for (int j = 0; j < 2; ++j) acc_w[j][k] = Mfma<T>::run(fx, fz[j], acc_w[j][k]);
+          for (int j = 0; j < 2; ++j)
+            acc_w[j][k] = PARTS ? mfma_dz<T>(fx, fz[j], fz_low[j], acc_w[j][k]) : Mfma<T>::run(fx, fz[j], acc_w[j][k]);
         }
       }
     }
@@ -384,14 +399,18 @@ __global__ __launch_bounds__((BackwardShape<T, KP, NS>::THREADS), (kResident<T, 
         f32x4 acc[IT][2] = {};
 #pragma unroll
         for (int n = 0; n < B::NP; n += D) {
-          typename Pack<T>::V fz[IT];
+          typename Pack<T>::V fz[IT], fz_low[IT];
 #pragma unroll
-          for (int i = 0; i < IT; ++i) fz[i] = fragment_of_row(lz, B::NPITCH, r0 + 16 * i + r, n, g);
+          for (int i = 0; i < IT; ++i) {
+            fz[i] = fragment_of_row(lz, B::NPITCH, r0 + 16 * i + r, n, g);
+            if (PARTS) fz_low[i] = fragment_of_row(lz_low, B::NPITCH, r0 + 16 * i + r, n, g);
+          }
 #pragma unroll
           for (int j = 0; j < 2; ++j) {
             const auto fk = fragment_of_columns<T>(lw, B::KPITCH, kt + j, n, lane);
 #pragma unroll
-            for (int i = 0; i < IT; ++i) acc[i][j] = Mfma<T>::run(fk, fz[i], acc[i][j]);
+            for (int i = 0; i < IT; ++i)
+              acc[i][j] = PARTS ? mfma_dz<T>(fk, fz[i], fz_low[i], acc[i][j]) : Mfma<T>::run(fk, fz[i], acc[i][j]);
           }
         }
         // the next tile's loads are waited for before these stores
@@ -409,7 +428,10 @@ __global__ __launch_bounds__((BackwardShape<T, KP, NS>::THREADS), (kResident<T, 
             const int64_t k = 16 * kt + (Q == 1 ? 8 * g : 16 * q + 4 * g);
             Pack<T> o;
 #pragma unroll
-            for (int e = 0; e < V; ++e) o.v[e] = T(acc[i][Q == 1 ? e / 4 : q][e % 4]);
+            for (int e = 0; e < V; ++e) {
+              const float c = acc[i][Q == 1 ? e / 4 : q][e % 4];
+              o.v[e] = T(PARTS ? c * (1.0f / kDzUnit<T>) : c);
+            }
             if (whole) {
               if (k < a.k)
                 store_some(static_cast<T*>(a.g_x) + t * B::ROWS * a.g_x_ld +
@@ -434,6 +456,12 @@ __global__ __launch_bounds__((BackwardShape<T, KP, NS>::THREADS), (kResident<T, 
     work(std::false_type{}, t, 0);
   }
 
+  if constexpr (PARTS) {
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+      for (int k = 0; k < KT; ++k) acc_w[j][k] *= 1.0f / kDzUnit<T>;
+  }
   // sums of the tile's columns, then those of the row groups, in order
 #pragma unroll
   for (int e = 0; e < 8; ++e)
@@ -515,11 +543,17 @@ hipError_t forward_kp(const LinearArgs& a, hipStream_t s) {
 
 template <typename T, int KP, int NS>
 hipError_t backward_run(const LinearArgs& a, float* partial, hipStream_t s) {
-  using B = BackwardShape<T, KP, NS>;
+  using B = BackwardShape<T, KP, NS, false>;
   if constexpr (B::FITS) {
     const int64_t tiles = ceil_div64(a.m, B::ROWS);
-    stream_backward_kernel<T, KP, NS>
-        <<<uint32_t(backward_blocks(tiles)), B::THREADS, 0, s>>>(a, partial, tiles);
+    const uint32_t blocks = uint32_t(backward_blocks(tiles));
+    if constexpr (sizeof(T) == 2) {
+      if (dz_in_parts(a.act, sizeof(T))) {
+        stream_backward_kernel<T, KP, NS, true><<<blocks, B::THREADS, 0, s>>>(a, partial, tiles);
+        return hipGetLastError();
+      }
+    }
+    stream_backward_kernel<T, KP, NS, false><<<blocks, B::THREADS, 0, s>>>(a, partial, tiles);
     return hipGetLastError();
   }
   return hipErrorInvalidValue;
