@@ -258,10 +258,11 @@ constexpr int kJoinRows = 32;           // rows per column sum of a joined dz
 constexpr int kSumRows = 256;           // rows per column sum of dl
 constexpr int64_t kFewRows = 64;        // rows up to which every block takes all of them
 
-// 16-bit gradients whose dz stays float: elements of dz, and inputs, up to which
-// (linear_small.h).  Beyond, dz's roundings average out.
+// 16-bit gradients with few elements of dz, and inputs, take two launches of
+// their own (linear_small.h), unless one block streams the rows past a small weight.
 constexpr int64_t kSmallElements = 1024;
 constexpr int64_t kSmallInputs = 16384;
+constexpr int64_t kSmallStreamInputs = 128, kSmallStreamWeight = 8192;
 
 struct BackwardPlan {
   bool small, stream;

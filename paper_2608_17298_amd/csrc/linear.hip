@@ -57,14 +57,15 @@ BackwardPlan backward_plan(int64_t m, int64_t k, int64_t n, gart_dtype t, gart_a
   auto floats = [](int64_t parts, int64_t rows, int64_t cols) {
     return size_t(parts) * size_t(rows) * size_t(cols) * 4;
   };
+  p.parts = stream_backward_parts(m, k, n, es);
+  const bool one_block = p.parts == 1 && k <= kSmallStreamInputs && n * k <= kSmallStreamWeight;
   p.small = es == 2 && act != GART_ACT_NONE && m > 0 && n > 0 && k > 0 && k <= kSmallInputs &&
-            m * n <= kSmallElements;
+            m * n <= kSmallElements && !one_block;
   if (p.small) {
     p.dz = take(size_t(m * n) * 4);
     p.total = off;
     return p;
   }
-  p.parts = stream_backward_parts(m, k, n, es);
   if (p.parts > 0) {
     p.stream = true;
     p.partial = take(p.parts > 1 ? floats(p.parts, n, k + 1) : 0);
