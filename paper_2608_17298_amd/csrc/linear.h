@@ -50,14 +50,15 @@ constexpr float kLog2e = 1.4426950408889634f;
 template <gart_activation ACT>
 constexpr float kEdge = ACT == GART_ACT_GELU ? 12.0f : 104.0f;
 
+// exp(-u)
 template <gart_activation ACT>
-__device__ __forceinline__ float gate(float z) {
+__device__ __forceinline__ float gate_exp(float z) {
   float h;
   if constexpr (ACT == GART_ACT_GELU)
     h = z * fmaf(z * z, -kGelu * kCubic * kLog2e, -kGelu * kLog2e);
   else
     h = z * -kLog2e;
-  return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(h));
+  return __builtin_amdgcn_exp2f(h);
 }
 
 template <gart_activation ACT>
@@ -65,18 +66,19 @@ __device__ __forceinline__ float activate(float z) {
   if constexpr (ACT == GART_ACT_NONE) return z;
   if constexpr (ACT == GART_ACT_RELU) return z < 0.0f ? 0.0f : z;  // a NaN stays
   const float c = __builtin_elementwise_maximum(z, -kEdge<ACT>);
-  return c * gate<ACT>(c);
+  return c * __builtin_amdgcn_rcpf(1.0f + gate_exp<ACT>(c));
 }
 
-// dl times act'(z)
+// dl times act'(z) = g + z u' g (1 - g), where 1 - g is exp(-u) g: the difference
+// would lose what the factor z u' brings back (gelu's slope near z = 4: 2e-6 off).
 template <gart_activation ACT>
 __device__ __forceinline__ float activate_grad(float z, float dl) {
   if constexpr (ACT == GART_ACT_NONE) return dl;
   if constexpr (ACT == GART_ACT_RELU) return z <= 0.0f ? 0.0f : dl;
   const float c = __builtin_elementwise_minimum(__builtin_elementwise_maximum(z, -kEdge<ACT>), kEdge<ACT>);
-  const float g = gate<ACT>(c);
+  const float x = gate_exp<ACT>(c), g = __builtin_amdgcn_rcpf(1.0f + x);
   const float s = ACT == GART_ACT_GELU ? c * fmaf(3.0f * kCubic * kGelu * c, c, kGelu) : c;
-  return dl * fmaf(s * g, 1.0f - g, g);
+  return dl * fmaf(s * g, fminf(x, 0x1p126f) * g, g);  // an infinite exp(-u) has g = 0
 }
 
 // f(integral constant of act): one branch a block of elements, none between them

@@ -114,3 +114,30 @@ def test_infinite_gradients_and_inputs_stay_infinite(m, k, n, act, dtype):
     want = np.where(dl[r].cpu().double().numpy() > 0, np.inf, -np.inf)
     assert np.array_equal(gw[up, c], want[up]) and np.isnan(gw[~up, c]).all()
     assert np.isfinite(np.delete(gw, c, 1)).all()
+
+
+@pytest.mark.parametrize("act", ["silu", "gelu"])
+@pytest.mark.parametrize("rows", [1, 70])
+def test_slopes_are_exact_to_a_few_roundings(act, rows):
+    """act'(z) of single pre-activations, which are exact: g + z u' g (1 - g) with g = 1 / (1 + exp(-u)).  A few
+    roundings of each term; the exponent's own, which moves exp(-u) by about |u| u32, moves g and 1 - g by g (1 - g)
+    of it."""
+    import torch
+    from paper_2608_17298_amd import gart
+    z = np.concatenate([np.linspace(-12.0, 12.0, 2001), np.linspace(-100.0, 100.0, 401)]).astype(np.float32)
+    x, w = torch.zeros((rows, 3), device="cuda"), torch.zeros((len(z), 3), device="cuda")
+    x[:, 0], w[:, 0] = 1.0, torch.from_numpy(z).cuda()
+    dl = torch.zeros((rows, len(z)), device="cuda")
+    dl[0] = 1.0
+    gb = torch.empty(len(z), device="cuda")
+    gart.gart_linear_backward(x, w, dl, None, None, gb, None, act,
+                              _scratch(gart.gart_linear_backward_scratch_bytes(rows, 3, len(z), torch.float32, act)))
+    z = z.astype(np.float64)
+    c = 2.0 * np.sqrt(2.0 / np.pi)
+    u = z if act == "silu" else c * (z + 0.044715 * z ** 3)
+    du = np.ones_like(z) if act == "silu" else c * (1.0 + 3.0 * 0.044715 * z ** 2)
+    e = np.exp(-np.abs(u))
+    g, h = np.where(u > 0, 1.0, e) / (1.0 + e), np.where(u > 0, e, 1.0) / (1.0 + e)  # gate, and 1 - gate
+    want = g + z * du * g * h
+    tol = ref.U32 * (6.0 * g + 12.0 * np.abs(z * du) * g * h + (4.0 * np.abs(u) + 8.0) * g * h * (1.0 + np.abs(z * du)))
+    _within(gb.cpu().double().numpy(), want, tol + 1e-35)
