@@ -269,8 +269,7 @@ __global__ __launch_bounds__(kSortThreads) void radix_scatter_kernel(
 // time (16384: 66 us both).
 // ---------------------------------------------------------------------------
 template <int ITEMS>
-__global__ __launch_bounds__(kSmallThreads) void radix_small_kernel(uint32_t* __restrict__ keys,
-                                                                    uint32_t* __restrict__ vals, int m, int bits) {
+__global__ __launch_bounds__(kSmallThreads) void radix_small_kernel(uint32_t* keys, uint32_t* vals, int m, int bits) {
   radix_small<ITEMS>(PairSource{keys, vals}, keys, vals, m, bits);
 }
 

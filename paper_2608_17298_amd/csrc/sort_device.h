@@ -80,10 +80,10 @@ __device__ __forceinline__ uint64_t same_digit(bool valid, uint32_t d) {
 }
 
 // source.key(j), source.val(j): the pairs to sort, j < m <= kSmallThreads *
-// ITEMS, by one block of kSmallThreads threads.
+// ITEMS, by one block of kSmallThreads threads.  They may lie in keys and vals
+// themselves (no restrict): all are read before any is written.
 template <int ITEMS, typename Source>
-__device__ __forceinline__ void radix_small(const Source& source, uint32_t* __restrict__ keys,
-                                            uint32_t* __restrict__ vals, int m, int bits) {
+__device__ __forceinline__ void radix_small(const Source& source, uint32_t* keys, uint32_t* vals, int m, int bits) {
   __shared__ uint32_t s_keys[kSmallThreads * ITEMS];
   __shared__ uint32_t s_vals[kSmallThreads * ITEMS];
   __shared__ uint32_t s_wave[kSmallWaves][256];
