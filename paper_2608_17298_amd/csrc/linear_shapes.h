@@ -52,13 +52,8 @@ constexpr int64_t kBackwardBlocks = 512;
 
 // All of them, so that CUs get equally many tiles (100000 x 32 -> 64 f32, 1563
 // tiles: 27 us; 391 blocks of four turns, on half of the CUs two, 29.5; 36000 x
-// 128 -> 100 f32: 72 and 83).  With three to four tiles a CU, two turns in fewer
-// blocks take as long and leave fewer sums to join (50000 x 64 -> 128 bf16: 24
-// us, in 391 blocks 23).
-inline int64_t backward_blocks(int64_t tiles) {
-  const bool two_turns = 2 * tiles > 3 * kBackwardBlocks && tiles <= 2 * kBackwardBlocks;
-  return two_turns ? (tiles + 1) / 2 : std::min(tiles, kBackwardBlocks);
-}
+// 128 -> 100 f32: 72 and 83).
+inline int64_t backward_blocks(int64_t tiles) { return std::min(tiles, kBackwardBlocks); }
 
 struct BackwardChoice {
   int kp, ns, rows;  // kp 0: none
