@@ -489,7 +489,8 @@ size_t gart_embedding_scratch_bytes(int64_t n, int64_t vocab, int64_t dim);
  *   g_table[v,:] = scale * sum over i with ids[i] = v of dl_dout[i,:]
  * for every v < g_table.rows (zero for rows no id names).  Rows are summed in
  * an order fixed by the ids alone, so the result is deterministic.
- * UNSUPPORTED for more than 2^23 columns. */
+ * UNSUPPORTED for more than 2^23 columns, and for 2^30 ids or more where a row
+ * has more than 2048 bytes. */
 gart_status gart_embedding_backward(const void* ids, int32_t ids64, const gart_matrix* dl_dout, float scale,
                                     gart_dtype dtype, const gart_matrix* g_table, void* scratch,
                                     size_t scratch_bytes, void* stream);
@@ -499,7 +500,9 @@ size_t gart_linear_scratch_bytes(int64_t rows, int64_t inputs, int64_t outputs, 
 
 /* y = act(x weight^T + bias) + residual, with x [rows, inputs], weight
  * [outputs, inputs], bias [outputs] or NULL, residual [rows, outputs] or NULL
- * (it may be y itself). */
+ * (it may be y itself).  UNSUPPORTED where y has more than 2^23 tiles of 64 x 64
+ * (begun ones count), unless it has up to 64 rows and 2^24 columns, or the
+ * weight is small: up to 512 bytes a row and about 64 KB. */
 gart_status gart_linear(const gart_matrix* x, const gart_matrix* weight, const void* bias,
                         const gart_matrix* residual, gart_activation act, gart_dtype dtype, const gart_matrix* y,
                         void* scratch, size_t scratch_bytes, void* stream);
@@ -513,7 +516,10 @@ size_t gart_linear_backward_scratch_bytes(int64_t rows, int64_t inputs, int64_t 
  * relu's derivative is 0 at z <= 0.  The residual's gradient is dl_dy.  Any of
  * the three outputs may be NULL.  With 16-bit types dz enters the products as
  * the sum of two numbers of that type, off by 2^-15 (bf16) or 2^-20 (f16, and
- * 2^-33) of itself at most, so the results are float32's, rounded once. */
+ * 2^-33) of itself at most, so the results are float32's, rounded once.
+ * UNSUPPORTED where dl_dy, x or weight has more than 2^23 tiles of 64 x 64 or
+ * there are more than 4194240 outputs, unless the weight is small: up to 256
+ * outputs and 512 bytes a row, and 160 KB with 64 to 128 rows beside it. */
 gart_status gart_linear_backward(const gart_matrix* x, const gart_matrix* weight, const void* bias,
                                  gart_activation act, const gart_matrix* dl_dy, gart_dtype dtype,
                                  const gart_matrix* g_x, const gart_matrix* g_weight, void* g_bias, void* scratch,

@@ -138,6 +138,8 @@ struct EmbeddingArgs {
   void* scratch;
 };
 size_t embedding_scratch_bytes(int64_t n, int64_t vocab, int64_t dim);
+// whether the gradient's sums fit the 2^32 threads of a launch
+bool embedding_backward_launchable(int64_t n, int64_t dim, gart_dtype t);
 hipError_t launch_embedding(const EmbeddingArgs& a, gart_dtype t, hipStream_t s);
 hipError_t launch_embedding_backward(const EmbeddingArgs& a, gart_dtype t, hipStream_t s);
 

@@ -142,7 +142,8 @@ gart_status gart_embedding_backward(const void* ids, int32_t ids64, const gart_m
   GART_REQUIRE(g_table->cols == dl_dout->cols, "g_table has %lld columns, dl_dout %lld", (long long)g_table->cols,
                (long long)dl_dout->cols);
   if (g_table->rows == 0 || g_table->cols == 0) return GART_OK;
-  if (g_table->cols > kMaxDim) return fail(GART_ERR_UNSUPPORTED, "%lld columns", (long long)g_table->cols);
+  if (g_table->cols > kMaxDim || !embedding_backward_launchable(dl_dout->rows, g_table->cols, dtype))
+    return fail(GART_ERR_UNSUPPORTED, "%lld ids of %lld columns", (long long)dl_dout->rows, (long long)g_table->cols);
   const size_t ids_bytes = ids64 ? 8 : 4;
   GART_REQUIRE(dl_dout->rows == 0 || ids != nullptr, "ids is NULL");
   GART_REQUIRE(reinterpret_cast<uintptr_t>(ids) % ids_bytes == 0, "ids is not aligned to its elements");

@@ -476,6 +476,12 @@ size_t embedding_scratch_bytes(int64_t n, int64_t vocab, int64_t dim) {
   return n > 0 && vocab > 0 && dim > 0 ? grad_layout(n, dim).total : 0;
 }
 
+bool embedding_backward_launchable(int64_t n, int64_t dim, gart_dtype t) {
+  if (n <= 0 || dim <= 0) return true;
+  const int64_t rows = int64_t(unit_rows_for(n, dim)) * units_per_block(dim, 16 / int(dtype_bytes(t)));
+  return ceil_div64(n, rows) < (int64_t(1) << 32) / kThreads;
+}
+
 hipError_t launch_embedding(const EmbeddingArgs& a, gart_dtype t, hipStream_t s) {
   if (t == GART_DTYPE_F32) return lookup<float>(a, s);
   if (t == GART_DTYPE_BF16) return lookup<bf16>(a, s);
