@@ -5,6 +5,7 @@
 #include <type_traits>
 
 #include "blocks.h"
+#include "linear_cut.h"
 
 namespace gart {
 
@@ -243,22 +244,10 @@ __device__ __forceinline__ void lds_barrier() {
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
 }
 
-// ---- how the work is cut (linear.hip) --------------------------------------------
-// Products that do not stream: tiles of 256 (one block of 8 waves a CU, straight
-// into LDS) where they fill the card, else of 128, else of 64, and 128 x 32 or 32
-// x 128 for narrow ones; where tiles are few, the sums are cut into parts, which
-// are joined afterwards.
-struct Cut {
-  int rows, cols;  // of a tile
-  int64_t part, parts;
-};
-// most: parts at most; wide: alignment and sizes allow tiles of 256
-Cut cut_product(int64_t rows, int64_t cols, int64_t depth, int64_t most, bool wide);
-constexpr int64_t kJoinParts = 16;      // of y, dz and g_x, whose join has an epilogue
-constexpr int64_t kWeightParts = 1024;  // of g_weight
-constexpr int kJoinRows = 32;           // rows per column sum of a joined dz
-constexpr int kSumRows = 256;           // rows per column sum of dl
-constexpr int64_t kFewRows = 64;        // rows up to which every block takes all of them
+// ---- how the work is cut (linear_cut.h, linear.hip) -----------------------------------
+constexpr int kJoinRows = 32;          // rows per column sum of a joined dz
+constexpr int kSumRows = 256;          // rows per column sum of dl
+constexpr int64_t kFewRows = 64;       // rows up to which every block takes all of them
 
 // 16-bit gradients with few elements of dz, and inputs, take two launches of
 // their own (linear_small.h), unless one block streams the rows past a small weight.

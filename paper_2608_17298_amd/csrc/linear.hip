@@ -6,34 +6,6 @@
 
 namespace gart {
 
-Cut cut_product(int64_t rows, int64_t cols, int64_t depth, int64_t most, bool wide) {
-  constexpr int64_t kCus = 256;
-  auto tiles = [&](int i, int j) { return ceil_div64(rows, i) * ceil_div64(cols, j); };
-  auto parts = [&](int i, int j, int64_t least) {  // two blocks a CU, `least` terms a part
-    return std::max<int64_t>(1, std::min({most, 2 * kCus / tiles(i, j), depth / least}));
-  };
-  auto with = [&](int i, int j, int64_t n) {
-    const int64_t part = std::max<int64_t>(64, ceil_div64(ceil_div64(depth, n), 64) * 64);
-    return Cut{i, j, part, std::max<int64_t>(1, ceil_div64(depth, part))};
-  };
-  // Narrow products are bound by their one large operand.
-  if (cols <= 32 && rows > 64) return with(128, 32, parts(128, 32, 256));
-  if (rows <= 32 && cols > 64) return with(32, 128, parts(32, 128, 256));
-  // Up to 128 rows or columns leave half of a tile of 256 empty (60000 x 1024 ->
-  // 128 bf16: 37 us, with 128 33; 100000 x 512 -> 16: 38 and, in narrow tiles, 20).
-  if (wide && std::min(rows, cols) > 128 && tiles(256, 256) >= kCus * 7 / 8) return with(256, 256, 1);
-  // Short sums are bound by their outputs: many small blocks overlap more of
-  // them (20000 x 256 -> 1024 f16: 49 us with 128, 44 with 64; 20000 x 200 -> 500
-  // f32: 99 and 62; 8000 x 512 -> 1000 f16: 22 and 25).
-  if (depth <= 256) return with(64, 64, 1);
-  if (tiles(128, 128) >= kCus * 3 / 2) return with(128, 128, 1);
-  // Fewer of 128 leave CUs with one block and nothing to overlap (2000 x 2048 ->
-  // 2000 f16: 45 us, in two parts 43, with 64 38); long sums are worth the parts.
-  if (tiles(64, 64) >= kCus * 2 && depth <= 4096) return with(64, 64, 1);
-  const int64_t p = parts(128, 128, 512);
-  return tiles(128, 128) * p >= kCus * 3 / 2 ? with(128, 128, p) : with(64, 64, parts(64, 64, 256));
-}
-
 // Without inputs there is nothing that a stream could read a pack of.
 bool stream_forward_fits(int64_t k, int64_t n, size_t es) {
   return k > 0 && k <= 512 / int64_t(es) && n <= 2048 && forward_lds(round_inputs(k), n, es) <= kForwardBytes;
