@@ -117,7 +117,8 @@ inline bool dz_in_parts(gart_activation act, size_t es) {
 // Two elements: their high parts, the first one's in the low bits, and their low parts.
 template <typename T>
 __device__ __forceinline__ void split_dz(float d0, float d1, uint32_t& high, uint32_t& low) {
-  float h[2] = {fmaf(d0, kDzUnit<T>, 0.0f), fmaf(d1, kDzUnit<T>, 0.0f)};  // -0 becomes 0
+  // 0 is added after the product, which may underflow to -0: neither zero has a number below it
+  const float h[2] = {d0 * kDzUnit<T> + 0.0f, d1 * kDzUnit<T> + 0.0f};
   uint32_t u[2];
 #pragma unroll
   for (int e = 0; e < 2; ++e) u[e] = __builtin_elementwise_sub_sat(__builtin_bit_cast(uint32_t, h[e]), 1u);
