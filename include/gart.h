@@ -501,8 +501,8 @@ size_t gart_linear_scratch_bytes(int64_t rows, int64_t inputs, int64_t outputs, 
 /* y = act(x weight^T + bias) + residual, with x [rows, inputs], weight
  * [outputs, inputs], bias [outputs] or NULL, residual [rows, outputs] or NULL
  * (it may be y itself).  UNSUPPORTED where y has more than 2^23 tiles of 64 x 64
- * (begun ones count), unless it has up to 64 rows and 2^24 columns, or the
- * weight is small: up to 512 bytes a row and about 64 KB. */
+ * (begun ones count), unless the weight is small: up to 512 bytes a row and
+ * about 64 KB. */
 gart_status gart_linear(const gart_matrix* x, const gart_matrix* weight, const void* bias,
                         const gart_matrix* residual, gart_activation act, gart_dtype dtype, const gart_matrix* y,
                         void* scratch, size_t scratch_bytes, void* stream);

@@ -248,7 +248,10 @@ __device__ __forceinline__ void lds_barrier() {
 // ---- how the work is cut (linear_cut.h, linear.hip) -----------------------------------
 constexpr int kJoinRows = 32;          // rows per column sum of a joined dz
 constexpr int kSumRows = 256;          // rows per column sum of dl
-constexpr int64_t kFewRows = 64;       // rows up to which every block takes all of them
+// Rows up to which every block takes all of them, and inputs, of 16 and of 32 bits,
+// up to which it does with so many rows (linear_rows.h).
+constexpr int64_t kFewRows = 32, kFewRowsShort = 4096, kFewRowsFloat = 2048;
+constexpr int64_t kMoreRows = 64, kMoreRowsShort = 2048, kMoreRowsFloat = 512;
 
 // 16-bit gradients with few elements of dz, and inputs, take two launches of
 // their own (linear_small.h), unless one block streams the rows past a small weight.
@@ -270,8 +273,11 @@ constexpr gart_dtype kType = sizeof(T) == 4                  ? GART_DTYPE_F32
                                                             : GART_DTYPE_F16;
 
 // ---- linear_rows.h, linear_stream.h, linear_gemm.h: one of each per type -----------
-inline bool few_rows(int64_t m, int64_t n) { return m <= kFewRows && n <= int64_t(1) << 24; }
-// y, or dz and g_bias (may be NULL), of up to kFewRows rows; dz_low: elements from
+inline bool few_rows(int64_t m, int64_t k, int64_t n, size_t es) {
+  return n <= int64_t(1) << 24 && ((m <= kFewRows && k <= (es == 2 ? kFewRowsShort : kFewRowsFloat)) ||
+                                   (m <= kMoreRows && k <= (es == 2 ? kMoreRowsShort : kMoreRowsFloat)));
+}
+// y, or dz and g_bias (may be NULL), of few rows; dz_low: elements from
 // dz's high parts to the low ones, 0 if it is not in parts
 template <typename T>
 hipError_t rows_forward(const LinearArgs& a, hipStream_t s);

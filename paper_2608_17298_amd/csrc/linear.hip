@@ -55,7 +55,7 @@ BackwardPlan backward_plan(int64_t m, int64_t k, int64_t n, gart_dtype t, gart_a
     const Cut c = cut_product(rows, cols, depth, most, false);
     if (c.parts > 1) parts = std::max(parts, floats(c.parts, rows, cols));
   };
-  if (act != GART_ACT_NONE && !few_rows(m, n)) cut(m, n, k, kJoinParts);
+  if (act != GART_ACT_NONE && !few_rows(m, k, n, es)) cut(m, n, k, kJoinParts);
   cut(m, k, n, kJoinParts);
   cut(n, k, m, kWeightParts);
   p.partial = take(parts);
@@ -73,7 +73,7 @@ bool launchable(int64_t rows, int64_t cols) { return ceil_div64(rows, 64) * ceil
 }  // namespace
 
 int64_t linear_scratch_bytes(int64_t m, int64_t k, int64_t n, gart_dtype t) {
-  if (m <= 0 || n <= 0 || few_rows(m, n) || stream_forward_fits(k, n, dtype_bytes(t))) return 0;
+  if (m <= 0 || n <= 0 || few_rows(m, k, n, dtype_bytes(t)) || stream_forward_fits(k, n, dtype_bytes(t))) return 0;
   if (!launchable(m, n)) return -1;
   const Cut c = cut_product(m, n, k, kJoinParts, false);
   return c.parts > 1 ? c.parts * m * n * 4 : 0;
@@ -90,7 +90,7 @@ namespace {
 
 template <typename T>
 hipError_t forward(const LinearArgs& a, hipStream_t s) {
-  if (few_rows(a.m, a.n)) return rows_forward<T>(a, s);
+  if (few_rows(a.m, a.k, a.n, sizeof(T))) return rows_forward<T>(a, s);
   return stream_forward_fits(a.k, a.n, sizeof(T)) ? stream_forward<T>(a, s) : gemm_forward<T>(a, s);
 }
 

@@ -636,7 +636,7 @@ hipError_t gemm_backward(const LinearArgs& a, hipStream_t s) {
     dz = base + p.dz;
     dz_ld = p.dz_ld;
     dz_low = p.dz_low;
-    if (few_rows(a.m, a.n)) {
+    if (few_rows(a.m, a.k, a.n, sizeof(T))) {
       e = rows_dz<T>(a, base + p.dz, dz_ld, dz_low, s);
       bias_done = a.m > 0;
     } else {

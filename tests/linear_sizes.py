@@ -30,4 +30,9 @@ SIZES = [
     (300, 1100, 24, 5, ALL, (TALL_PARTS, None, FLAT)),
     (24, 900, 1100, 5, ALL, (None, FLAT_PARTS, None)),
     (20011, 9, 300, 0, ALL, (None, TALL, TALL_PARTS)),
+    # few rows whose sums are long
+    (24, 5000, 300, 5, ALL, (FLAT_PARTS, None, None)),
+    (16, 9001, 16, 0, ALL, (P64, None, None)),
+    (1, 20000, 40, 0, ALL, (P64, None, None)),
+    (50, 2100, 130, 0, ALL, (P64, None, None)),
 ]

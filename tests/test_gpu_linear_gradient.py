@@ -19,6 +19,8 @@ STREAMS = [(300, 24, 20), (1000, 64, 48), (2051, 64, 128), (700, 200, 100), (129
 TILES = [(700, 520, 130), (300, 300, 40), (2000, 300, 500), (90, 1000, 1000), (40, 1500, 700), (3592, 64, 4040),
          (20000, 272, 40), (100, 4040, 72), (257, 513, 259)]
 
+FEW_ROWS = [(10, 1500, 700), (20, 1500, 700), (50, 900, 700)]
+
 
 def _tolerance(x, w, b, dl, act, dtype):
     """float32's own errors (blocks_ref.linear_grads_tolerance), those of dz's parts, twice as many terms, one
@@ -44,7 +46,7 @@ def _gradients(x, w, dl, b, act, dtype, pad=0):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f16"])
-@pytest.mark.parametrize("m,k,n", STREAMS + TILES)
+@pytest.mark.parametrize("m,k,n", STREAMS + TILES + FEW_ROWS)
 @pytest.mark.parametrize("act,pad", [("silu", 0), ("gelu", 3)])
 def test_gradient_rounds_once(m, k, n, act, pad, dtype):
     rng = np.random.default_rng(m + 3 * k + 5 * n)
