@@ -46,8 +46,11 @@ struct BackwardSizes {
 };
 
 // Blocks: two of four waves for each of the 256 CUs, as many as the registers
-// hold (100000 x 32 -> 64 f32: three with fewer registers each took a tenth longer, four
-// a third); their partial sums are then far fewer than the rows.
+// hold where weights are small (100000 x 32 -> 64 f32: three with fewer registers each
+// took a tenth longer, four a third).  Of larger weights (64 x 256, 128 x 128 and up
+// in 16 bits) a CU holds one, and the n (k + 1) sums that each leaves count: 32000
+// rows of 256 -> 128 bf16 write and read 67 MB of them beside 42 MB of rows (63 us,
+// in tiles 53; 2000 rows 24 and 30, 100000 rows 98 and 112).
 constexpr int64_t kBackwardBlocks = 512;
 
 // All of them, so that CUs get equally many tiles (100000 x 32 -> 64 f32, 1563
