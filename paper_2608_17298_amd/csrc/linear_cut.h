@@ -37,8 +37,9 @@ inline Cut cut_product(int64_t rows, int64_t cols, int64_t depth, int64_t most, 
   // 128 bf16: 37 us, with 128 33; 100000 x 512 -> 16: 38 and, in narrow tiles, 20).
   if (wide && std::min(rows, cols) > 128 && tiles(256, 256) >= kCus * 7 / 8) return with(256, 256, 1);
   // Short sums are bound by their outputs: many small blocks overlap more of
-  // them (20000 x 256 -> 1024 f16: 49 us with 128, 44 with 64; 20000 x 200 -> 500
-  // f32: 99 and 62; 8000 x 512 -> 1000 f16: 22 and 25).
+  // them (with 64 and with 128, f32: 20000 x 200 -> 500 53 us and 69, 20000 x 256 ->
+  // 500 54 and 71; f16: 20000 x 250 -> 400 19 and 21, 5000 x 256 -> 1024 11 both, but
+  // 20000 x 250 -> 1024 46 and 41, 60000 x 100 -> 2300 186 and 162).
   if (depth <= 256) return with(64, 64, 1);
   if (tiles(128, 128) >= kCus * 3 / 2) return with(128, 128, 1);
   // Fewer of 128 leave CUs with one block and nothing to overlap (2000 x 2048 ->

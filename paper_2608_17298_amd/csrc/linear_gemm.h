@@ -10,7 +10,7 @@
 // so that lanes that read together meet different banks.
 //
 // Large products are bound by the matrix cores: 4096 x 1024 -> 4096 f16 with
-// gelu and residual takes 42 us (810 TFLOP/s), of which about 12 are the first
+// gelu and residual takes 43 us (800 TFLOP/s), of which about 12 are the first
 // loads and the outputs; each further 1024 of k costs 26 us (1300 TFLOP/s).
 // Products with short sums or few tiles are bound by the way from memory, so
 // two steps of k are on the way while one is multiplied.

@@ -15,10 +15,11 @@
 //   registers for all of the block's tiles;
 //   g_x (rows, k) = dz W, stored.
 // Each block leaves one partial sum of g_weight and g_bias; a block that is
-// alone leaves the gradients.  1M x 64 -> 128 bf16 with silu takes 157 us (3.3
-// TB/s; product by product it took 3094), f16 172; with dz rounded to the type
-// it was 132, in error by 1.4 times a rounding of the results.  Bound by vector
-// instructions, mostly the activation's slope and dz's parts, beside LDS and bytes.
+// alone leaves the gradients.  1M x 64 -> 128 bf16 with silu takes 160 us (3.2
+// TB/s; product by product it took 3094), f16 181; with dz rounded to the type
+// it was 132, in error by 1.4 times a rounding of the results.  Vector
+// instructions, mostly the activation's slope and dz's parts, fill 53 % of the
+// time (f16 61 %), LDS and bytes the rest.
 #pragma once
 
 #include <algorithm>
