@@ -442,8 +442,8 @@ gart_status gart_frame_status(const gart_frame* frame, uint32_t* flags_host, voi
 
 /* ---- Learned blocks in front of the parameters ----
  * An appearance model looks a latent code up for every Gaussian, turns the
- * codes into SH coefficients with linear layers and dropout, and takes
- * gart_backward's g_sh back into its weights and codes.  These calls are its
+ * codes into SH coefficients with linear layers, dropout and layer norm, and
+ * takes gart_backward's g_sh back into its weights and codes.  These calls are its
  * operators.
  *
  *  - All tensors of a call have one element type; ids and random state aside.
@@ -536,6 +536,26 @@ gart_status gart_linear_backward(const gart_matrix* x, const gart_matrix* weight
  * residual, is the gradient.  y may be x or the residual. */
 gart_status gart_dropout(const gart_matrix* x, const gart_matrix* residual, float p, uint64_t seed, uint64_t offset,
                          gart_dtype dtype, const gart_matrix* y, void* stream);
+
+/* Layer norm by rows: y = (x - mean) / sqrt(var + eps) * gain + bias with each
+ * row's mean and its mean squared distance from it; gain and bias are [cols] or
+ * NULL (1 and 0).  y may be x.  eps is at least 0; where var + eps is 0 the row
+ * becomes NaN, as the formula says.  A NaN or an infinity in x makes its own row
+ * NaN and no other. */
+gart_status gart_layer_norm(const gart_matrix* x, const void* gain, const void* bias, float eps, gart_dtype dtype,
+                            const gart_matrix* y, void* stream);
+
+size_t gart_layer_norm_backward_scratch_bytes(int64_t rows, int64_t cols, gart_dtype dtype);
+
+/* Gradients of gart_layer_norm from x and dl_dy (no statistics are stored): with
+ * h = (x - mean) rstd, rstd = 1 / sqrt(var + eps) and w = dl_dy gain,
+ *   g_x = rstd (w - mean(w) - h mean(w h)) by rows;
+ *   g_gain = sum of dl_dy h, g_bias = sum of dl_dy over the rows.
+ * Any of the three outputs may be NULL.  The sums over rows have an order fixed
+ * by the sizes, so the result is deterministic. */
+gart_status gart_layer_norm_backward(const gart_matrix* x, const gart_matrix* dl_dy, const void* gain, float eps,
+                                     gart_dtype dtype, const gart_matrix* g_x, void* g_gain, void* g_bias,
+                                     void* scratch, size_t scratch_bytes, void* stream);
 
 /* Human-readable name of a status code (static string). */
 const char* gart_status_string(gart_status status);

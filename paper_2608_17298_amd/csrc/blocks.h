@@ -1,4 +1,4 @@
-// Shared by the learned blocks (embedding, linear layer, dropout): element
+// Shared by the learned blocks (embedding, linear layer, dropout, layer norm): element
 // types, 16-byte accesses of any alignment, and the launchers' arguments.
 #pragma once
 
@@ -153,6 +153,20 @@ struct DropoutArgs {
   uint64_t seed, offset;
 };
 hipError_t launch_dropout(const DropoutArgs& a, gart_dtype t, hipStream_t s);
+
+// ---- layer_norm.hip --------------------------------------------------------
+struct LayerNormArgs {
+  int64_t rows, cols;
+  float eps;
+  const void *x, *gain, *bias, *dl;  // gain and bias may be NULL
+  int64_t x_ld, dl_ld;
+  void *y, *g_x, *g_gain, *g_bias;  // any gradient may be NULL
+  int64_t y_ld, g_x_ld;
+  void* scratch;
+};
+size_t layer_norm_backward_scratch_bytes(int64_t rows, int64_t cols, gart_dtype t);
+hipError_t launch_layer_norm(const LayerNormArgs& a, gart_dtype t, hipStream_t s);
+hipError_t launch_layer_norm_backward(const LayerNormArgs& a, gart_dtype t, hipStream_t s);
 
 // ---- linear.hip ------------------------------------------------------------
 struct LinearArgs {

@@ -333,4 +333,85 @@ gart_status gart_linear_backward(const gart_matrix* x, const gart_matrix* weight
   return GART_OK;
 }
 
+gart_status gart_layer_norm(const gart_matrix* x, const void* gain, const void* bias, float eps, gart_dtype dtype,
+                            const gart_matrix* y, void* stream) {
+  clear_error();
+  GART_CHECK(check_dtype(dtype));
+  GART_CHECK(check_matrix("x", x, dtype, false));
+  GART_CHECK(check_matrix("y", y, dtype, true));
+  GART_REQUIRE(x->rows == y->rows && x->cols == y->cols, "x and y differ in size");
+  GART_REQUIRE(eps >= 0.0f && std::isfinite(eps), "eps must be at least 0 and finite");
+  GART_CHECK(check_vector("gain", gain, y->cols, dtype));
+  GART_CHECK(check_vector("bias", bias, y->cols, dtype));
+  if (y->rows == 0 || y->cols == 0) return GART_OK;
+  const Span o = span_of(y, dtype);
+  const int64_t vec = y->cols * int64_t(dtype_bytes(dtype));
+  GART_REQUIRE(same(x, y) || !overlap(o, span_of(x, dtype)), "y overlaps x");
+  GART_REQUIRE(!overlap(o, span_of(gain, vec)) && !overlap(o, span_of(bias, vec)), "y overlaps gain or bias");
+  LayerNormArgs a{};
+  a.rows = x->rows;
+  a.cols = x->cols;
+  a.eps = eps;
+  a.x = x->data;
+  a.x_ld = x->stride;
+  a.gain = gain;
+  a.bias = bias;
+  a.y = y->data;
+  a.y_ld = y->stride;
+  GART_HIP(launch_layer_norm(a, dtype, static_cast<hipStream_t>(stream)));
+  return GART_OK;
+}
+
+size_t gart_layer_norm_backward_scratch_bytes(int64_t rows, int64_t cols, gart_dtype dtype) {
+  clear_error();
+  if (!size_ok(rows) || !size_ok(cols) || check_dtype(dtype) != GART_OK) return 0;
+  return layer_norm_backward_scratch_bytes(rows, cols, dtype);
+}
+
+gart_status gart_layer_norm_backward(const gart_matrix* x, const gart_matrix* dl_dy, const void* gain, float eps,
+                                     gart_dtype dtype, const gart_matrix* g_x, void* g_gain, void* g_bias,
+                                     void* scratch, size_t scratch_bytes, void* stream) {
+  clear_error();
+  GART_CHECK(check_dtype(dtype));
+  GART_CHECK(check_matrix("x", x, dtype, false));
+  GART_CHECK(check_matrix("dl_dy", dl_dy, dtype, false));
+  GART_REQUIRE(x->rows == dl_dy->rows && x->cols == dl_dy->cols, "x and dl_dy differ in size");
+  GART_REQUIRE(eps >= 0.0f && std::isfinite(eps), "eps must be at least 0 and finite");
+  GART_CHECK(check_vector("gain", gain, x->cols, dtype));
+  GART_CHECK(check_vector("g_gain", g_gain, x->cols, dtype));
+  GART_CHECK(check_vector("g_bias", g_bias, x->cols, dtype));
+  if (g_x) {
+    GART_CHECK(check_matrix("g_x", g_x, dtype, true));
+    GART_REQUIRE(g_x->rows == x->rows && g_x->cols == x->cols, "g_x and x differ in size");
+  }
+  const size_t need = layer_norm_backward_scratch_bytes(x->rows, x->cols, dtype);
+  GART_CHECK(check_scratch(scratch, scratch_bytes, need));
+  const int64_t vec = x->cols * int64_t(dtype_bytes(dtype));
+  const Span out[3] = {span_of(g_x, dtype), span_of(g_gain, vec), span_of(g_bias, vec)};
+  const Span in[3] = {span_of(x, dtype), span_of(dl_dy, dtype), span_of(gain, vec)};
+  const Span s = span_of(scratch, int64_t(need));
+  for (int j = 0; j < 3; ++j) GART_REQUIRE(!overlap(s, in[j]), "scratch overlaps an input");
+  for (int i = 0; i < 3; ++i) {
+    GART_REQUIRE(!overlap(s, out[i]), "scratch overlaps a gradient");
+    for (int j = 0; j < 3; ++j) GART_REQUIRE(!overlap(out[i], in[j]), "a gradient overlaps an input");
+    for (int j = 0; j < i; ++j) GART_REQUIRE(!overlap(out[i], out[j]), "gradients overlap");
+  }
+  LayerNormArgs a{};
+  a.rows = x->rows;
+  a.cols = x->cols;
+  a.eps = eps;
+  a.x = x->data;
+  a.x_ld = x->stride;
+  a.gain = gain;
+  a.dl = dl_dy->data;
+  a.dl_ld = dl_dy->stride;
+  a.g_x = g_x ? g_x->data : nullptr;
+  a.g_x_ld = g_x ? g_x->stride : 0;
+  a.g_gain = g_gain;
+  a.g_bias = g_bias;
+  a.scratch = scratch;
+  GART_HIP(launch_layer_norm_backward(a, dtype, static_cast<hipStream_t>(stream)));
+  return GART_OK;
+}
+
 }  // extern "C"

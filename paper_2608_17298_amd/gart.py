@@ -150,6 +150,13 @@ def lib():
                                            ctypes.c_size_t, _P]
         L.gart_dropout.restype = ctypes.c_int
         L.gart_dropout.argtypes = [_P, _P, ctypes.c_float, ctypes.c_uint64, ctypes.c_uint64, ctypes.c_int, _P, _P]
+        L.gart_layer_norm.restype = ctypes.c_int
+        L.gart_layer_norm.argtypes = [_P, _P, _P, ctypes.c_float, ctypes.c_int, _P, _P]
+        L.gart_layer_norm_backward_scratch_bytes.restype = ctypes.c_size_t
+        L.gart_layer_norm_backward_scratch_bytes.argtypes = [ctypes.c_int64] * 2 + [ctypes.c_int]
+        L.gart_layer_norm_backward.restype = ctypes.c_int
+        L.gart_layer_norm_backward.argtypes = [_P, _P, _P, ctypes.c_float, ctypes.c_int, _P, _P, _P, _P,
+                                               ctypes.c_size_t, _P]
         _lib = L
     return _lib
 
@@ -501,7 +508,7 @@ def gart_adam_step(param: torch.Tensor, grad: torch.Tensor, m: torch.Tensor, v: 
 
 
 # ---------------------------------------------------------------------------
-# Learned blocks in front of the parameters: embedding, linear layer, dropout
+# Learned blocks in front of the parameters: embedding, linear layer, dropout, layer norm
 # ---------------------------------------------------------------------------
 DTYPE_F32, DTYPE_BF16, DTYPE_F16 = 0, 1, 2
 DTYPES = {torch.float32: DTYPE_F32, torch.bfloat16: DTYPE_BF16, torch.float16: DTYPE_F16}
@@ -660,6 +667,35 @@ def gart_dropout(x: torch.Tensor, y: torch.Tensor, p: float, seed: int, offset: 
         raise ValueError("seed and offset are 64-bit unsigned")
     _check(lib().gart_dropout(ctypes.byref(mx), mr, p, seed, offset, d, ctypes.byref(my), _stream_on(stream, x)),
            "gart_dropout")
+
+
+def gart_layer_norm(x: torch.Tensor, y: torch.Tensor, gain: torch.Tensor | None = None,
+                    bias: torch.Tensor | None = None, eps: float = 1e-5, stream=None):
+    """y = (x - mean) / sqrt(var + eps) * gain + bias by rows; x and y [rows, cols] (y may be x), gain and bias
+    [cols]."""
+    d = _dtype(x)
+    mx, my, n = _matrix(x, x, "x"), _matrix(y, x, "y"), x.shape[1]
+    _check(lib().gart_layer_norm(ctypes.byref(mx), _vector(gain, x, n, "gain"), _vector(bias, x, n, "bias"), eps, d,
+                                 ctypes.byref(my), _stream_on(stream, x)), "gart_layer_norm")
+
+
+def gart_layer_norm_backward_scratch_bytes(rows: int, cols: int, dtype: torch.dtype = torch.float32) -> int:
+    return int(lib().gart_layer_norm_backward_scratch_bytes(int(rows), int(cols), DTYPES[dtype]))
+
+
+def gart_layer_norm_backward(x: torch.Tensor, dl_dy: torch.Tensor, g_x: torch.Tensor | None = None,
+                             g_gain: torch.Tensor | None = None, g_bias: torch.Tensor | None = None,
+                             gain: torch.Tensor | None = None, eps: float = 1e-5,
+                             scratch: torch.Tensor | None = None, stream=None):
+    """Gradients of gart_layer_norm (overwritten; None for those not wanted) from x and dl_dy; scratch of
+    gart_layer_norm_backward_scratch_bytes(rows, cols, dtype) bytes."""
+    d = _dtype(x)
+    mx, md, n = _matrix(x, x, "x"), _matrix(dl_dy, x, "dl_dy"), x.shape[1]
+    gx = None if g_x is None else ctypes.byref(_matrix(g_x, x, "g_x"))
+    sp, sn = _scratch(scratch, x)
+    _check(lib().gart_layer_norm_backward(ctypes.byref(mx), ctypes.byref(md), _vector(gain, x, n, "gain"), eps, d, gx,
+                                          _vector(g_gain, x, n, "g_gain"), _vector(g_bias, x, n, "g_bias"), sp, sn,
+                                          _stream_on(stream, x)), "gart_layer_norm_backward")
 
 
 def empty_grads(g: Gaussians) -> dict:
