@@ -557,6 +557,55 @@ gart_status gart_layer_norm_backward(const gart_matrix* x, const gart_matrix* dl
                                      gart_dtype dtype, const gart_matrix* g_x, void* g_gain, void* g_bias,
                                      void* scratch, size_t scratch_bytes, void* stream);
 
+/* ---- Orthogonalised steps of weight matrices ----
+ * The Muon optimiser (Jordan and others, 2024) steps a weight matrix by the
+ * nearest orthogonal matrix of its momentum, so that all directions of a gradient
+ * learn alike; biases, norms and codes keep Adam.  The conventions of the learned
+ * blocks hold: types, strides, scratch, graphs, errors. */
+
+/* The iteration (host struct): X = x / (|x| + eps) with the square root of the
+ * sum of squares, then `steps` times, with X lying flat (the transpose of an x
+ * with more rows than columns),
+ *   A = X X^T;  X <- a X + (b A + c A^2) X
+ * which takes each singular value s to a s + b s^3 + c s^5. */
+typedef struct {
+  float a, b, c;
+  float eps;     /* >= 0 */
+  int32_t steps; /* 1 .. 64 */
+} gart_newton_schulz;
+
+size_t gart_orthogonalize_scratch_bytes(int64_t rows, int64_t cols, gart_dtype dtype);
+
+/* y = the iteration's result for x; y may be x.  Products are formed of operands
+ * of 22 bits with float32 sums and rounded to the type once, at the end, so the
+ * result is as exact as the same steps in float32.  x = 0 gives 0 (NaN with
+ * eps = 0); an x that holds a NaN or an infinity gives NaN throughout.
+ * INVALID_ARG also for coefficients whose steps may take a singular value of 1
+ * or less past 1024.  UNSUPPORTED for more than 2^23 tiles of 64 x 64. */
+gart_status gart_orthogonalize(const gart_matrix* x, const gart_newton_schulz* how, gart_dtype dtype,
+                               const gart_matrix* y, void* scratch, size_t scratch_bytes, void* stream);
+
+/* Hyper-parameters of a momentum step (host struct). */
+typedef struct {
+  float lr;           /* step size, > 0 */
+  float momentum;     /* decay of m, in [0, 1) */
+  float weight_decay; /* of the parameters, times lr, >= 0 */
+  float scale;        /* of the orthogonalised update, > 0 */
+  int32_t nesterov;
+  gart_newton_schulz how;
+} gart_muon;
+
+size_t gart_muon_scratch_bytes(int64_t rows, int64_t cols, gart_dtype dtype);
+
+/* One step of a weight matrix, in place; m (float32 whatever dtype is, zero
+ * before the first step) is its momentum:
+ *   m <- momentum m + grad;  u = grad + momentum m (nesterov) or m
+ *   param <- param - lr weight_decay param - lr scale orthogonalize(u)
+ * param is rounded to its type once.  No two of param, grad, m and scratch may
+ * overlap.  A NaN or an infinity in u makes all of param NaN. */
+gart_status gart_muon_step(const gart_matrix* param, const gart_matrix* grad, const gart_matrix* m,
+                           const gart_muon* h, gart_dtype dtype, void* scratch, size_t scratch_bytes, void* stream);
+
 /* Human-readable name of a status code (static string). */
 const char* gart_status_string(gart_status status);
 

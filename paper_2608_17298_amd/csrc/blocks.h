@@ -168,6 +168,26 @@ size_t layer_norm_backward_scratch_bytes(int64_t rows, int64_t cols, gart_dtype 
 hipError_t launch_layer_norm(const LayerNormArgs& a, gart_dtype t, hipStream_t s);
 hipError_t launch_layer_norm_backward(const LayerNormArgs& a, gart_dtype t, hipStream_t s);
 
+// ---- orthogonalize.hip -----------------------------------------------------
+struct OrthogonalizeArgs {
+  int64_t rows, cols;
+  float a, b, c, eps;  // the polynomial; eps is added to the norm
+  int steps;
+  const void* x;  // the matrix, or a momentum step's gradient
+  int64_t x_ld;
+  float* m;  // a momentum step's momentum, or NULL
+  int64_t m_ld;
+  float momentum;
+  bool nesterov;
+  void* y;  // the result, or param -= decay param + step result
+  int64_t y_ld;
+  float decay, step;
+  void* scratch;
+};
+// -1 if the sizes are beyond what a launch can index
+int64_t orthogonalize_scratch_bytes(int64_t rows, int64_t cols);
+hipError_t launch_orthogonalize(const OrthogonalizeArgs& a, gart_dtype t, hipStream_t s);
+
 // ---- linear.hip ------------------------------------------------------------
 struct LinearArgs {
   int64_t m, k, n;  // rows, inputs, outputs

@@ -5,6 +5,7 @@
 #include <cmath>
 
 #include "blocks.h"
+#include "orthogonalize.h"
 #include "status.h"
 
 using namespace gart;
@@ -82,6 +83,15 @@ gart_status check_scratch(const void* scratch, size_t have, size_t need) {
   GART_REQUIRE(have >= need, "scratch_bytes %zu < required %zu", have, need);
   GART_REQUIRE(need == 0 || scratch != nullptr, "scratch is NULL");
   GART_REQUIRE(need == 0 || reinterpret_cast<uintptr_t>(scratch) % 16 == 0, "scratch must be 16-byte aligned");
+  return GART_OK;
+}
+
+gart_status check_steps(const gart_newton_schulz& n) {
+  GART_REQUIRE(std::isfinite(n.a) && std::isfinite(n.b) && std::isfinite(n.c), "coefficients must be finite");
+  GART_REQUIRE(n.eps >= 0.0f && std::isfinite(n.eps), "eps must be at least 0 and finite");
+  GART_REQUIRE(n.steps >= 1 && n.steps <= kMaxSteps, "steps must be in [1, %d]", kMaxSteps);
+  Factors f;
+  GART_REQUIRE(step_factors(n.a, n.b, n.c, n.steps, 1.0, &f.x, f.step), "singular values may pass 1024 in these steps");
   return GART_OK;
 }
 
@@ -411,6 +421,95 @@ gart_status gart_layer_norm_backward(const gart_matrix* x, const gart_matrix* dl
   a.g_bias = g_bias;
   a.scratch = scratch;
   GART_HIP(launch_layer_norm_backward(a, dtype, static_cast<hipStream_t>(stream)));
+  return GART_OK;
+}
+
+size_t gart_orthogonalize_scratch_bytes(int64_t rows, int64_t cols, gart_dtype dtype) {
+  clear_error();
+  if (!size_ok(rows) || !size_ok(cols) || check_dtype(dtype) != GART_OK) return 0;
+  const int64_t b = orthogonalize_scratch_bytes(rows, cols);
+  return b < 0 ? 0 : size_t(b);
+}
+
+gart_status gart_orthogonalize(const gart_matrix* x, const gart_newton_schulz* how, gart_dtype dtype,
+                               const gart_matrix* y, void* scratch, size_t scratch_bytes, void* stream) {
+  clear_error();
+  GART_CHECK(check_dtype(dtype));
+  GART_REQUIRE(how != nullptr, "how is NULL");
+  GART_CHECK(check_steps(*how));
+  GART_CHECK(check_matrix("x", x, dtype, false));
+  GART_CHECK(check_matrix("y", y, dtype, true));
+  GART_REQUIRE(x->rows == y->rows && x->cols == y->cols, "x and y differ in size");
+  if (y->rows == 0 || y->cols == 0) return GART_OK;
+  const int64_t need = orthogonalize_scratch_bytes(x->rows, x->cols);
+  if (need < 0) return fail(GART_ERR_UNSUPPORTED, "%lld x %lld", (long long)x->rows, (long long)x->cols);
+  GART_CHECK(check_scratch(scratch, scratch_bytes, size_t(need)));
+  const Span o = span_of(y, dtype), w = span_of(scratch, need);
+  GART_REQUIRE(same(x, y) || !overlap(o, span_of(x, dtype)), "y overlaps x");
+  GART_REQUIRE(!overlap(w, o) && !overlap(w, span_of(x, dtype)), "scratch overlaps an argument");
+  OrthogonalizeArgs a{};
+  a.rows = x->rows;
+  a.cols = x->cols;
+  a.a = how->a;
+  a.b = how->b;
+  a.c = how->c;
+  a.eps = how->eps;
+  a.steps = how->steps;
+  a.x = x->data;
+  a.x_ld = x->stride;
+  a.y = y->data;
+  a.y_ld = y->stride;
+  a.scratch = scratch;
+  GART_HIP(launch_orthogonalize(a, dtype, static_cast<hipStream_t>(stream)));
+  return GART_OK;
+}
+
+size_t gart_muon_scratch_bytes(int64_t rows, int64_t cols, gart_dtype dtype) {
+  return gart_orthogonalize_scratch_bytes(rows, cols, dtype);
+}
+
+gart_status gart_muon_step(const gart_matrix* param, const gart_matrix* grad, const gart_matrix* m,
+                           const gart_muon* h, gart_dtype dtype, void* scratch, size_t scratch_bytes, void* stream) {
+  clear_error();
+  GART_CHECK(check_dtype(dtype));
+  GART_REQUIRE(h != nullptr, "h is NULL");
+  GART_REQUIRE(h->lr > 0.0f && std::isfinite(h->lr), "lr must be above 0 and finite");
+  GART_REQUIRE(h->momentum >= 0.0f && h->momentum < 1.0f, "momentum must be in [0, 1)");
+  GART_REQUIRE(h->weight_decay >= 0.0f && std::isfinite(h->weight_decay), "weight_decay must be at least 0 and finite");
+  GART_REQUIRE(h->scale > 0.0f && std::isfinite(h->scale), "scale must be above 0 and finite");
+  GART_CHECK(check_steps(h->how));
+  GART_CHECK(check_matrix("param", param, dtype, true));
+  GART_CHECK(check_matrix("grad", grad, dtype, false));
+  GART_CHECK(check_matrix("m", m, GART_DTYPE_F32, true));
+  GART_REQUIRE(grad->rows == param->rows && grad->cols == param->cols, "grad and param differ in size");
+  GART_REQUIRE(m->rows == param->rows && m->cols == param->cols, "m and param differ in size");
+  if (param->rows == 0 || param->cols == 0) return GART_OK;
+  const int64_t need = orthogonalize_scratch_bytes(param->rows, param->cols);
+  if (need < 0) return fail(GART_ERR_UNSUPPORTED, "%lld x %lld", (long long)param->rows, (long long)param->cols);
+  GART_CHECK(check_scratch(scratch, scratch_bytes, size_t(need)));
+  const Span t[4] = {span_of(param, dtype), span_of(grad, dtype), span_of(m, GART_DTYPE_F32), span_of(scratch, need)};
+  for (int i = 0; i < 4; ++i)
+    for (int j = 0; j < i; ++j) GART_REQUIRE(!overlap(t[i], t[j]), "param, grad, m and scratch overlap");
+  OrthogonalizeArgs a{};
+  a.rows = param->rows;
+  a.cols = param->cols;
+  a.a = h->how.a;
+  a.b = h->how.b;
+  a.c = h->how.c;
+  a.eps = h->how.eps;
+  a.steps = h->how.steps;
+  a.x = grad->data;
+  a.x_ld = grad->stride;
+  a.m = static_cast<float*>(m->data);
+  a.m_ld = m->stride;
+  a.momentum = h->momentum;
+  a.nesterov = h->nesterov != 0;
+  a.y = param->data;
+  a.y_ld = param->stride;
+  a.decay = float(double(h->lr) * double(h->weight_decay));
+  a.step = float(double(h->lr) * double(h->scale));
+  a.scratch = scratch;
+  GART_HIP(launch_orthogonalize(a, dtype, static_cast<hipStream_t>(stream)));
   return GART_OK;
 }
 

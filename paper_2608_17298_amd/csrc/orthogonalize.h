@@ -1,0 +1,132 @@
+// How the orthogonalising iteration is scaled and laid out.  Plain C++, so that it
+// can be asked without a GPU; the scales are also worked out on it.
+#pragma once
+
+#include <algorithm>
+#include <cmath>
+#include <cstdint>
+
+namespace gart {
+
+#ifdef __HIPCC__
+#define GART_HOST_DEVICE __host__ __device__
+#else
+#define GART_HOST_DEVICE
+#endif
+
+// X, A = X X^T and P = b A + c A^2 are held as sums of two float16 numbers, high +
+// low, both times a power of two that fits the step: off by 2^-22 of an element.
+// Singular values of X start at |x| / (|x| + eps) or less, and after each step they
+// are values of p(s) = a s + b s^3 + c s^5; so the largest |p| over the interval
+// where they lie bounds every element of X, its square those of A, and the largest
+// |b t + c t^2| those of P.  With elements times their scale of 2^14 at most, float16
+// never overflows (65504), and 2^-24, its smallest number, is 2^-38 of the bound.
+//
+// |x| is known on the GPU alone.  The bounds are those of a start at 1 unless it is
+// below kNearOne, that is unless x is about as small as eps: then the scales are
+// worked out there, from where the values start.
+constexpr int kMaxSteps = 64;
+constexpr double kMaxValue = 0x1p10, kMaxPolynomial = 0x1p60;  // bounds of X and P that steps may reach
+constexpr double kNearOne = 0.0625;
+
+struct StepScales {
+  double x, a, p;  // powers of two
+};
+
+// The power of two by which numbers up to `bound` are multiplied.  Beyond the clamps
+// a result of float has nothing left (X), or the matrix adds nothing to a X (A, P).
+GART_HOST_DEVICE inline double pair_scale(double bound, int most) {
+  if (!(bound > 0.0)) return 1.0;
+  const int e = 13 - ilogb(bound);
+  return ldexp(1.0, e > most ? most : e < -60 ? -60 : e);
+}
+constexpr int kMostX = 120, kMostA = 60;
+
+GART_HOST_DEVICE inline double larger(double a, double b) { return a > b ? a : b; }
+
+// Scales of the step of values up to bound, and the bound of those after it.
+GART_HOST_DEVICE inline double step_scales(double a, double b, double c, double bound, StepScales* out) {
+  const double s2 = bound * bound;
+  double p = fabs(b * s2 + c * s2 * s2);
+  const double top = c != 0.0 ? -b / (2.0 * c) : -1.0;
+  if (top > 0.0 && top < s2) p = larger(p, fabs(b * top + c * top * top));
+  *out = StepScales{pair_scale(bound, kMostX), pair_scale(s2, kMostA), pair_scale(p, kMostA)};
+  if (!(p <= kMaxPolynomial)) return HUGE_VAL;
+  // p'(s) = a + 3 b t + 5 c t^2 = 0 with t = s^2
+  double next = sqrt(s2) * fabs(a + b * s2 + c * s2 * s2);
+  double t[2] = {-1.0, -1.0};
+  const double disc = 9.0 * b * b - 20.0 * a * c;
+  if (c != 0.0 && disc >= 0.0) {
+    t[0] = (-3.0 * b - sqrt(disc)) / (10.0 * c);
+    t[1] = (-3.0 * b + sqrt(disc)) / (10.0 * c);
+  } else if (c == 0.0 && b != 0.0) {
+    t[0] = -a / (3.0 * b);
+  }
+  for (int k = 0; k < 2; ++k)
+    if (t[k] > 0.0 && t[k] < s2) next = larger(next, sqrt(t[k]) * fabs(a + b * t[k] + c * t[k] * t[k]));
+  return next;
+}
+
+// What a step's products are multiplied by, scales included: A = gram (X X^T),
+// P = square (A A) + linear A, X = apply (P X) + keep X.
+struct StepFactors {
+  float gram, none, square, linear, apply, keep;
+};
+
+struct Factors {
+  float x;  // the first scale of X
+  StepFactors step[kMaxSteps];
+};
+
+// Of values that start at `bound`; false if they may pass the bounds above.
+GART_HOST_DEVICE inline bool step_factors(float a, float b, float c, int steps, double bound, float* x,
+                                          StepFactors* out) {
+  StepScales s, next;
+  bound = step_scales(a, b, c, bound, &s);
+  *x = float(s.x);
+  for (int k = 0; k < steps; ++k) {
+    if (!(bound <= kMaxValue)) return false;
+    if (k + 1 < steps)
+      bound = step_scales(a, b, c, bound, &next);
+    else
+      next.x = 1.0;  // the result itself
+    out[k] = StepFactors{float(s.a / s.x / s.x), 0.0f, float(c * (s.p / s.a / s.a)), float(b * (s.p / s.a)),
+                         float(next.x / s.p / s.x), float(a * (next.x / s.x))};
+    s = next;
+  }
+  return true;
+}
+
+// Where things lie in scratch, in bytes; sizes of the padded matrices.
+struct MatrixPlan {
+  bool tall;            // more rows than columns: X is the transpose
+  int64_t n, m;         // the smaller and the larger size
+  int64_t n_pad, m_pad;
+  int64_t x_low, a_low;  // elements from the high parts to the low ones
+  size_t sums, factors, x[2], a, p, total;
+};
+constexpr int64_t kTileSide = 64;
+constexpr int64_t kSumBlocks = 256;  // partial sums of squares
+constexpr int64_t kMostTiles = int64_t(1) << 23;
+
+inline MatrixPlan matrix_plan(int64_t rows, int64_t cols) {
+  MatrixPlan p{};
+  p.tall = rows > cols;
+  p.n = std::min(rows, cols);
+  p.m = std::max(rows, cols);
+  p.n_pad = (p.n + kTileSide - 1) / kTileSide * kTileSide;
+  p.m_pad = (p.m + kTileSide - 1) / kTileSide * kTileSide;
+  p.x_low = p.n_pad * p.m_pad;
+  p.a_low = p.n_pad * p.n_pad;
+  const size_t x = size_t(p.x_low) * 4, a = size_t(p.a_low) * 4;  // two float16 planes
+  p.sums = 0;
+  p.factors = kSumBlocks * sizeof(double);
+  p.x[0] = p.factors + sizeof(StepFactors) * kMaxSteps;
+  p.x[1] = p.x[0] + x;
+  p.a = p.x[1] + x;
+  p.p = p.a + a;
+  p.total = p.p + a;
+  return p;
+}
+
+}  // namespace gart

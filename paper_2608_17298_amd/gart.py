@@ -157,6 +157,13 @@ def lib():
         L.gart_layer_norm_backward.restype = ctypes.c_int
         L.gart_layer_norm_backward.argtypes = [_P, _P, _P, ctypes.c_float, ctypes.c_int, _P, _P, _P, _P,
                                                ctypes.c_size_t, _P]
+        for name in ("gart_orthogonalize_scratch_bytes", "gart_muon_scratch_bytes"):
+            getattr(L, name).restype = ctypes.c_size_t
+            getattr(L, name).argtypes = [ctypes.c_int64] * 2 + [ctypes.c_int]
+        L.gart_orthogonalize.restype = ctypes.c_int
+        L.gart_orthogonalize.argtypes = [_P, _P, ctypes.c_int, _P, _P, ctypes.c_size_t, _P]
+        L.gart_muon_step.restype = ctypes.c_int
+        L.gart_muon_step.argtypes = [_P, _P, _P, _P, ctypes.c_int, _P, ctypes.c_size_t, _P]
         _lib = L
     return _lib
 
@@ -696,6 +703,51 @@ def gart_layer_norm_backward(x: torch.Tensor, dl_dy: torch.Tensor, g_x: torch.Te
     _check(lib().gart_layer_norm_backward(ctypes.byref(mx), ctypes.byref(md), _vector(gain, x, n, "gain"), eps, d, gx,
                                           _vector(g_gain, x, n, "g_gain"), _vector(g_bias, x, n, "g_bias"), sp, sn,
                                           _stream_on(stream, x)), "gart_layer_norm_backward")
+
+
+# ---------------------------------------------------------------------------
+# Orthogonalised steps of weight matrices
+# ---------------------------------------------------------------------------
+class gart_newton_schulz(ctypes.Structure):
+    _fields_ = [("a", ctypes.c_float), ("b", ctypes.c_float), ("c", ctypes.c_float), ("eps", ctypes.c_float),
+                ("steps", ctypes.c_int32)]
+
+
+class gart_muon(ctypes.Structure):
+    _fields_ = [("lr", ctypes.c_float), ("momentum", ctypes.c_float), ("weight_decay", ctypes.c_float),
+                ("scale", ctypes.c_float), ("nesterov", ctypes.c_int32), ("how", gart_newton_schulz)]
+
+
+def gart_orthogonalize_scratch_bytes(rows: int, cols: int, dtype: torch.dtype = torch.float32) -> int:
+    return int(lib().gart_orthogonalize_scratch_bytes(int(rows), int(cols), DTYPES[dtype]))
+
+
+def gart_orthogonalize(x: torch.Tensor, y: torch.Tensor, how: gart_newton_schulz,
+                       scratch: torch.Tensor | None = None, stream=None):
+    """y = x over its norm, taken through how.steps steps of the polynomial (y may be x); scratch of
+    gart_orthogonalize_scratch_bytes(rows, cols, dtype) bytes."""
+    d = _dtype(x)
+    mx, my = _matrix(x, x, "x"), _matrix(y, x, "y")
+    sp, sn = _scratch(scratch, x)
+    _check(lib().gart_orthogonalize(ctypes.byref(mx), ctypes.byref(how), d, ctypes.byref(my), sp, sn,
+                                    _stream_on(stream, x)), "gart_orthogonalize")
+
+
+def gart_muon_scratch_bytes(rows: int, cols: int, dtype: torch.dtype = torch.float32) -> int:
+    return int(lib().gart_muon_scratch_bytes(int(rows), int(cols), DTYPES[dtype]))
+
+
+def gart_muon_step(param: torch.Tensor, grad: torch.Tensor, m: torch.Tensor, h: gart_muon,
+                   scratch: torch.Tensor | None = None, stream=None):
+    """One orthogonalised momentum step in place on a weight matrix (m, float32, is its momentum); scratch of
+    gart_muon_scratch_bytes(rows, cols, dtype) bytes."""
+    d = _dtype(param)
+    if m.dtype != torch.float32 or m.get_device() != param.get_device():
+        raise ValueError(f"m must be a float32 tensor on {param.device}")
+    mp, mg, mm = _matrix(param, param, "param"), _matrix(grad, param, "grad"), _matrix(m, m, "m")
+    sp, sn = _scratch(scratch, param)
+    _check(lib().gart_muon_step(ctypes.byref(mp), ctypes.byref(mg), ctypes.byref(mm), ctypes.byref(h), d, sp, sn,
+                                _stream_on(stream, param)), "gart_muon_step")
 
 
 def empty_grads(g: Gaussians) -> dict:
