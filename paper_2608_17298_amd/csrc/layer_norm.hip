@@ -9,6 +9,7 @@
 #include <algorithm>
 
 #include "blocks.h"
+#include "linear.h"
 
 namespace gart {
 namespace {
@@ -23,28 +24,325 @@ __device__ __forceinline__ float rsqrt_of(float v) {
   return __builtin_amdgcn_rsqf(small ? v * 0x1p100f : v) * (small ? 0x1p50f : 1.0f);
 }
 
-__device__ __forceinline__ float wave_sum(float v) {
-#pragma unroll
-  for (int off = 32; off > 0; off >>= 1) v += __shfl_xor(v, off);
+// Sums over groups of G neighbouring lanes, the same bits in all of them: each
+// step adds what a lane's partner holds.  Up to 16 lanes the partner's value comes
+// with the addition (DPP: quads, half rows and rows mirrored); halves of 32 and of
+// 64 trade places by the swapping moves.
+template <int CTRL>
+__device__ __forceinline__ float add_dpp(float v) {
+  const int o = __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 0xF, 0xF, true);
+  return v + __builtin_bit_cast(float, o);
+}
+template <int G>
+__device__ __forceinline__ float group_sum(float v) {
+  if constexpr (G >= 2) v = add_dpp<0xB1>(v);    // lanes 1 0 3 2 of each quad
+  if constexpr (G >= 4) v = add_dpp<0x4E>(v);    // lanes 2 3 0 1
+  if constexpr (G >= 8) v = add_dpp<0x141>(v);   // half row mirrored
+  if constexpr (G >= 16) v = add_dpp<0x140>(v);  // row mirrored
+  if constexpr (G >= 32) {
+    const uint32_t w = __builtin_bit_cast(uint32_t, v);
+    const auto p = __builtin_amdgcn_permlane16_swap(w, w, false, false);
+    const uint32_t x = p[0], y = p[1];
+    v = __builtin_bit_cast(float, x) + __builtin_bit_cast(float, y);
+  }
+  if constexpr (G >= 64) {
+    const uint32_t w = __builtin_bit_cast(uint32_t, v);
+    const auto p = __builtin_amdgcn_permlane32_swap(w, w, false, false);
+    const uint32_t x = p[0], y = p[1];
+    v = __builtin_bit_cast(float, x) + __builtin_bit_cast(float, y);
+  }
   return v;
 }
 
 // Sums over the block, the same in every thread; s holds a float per wave and value.
-template <int COUNT>
-__device__ __forceinline__ void block_sums(float (&v)[COUNT], float (*s)[COUNT]) {
+template <int COUNT, int WAVES>
+__device__ __forceinline__ void block_sums(float (&v)[COUNT], float (&s)[WAVES][COUNT]) {
   const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
 #pragma unroll
   for (int q = 0; q < COUNT; ++q) {
-    v[q] = wave_sum(v[q]);
+    v[q] = group_sum<64>(v[q]);
     if (lane == 0) s[wave][q] = v[q];
   }
-  __syncthreads();
+  lds_barrier();
 #pragma unroll
   for (int q = 0; q < COUNT; ++q) {
-    v[q] = 0.0f;
-    for (int w = 0; w < kWaves; ++w) v[q] += s[w][q];
+    v[q] = s[0][q];
+#pragma unroll
+    for (int w = 1; w < WAVES; ++w) v[q] += s[w][q];
   }
-  __syncthreads();
+  lds_barrier();
+}
+
+// ---- rows that registers hold ---------------------------------------------------
+// A row belongs to a group of lanes that hold U packs each, the group's first packs
+// side by side.  The last pack of a row ends with the row and overlaps the one
+// before; what it holds of that counts once (`skip` leading elements do not) and is
+// stored twice with the same value.  Rows shorter than a pack are a lane's.
+enum RowEnd {
+  END_EXACT,  // whole packs, one for each lane
+  END_SHARED,
+  END_TINY
+};
+
+template <typename T, int U, RowEnd END>
+struct RowPacks {
+  static constexpr int V = Pack<T>::N;
+  int at[U], skip[U];
+  int cols;
+  // lanes of the group, and this one's place in it
+  __device__ __forceinline__ RowPacks(int cols, int lanes, int lane) : cols(cols) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int c = (u * lanes + lane) * V;
+      at[u] = END == END_SHARED ? min(c, cols - V) : c;
+      skip[u] = END == END_SHARED ? c - at[u] : 0;
+    }
+  }
+  // Groups with two or three packs a lane are chosen for rows that reach the lanes'
+  // last ones (with_lanes, with_block).
+  static __device__ __forceinline__ constexpr bool full(int u) { return U <= 3 && u < U - 1; }
+  __device__ __forceinline__ bool on(int u) const { return END != END_SHARED || full(u) || skip[u] < V; }
+  __device__ __forceinline__ bool counts(int u, int e) const {
+    return END == END_EXACT || (END == END_SHARED ? full(u) || e >= skip[u] : e < cols);
+  }
+  __device__ __forceinline__ Pack<T> load(const T* row, int u) const {
+    return END == END_TINY ? load_some(row, cols) : load_pack(row + at[u]);
+  }
+  __device__ __forceinline__ void store(T* row, int u, const Pack<T>& p) const {
+    if (END == END_TINY)
+      store_some(row, p, cols);
+    else if (on(u))
+      store_pack(row + at[u], p);
+  }
+  // sum over this lane of f(u, e) where the element counts
+  template <typename F>
+  __device__ __forceinline__ float sum(F&& f) const {
+    float t = 0.0f;
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int e = 0; e < V; ++e) t = counts(u, e) ? f(u, e, t) : t;
+    return t;
+  }
+};
+
+// Mean and 1 / sqrt(var + eps) of a row in registers; SUM adds over its lanes.
+template <typename T, int U, RowEnd END, typename SUM>
+__device__ __forceinline__ float row_mean(const RowPacks<T, U, END>& at, const Pack<T> (&x)[U], float n, SUM&& sum) {
+  return sum(at.sum([&](int u, int e, float t) { return t + float(x[u].v[e]); })) / n;
+}
+
+template <typename T, int G, int U, RowEnd END>
+__global__ __launch_bounds__(kThreads) void rows_kernel(const LayerNormArgs a) {
+  constexpr int V = Pack<T>::N, ROWS = kThreads / G;
+  const RowPacks<T, U, END> at(int(a.cols), G, threadIdx.x % G);
+  const T* gain = static_cast<const T*>(a.gain);
+  const T* bias = static_cast<const T*>(a.bias);
+  Pack<T> g[U], b[U], x[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    if (gain) g[u] = at.load(gain, u);
+    if (bias) b[u] = at.load(bias, u);
+  }
+  const float n = float(a.cols);
+  const int64_t step = int64_t(gridDim.x) * ROWS;
+  int64_t row = int64_t(blockIdx.x) * ROWS + threadIdx.x / G;
+  auto load = [&](int64_t r) {
+    const T* p = static_cast<const T*>(a.x) + min(r, a.rows - 1) * a.x_ld;
+#pragma unroll
+    for (int u = 0; u < U; ++u) x[u] = at.load(p, u);
+  };
+  load(row);
+  for (int64_t first = int64_t(blockIdx.x) * ROWS; first < a.rows; first += step, row += step) {
+    auto sum = [](float v) { return group_sum<G>(v); };
+    const float mean = row_mean(at, x, n, sum);
+    const float var = sum(at.sum([&](int u, int e, float t) {
+      const float d = float(x[u].v[e]) - mean;
+      return fmaf(d, d, t);
+    })) / n;
+    const float rstd = rsqrt_of(var + a.eps);
+    Pack<T> y[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        float h = (float(x[u].v[e]) - mean) * rstd;
+        if (gain) h *= float(g[u].v[e]);
+        if (bias) h += float(b[u].v[e]);
+        y[u].v[e] = T(h);
+      }
+    if (first + step < a.rows) load(row + step);  // before the stores, which it would wait for
+    if (row < a.rows) {
+      T* p = static_cast<T*>(a.y) + row * a.y_ld;
+#pragma unroll
+      for (int u = 0; u < U; ++u) at.store(p, u, y[u]);
+    }
+  }
+}
+
+// A block a row, for rows past what a wave holds.
+template <typename T, int THREADS, int U>
+__global__ __launch_bounds__(THREADS) void block_rows_kernel(const LayerNormArgs a) {
+  constexpr int V = Pack<T>::N;
+  __shared__ float s[2][THREADS / 64][1];
+  const RowPacks<T, U, END_SHARED> at(int(a.cols), THREADS, threadIdx.x);
+  const T* gain = static_cast<const T*>(a.gain);
+  const T* bias = static_cast<const T*>(a.bias);
+  const float n = float(a.cols);
+  for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+    const T* p = static_cast<const T*>(a.x) + row * a.x_ld;
+    Pack<T> x[U], g[U], b[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) x[u] = at.load(p, u);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (gain) g[u] = at.load(gain, u);
+      if (bias) b[u] = at.load(bias, u);
+    }
+    auto sum = [&](float v, int h) {
+      float w[1] = {v};
+      block_sums(w, s[h]);
+      return w[0];
+    };
+    const float mean = row_mean(at, x, n, [&](float v) { return sum(v, 0); });
+    const float var = sum(at.sum([&](int u, int e, float t) {
+      const float d = float(x[u].v[e]) - mean;
+      return fmaf(d, d, t);
+    }), 1) / n;
+    const float rstd = rsqrt_of(var + a.eps);
+    T* q = static_cast<T*>(a.y) + row * a.y_ld;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        float h = (float(x[u].v[e]) - mean) * rstd;
+        if (gain) h *= float(g[u].v[e]);
+        if (bias) h += float(b[u].v[e]);
+        x[u].v[e] = T(h);
+      }
+      at.store(q, u, x[u]);
+    }
+  }
+}
+
+// The gradient: THREADS / G rows at a time, or one of a whole block (G = THREADS).
+// Lanes add dl h and dl of their columns up over the rows that the block takes, and
+// the block leaves its sums in sums[block] = [g_gain, g_bias], or, alone, the result.
+template <typename T, int G, int U, RowEnd END, int THREADS>
+__global__ __launch_bounds__(THREADS) void rows_grad_kernel(const LayerNormArgs a, float* __restrict__ sums) {
+  constexpr int V = Pack<T>::N, ROWS = THREADS / G, WAVES = THREADS / 64;
+  constexpr bool BLOCK = G > 64;
+  __shared__ float s1[BLOCK ? WAVES : 1][1], s3[BLOCK ? WAVES : 1][3];
+  __shared__ float s_join[BLOCK ? 1 : WAVES][BLOCK ? 1 : G * V];
+  const int lane = threadIdx.x % G;
+  const RowPacks<T, U, END> at(int(a.cols), G, lane);
+  const T* gain = static_cast<const T*>(a.gain);
+  Pack<T> g[U], x[U], dl[U];
+  if (gain) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) g[u] = at.load(gain, u);
+  }
+  float g_gain[U][V] = {}, g_bias[U][V] = {};
+  const float n = float(a.cols);
+  const int64_t step = int64_t(gridDim.x) * ROWS;
+  int64_t row = int64_t(blockIdx.x) * ROWS + threadIdx.x / G;
+  auto load = [&](int64_t r) {
+    r = min(r, a.rows - 1);
+    const T* p = static_cast<const T*>(a.x) + r * a.x_ld;
+    const T* q = static_cast<const T*>(a.dl) + r * a.dl_ld;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      x[u] = at.load(p, u);
+      dl[u] = at.load(q, u);
+    }
+  };
+  load(row);
+  for (int64_t first = int64_t(blockIdx.x) * ROWS; first < a.rows; first += step, row += step) {
+    float m[1] = {at.sum([&](int u, int e, float t) { return t + float(x[u].v[e]); })};
+    if constexpr (BLOCK)
+      block_sums(m, s1);
+    else
+      m[0] = group_sum<G>(m[0]);
+    const float mean = m[0] / n;
+    auto weighted = [&](int u, int e) { return gain ? float(dl[u].v[e]) * float(g[u].v[e]) : float(dl[u].v[e]); };
+    float v[3] = {0.0f, 0.0f, 0.0f};  // d^2, w, w d
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        const bool in = at.counts(u, e);
+        const float d = in ? float(x[u].v[e]) - mean : 0.0f, w = in ? weighted(u, e) : 0.0f;
+        v[0] = fmaf(d, d, v[0]);
+        v[1] += w;
+        v[2] = fmaf(w, d, v[2]);
+      }
+    if constexpr (BLOCK) {
+      block_sums(v, s3);
+    } else {
+#pragma unroll
+      for (int q = 0; q < 3; ++q) v[q] = group_sum<G>(v[q]);
+    }
+    const float rstd = rsqrt_of(v[0] / n + a.eps), mw = v[1] / n, along = v[2] / n * rstd;
+    Pack<T> out[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        const float h = (float(x[u].v[e]) - mean) * rstd, w = weighted(u, e);
+        out[u].v[e] = T(rstd * (w - mw - h * along));
+        if (row < a.rows) {
+          g_gain[u][e] = fmaf(float(dl[u].v[e]), h, g_gain[u][e]);
+          g_bias[u][e] += float(dl[u].v[e]);
+        }
+      }
+    if (first + step < a.rows) load(row + step);  // before the stores, which it would wait for
+    if (a.g_x && row < a.rows) {
+      T* p = static_cast<T*>(a.g_x) + row * a.g_x_ld;
+#pragma unroll
+      for (int u = 0; u < U; ++u) at.store(p, u, out[u]);
+    }
+  }
+
+  auto put = [&](int which, int64_t c, float t) {
+    T* result = static_cast<T*>(which ? a.g_bias : a.g_gain);
+    if (!result) return;
+    if (gridDim.x == 1)
+      result[c] = T(t);
+    else
+      sums[(int64_t(blockIdx.x) * 2 + which) * a.cols + c] = t;
+  };
+#pragma unroll
+  for (int which = 0; which < 2; ++which)
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        float t = which ? g_bias[u][e] : g_gain[u][e];
+        if constexpr (BLOCK) {
+          if (at.on(u) && at.counts(u, e)) put(which, at.at[u] + e, t);
+        } else {
+#pragma unroll
+          for (int off = G; off < 64; off <<= 1) t += __shfl_xor(t, off);
+          if (threadIdx.x % 64 < G) s_join[threadIdx.x / 64][lane * V + e] = t;
+        }
+      }
+      if constexpr (!BLOCK) {
+        __syncthreads();
+        for (int c = threadIdx.x; c < G * V; c += THREADS) {
+          const int col = u * G * V + c;  // packs that end with the row hold it further back
+          const int l = c / V, shared = END == END_SHARED ? max(0, (u * G + l) * V - (int(a.cols) - V)) : 0;
+          if (shared >= V) continue;
+          const int e = c % V;
+          const bool in = END == END_TINY ? e < a.cols : e >= shared;
+          if (!in) continue;
+          float t = s_join[0][c];
+#pragma unroll
+          for (int w = 1; w < WAVES; ++w) t += s_join[w][c];
+          put(which, col - shared, t);
+        }
+        __syncthreads();
+      }
+    }
 }
 
 // ---- rows of any length: a block a row, read once for each sum -----------------
@@ -55,7 +353,7 @@ __device__ __forceinline__ void for_packs(int64_t cols, F&& f) {
 }
 
 template <typename T>
-__device__ __forceinline__ float row_mean(const T* x, int64_t cols, float (*s)[1]) {
+__device__ __forceinline__ float row_mean(const T* x, int64_t cols, float (&s)[kWaves][1]) {
   float v[1] = {0.0f};
   for_packs<T>(cols, [&](int64_t c, int count) {
     const Pack<T> p = load_some(x + c, count);
@@ -170,39 +468,135 @@ __global__ __launch_bounds__(kThreads) void column_grads_kernel(const LayerNormA
   }
 }
 
-// g_gain and g_bias (either may be NULL) from the parts' sums
-constexpr int kJoinWaves = 16;
+// g_gain and g_bias (either may be NULL) from the parts' sums: a block takes 16
+// neighbouring sums, and its 64 groups of 16 lanes every 64th part.
+constexpr int kJoinThreads = 1024, kJoinCols = 16, kJoinRows = kJoinThreads / kJoinCols;
 template <typename T>
-__global__ __launch_bounds__(64 * kJoinWaves) void join_column_grads_kernel(const float* __restrict__ sums,
-                                                                            int64_t parts, int64_t cols,
-                                                                            T* __restrict__ g_gain,
-                                                                            T* __restrict__ g_bias) {
-  __shared__ float s[kJoinWaves][64];
-  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-  for (int64_t b = int64_t(blockIdx.x) * 64; b < 2 * cols; b += int64_t(gridDim.x) * 64) {
-    const int64_t e = b + lane;
+__global__ __launch_bounds__(kJoinThreads) void join_column_grads_kernel(const float* __restrict__ sums,
+                                                                         int64_t parts, int64_t cols,
+                                                                         T* __restrict__ g_gain,
+                                                                         T* __restrict__ g_bias) {
+  __shared__ float s[kJoinRows][kJoinCols + 1];
+  const int c = threadIdx.x % kJoinCols, r = threadIdx.x / kJoinCols;
+  for (int64_t b = int64_t(blockIdx.x) * kJoinCols; b < 2 * cols; b += int64_t(gridDim.x) * kJoinCols) {
+    const int64_t e = b + c;
     T* to = e < cols ? g_gain : g_bias;
     float t = 0.0f;
-    if (e < 2 * cols && to)
-      for (int64_t p = wave; p < parts; p += kJoinWaves) t += sums[p * 2 * cols + e];
-    s[wave][lane] = t;
-    __syncthreads();
-    if (wave == 0 && e < 2 * cols && to) {
-#pragma unroll
-      for (int w = 1; w < kJoinWaves; ++w) t += s[w][lane];
-      to[e < cols ? e : e - cols] = T(t);
+    if (e < 2 * cols && to) {
+#pragma unroll 8
+      for (int64_t p = r; p < parts; p += kJoinRows) t += sums[p * 2 * cols + e];
     }
+    s[r][c] = t;
+    __syncthreads();
+    static_assert(kJoinThreads / 64 == kJoinCols && kJoinRows == 64, "a wave a column");
+    const int col = threadIdx.x / 64, at = threadIdx.x % 64;
+    const float v = group_sum<64>(s[at][col]);
+    const int64_t o = b + col;
+    T* out = o < cols ? g_gain : g_bias;
+    if (at == 0 && o < 2 * cols && out) out[o < cols ? o : o - cols] = T(v);
     __syncthreads();
   }
 }
 
-constexpr int64_t kPartRows = 256, kMaxParts = 512;
+// f(integral constants G, U) for rows of `packs` packs: a wave's lanes up to 128 of
+// them, with as few idle ones as two or three packs a lane allow (200000 x 130 f16,
+// 17 packs: 30 us with 32 lanes, 22 with three packs in each of 8).
+template <int N>
+using Int = std::integral_constant<int, N>;
+template <typename F>
+void with_lanes(int64_t packs, F&& f) {
+  if (packs <= 1) return f(Int<1>{}, Int<1>{});
+  if (packs <= 2) return f(Int<2>{}, Int<1>{});
+  if (packs <= 4) return f(Int<4>{}, Int<1>{});
+  if (packs <= 8) return f(Int<8>{}, Int<1>{});
+  if (packs <= 12) return f(Int<4>{}, Int<3>{});
+  if (packs <= 16) return f(Int<16>{}, Int<1>{});
+  if (packs <= 24) return f(Int<8>{}, Int<3>{});
+  if (packs <= 32) return f(Int<32>{}, Int<1>{});
+  if (packs <= 48) return f(Int<16>{}, Int<3>{});
+  if (packs <= 64) return f(Int<64>{}, Int<1>{});
+  if (packs <= 96) return f(Int<32>{}, Int<3>{});
+  f(Int<64>{}, Int<2>{});
+}
+// f(threads, packs a thread) for longer rows, up to 8192 packs
+template <typename F>
+void with_block(int64_t packs, F&& f) {
+  if (packs <= 256) return f(Int<256>{}, Int<1>{});
+  if (packs <= 512) return f(Int<256>{}, Int<2>{});
+  if (packs <= 1024) return f(Int<256>{}, Int<4>{});
+  if (packs <= 2048) return f(Int<256>{}, Int<8>{});
+  if (packs <= 4096) return f(Int<512>{}, Int<8>{});
+  f(Int<1024>{}, Int<8>{});
+}
+constexpr int64_t kWavePacks = 128, kBlockPacks = 8192;
+constexpr int64_t kRowBlocks = 256 * 16;  // blocks that walk over the rows
+
+template <typename T>
+hipError_t forward(const LayerNormArgs& a, hipStream_t s) {
+  if (a.rows <= 0 || a.cols <= 0) return hipSuccess;
+  constexpr int V = Pack<T>::N;
+  const int64_t packs = ceil_div64(a.cols, V);
+  if (packs <= kWavePacks) {
+    with_lanes(packs, [&](auto g, auto u) {
+      constexpr int G = decltype(g)::value, U = decltype(u)::value;
+      const uint32_t grid = uint32_t(std::min(ceil_div64(a.rows * G, kThreads), kRowBlocks));
+      if (a.cols < V) {
+        if constexpr (G == 1) rows_kernel<T, 1, 1, END_TINY><<<grid, kThreads, 0, s>>>(a);
+      } else if (a.cols == G * U * V) {
+        rows_kernel<T, G, U, END_EXACT><<<grid, kThreads, 0, s>>>(a);
+      } else {
+        rows_kernel<T, G, U, END_SHARED><<<grid, kThreads, 0, s>>>(a);
+      }
+    });
+    return hipGetLastError();
+  }
+  if (packs <= kBlockPacks) {
+    const uint32_t grid = uint32_t(std::min(a.rows, kMaxBlocks));
+    with_block(packs, [&](auto t, auto u) {
+      constexpr int THREADS = decltype(t)::value;
+      block_rows_kernel<T, THREADS, decltype(u)::value><<<grid, THREADS, 0, s>>>(a);
+    });
+    return hipGetLastError();
+  }
+  long_rows_kernel<T><<<uint32_t(std::min(a.rows, kMaxBlocks)), kThreads, 0, s>>>(a);
+  return hipGetLastError();
+}
+
+// The gradient's blocks: as above with eight waves, and for longer rows as many
+// threads as leave two packs a lane (four of float32), whose column sums still fit.
+constexpr int kGradThreads = 512;
+template <int V, typename F>
+void with_grad_block(int64_t packs, F&& f) {
+  if (packs <= 256) return f(Int<256>{}, Int<1>{});
+  if (packs <= 512) return f(Int<256>{}, Int<2>{});
+  if (packs <= 1024) return f(Int<512>{}, Int<2>{});
+  if (V == 8 || packs <= 2048) return f(Int<1024>{}, Int<2>{});
+  if constexpr (V == 4) f(Int<1024>{}, Int<4>{});
+}
+
 struct Plan {
-  int64_t part, parts;
+  bool fused;      // one kernel for rows and column sums
+  int64_t parts;   // of the rows, that leave column sums
+  int64_t part;    // rows of a part (not fused)
   size_t stats, total;
 };
-Plan plan_of(int64_t rows, int64_t cols) {
+constexpr int64_t kPartRows = 256, kMaxParts = 512;
+Plan plan_of(int64_t rows, int64_t cols, int64_t es) {
   Plan p{};
+  const int64_t V = 16 / es, packs = ceil_div64(cols, V);
+  p.fused = cols <= 16384;
+  if (p.fused) {
+    int64_t at_once = 1;  // rows a block takes at a time
+    if (packs <= kWavePacks) with_lanes(packs, [&](auto g, auto) { at_once = kGradThreads / decltype(g)::value; });
+    const int64_t turns = ceil_div64(rows, at_once);
+    // A block alone spares the second launch.  Else parts as many as fill the card, as
+    // long as their sums stay an eighth of the rows, or each has four turns left.
+    const int64_t most = std::max(rows * es / 43, turns / 4);
+    p.parts = turns <= 4 ? 1 : std::min({most, turns, kMaxParts});
+    p.stats = p.parts > 1 ? size_t(ceil_div64(p.parts * 2 * cols * 4, 16)) * 16 : 0;
+    p.total = p.stats;
+    return p;
+  }
   p.part = std::max(kPartRows, ceil_div64(rows, kMaxParts));
   p.parts = ceil_div64(rows, p.part);
   p.stats = size_t(ceil_div64(p.parts * 2 * cols * 4, 16)) * 16;
@@ -211,42 +605,63 @@ Plan plan_of(int64_t rows, int64_t cols) {
 }
 
 template <typename T>
-hipError_t forward(const LayerNormArgs& a, hipStream_t s) {
-  if (a.rows <= 0 || a.cols <= 0) return hipSuccess;
-  long_rows_kernel<T><<<uint32_t(std::min(a.rows, kMaxBlocks)), kThreads, 0, s>>>(a);
+hipError_t rows_grad(const LayerNormArgs& a, const Plan& p, float* sums, hipStream_t s) {
+  constexpr int V = Pack<T>::N;
+  const int64_t packs = ceil_div64(a.cols, V);
+  const uint32_t grid = uint32_t(p.parts);
+  if (packs <= kWavePacks)
+    with_lanes(packs, [&](auto g, auto u) {
+      constexpr int G = decltype(g)::value, U = decltype(u)::value;
+      if (a.cols < V) {
+        if constexpr (G == 1) rows_grad_kernel<T, 1, 1, END_TINY, kGradThreads><<<grid, kGradThreads, 0, s>>>(a, sums);
+      } else if (a.cols == G * U * V) {
+        rows_grad_kernel<T, G, U, END_EXACT, kGradThreads><<<grid, kGradThreads, 0, s>>>(a, sums);
+      } else {
+        rows_grad_kernel<T, G, U, END_SHARED, kGradThreads><<<grid, kGradThreads, 0, s>>>(a, sums);
+      }
+    });
+  else
+    with_grad_block<V>(packs, [&](auto t, auto u) {
+      constexpr int THREADS = decltype(t)::value;
+      rows_grad_kernel<T, THREADS, decltype(u)::value, END_SHARED, THREADS><<<grid, THREADS, 0, s>>>(a, sums);
+    });
   return hipGetLastError();
 }
 
 template <typename T>
 hipError_t backward(const LayerNormArgs& a, hipStream_t s) {
   if (a.cols <= 0) return hipSuccess;
-  const Plan p = plan_of(a.rows, a.cols);
+  const Plan p = plan_of(a.rows, a.cols, sizeof(T));
   const bool columns = a.g_gain || a.g_bias;
   float* sums = static_cast<float*>(a.scratch);
-  float2* stats = reinterpret_cast<float2*>(static_cast<char*>(a.scratch) + p.stats);
   hipError_t e = hipSuccess;
   if (a.rows > 0 && (a.g_x || columns)) {
-    long_rows_grad_kernel<T><<<uint32_t(std::min(a.rows, kMaxBlocks)), kThreads, 0, s>>>(a, columns ? stats : nullptr);
-    if ((e = hipGetLastError()) != hipSuccess) return e;
+    if (p.fused) {
+      if ((e = rows_grad<T>(a, p, sums, s)) != hipSuccess || p.parts == 1) return e;
+    } else {
+      float2* stats = reinterpret_cast<float2*>(static_cast<char*>(a.scratch) + p.stats);
+      const uint32_t grid = uint32_t(std::min(a.rows, kMaxBlocks));
+      long_rows_grad_kernel<T><<<grid, kThreads, 0, s>>>(a, columns ? stats : nullptr);
+      if ((e = hipGetLastError()) != hipSuccess) return e;
+      if (columns) {
+        const dim3 parts(uint32_t(p.parts), uint32_t(std::min<int64_t>(ceil_div64(a.cols, 64), 65535)));
+        column_grads_kernel<T><<<parts, kThreads, 0, s>>>(a, stats, p.part, sums);
+        if ((e = hipGetLastError()) != hipSuccess) return e;
+      }
+    }
   }
   if (!columns) return e;
-  const int64_t groups = ceil_div64(a.cols, 64);
-  if (p.parts > 0) {
-    const dim3 grid(uint32_t(p.parts), uint32_t(std::min<int64_t>(groups, 65535)));
-    column_grads_kernel<T><<<grid, kThreads, 0, s>>>(a, stats, p.part, sums);
-    if ((e = hipGetLastError()) != hipSuccess) return e;
-  }
-  const int64_t blocks = std::min<int64_t>(ceil_div64(2 * a.cols, 64), 1 << 16);
-  join_column_grads_kernel<T><<<uint32_t(blocks), 64 * kJoinWaves, 0, s>>>(
-      sums, p.parts, a.cols, static_cast<T*>(a.g_gain), static_cast<T*>(a.g_bias));
+  const int64_t blocks = std::min<int64_t>(ceil_div64(2 * a.cols, kJoinCols), 1 << 16);
+  join_column_grads_kernel<T><<<uint32_t(blocks), kJoinThreads, 0, s>>>(
+      sums, a.rows > 0 ? p.parts : 0, a.cols, static_cast<T*>(a.g_gain), static_cast<T*>(a.g_bias));
   return hipGetLastError();
 }
 
 }  // namespace
 
-size_t layer_norm_backward_scratch_bytes(int64_t rows, int64_t cols, gart_dtype) {
+size_t layer_norm_backward_scratch_bytes(int64_t rows, int64_t cols, gart_dtype t) {
   if (rows <= 0 || cols <= 0) return 0;
-  return plan_of(rows, cols).total;
+  return plan_of(rows, cols, int64_t(dtype_bytes(t))).total;
 }
 
 hipError_t launch_layer_norm(const LayerNormArgs& a, gart_dtype t, hipStream_t s) {

@@ -374,7 +374,7 @@ def test_refusals_on_tensors():
             f()
     worse = [lambda: gart.gart_layer_norm(x, y[:3]), lambda: gart.gart_layer_norm(x, y, eps=-1.0),
              lambda: gart.gart_layer_norm(x[1:], x[:3]), lambda: gart.gart_layer_norm(x, y[:1].expand(4, 8)),
-             lambda: gart.gart_layer_norm_backward(x, x, y), lambda: gart.gart_layer_norm_backward(x, y[:3])]
+             lambda: gart.gart_layer_norm_backward(x, y, x), lambda: gart.gart_layer_norm_backward(x, y[:3])]
     for f in worse:
         with pytest.raises(gart.GartError):
             f()
