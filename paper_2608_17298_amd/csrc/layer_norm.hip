@@ -24,6 +24,18 @@ __device__ __forceinline__ float rsqrt_of(float v) {
   return __builtin_amdgcn_rsqf(small ? v * 0x1p100f : v) * (small ? 0x1p50f : 1.0f);
 }
 
+// s / n by n's reciprocal, the quotient set right by its own remainder: exact where
+// it is a float, as the mean of a row of one value has to be, in a fourth of the
+// division's instructions.  An infinite s stays.
+struct Count {
+  float n, inv;
+  __device__ __forceinline__ explicit Count(int64_t c) : n(float(c)), inv(1.0f / float(c)) {}
+  __device__ __forceinline__ float mean(float s) const {
+    const float q = s * inv, r = fmaf(-q, n, s);
+    return r == r ? fmaf(r, inv, q) : q;
+  }
+};
+
 // Sums over groups of G neighbouring lanes, the same bits in all of them: each
 // step adds what a lane's partner holds.  Up to 16 lanes the partner's value comes
 // with the addition (DPP: quads, half rows and rows mirrored); halves of 32 and of
@@ -76,7 +88,8 @@ __device__ __forceinline__ void block_sums(float (&v)[COUNT], float (&s)[WAVES][
 // ---- rows that registers hold ---------------------------------------------------
 // A row belongs to a group of lanes that hold U packs each, the group's first packs
 // side by side.  The last pack of a row ends with the row and overlaps the one
-// before; what it holds of that counts once (`skip` leading elements do not) and is
+// before; what it holds of that counts once (`skip` leading elements do not, by a
+// weight of 0: they are the row's, so a NaN among them is the row's as well) and is
 // stored twice with the same value.  Rows shorter than a pack are a lane's.
 enum RowEnd {
   END_EXACT,  // whole packs, one for each lane
@@ -89,6 +102,7 @@ struct RowPacks {
   static constexpr int V = Pack<T>::N;
   int at[U], skip[U];
   int cols;
+  float weight[U][V];  // of the packs that may not be full
   // lanes of the group, and this one's place in it
   __device__ __forceinline__ RowPacks(int cols, int lanes, int lane) : cols(cols) {
 #pragma unroll
@@ -96,14 +110,22 @@ struct RowPacks {
       const int c = (u * lanes + lane) * V;
       at[u] = END == END_SHARED ? min(c, cols - V) : c;
       skip[u] = END == END_SHARED ? c - at[u] : 0;
+#pragma unroll
+      for (int e = 0; e < V; ++e) weight[u][e] = (END == END_TINY ? e < cols : e >= skip[u]) ? 1.0f : 0.0f;
     }
   }
   // Groups with two or three packs a lane are chosen for rows that reach the lanes'
   // last ones (with_lanes, with_block).
-  static __device__ __forceinline__ constexpr bool full(int u) { return U <= 3 && u < U - 1; }
+  static __device__ __forceinline__ constexpr bool full(int u) {
+    return END == END_EXACT || (END == END_SHARED && U <= 3 && u < U - 1);
+  }
   __device__ __forceinline__ bool on(int u) const { return END != END_SHARED || full(u) || skip[u] < V; }
   __device__ __forceinline__ bool counts(int u, int e) const {
-    return END == END_EXACT || (END == END_SHARED ? full(u) || e >= skip[u] : e < cols);
+    return full(u) || (END == END_SHARED ? e >= skip[u] : e < cols);
+  }
+  __device__ __forceinline__ float weighed(int u, int e, float v) const { return full(u) ? v : v * weight[u][e]; }
+  __device__ __forceinline__ float add(int u, int e, float v, float t) const {
+    return full(u) ? t + v : fmaf(v, weight[u][e], t);
   }
   __device__ __forceinline__ Pack<T> load(const T* row, int u) const {
     return END == END_TINY ? load_some(row, cols) : load_pack(row + at[u]);
@@ -114,37 +136,48 @@ struct RowPacks {
     else if (on(u))
       store_pack(row + at[u], p);
   }
-  // sum over this lane of f(u, e) where the element counts
-  template <typename F>
-  __device__ __forceinline__ float sum(F&& f) const {
+  // gain or bias, or `none` in its place: a choice for each element would cost more than its product
+  __device__ __forceinline__ void load_or(Pack<T> (&p)[U], const T* from, float none) const {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (from)
+        p[u] = load(from, u);
+      else
+        p[u].v = T(none);
+    }
+  }
+  // this lane's sums of the elements, and of their squared distances from the mean
+  __device__ __forceinline__ float sum(const Pack<T> (&x)[U]) const {
     float t = 0.0f;
 #pragma unroll
     for (int u = 0; u < U; ++u)
 #pragma unroll
-      for (int e = 0; e < V; ++e) t = counts(u, e) ? f(u, e, t) : t;
+      for (int e = 0; e < V; ++e) t = add(u, e, float(x[u].v[e]), t);
+    return t;
+  }
+  __device__ __forceinline__ float squares(const Pack<T> (&x)[U], float mean) const {
+    float t = 0.0f;
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        const float d = float(x[u].v[e]) - mean;
+        t = fmaf(weighed(u, e, d), d, t);
+      }
     return t;
   }
 };
 
-// Mean and 1 / sqrt(var + eps) of a row in registers; SUM adds over its lanes.
-template <typename T, int U, RowEnd END, typename SUM>
-__device__ __forceinline__ float row_mean(const RowPacks<T, U, END>& at, const Pack<T> (&x)[U], float n, SUM&& sum) {
-  return sum(at.sum([&](int u, int e, float t) { return t + float(x[u].v[e]); })) / n;
-}
-
 template <typename T, int G, int U, RowEnd END>
-__global__ __launch_bounds__(kThreads) void rows_kernel(const LayerNormArgs a) {
+__global__ __launch_bounds__(kThreads, U == 1 ? 8 : 3) void rows_kernel(const LayerNormArgs a) {
   constexpr int V = Pack<T>::N, ROWS = kThreads / G;
   const RowPacks<T, U, END> at(int(a.cols), G, threadIdx.x % G);
   const T* gain = static_cast<const T*>(a.gain);
   const T* bias = static_cast<const T*>(a.bias);
   Pack<T> g[U], b[U], x[U];
-#pragma unroll
-  for (int u = 0; u < U; ++u) {
-    if (gain) g[u] = at.load(gain, u);
-    if (bias) b[u] = at.load(bias, u);
-  }
-  const float n = float(a.cols);
+  at.load_or(g, gain, 1.0f);
+  at.load_or(b, bias, 0.0f);
+  const Count n(a.cols);
   const int64_t step = int64_t(gridDim.x) * ROWS;
   int64_t row = int64_t(blockIdx.x) * ROWS + threadIdx.x / G;
   auto load = [&](int64_t r) {
@@ -154,22 +187,15 @@ __global__ __launch_bounds__(kThreads) void rows_kernel(const LayerNormArgs a) {
   };
   load(row);
   for (int64_t first = int64_t(blockIdx.x) * ROWS; first < a.rows; first += step, row += step) {
-    auto sum = [](float v) { return group_sum<G>(v); };
-    const float mean = row_mean(at, x, n, sum);
-    const float var = sum(at.sum([&](int u, int e, float t) {
-      const float d = float(x[u].v[e]) - mean;
-      return fmaf(d, d, t);
-    })) / n;
-    const float rstd = rsqrt_of(var + a.eps);
+    const float mean = n.mean(group_sum<G>(at.sum(x)));
+    const float rstd = rsqrt_of(n.mean(group_sum<G>(at.squares(x, mean))) + a.eps);
     Pack<T> y[U];
 #pragma unroll
     for (int u = 0; u < U; ++u)
 #pragma unroll
       for (int e = 0; e < V; ++e) {
-        float h = (float(x[u].v[e]) - mean) * rstd;
-        if (gain) h *= float(g[u].v[e]);
-        if (bias) h += float(b[u].v[e]);
-        y[u].v[e] = T(h);
+        const float h = (float(x[u].v[e]) - mean) * rstd;
+        y[u].v[e] = T(fmaf(h, float(g[u].v[e]), float(b[u].v[e])));
       }
     if (first + step < a.rows) load(row + step);  // before the stores, which it would wait for
     if (row < a.rows) {
@@ -188,37 +214,28 @@ __global__ __launch_bounds__(THREADS) void block_rows_kernel(const LayerNormArgs
   const RowPacks<T, U, END_SHARED> at(int(a.cols), THREADS, threadIdx.x);
   const T* gain = static_cast<const T*>(a.gain);
   const T* bias = static_cast<const T*>(a.bias);
-  const float n = float(a.cols);
+  const Count n(a.cols);
   for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
     const T* p = static_cast<const T*>(a.x) + row * a.x_ld;
     Pack<T> x[U], g[U], b[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) x[u] = at.load(p, u);
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      if (gain) g[u] = at.load(gain, u);
-      if (bias) b[u] = at.load(bias, u);
-    }
+    at.load_or(g, gain, 1.0f);
+    at.load_or(b, bias, 0.0f);
     auto sum = [&](float v, int h) {
       float w[1] = {v};
       block_sums(w, s[h]);
       return w[0];
     };
-    const float mean = row_mean(at, x, n, [&](float v) { return sum(v, 0); });
-    const float var = sum(at.sum([&](int u, int e, float t) {
-      const float d = float(x[u].v[e]) - mean;
-      return fmaf(d, d, t);
-    }), 1) / n;
-    const float rstd = rsqrt_of(var + a.eps);
+    const float mean = n.mean(sum(at.sum(x), 0));
+    const float rstd = rsqrt_of(n.mean(sum(at.squares(x, mean), 1)) + a.eps);
     T* q = static_cast<T*>(a.y) + row * a.y_ld;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
 #pragma unroll
       for (int e = 0; e < V; ++e) {
-        float h = (float(x[u].v[e]) - mean) * rstd;
-        if (gain) h *= float(g[u].v[e]);
-        if (bias) h += float(b[u].v[e]);
-        x[u].v[e] = T(h);
+        const float h = (float(x[u].v[e]) - mean) * rstd;
+        x[u].v[e] = T(fmaf(h, float(g[u].v[e]), float(b[u].v[e])));
       }
       at.store(q, u, x[u]);
     }
@@ -238,12 +255,9 @@ __global__ __launch_bounds__(THREADS) void rows_grad_kernel(const LayerNormArgs 
   const RowPacks<T, U, END> at(int(a.cols), G, lane);
   const T* gain = static_cast<const T*>(a.gain);
   Pack<T> g[U], x[U], dl[U];
-  if (gain) {
-#pragma unroll
-    for (int u = 0; u < U; ++u) g[u] = at.load(gain, u);
-  }
+  at.load_or(g, gain, 1.0f);
   float g_gain[U][V] = {}, g_bias[U][V] = {};
-  const float n = float(a.cols);
+  const Count n(a.cols);
   const int64_t step = int64_t(gridDim.x) * ROWS;
   int64_t row = int64_t(blockIdx.x) * ROWS + threadIdx.x / G;
   auto load = [&](int64_t r) {
@@ -258,21 +272,33 @@ __global__ __launch_bounds__(THREADS) void rows_grad_kernel(const LayerNormArgs 
   };
   load(row);
   for (int64_t first = int64_t(blockIdx.x) * ROWS; first < a.rows; first += step, row += step) {
-    float m[1] = {at.sum([&](int u, int e, float t) { return t + float(x[u].v[e]); })};
+    float m[1] = {at.sum(x)};
     if constexpr (BLOCK)
       block_sums(m, s1);
     else
       m[0] = group_sum<G>(m[0]);
-    const float mean = m[0] / n;
-    auto weighted = [&](int u, int e) { return gain ? float(dl[u].v[e]) * float(g[u].v[e]) : float(dl[u].v[e]); };
+    const float mean = n.mean(m[0]);
+    // With more than eight elements a lane, packs are converted again where they are
+    // used: kept as floats through the sums they would take too many registers.
+    auto renew = [&]() {
+      if constexpr (sizeof(T) == 2 && U > 1) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          arrive(x[u].v);
+          arrive(dl[u].v);
+          arrive(g[u].v);
+        }
+      }
+    };
+    renew();
+    auto weighted = [&](int u, int e) { return float(dl[u].v[e]) * float(g[u].v[e]); };
     float v[3] = {0.0f, 0.0f, 0.0f};  // d^2, w, w d
 #pragma unroll
     for (int u = 0; u < U; ++u)
 #pragma unroll
       for (int e = 0; e < V; ++e) {
-        const bool in = at.counts(u, e);
-        const float d = in ? float(x[u].v[e]) - mean : 0.0f, w = in ? weighted(u, e) : 0.0f;
-        v[0] = fmaf(d, d, v[0]);
+        const float d = float(x[u].v[e]) - mean, w = at.weighed(u, e, weighted(u, e));
+        v[0] = fmaf(at.weighed(u, e, d), d, v[0]);
         v[1] += w;
         v[2] = fmaf(w, d, v[2]);
       }
@@ -282,21 +308,22 @@ __global__ __launch_bounds__(THREADS) void rows_grad_kernel(const LayerNormArgs 
 #pragma unroll
       for (int q = 0; q < 3; ++q) v[q] = group_sum<G>(v[q]);
     }
-    const float rstd = rsqrt_of(v[0] / n + a.eps), mw = v[1] / n, along = v[2] / n * rstd;
+    const float rstd = rsqrt_of(n.mean(v[0]) + a.eps), mw = n.mean(v[1]), along = n.mean(v[2]) * rstd;
+    renew();
     Pack<T> out[U];
+    if (BLOCK || row < a.rows) {
 #pragma unroll
-    for (int u = 0; u < U; ++u)
+      for (int u = 0; u < U; ++u)
 #pragma unroll
-      for (int e = 0; e < V; ++e) {
-        const float h = (float(x[u].v[e]) - mean) * rstd, w = weighted(u, e);
-        out[u].v[e] = T(rstd * (w - mw - h * along));
-        if (row < a.rows) {
-          g_gain[u][e] = fmaf(float(dl[u].v[e]), h, g_gain[u][e]);
-          g_bias[u][e] += float(dl[u].v[e]);
+        for (int e = 0; e < V; ++e) {
+          const float h = (float(x[u].v[e]) - mean) * rstd, y = float(dl[u].v[e]);
+          out[u].v[e] = T(rstd * fmaf(-h, along, weighted(u, e) - mw));
+          g_gain[u][e] = fmaf(y, h, g_gain[u][e]);
+          g_bias[u][e] += y;
         }
-      }
+    }
     if (first + step < a.rows) load(row + step);  // before the stores, which it would wait for
-    if (a.g_x && row < a.rows) {
+    if (a.g_x && (BLOCK || row < a.rows)) {
       T* p = static_cast<T*>(a.g_x) + row * a.g_x_ld;
 #pragma unroll
       for (int u = 0; u < U; ++u) at.store(p, u, out[u]);
@@ -441,30 +468,39 @@ __global__ __launch_bounds__(kThreads) void long_rows_grad_kernel(const LayerNor
   }
 }
 
-// Sums over one part of the rows, for 64 columns a block: sums[part] = [g_gain, g_bias]
+// Sums over one part of the rows, for 64 packs of columns a block: sums[part] = [g_gain, g_bias]
 template <typename T>
 __global__ __launch_bounds__(kThreads) void column_grads_kernel(const LayerNormArgs a, const float2* __restrict__ stats,
                                                                 int64_t part, float* __restrict__ sums) {
-  __shared__ float s[kWaves][2][64];
+  constexpr int V = Pack<T>::N;
+  __shared__ float s[kWaves][64 * V];
   const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
   const int64_t r0 = int64_t(blockIdx.x) * part, r1 = min(a.rows, r0 + part);
-  for (int64_t j0 = int64_t(blockIdx.y) * 64; j0 < a.cols; j0 += int64_t(gridDim.y) * 64) {
-    const int64_t j = j0 + lane;
-    float gain = 0.0f, bias = 0.0f;
-    if (j < a.cols)
+  for (int64_t j0 = int64_t(blockIdx.y) * 64 * V; j0 < a.cols; j0 += int64_t(gridDim.y) * 64 * V) {
+    const int64_t j = j0 + lane * V;
+    const int count = int(max(int64_t(0), min(int64_t(V), a.cols - j)));
+    float gain[V] = {}, bias[V] = {};
+    if (count > 0)
       for (int64_t r = r0 + wave; r < r1; r += kWaves) {
-        const float dl = float(static_cast<const T*>(a.dl)[r * a.dl_ld + j]);
+        const Pack<T> x = load_some(static_cast<const T*>(a.x) + r * a.x_ld + j, count);
+        const Pack<T> dl = load_some(static_cast<const T*>(a.dl) + r * a.dl_ld + j, count);
         const float2 st = stats[r];
-        gain = fmaf(dl, (float(static_cast<const T*>(a.x)[r * a.x_ld + j]) - st.x) * st.y, gain);
-        bias += dl;
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          gain[e] = fmaf(float(dl.v[e]), (float(x.v[e]) - st.x) * st.y, gain[e]);
+          bias[e] += float(dl.v[e]);
+        }
       }
-    s[wave][0][lane] = gain;
-    s[wave][1][lane] = bias;
-    __syncthreads();
-    if (wave < 2 && j < a.cols)
-      sums[(int64_t(blockIdx.x) * 2 + wave) * a.cols + j] =
-          (s[0][wave][lane] + s[1][wave][lane]) + (s[2][wave][lane] + s[3][wave][lane]);
-    __syncthreads();
+#pragma unroll
+    for (int which = 0; which < 2; ++which) {
+#pragma unroll
+      for (int e = 0; e < V; ++e) s[wave][lane * V + e] = which ? bias[e] : gain[e];
+      __syncthreads();
+      for (int c = threadIdx.x; c < 64 * V; c += kThreads)
+        if (j0 + c < a.cols)
+          sums[(int64_t(blockIdx.x) * 2 + which) * a.cols + j0 + c] = (s[0][c] + s[1][c]) + (s[2][c] + s[3][c]);
+      __syncthreads();
+    }
   }
 }
 
@@ -518,17 +554,16 @@ void with_lanes(int64_t packs, F&& f) {
   if (packs <= 96) return f(Int<32>{}, Int<3>{});
   f(Int<64>{}, Int<2>{});
 }
-// f(threads, packs a thread) for longer rows, up to 8192 packs
+// f(threads, packs a thread) for longer rows, up to 4096 packs
 template <typename F>
 void with_block(int64_t packs, F&& f) {
   if (packs <= 256) return f(Int<256>{}, Int<1>{});
   if (packs <= 512) return f(Int<256>{}, Int<2>{});
   if (packs <= 1024) return f(Int<256>{}, Int<4>{});
   if (packs <= 2048) return f(Int<256>{}, Int<8>{});
-  if (packs <= 4096) return f(Int<512>{}, Int<8>{});
-  f(Int<1024>{}, Int<8>{});
+  f(Int<512>{}, Int<8>{});
 }
-constexpr int64_t kWavePacks = 128, kBlockPacks = 8192;
+constexpr int64_t kWavePacks = 128, kBlockPacks = 4096;
 constexpr int64_t kRowBlocks = 256 * 16;  // blocks that walk over the rows
 
 template <typename T>
@@ -562,16 +597,28 @@ hipError_t forward(const LayerNormArgs& a, hipStream_t s) {
   return hipGetLastError();
 }
 
-// The gradient's blocks: as above with eight waves, and for longer rows as many
-// threads as leave two packs a lane (four of float32), whose column sums still fit.
+// The gradient's lanes and blocks: two packs a lane at most, whose column sums and
+// copies still fit the registers of four waves a SIMD.
 constexpr int kGradThreads = 512;
-template <int V, typename F>
+template <typename F>
+void with_grad_lanes(int64_t packs, F&& f) {
+  if (packs <= 1) return f(Int<1>{}, Int<1>{});
+  if (packs <= 2) return f(Int<2>{}, Int<1>{});
+  if (packs <= 4) return f(Int<4>{}, Int<1>{});
+  if (packs <= 8) return f(Int<8>{}, Int<1>{});
+  if (packs <= 16) return f(Int<16>{}, Int<1>{});
+  if (packs <= 32) return f(Int<32>{}, Int<1>{});
+  if (packs <= 64) return f(Int<64>{}, Int<1>{});
+  f(Int<64>{}, Int<2>{});
+}
+// Longer rows, up to 8192 columns; past those the blocks would be one a CU.
+constexpr int64_t kGradCols = 8192;
+template <typename F>
 void with_grad_block(int64_t packs, F&& f) {
   if (packs <= 256) return f(Int<256>{}, Int<1>{});
   if (packs <= 512) return f(Int<256>{}, Int<2>{});
   if (packs <= 1024) return f(Int<512>{}, Int<2>{});
-  if (V == 8 || packs <= 2048) return f(Int<1024>{}, Int<2>{});
-  if constexpr (V == 4) f(Int<1024>{}, Int<4>{});
+  f(Int<1024>{}, Int<2>{});
 }
 
 struct Plan {
@@ -580,24 +627,30 @@ struct Plan {
   int64_t part;    // rows of a part (not fused)
   size_t stats, total;
 };
-constexpr int64_t kPartRows = 256, kMaxParts = 512;
+constexpr int64_t kPartRows = 16, kMaxParts = 2048, kCardThreads = 256 * 1024;
 Plan plan_of(int64_t rows, int64_t cols, int64_t es) {
   Plan p{};
   const int64_t V = 16 / es, packs = ceil_div64(cols, V);
-  p.fused = cols <= 16384;
+  p.fused = cols <= kGradCols;
   if (p.fused) {
-    int64_t at_once = 1;  // rows a block takes at a time
-    if (packs <= kWavePacks) with_lanes(packs, [&](auto g, auto) { at_once = kGradThreads / decltype(g)::value; });
+    int64_t at_once = 1, threads = kGradThreads;  // rows a block takes at a time
+    if (packs <= kWavePacks)
+      with_grad_lanes(packs, [&](auto g, auto) { at_once = kGradThreads / decltype(g)::value; });
+    else
+      with_grad_block(packs, [&](auto t, auto) { threads = decltype(t)::value; });
     const int64_t turns = ceil_div64(rows, at_once);
     // A block alone spares the second launch.  Else parts as many as fill the card, as
-    // long as their sums stay an eighth of the rows, or each has four turns left.
-    const int64_t most = std::max(rows * es / 43, turns / 4);
-    p.parts = turns <= 4 ? 1 : std::min({most, turns, kMaxParts});
+    // long as their sums stay an eighth of the rows, or each has four turns left; and
+    // all with as many turns.
+    const int64_t most = std::min(std::max(rows * es / 43, turns / 4), kCardThreads / threads);
+    p.parts = turns <= 4 ? 1 : ceil_div64(turns, ceil_div64(turns, most));
     p.stats = p.parts > 1 ? size_t(ceil_div64(p.parts * 2 * cols * 4, 16)) * 16 : 0;
     p.total = p.stats;
     return p;
   }
-  p.part = std::max(kPartRows, ceil_div64(rows, kMaxParts));
+  // blocks of the column sums fill the card, with 16 rows each at least
+  const int64_t across = ceil_div64(packs, 64);
+  p.part = std::max(kPartRows, ceil_div64(rows, std::max<int64_t>(1, kMaxParts / across)));
   p.parts = ceil_div64(rows, p.part);
   p.stats = size_t(ceil_div64(p.parts * 2 * cols * 4, 16)) * 16;
   p.total = p.stats + size_t(rows) * sizeof(float2);
@@ -610,7 +663,7 @@ hipError_t rows_grad(const LayerNormArgs& a, const Plan& p, float* sums, hipStre
   const int64_t packs = ceil_div64(a.cols, V);
   const uint32_t grid = uint32_t(p.parts);
   if (packs <= kWavePacks)
-    with_lanes(packs, [&](auto g, auto u) {
+    with_grad_lanes(packs, [&](auto g, auto u) {
       constexpr int G = decltype(g)::value, U = decltype(u)::value;
       if (a.cols < V) {
         if constexpr (G == 1) rows_grad_kernel<T, 1, 1, END_TINY, kGradThreads><<<grid, kGradThreads, 0, s>>>(a, sums);
@@ -621,7 +674,7 @@ hipError_t rows_grad(const LayerNormArgs& a, const Plan& p, float* sums, hipStre
       }
     });
   else
-    with_grad_block<V>(packs, [&](auto t, auto u) {
+    with_grad_block(packs, [&](auto t, auto u) {
       constexpr int THREADS = decltype(t)::value;
       rows_grad_kernel<T, THREADS, decltype(u)::value, END_SHARED, THREADS><<<grid, THREADS, 0, s>>>(a, sums);
     });
@@ -644,7 +697,7 @@ hipError_t backward(const LayerNormArgs& a, hipStream_t s) {
       long_rows_grad_kernel<T><<<grid, kThreads, 0, s>>>(a, columns ? stats : nullptr);
       if ((e = hipGetLastError()) != hipSuccess) return e;
       if (columns) {
-        const dim3 parts(uint32_t(p.parts), uint32_t(std::min<int64_t>(ceil_div64(a.cols, 64), 65535)));
+        const dim3 parts(uint32_t(p.parts), uint32_t(std::min<int64_t>(ceil_div64(a.cols, 64 * Pack<T>::N), 65535)));
         column_grads_kernel<T><<<parts, kThreads, 0, s>>>(a, stats, p.part, sums);
         if ((e = hipGetLastError()) != hipSuccess) return e;
       }
