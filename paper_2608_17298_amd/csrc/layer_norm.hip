@@ -627,22 +627,26 @@ struct Plan {
   int64_t part;    // rows of a part (not fused)
   size_t stats, total;
 };
-constexpr int64_t kPartRows = 16, kMaxParts = 2048, kCardThreads = 256 * 1024;
+constexpr int64_t kPartRows = 16, kMaxParts = 2048, kCardPacks = 256 * 1024;
 Plan plan_of(int64_t rows, int64_t cols, int64_t es) {
   Plan p{};
   const int64_t V = 16 / es, packs = ceil_div64(cols, V);
   p.fused = cols <= kGradCols;
   if (p.fused) {
-    int64_t at_once = 1, threads = kGradThreads;  // rows a block takes at a time
+    int64_t at_once = 1, lanes = 0;  // rows a block takes at a time; its threads times their packs
     if (packs <= kWavePacks)
-      with_grad_lanes(packs, [&](auto g, auto) { at_once = kGradThreads / decltype(g)::value; });
+      with_grad_lanes(packs, [&](auto g, auto u) {
+        at_once = kGradThreads / decltype(g)::value;
+        lanes = kGradThreads * decltype(u)::value;
+      });
     else
-      with_grad_block(packs, [&](auto t, auto) { threads = decltype(t)::value; });
+      with_grad_block(packs, [&](auto t, auto u) { lanes = decltype(t)::value * decltype(u)::value; });
     const int64_t turns = ceil_div64(rows, at_once);
-    // A block alone spares the second launch.  Else parts as many as fill the card, as
-    // long as their sums stay an eighth of the rows, or each has four turns left; and
+    // A block alone spares the second launch.  Else parts as many as fill the card (twice
+    // as many: 8191 x 4096 f16 65 us, so 60; half as many: 30000 x 2000 f16 101, so 86),
+    // as long as their sums stay an eighth of the rows, or each has four turns left; and
     // all with as many turns.
-    const int64_t most = std::min(std::max(rows * es / 43, turns / 4), kCardThreads / threads);
+    const int64_t most = std::min(std::max(rows * es / 43, turns / 4), std::max<int64_t>(256, kCardPacks / lanes));
     p.parts = turns <= 4 ? 1 : ceil_div64(turns, ceil_div64(turns, most));
     p.stats = p.parts > 1 ? size_t(ceil_div64(p.parts * 2 * cols * 4, 16)) * 16 : 0;
     p.total = p.stats;
