@@ -97,15 +97,51 @@ GART_HOST_DEVICE inline bool step_factors(float a, float b, float c, int steps, 
   return true;
 }
 
+// How a product is cut: square tiles of 64 or 128 a block, one block a CU, and
+// parts of the sums that a second launch joins.
+struct PairCut {
+  int side, parts;
+  bool symmetric;  // only tiles on and above the diagonal
+};
+constexpr int64_t kTileSide = 64;
+// Launched for them: a triangle with an odd number of rows is folded with one more.
+inline int64_t blocks_of(int64_t rows, int64_t cols, int side, bool symmetric) {
+  const int64_t i = (rows + side - 1) / side, j = (cols + side - 1) / side, even = i + i % 2;
+  return symmetric ? even / 2 * (even + 1) : i * j;
+}
+inline PairCut cut_pair(int64_t rows, int64_t cols, int64_t steps, bool symmetric) {
+  // measured: us of a step of 32 terms, of what surrounds the steps, and of a join
+  constexpr double kStep64 = 0.11, kStep128 = 0.43, kAround = 3.0, kJoin = 3.0;
+  PairCut best{64, 1, symmetric};
+  double least = HUGE_VAL;
+  for (const int side : {64, 128}) {
+    const int64_t tiles = blocks_of(rows, cols, side, symmetric);
+    const int most = symmetric ? int(std::min<int64_t>(16, std::max<int64_t>(1, steps / 16))) : 1;
+    for (int parts = 1; parts <= most; ++parts) {
+      const double turns = double((tiles * parts + 255) / 256), length = double((steps + parts - 1) / parts);
+      double t = turns * (kAround + length * (side == 64 ? kStep64 : kStep128));
+      if (parts > 1) t += kJoin + double(tiles * parts) * (side == 64 ? 0.01 : 0.04);
+      if (t < least) {
+        least = t;
+        best.side = side;
+        best.parts = parts;
+      }
+    }
+  }
+  return best;
+}
+inline size_t partial_floats(int64_t n, int64_t steps) {
+  const PairCut c = cut_pair(n, n, steps, true);
+  return c.parts == 1 ? 0 : size_t(blocks_of(n, n, c.side, true)) * size_t(c.parts * c.side) * size_t(c.side);
+}
+
 // Where things lie in scratch, in bytes; sizes of the padded matrices.
 struct MatrixPlan {
   bool tall;            // more rows than columns: X is the transpose
   int64_t n, m;         // the smaller and the larger size
-  int64_t n_pad, m_pad;
-  int64_t x_low, a_low;  // elements from the high parts to the low ones
-  size_t sums, factors, x[2], a, p, total;
+  int64_t n_pad, m_pad;  // multiples of kTileSide
+  size_t sums, factors, x[2], xt[2], a, p, partial, total;
 };
-constexpr int64_t kTileSide = 64;
 constexpr int64_t kSumBlocks = 256;  // partial sums of squares
 constexpr int64_t kMostTiles = int64_t(1) << 23;
 
@@ -116,16 +152,18 @@ inline MatrixPlan matrix_plan(int64_t rows, int64_t cols) {
   p.m = std::max(rows, cols);
   p.n_pad = (p.n + kTileSide - 1) / kTileSide * kTileSide;
   p.m_pad = (p.m + kTileSide - 1) / kTileSide * kTileSide;
-  p.x_low = p.n_pad * p.m_pad;
-  p.a_low = p.n_pad * p.n_pad;
-  const size_t x = size_t(p.x_low) * 4, a = size_t(p.a_low) * 4;  // two float16 planes
+  const size_t x = size_t(p.n_pad) * size_t(p.m_pad) * 4, a = size_t(p.n_pad) * size_t(p.n_pad) * 4;  // two float16
   p.sums = 0;
   p.factors = kSumBlocks * sizeof(double);
   p.x[0] = p.factors + sizeof(StepFactors) * kMaxSteps;
   p.x[1] = p.x[0] + x;
-  p.a = p.x[1] + x;
+  p.xt[0] = p.x[1] + x;
+  p.xt[1] = p.xt[0] + x;
+  p.a = p.xt[1] + x;
   p.p = p.a + a;
-  p.total = p.p + a;
+  p.partial = p.p + a;
+  p.total = p.partial + 4 * std::max(partial_floats(p.n_pad, p.m_pad / 32),
+                                     partial_floats(p.n_pad, p.n_pad / 32));
   return p;
 }
 

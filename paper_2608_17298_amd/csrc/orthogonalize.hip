@@ -67,7 +67,44 @@ __device__ __forceinline__ void split(float v, f16& high, f16& low) {
   low = f16(v - float(high));
 }
 
-// X in two parts, zero in the padding, from u over its norm: 64 x 64 elements a
+// ---- matrices in the order of fragments ------------------------------------------
+// The matrix instruction takes 16 rows by 32 k of an operand, eight consecutive k of
+// row r = lane % 16 from k = 8 (lane / 16) in each lane.  X, A and P are stored in
+// such blocks, a kilobyte of high parts and one of low parts, side by side along k:
+// a wave loads a fragment as it stands, past LDS.  X is stored twice, as itself for
+// X X^T and transposed for P X; A and P are symmetric.
+struct Blocks {
+  f16* data;
+  int64_t across;  // blocks along k
+  static constexpr int kBlock = 16 * 32, kPair = 2 * kBlock;  // elements
+  // the block of rows 16 i and k 32 k
+  __device__ __forceinline__ f16* at(int64_t i, int64_t k) const { return data + (i * across + k) * kPair; }
+};
+
+// Of a 64 x 64 tile in LDS, element (i, j) at tile[i * pitch + j], into blocks: those
+// of rows i, or, transposed, of rows j.  Values are split into two parts.
+constexpr int kTilePitch = 64 + 4;
+template <bool TRANSPOSED>
+__device__ __forceinline__ void store_blocks(const float* tile, const Blocks& to, int64_t row0, int64_t col0, int lane,
+                                             int first, int step) {
+  const int r = lane % 16, g = lane / 16;
+  for (int b = first; b < 8; b += step) {
+    const int row = 16 * (b / 2) + r, k = 32 * (b % 2) + 8 * g;
+    Pack<f16> high, low;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      f16 h, l;
+      split(TRANSPOSED ? tile[(k + e) * kTilePitch + row] : tile[row * kTilePitch + k + e], h, l);
+      high.v[e] = h;
+      low.v[e] = l;
+    }
+    f16* block = to.at(row0 / 16 + b / 2, col0 / 32 + b % 2) + lane * 8;
+    store_pack(block, high);
+    store_pack(block + Blocks::kBlock, low);
+  }
+}
+
+// X and its transpose, zero in the padding, from u over its norm: 64 x 64 elements a
 // block; and the steps' factors, by the first one.
 struct Iteration {
   float a, b, c, eps;
@@ -77,24 +114,16 @@ struct Iteration {
 template <typename T>
 __global__ __launch_bounds__(kThreads) void prepare_kernel(const Source<T> u, int64_t n, int64_t m, bool tall,
                                                            const double* __restrict__ sums, const Iteration it,
-                                                           StepFactors* __restrict__ factors, f16* __restrict__ x,
-                                                           int64_t x_ld, int64_t x_low) {
+                                                           StepFactors* __restrict__ factors, const Blocks x,
+                                                           const Blocks xt) {
   __shared__ double s_sum[kThreads / 64];
-  __shared__ float s_tile[64][65];
+  __shared__ float s_tile[64 * kTilePitch];
   const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
   static_assert(kSumBlocks == kThreads, "a partial sum a thread");
   double t = sums[threadIdx.x];
 #pragma unroll
   for (int off = 32; off > 0; off >>= 1) t += __shfl_xor(t, off);
   if (lane == 0) s_sum[wave] = t;
-  const int64_t i0 = int64_t(blockIdx.y) * 64, j0 = int64_t(blockIdx.x) * 64;
-  for (int k = wave; k < 64; k += kThreads / 64) {
-    // lanes along the source's columns
-    const int i = tall ? lane : k, j = tall ? k : lane;
-    float v = 0.0f;
-    if (i0 + i < n && j0 + j < m) v = tall ? u.at(j0 + j, i0 + i) : u.at(i0 + i, j0 + j);
-    s_tile[i][j] = v;
-  }
   __syncthreads();
   const double size = sqrt((s_sum[0] + s_sum[1]) + (s_sum[2] + s_sum[3])), norm = size + double(it.eps);
   const bool tiny = size / norm < kNearOne;  // not if it is a NaN
@@ -107,177 +136,274 @@ __global__ __launch_bounds__(kThreads) void prepare_kernel(const Source<T> u, in
       step_factors(it.a, it.b, it.c, it.steps, size / norm, &first, factors);
     }
   }
-  for (int c = threadIdx.x; c < 64 * 8; c += kThreads) {
-    const int i = c / 8, j = c % 8 * 8;
-    Pack<f16> high, low;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const bool in = i0 + i < n && j0 + j + e < m;
-      const float v = in ? float(double(s_tile[i][j + e]) * inv) : 0.0f;  // padding stays 0 whatever the norm
-      f16 h, l;
-      split(v, h, l);
-      high.v[e] = h;
-      low.v[e] = l;
-    }
-    f16* to = x + (i0 + i) * x_ld + j0 + j;
-    store_pack(to, high);
-    store_pack(to + x_low, low);
+  const int64_t i0 = int64_t(blockIdx.y) * 64, j0 = int64_t(blockIdx.x) * 64;
+  for (int k = wave; k < 64; k += kThreads / 64) {
+    // lanes along the source's columns
+    const int i = tall ? lane : k, j = tall ? k : lane;
+    float v = 0.0f;  // the padding stays 0 whatever the norm
+    if (i0 + i < n && j0 + j < m) v = float(double(tall ? u.at(j0 + j, i0 + i) : u.at(i0 + i, j0 + j)) * inv);
+    s_tile[i * kTilePitch + j] = v;
   }
+  __syncthreads();
+  store_blocks<false>(s_tile, x, i0, j0, lane, wave, kThreads / 64);
+  store_blocks<true>(s_tile, xt, j0, i0, lane, wave, kThreads / 64);
 }
 
 // ---- products of pairs ----------------------------------------------------------
 enum PairEpilogue {
-  PAIR_PAIR,  // the result in two parts
-  PAIR_OUT,   // y
-  PAIR_STEP   // param
+  PAIR_BLOCKS,  // the result in blocks, and its transpose
+  PAIR_OUT,     // y
+  PAIR_STEP,    // param
+  PAIR_PART     // float sums of one part of k
 };
 
-// C = alpha sum_k A(i,k) B(j,k) + beta D(i,j).  All sizes are whole tiles.
+// C = alpha sum_k A(i,k) B(j,k) + beta D(i,j).  Sizes are multiples of 64, of zeros
+// where the matrix ends.
 struct PairArgs {
-  const f16 *a, *b, *d;  // high parts; d may be NULL
-  int64_t a_ld, b_ld, d_ld, a_low, b_low, d_low;
-  int64_t tiles_i, tiles_j, depth;
-  const float* factors;  // alpha, beta
-  void* out;
-  int64_t out_ld, out_low;  // PAIR_PAIR: elements to the low parts
-  int64_t rows, cols;       // else: of out
-  float decay, step;        // PAIR_STEP: param -= decay param + step C
+  Blocks a, b, d;       // d.data may be NULL
+  int64_t rows, cols;   // of C
+  int64_t steps;        // blocks along k
+  int tiles_i, tiles_j, band;
+  bool symmetric;       // C is: tiles above the diagonal are stored on both sides of it
+  int parts;            // of k: blockIdx.y
+  float* partial;       // their sums
+  const float* factors; // alpha, beta
+  Blocks out, across;   // PAIR_BLOCKS: C and, unless it is symmetric, its transpose
+  void* y;              // else: the result
+  int64_t y_ld, y_rows, y_cols;
+  float decay, step;    // PAIR_STEP: y -= decay y + step C
 };
 
-// AKC, BKC: k runs along the operand's rows.  With A across k, D is read transposed.
-template <typename T, bool AKC, bool BKC, int TI, int TJ, int WI, int WJ, PairEpilogue EPI>
-__global__ __launch_bounds__(64 * WI * WJ) void pair_kernel(const PairArgs g) {
-  using TA = Tile<f16, AKC, 16 * TI * WI, WI * WJ, false>;
-  using TB = Tile<f16, BKC, 16 * TJ * WJ, WI * WJ, true>;
-  constexpr int BI = 16 * TI * WI, BJ = 16 * TJ * WJ;
-  constexpr int A_LOW = TA::ELEMS, B_HIGH = 2 * TA::ELEMS, B_LOW = B_HIGH + TB::ELEMS, ELEMS = B_LOW + TB::ELEMS;
-  __shared__ __attribute__((aligned(16))) f16 lds[2][ELEMS];
+// Blocks go to the eight XCDs in turn.  Each gets a run of tiles that covers a patch
+// of `band` rows, so that its cache takes in few rows of both operands.  A triangle of
+// tiles (i <= j) is folded to half as many rows: row r, then row n - 1 - r.
+__device__ __forceinline__ bool find_tile(const PairArgs& g, int b, int total, int& ti, int& tj) {
+  const int t = int(xcd_tile(b, total));
+  const int n = g.tiles_i, even = n + n % 2;
+  const int rows = g.symmetric ? even / 2 : n, cols = g.symmetric ? even + 1 : g.tiles_j;
+  const int top = t / (g.band * cols) * g.band, high = min(g.band, rows - top);
+  const int in = t - top * cols, r = top + in % high, c = in / high;
+  ti = r;
+  tj = c;
+  if (g.symmetric) {
+    const bool folded = c >= even - r;
+    ti = folded ? even - 1 - r : r;
+    tj = folded ? ti + c - (even - r) : r + c;
+  }
+  return ti < n && tj < g.tiles_j;
+}
+
+// A wave has 64 x 64 elements: WI x WJ waves a block, and WK of them take every WK-th
+// block of k.  Two fragments' loads are on their way while one set is multiplied: the
+// waves meet only when their sums are joined, in LDS.  JOIN: the sums of k are those
+// of g.parts parts.
+constexpr int kSide = 64, kFrag = 4;  // 16-row tiles a wave's side
+template <typename T, int WI, int WJ, int WK, PairEpilogue EPI, bool JOIN>
+__global__ __launch_bounds__(64 * WI * WJ * WK, 1) void pair_kernel(const PairArgs g) {
+  constexpr int WAVES = WI * WJ * WK, THREADS = 64 * WAVES;
+  constexpr int ROWS = kFrag / WK;  // 16-row tiles of a wave's result
+  static_assert(WK == 1 || (WI == 1 && WJ == 1 && WK == kFrag), "one tile, or waves that share nothing");
+  // joined sums, then tiles that are transposed
+  __shared__ __attribute__((aligned(16))) float lds[WK > 1 && !JOIN ? WK * kSide * kSide
+                                                    : EPI == PAIR_BLOCKS ? WI * WJ * kSide * kTilePitch : 4];
   const int tid = threadIdx.x, lane = tid % 64, wave = __builtin_amdgcn_readfirstlane(tid / 64);
-  const int wi = wave / WJ, wj = wave % WJ;
-  const int64_t tile = xcd_tile(blockIdx.x, g.tiles_i * g.tiles_j);
-  const int64_t i0 = tile / g.tiles_j * BI, j0 = tile % g.tiles_j * BJ;
+  const int wk = wave % WK, wi = wave / WK / WJ, wj = wave / WK % WJ;
+  int ti, tj;
+  if (!find_tile(g, blockIdx.x, gridDim.x, ti, tj)) return;
+  const int64_t i0 = (int64_t(ti) * WI + wi) * kSide, j0 = (int64_t(tj) * WJ + wj) * kSide;
+  const bool inside = i0 < g.rows && j0 < g.cols;
 
-  f32x4 acc[TI][TJ];
+  f32x4 acc[ROWS][kFrag];
+  if constexpr (JOIN) {
 #pragma unroll
-  for (int i = 0; i < TI; ++i)
+    for (int i = 0; i < ROWS; ++i)
 #pragma unroll
-    for (int j = 0; j < TJ; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-
-  TA ta;
-  TB tb;
-  ta.template aim<true>(g.a, g.a_ld, i0, g.tiles_i * BI, 0, tid);
-  tb.template aim<true>(g.b, g.b_ld, j0, g.tiles_j * BJ, 0, tid);
-  const int64_t a_step = TA::stride(g.a_ld), b_step = TB::stride(g.b_ld), steps = g.depth / kStep<f16>;
-  auto fetch = [&](int h, int64_t n) {
-    ta.fetch(lds[h], n * a_step, wave);
-    ta.fetch(lds[h] + A_LOW, n * a_step + g.a_low, wave);
-    tb.fetch(lds[h] + B_HIGH, n * b_step, wave);
-    tb.fetch(lds[h] + B_LOW, n * b_step + g.b_low, wave);
-  };
-  fetch(0, 0);
-  for (int64_t n = 0; n < steps; ++n) {
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // this wave's part of the buffer has landed
-    __syncthreads();                                  // everyone's has, and the other buffer has been read
-    if (n + 1 < steps) fetch((n + 1) & 1, n + 1);
-    const f16* l = lds[n & 1];
+      for (int j = 0; j < kFrag; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    for (int part = 0; part < g.parts; ++part) {
+      const float* from = g.partial + (int64_t(part) * gridDim.x + blockIdx.x) * (THREADS * ROWS * kFrag * 4) + tid * 4;
 #pragma unroll
-    for (int s = 0; s < 2; ++s) {
-      Pack<f16>::V ah[TI], al[TI], bh[TJ], bl[TJ];
+      for (int i = 0; i < ROWS; ++i)
 #pragma unroll
-      for (int i = 0; i < TI; ++i) {
-        ah[i] = TA::fragment(l, wi * TI + i, s, lane);
-        al[i] = TA::fragment(l + A_LOW, wi * TI + i, s, lane);
-      }
+        for (int j = 0; j < kFrag; ++j)
+          acc[i][j] += *reinterpret_cast<const f32x4*>(from + (i * kFrag + j) * THREADS * 4);
+    }
+  } else {
+    f32x4 sum[kFrag][kFrag];
 #pragma unroll
-      for (int j = 0; j < TJ; ++j) {
-        bh[j] = TB::fragment(l + B_HIGH, wj * TJ + j, s, lane);
-        bl[j] = TB::fragment(l + B_LOW, wj * TJ + j, s, lane);
-      }
+    for (int i = 0; i < kFrag; ++i)
 #pragma unroll
-      for (int i = 0; i < TI; ++i)
+      for (int j = 0; j < kFrag; ++j) sum[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    const int part = EPI == PAIR_PART ? int(blockIdx.y) : 0, parts = EPI == PAIR_PART ? g.parts : 1;
+    const int k0 = int(g.steps * part / parts) + wk, k1 = int(g.steps * (part + 1) / parts);
+    if (inside && k0 < k1) {
+      const int64_t a_row = g.a.across * Blocks::kPair, b_row = g.b.across * Blocks::kPair;
+      const f16* a = g.a.at(i0 / 16, k0) + lane * 8;
+      const f16* b = g.b.at(j0 / 16, k0) + lane * 8;
+      struct Set {
+        Pack<f16>::V ah[kFrag], al[kFrag], bh[kFrag], bl[kFrag];
+      } set[3];
+      auto load = [&](Set& f, int n) {  // past the end the last one again
+        const int64_t at = int64_t(min(n, (k1 - 1 - k0) / WK)) * (WK * Blocks::kPair);
 #pragma unroll
-        for (int j = 0; j < TJ; ++j) {
-          acc[i][j] = Mfma<f16>::run(bl[j], ah[i], acc[i][j]);
-          acc[i][j] = Mfma<f16>::run(bh[j], al[i], acc[i][j]);
-          acc[i][j] = Mfma<f16>::run(bh[j], ah[i], acc[i][j]);
+        for (int i = 0; i < kFrag; ++i) {
+          f.ah[i] = *reinterpret_cast<const Pack<f16>::V*>(a + i * a_row + at);
+          f.al[i] = *reinterpret_cast<const Pack<f16>::V*>(a + i * a_row + at + Blocks::kBlock);
+          f.bh[i] = *reinterpret_cast<const Pack<f16>::V*>(b + i * b_row + at);
+          f.bl[i] = *reinterpret_cast<const Pack<f16>::V*>(b + i * b_row + at + Blocks::kBlock);
         }
+        __builtin_amdgcn_sched_barrier(0);  // loads are asked for here, not where they are used
+      };
+      auto multiply = [&](const Set& f) {
+#pragma unroll
+        for (int p = 0; p < 3; ++p)
+#pragma unroll
+          for (int i = 0; i < kFrag; ++i)
+#pragma unroll
+            for (int j = 0; j < kFrag; ++j)
+              sum[i][j] = Mfma<f16>::run(p == 0 ? f.bl[j] : f.bh[j], p == 1 ? f.al[i] : f.ah[i], sum[i][j]);
+        __builtin_amdgcn_sched_barrier(0);
+      };
+      const int count = (k1 - k0 + WK - 1) / WK;
+      load(set[0], 0);
+      load(set[1], 1);
+      int n = 0;
+      for (; n + 2 < count; n += 3) {
+        load(set[2], n + 2);
+        multiply(set[0]);
+        load(set[0], n + 3);
+        multiply(set[1]);
+        load(set[1], n + 4);
+        multiply(set[2]);
+      }
+      if (n < count) multiply(set[0]);
+      if (n + 1 < count) multiply(set[1]);
+    }
+    if constexpr (WK == 1) {
+#pragma unroll
+      for (int i = 0; i < kFrag; ++i)
+#pragma unroll
+        for (int j = 0; j < kFrag; ++j) acc[i][j] = sum[i][j];
+    } else {
+      // wave w takes the 16-row tile w of the others
+#pragma unroll
+      for (int i = 0; i < kFrag; ++i)
+#pragma unroll
+        for (int j = 0; j < kFrag; ++j)
+          *reinterpret_cast<f32x4*>(lds + ((wave * kFrag + i) * kFrag + j) * 256 + lane * 4) = sum[i][j];
+      __syncthreads();
+#pragma unroll
+      for (int j = 0; j < kFrag; ++j) {
+        acc[0][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int w = 0; w < WK; ++w)
+          acc[0][j] += *reinterpret_cast<const f32x4*>(lds + ((w * kFrag + wave) * kFrag + j) * 256 + lane * 4);
+      }
+      __syncthreads();
     }
   }
 
-  // A lane's columns: eight consecutive ones from each two tiles.
-  const int r = lane % 16, q4 = lane / 16;
+  if constexpr (EPI == PAIR_PART) {
+    float* to = g.partial + (int64_t(blockIdx.y) * gridDim.x + blockIdx.x) * (THREADS * ROWS * kFrag * 4) + tid * 4;
+#pragma unroll
+    for (int i = 0; i < ROWS; ++i)
+#pragma unroll
+      for (int j = 0; j < kFrag; ++j) *reinterpret_cast<f32x4*>(to + (i * kFrag + j) * THREADS * 4) = acc[i][j];
+    return;
+  }
+
+  // The fragments of B are not paired up: a lane has four consecutive columns of a row.
+  const int r = lane % 16, g4 = lane / 16;
   const float alpha = g.factors[0], beta = g.factors[1];
+  float* tile = lds + (WK > 1 ? 0 : wave * kSide * kTilePitch);
+  if (inside) {
 #pragma unroll
-  for (int jq = 0; jq < TJ / 2; ++jq) {
-    const int64_t j = j0 + 32 * ((wj * TJ + jq * 2) / 2) + 8 * q4;
+    for (int i = 0; i < ROWS; ++i) {
+      const int row = 16 * (WK > 1 ? wave : i) + r;
 #pragma unroll
-    for (int i = 0; i < TI; ++i) {
-      const int64_t row = i0 + 16 * (wi * TI + i) + r;
-      float c[8];
+      for (int j = 0; j < kFrag; ++j) {
+        const int col = 16 * j + 4 * g4;
+        f32x4 c = alpha * acc[i][j];
+        if (g.d.data) {
+          typedef f16 f16x4 __attribute__((ext_vector_type(4)));
+          const f16* d = g.d.at((i0 + row) / 16, (j0 + col) / 32) + ((col % 32) / 8 * 16 + r) * 8 + col % 8;
+          const f16x4 dh = *reinterpret_cast<const f16x4*>(d), dl = *reinterpret_cast<const f16x4*>(d + Blocks::kBlock);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) c[e] = alpha * acc[i][jq * 2 + e / 4][e % 4];
-      if (g.d) {
-        Pack<f16> dh, dl;
-        if constexpr (AKC) {
-          const f16* d = g.d + row * g.d_ld + j;
-          dh = load_pack(d);
-          dl = load_pack(d + g.d_low);
+          for (int e = 0; e < 4; ++e) c[e] = fmaf(beta, float(dh[e]) + float(dl[e]), c[e]);
+        }
+        if constexpr (EPI == PAIR_BLOCKS) {
+          *reinterpret_cast<f32x4*>(tile + row * kTilePitch + col) = c;
         } else {
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            const f16* d = g.d + (j + e) * g.d_ld + row;
-            dh.v[e] = d[0];
-            dl.v[e] = d[g.d_low];
-          }
-        }
-#pragma unroll
-        for (int e = 0; e < 8; ++e) c[e] = fmaf(beta, float(dh.v[e]) + float(dl.v[e]), c[e]);
-      }
-      if constexpr (EPI == PAIR_PAIR) {
-        Pack<f16> high, low;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          f16 h, l;
-          split(c[e], h, l);
-          high.v[e] = h;
-          low.v[e] = l;
-        }
-        f16* out = static_cast<f16*>(g.out) + row * g.out_ld + j;
-        store_pack(out, high);
-        store_pack(out + g.out_low, low);
-      } else {
-        if (row >= g.rows || j >= g.cols) continue;
-        constexpr int V = Pack<T>::N;
-        T* out = static_cast<T*>(g.out) + row * g.out_ld + j;
-#pragma unroll
-        for (int h = 0; h < 8 / V; ++h) {
-          const int count = int(min(int64_t(V), g.cols - j - h * V));
-          if (count <= 0) continue;
-          Pack<T> p;
-          if constexpr (EPI == PAIR_STEP) {
-            p = load_some(out + h * V, count);
-#pragma unroll
-            for (int e = 0; e < V; ++e) {
-              const float v = float(p.v[e]);
-              p.v[e] = T(fmaf(-g.step, c[h * V + e], fmaf(-g.decay, v, v)));
+          if (i0 + row >= g.y_rows || j0 + col >= g.y_cols) continue;
+          T* y = static_cast<T*>(g.y) + (i0 + row) * g.y_ld + j0 + col;
+          const int count = int(min(int64_t(4), g.y_cols - j0 - col));
+          struct __attribute__((packed)) Four {
+            T v[4];
+          };
+          Four f;
+          auto each = [&](int e, T& v) {
+            if constexpr (EPI == PAIR_STEP) {
+              const float p = float(v);
+              v = T(fmaf(-g.step, c[e], fmaf(-g.decay, p, p)));
+            } else {
+              v = T(c[e]);
             }
+          };
+          if (count == 4) {
+            if constexpr (EPI == PAIR_STEP) f = *reinterpret_cast<const Four*>(y);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) each(e, f.v[e]);
+            *reinterpret_cast<Four*>(y) = f;
           } else {
 #pragma unroll
-            for (int e = 0; e < V; ++e) p.v[e] = T(c[h * V + e]);
+            for (int e = 0; e < 4; ++e)
+              if (e < count) each(e, y[e]);
           }
-          store_some(out + h * V, p, count);
         }
       }
+    }
+  }
+  if constexpr (EPI == PAIR_BLOCKS) {
+    __syncthreads();
+    if (!inside) return;
+    constexpr int SHARE = WK;  // waves that store the tile
+    store_blocks<false>(tile, g.out, i0, j0, lane, wk, SHARE);
+    if (g.symmetric) {
+      if (i0 != j0) store_blocks<true>(tile, g.out, j0, i0, lane, wk, SHARE);
+    } else {
+      store_blocks<true>(tile, g.across, j0, i0, lane, wk, SHARE);
     }
   }
 }
 
-template <typename T, bool AKC, bool BKC, PairEpilogue EPI>
-hipError_t run_pair(PairArgs g, int64_t rows, int64_t cols, hipStream_t s) {
-  g.tiles_i = rows / 64;
-  g.tiles_j = cols / 64;
-  pair_kernel<T, AKC, BKC, 2, 2, 2, 2, EPI><<<uint32_t(g.tiles_i * g.tiles_j), 256, 0, s>>>(g);
-  return hipGetLastError();
+template <typename T, int W, int WK, PairEpilogue EPI>
+hipError_t run_tiles(PairArgs g, const PairCut& c, hipStream_t s) {
+  g.tiles_i = int((g.rows + c.side - 1) / c.side);
+  g.tiles_j = int((g.cols + c.side - 1) / c.side);
+  g.symmetric = c.symmetric;
+  g.parts = c.parts;
+  const uint32_t blocks = uint32_t(blocks_of(g.rows, g.cols, c.side, c.symmetric));
+  g.band = 1;
+  while (g.band * g.band * 8 < int(blocks)) ++g.band;
+  constexpr int THREADS = 64 * W * W * WK;
+  if (c.parts == 1) {
+    pair_kernel<T, W, W, WK, EPI, false><<<blocks, THREADS, 0, s>>>(g);
+    return hipGetLastError();
+  }
+  if constexpr (EPI == PAIR_BLOCKS) {
+    pair_kernel<T, W, W, WK, PAIR_PART, false><<<dim3(blocks, uint32_t(c.parts)), THREADS, 0, s>>>(g);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    pair_kernel<T, W, W, WK, PAIR_BLOCKS, true><<<blocks, THREADS, 0, s>>>(g);
+    return hipGetLastError();
+  }
+  return hipErrorInvalidValue;
+}
+
+template <typename T, PairEpilogue EPI>
+hipError_t run_pair(const PairArgs& g, bool symmetric, hipStream_t s) {
+  const PairCut c = cut_pair(g.rows, g.cols, g.steps, symmetric);
+  if (c.side == 64) return run_tiles<T, 1, 4, EPI>(g, c, s);
+  return run_tiles<T, 2, 1, EPI>(g, c, s);
 }
 
 template <typename T>
@@ -289,66 +415,58 @@ hipError_t run(const OrthogonalizeArgs& a, hipStream_t s) {
   char* base = static_cast<char*>(a.scratch);
   double* sums = reinterpret_cast<double*>(base + p.sums);
   StepFactors* factors = reinterpret_cast<StepFactors*>(base + p.factors);
-  f16* x[2] = {reinterpret_cast<f16*>(base + p.x[0]), reinterpret_cast<f16*>(base + p.x[1])};
-  f16* gram = reinterpret_cast<f16*>(base + p.a);
-  f16* poly = reinterpret_cast<f16*>(base + p.p);
+  auto blocks = [&](size_t at, int64_t across) { return Blocks{reinterpret_cast<f16*>(base + at), across}; };
+  const int64_t n_blocks = p.n_pad / 32, m_blocks = p.m_pad / 32;
+  const Blocks x[2] = {blocks(p.x[0], m_blocks), blocks(p.x[1], m_blocks)};
+  const Blocks xt[2] = {blocks(p.xt[0], n_blocks), blocks(p.xt[1], n_blocks)};
+  const Blocks gram = blocks(p.a, n_blocks), poly = blocks(p.p, n_blocks);
 
   Source<T> u{static_cast<const T*>(a.x), a.x_ld, a.m, a.m_ld, a.momentum, a.nesterov};
   squares_kernel<T><<<uint32_t(kSumBlocks), kThreads, 0, s>>>(u, a.m, a.rows, a.cols, sums);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   const dim3 grid(uint32_t(p.m_pad / 64), uint32_t(p.n_pad / 64));
-  prepare_kernel<T><<<grid, kThreads, 0, s>>>(u, p.n, p.m, p.tall, sums, it, factors, x[0], p.m_pad, p.x_low);
+  prepare_kernel<T><<<grid, kThreads, 0, s>>>(u, p.n, p.m, p.tall, sums, it, factors, x[0], xt[0]);
   if ((e = hipGetLastError()) != hipSuccess) return e;
 
   for (int k = 0; k < a.steps; ++k) {
+    const int now = k % 2, next = 1 - now;
     PairArgs g{};
-    g.a = g.b = x[k % 2];  // A = X X^T
-    g.a_ld = g.b_ld = p.m_pad;
-    g.a_low = g.b_low = p.x_low;
-    g.depth = p.m_pad;
+    g.partial = reinterpret_cast<float*>(base + p.partial);
+    g.a = g.b = x[now];  // A = X X^T
+    g.rows = g.cols = p.n_pad;
+    g.steps = m_blocks;
     g.factors = &factors[k].gram;
     g.out = gram;
-    g.out_ld = p.n_pad;
-    g.out_low = p.a_low;
-    if ((e = run_pair<T, true, true, PAIR_PAIR>(g, p.n_pad, p.n_pad, s)) != hipSuccess) return e;
+    if ((e = run_pair<T, PAIR_BLOCKS>(g, true, s)) != hipSuccess) return e;
     g.a = g.b = g.d = gram;  // P = b A + c A A^T
-    g.a_ld = g.b_ld = g.d_ld = p.n_pad;
-    g.a_low = g.b_low = g.d_low = p.a_low;
-    g.depth = p.n_pad;
+    g.steps = n_blocks;
     g.factors = &factors[k].square;
     g.out = poly;
-    if ((e = run_pair<T, true, true, PAIR_PAIR>(g, p.n_pad, p.n_pad, s)) != hipSuccess) return e;
-    const bool last = k + 1 == a.steps;
-    g.a = poly;  // a X + P X
-    g.b = g.d = x[k % 2];
-    g.b_ld = g.d_ld = p.m_pad;
-    g.b_low = g.d_low = p.x_low;
-    g.factors = &factors[k].apply;
-    if (!last) {
-      g.out = x[(k + 1) % 2];
-      g.out_ld = p.m_pad;
-      g.out_low = p.x_low;
-      e = run_pair<T, true, false, PAIR_PAIR>(g, p.n_pad, p.m_pad, s);
-    } else {
-      g.out = a.y;
-      g.out_ld = a.y_ld;
-      g.rows = a.rows;
-      g.cols = a.cols;
-      g.decay = a.decay;
-      g.step = a.step;
-      if (p.tall) {  // the transpose: rows of the result are columns of X
-        std::swap(g.a, g.b);
-        std::swap(g.a_ld, g.b_ld);
-        std::swap(g.a_low, g.b_low);
-        e = a.m ? run_pair<T, false, true, PAIR_STEP>(g, p.m_pad, p.n_pad, s)
-                : run_pair<T, false, true, PAIR_OUT>(g, p.m_pad, p.n_pad, s);
-      } else {
-        e = a.m ? run_pair<T, true, false, PAIR_STEP>(g, p.n_pad, p.m_pad, s)
-                : run_pair<T, true, false, PAIR_OUT>(g, p.n_pad, p.m_pad, s);
-      }
+    if ((e = run_pair<T, PAIR_BLOCKS>(g, true, s)) != hipSuccess) return e;
+    g.factors = &factors[k].apply;  // a X + P X
+    if (k + 1 < a.steps) {
+      g.a = poly;
+      g.b = xt[now];
+      g.d = x[now];
+      g.cols = p.m_pad;
+      g.out = x[next];
+      g.across = xt[next];
+      if ((e = run_pair<T, PAIR_BLOCKS>(g, false, s)) != hipSuccess) return e;
+      continue;
     }
-    if (e != hipSuccess) return e;
+    // the result, or its transpose: rows of a tall one are columns of X
+    g.a = p.tall ? xt[now] : poly;
+    g.b = p.tall ? poly : xt[now];
+    g.d = p.tall ? xt[now] : x[now];
+    (p.tall ? g.rows : g.cols) = p.m_pad;
+    g.y = a.y;
+    g.y_ld = a.y_ld;
+    g.y_rows = a.rows;
+    g.y_cols = a.cols;
+    g.decay = a.decay;
+    g.step = a.step;
+    e = a.m ? run_pair<T, PAIR_STEP>(g, false, s) : run_pair<T, PAIR_OUT>(g, false, s);
   }
   return e;
 }

@@ -118,7 +118,7 @@ def test_empty_calls_and_scratch():
     for rows, cols in ((1, 1), (48, 64), (1024, 4096), (4096, 1024), (1, 100000)):
         assert 0 < size(rows, cols, 1) == lib.gart_muon_scratch_bytes(rows, cols, 1)
     # a large weight's scratch stays within a few times its size in float32
-    assert size(1024, 4096, 0) <= 4 * 4 * 1024 * 4096
+    assert size(1024, 4096, 0) <= 5 * 4 * 1024 * 4096
     x = _m(gart, MB, 1 << 30, 1 << 30)
     assert lib.gart_orthogonalize(x, ctypes.byref(how), 0, x, 8 * MB, MB, None) == -4  # beyond a launch
 
