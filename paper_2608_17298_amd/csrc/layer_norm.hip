@@ -81,6 +81,7 @@ __device__ __forceinline__ void block_sums(float (&v)[COUNT], float (&s)[WAVES][
     v[q] = s[0][q];
 #pragma unroll
     for (int w = 1; w < WAVES; ++w) v[q] += s[w][q];
+    asm volatile("" : "+v"(v[q]));  // read before the barrier, also where the sum is used in a branch alone
   }
   lds_barrier();
 }

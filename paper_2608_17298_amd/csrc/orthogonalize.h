@@ -97,7 +97,7 @@ GART_HOST_DEVICE inline bool step_factors(float a, float b, float c, int steps, 
   return true;
 }
 
-// How a product is cut: square tiles of 64 or 128 a block, one block a CU, and
+// How a product is cut: square tiles of 32, 64 or 128 a block, one block a CU, and
 // parts of the sums that a second launch joins.
 struct PairCut {
   int side, parts;
@@ -110,17 +110,19 @@ inline int64_t blocks_of(int64_t rows, int64_t cols, int side, bool symmetric) {
   return symmetric ? even / 2 * (even + 1) : i * j;
 }
 inline PairCut cut_pair(int64_t rows, int64_t cols, int64_t steps, bool symmetric) {
-  // measured: us of a step of 32 terms, of what surrounds the steps, and of a join
-  constexpr double kStep64 = 0.11, kStep128 = 0.43, kAround = 3.0, kJoin = 3.0;
+  // measured: us of a block of k for each tile, and of what surrounds the sums
+  constexpr int kSides[3] = {32, 64, 128};
+  constexpr double kStep[3] = {0.10, 0.20, 0.40}, kAround = 4.0, kJoin = 3.0;
   PairCut best{64, 1, symmetric};
   double least = HUGE_VAL;
-  for (const int side : {64, 128}) {
+  for (int q = 0; q < 3; ++q) {
+    const int side = kSides[q];
     const int64_t tiles = blocks_of(rows, cols, side, symmetric);
     const int most = symmetric ? int(std::min<int64_t>(16, std::max<int64_t>(1, steps / 16))) : 1;
     for (int parts = 1; parts <= most; ++parts) {
       const double turns = double((tiles * parts + 255) / 256), length = double((steps + parts - 1) / parts);
-      double t = turns * (kAround + length * (side == 64 ? kStep64 : kStep128));
-      if (parts > 1) t += kJoin + double(tiles * parts) * (side == 64 ? 0.01 : 0.04);
+      double t = kAround + turns * length * kStep[q];
+      if (parts > 1) t += kJoin + double(tiles * parts) * double(side * side) * 2e-6;
       if (t < least) {
         least = t;
         best.side = side;
@@ -140,7 +142,7 @@ struct MatrixPlan {
   bool tall;            // more rows than columns: X is the transpose
   int64_t n, m;         // the smaller and the larger size
   int64_t n_pad, m_pad;  // multiples of kTileSide
-  size_t sums, factors, x[2], xt[2], a, p, partial, total;
+  size_t sums, factors, x[2], xt[2], a, p, total;
 };
 constexpr int64_t kSumBlocks = 256;  // partial sums of squares
 constexpr int64_t kMostTiles = int64_t(1) << 23;
@@ -155,15 +157,16 @@ inline MatrixPlan matrix_plan(int64_t rows, int64_t cols) {
   const size_t x = size_t(p.n_pad) * size_t(p.m_pad) * 4, a = size_t(p.n_pad) * size_t(p.n_pad) * 4;  // two float16
   p.sums = 0;
   p.factors = kSumBlocks * sizeof(double);
+  // The X that a step writes is free until then, for the parts of the products before it.
+  const size_t partial = 4 * std::max(partial_floats(p.n_pad, p.m_pad / 32), partial_floats(p.n_pad, p.n_pad / 32));
+  const size_t both = std::max(2 * x, partial);
   p.x[0] = p.factors + sizeof(StepFactors) * kMaxSteps;
-  p.x[1] = p.x[0] + x;
-  p.xt[0] = p.x[1] + x;
-  p.xt[1] = p.xt[0] + x;
-  p.a = p.xt[1] + x;
+  p.x[1] = p.x[0] + both;
+  p.xt[0] = p.x[0] + x;
+  p.xt[1] = p.x[1] + x;
+  p.a = p.x[1] + both;
   p.p = p.a + a;
-  p.partial = p.p + a;
-  p.total = p.partial + 4 * std::max(partial_floats(p.n_pad, p.m_pad / 32),
-                                     partial_floats(p.n_pad, p.n_pad / 32));
+  p.total = p.p + a;
   return p;
 }
 

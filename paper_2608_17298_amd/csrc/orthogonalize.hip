@@ -81,15 +81,16 @@ struct Blocks {
   __device__ __forceinline__ f16* at(int64_t i, int64_t k) const { return data + (i * across + k) * kPair; }
 };
 
-// Of a 64 x 64 tile in LDS, element (i, j) at tile[i * pitch + j], into blocks: those
-// of rows i, or, transposed, of rows j.  Values are split into two parts.
+// Of a tile in LDS, element (i, j) at tile[i * pitch + j], into blocks: those of rows
+// i, or, transposed, of rows j.  Values are split into two parts.
 constexpr int kTilePitch = 64 + 4;
-template <bool TRANSPOSED>
+template <int SIDE, bool TRANSPOSED>
 __device__ __forceinline__ void store_blocks(const float* tile, const Blocks& to, int64_t row0, int64_t col0, int lane,
                                              int first, int step) {
   const int r = lane % 16, g = lane / 16;
-  for (int b = first; b < 8; b += step) {
-    const int row = 16 * (b / 2) + r, k = 32 * (b % 2) + 8 * g;
+  constexpr int DEEP = SIDE / 32;
+  for (int b = first; b < SIDE / 16 * DEEP; b += step) {
+    const int row = 16 * (b / DEEP) + r, k = 32 * (b % DEEP) + 8 * g;
     Pack<f16> high, low;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
@@ -98,7 +99,7 @@ __device__ __forceinline__ void store_blocks(const float* tile, const Blocks& to
       high.v[e] = h;
       low.v[e] = l;
     }
-    f16* block = to.at(row0 / 16 + b / 2, col0 / 32 + b % 2) + lane * 8;
+    f16* block = to.at(row0 / 16 + b / DEEP, col0 / 32 + b % DEEP) + lane * 8;
     store_pack(block, high);
     store_pack(block + Blocks::kBlock, low);
   }
@@ -145,8 +146,8 @@ __global__ __launch_bounds__(kThreads) void prepare_kernel(const Source<T> u, in
     s_tile[i * kTilePitch + j] = v;
   }
   __syncthreads();
-  store_blocks<false>(s_tile, x, i0, j0, lane, wave, kThreads / 64);
-  store_blocks<true>(s_tile, xt, j0, i0, lane, wave, kThreads / 64);
+  store_blocks<64, false>(s_tile, x, i0, j0, lane, wave, kThreads / 64);
+  store_blocks<64, true>(s_tile, xt, j0, i0, lane, wave, kThreads / 64);
 }
 
 // ---- products of pairs ----------------------------------------------------------
@@ -193,142 +194,289 @@ __device__ __forceinline__ bool find_tile(const PairArgs& g, int b, int total, i
   return ti < n && tj < g.tiles_j;
 }
 
-// A wave has 64 x 64 elements: WI x WJ waves a block, and WK of them take every WK-th
-// block of k.  Two fragments' loads are on their way while one set is multiplied: the
-// waves meet only when their sums are joined, in LDS.  JOIN: the sums of k are those
-// of g.parts parts.
-constexpr int kSide = 64, kFrag = 4;  // 16-row tiles a wave's side
-template <typename T, int WI, int WJ, int WK, PairEpilogue EPI, bool JOIN>
-__global__ __launch_bounds__(64 * WI * WJ * WK, 1) void pair_kernel(const PairArgs g) {
-  constexpr int WAVES = WI * WJ * WK, THREADS = 64 * WAVES;
-  constexpr int ROWS = kFrag / WK;  // 16-row tiles of a wave's result
-  static_assert(WK == 1 || (WI == 1 && WJ == 1 && WK == kFrag), "one tile, or waves that share nothing");
-  // joined sums, then tiles that are transposed
-  __shared__ __attribute__((aligned(16))) float lds[WK > 1 && !JOIN ? WK * kSide * kSide
-                                                    : EPI == PAIR_BLOCKS ? WI * WJ * kSide * kTilePitch : 4];
+// The sums of a product, two ways:
+//
+//  - Waves that split k (WK of them).  Each has all FRAG x FRAG fragments of the tile
+//    and takes every WK-th block of k straight from memory: nothing is shared, so
+//    nothing passes through LDS.  Two sets of fragments are on their way while one is
+//    multiplied; the waves meet when their sums are joined.  Bound by the bytes a CU
+//    takes in (100 a ns from its cache, 65 from another die's), for products with few
+//    tiles.
+//  - W x W waves of 64 x 64 that share the operands in LDS (tiles of 128).  Four
+//    blocks of k are there or on their way; the next fragments are read while the last
+//    ones are multiplied.
+template <int FRAG>
+struct Fragments {
+  Pack<f16>::V ah[FRAG], al[FRAG], bh[FRAG], bl[FRAG];
+};
+template <int FRAG>
+__device__ __forceinline__ void multiply(f32x4 (&sum)[FRAG][FRAG], const Fragments<FRAG>& f) {
+#pragma unroll
+  for (int p = 0; p < 3; ++p)
+#pragma unroll
+    for (int i = 0; i < FRAG; ++i)
+#pragma unroll
+      for (int j = 0; j < FRAG; ++j)
+        sum[i][j] = Mfma<f16>::run(p == 0 ? f.bl[j] : f.bh[j], p == 1 ? f.al[i] : f.ah[i], sum[i][j]);
+}
+
+template <int FRAG, int WK, typename F>
+__device__ __forceinline__ void split_sums(f32x4 (&sum)[FRAG][FRAG], const PairArgs& g, int64_t i0, int64_t j0, int k0,
+                                           int k1, int lane, F&& meanwhile) {
+  const int64_t a_row = g.a.across * Blocks::kPair, b_row = g.b.across * Blocks::kPair;
+  const f16* a = g.a.at(i0 / 16, k0) + lane * 8;
+  const f16* b = g.b.at(j0 / 16, k0) + lane * 8;
+  Fragments<FRAG> set[3];
+  auto load = [&](Fragments<FRAG>& f, int n) {  // past the end the last one again
+    const int64_t at = int64_t(min(n, (k1 - 1 - k0) / WK)) * (WK * Blocks::kPair);
+#pragma unroll
+    for (int i = 0; i < FRAG; ++i) {
+      f.ah[i] = *reinterpret_cast<const Pack<f16>::V*>(a + i * a_row + at);
+      f.al[i] = *reinterpret_cast<const Pack<f16>::V*>(a + i * a_row + at + Blocks::kBlock);
+      f.bh[i] = *reinterpret_cast<const Pack<f16>::V*>(b + i * b_row + at);
+      f.bl[i] = *reinterpret_cast<const Pack<f16>::V*>(b + i * b_row + at + Blocks::kBlock);
+    }
+    __builtin_amdgcn_sched_barrier(0);  // asked for here, not where they are used
+  };
+  auto product = [&](const Fragments<FRAG>& f) {
+    multiply<FRAG>(sum, f);
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  const int count = (k1 - k0 + WK - 1) / WK;
+  load(set[0], 0);
+  load(set[1], 1);
+  meanwhile();
+  int n = 0;
+  for (; n + 2 < count; n += 3) {
+    load(set[2], n + 2);
+    product(set[0]);
+    load(set[0], n + 3);
+    product(set[1]);
+    load(set[1], n + 4);
+    product(set[2]);
+  }
+  if (n < count) product(set[0]);
+  if (n + 1 < count) product(set[1]);
+}
+
+constexpr int kStages = 4;
+template <int W>
+__device__ __forceinline__ void shared_sums(f32x4 (&sum)[4][4], const PairArgs& g, int64_t ti, int64_t tj, int k0, int k1,
+                                            int wave, int lane, f16* lds) {
+  // a stage: 4 W row tiles of A, then of B, each a pair of blocks
+  constexpr int TILES = 4 * W, STAGE = 2 * TILES * Blocks::kPair, WAVES = W * W, MINE = TILES / WAVES;
+  static_assert(TILES % WAVES == 0, "whole tiles a wave");
+  typedef const __attribute__((address_space(1))) uint32_t* global_ptr;
+  typedef __attribute__((address_space(3))) uint32_t* lds_ptr;
+  const int64_t a_last = g.rows / 16 - 1, b_last = g.cols / 16 - 1;  // tiles past the end: the last one again
+  const f16 *a[MINE], *b[MINE];
+#pragma unroll
+  for (int u = 0; u < MINE; ++u) {
+    a[u] = g.a.at(min(ti * TILES + wave * MINE + u, a_last), 0) + lane * 8;
+    b[u] = g.b.at(min(tj * TILES + wave * MINE + u, b_last), 0) + lane * 8;
+  }
+  auto fetch = [&](int k) {  // past the end the last one again: the waits below count on it
+    f16* to = lds + k % kStages * STAGE + wave * MINE * Blocks::kPair;
+    const int64_t at = int64_t(min(k, k1 - 1)) * Blocks::kPair;
+#pragma unroll
+    for (int u = 0; u < MINE; ++u)
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        const int64_t off = half * Blocks::kBlock;
+        __builtin_amdgcn_global_load_lds((global_ptr)(a[u] + at + off), (lds_ptr)(to + u * Blocks::kPair + off), 16, 0, 0);
+        __builtin_amdgcn_global_load_lds((global_ptr)(b[u] + at + off),
+                                         (lds_ptr)(to + (TILES + u) * Blocks::kPair + off), 16, 0, 0);
+      }
+  };
+  const int wi = wave / W, wj = wave % W;
+  auto read = [&](Fragments<4>& f, int k) {
+    const f16* from = lds + k % kStages * STAGE + lane * 8;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const f16* p = from + (wi * 4 + i) * Blocks::kPair;
+      const f16* q = from + (TILES + wj * 4 + i) * Blocks::kPair;
+      f.ah[i] = *reinterpret_cast<const Pack<f16>::V*>(p);
+      f.al[i] = *reinterpret_cast<const Pack<f16>::V*>(p + Blocks::kBlock);
+      f.bh[i] = *reinterpret_cast<const Pack<f16>::V*>(q);
+      f.bl[i] = *reinterpret_cast<const Pack<f16>::V*>(q + Blocks::kBlock);
+    }
+  };
+  constexpr int LOADS = 4 * MINE;
+  auto arrived = [&]() {
+    // this wave's part of the oldest stage has landed, and it has read the one before
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((kStages - 2) * LOADS) : "memory");
+    __builtin_amdgcn_s_barrier();  // so has everyone's, and have they
+    asm volatile("" ::: "memory");
+  };
+  // Reads of the next fragments among the products of the last.
+  auto interleave = [&]() {
+#pragma unroll
+    for (int q = 0; q < 16; ++q) {
+      __builtin_amdgcn_sched_group_barrier(0x008, 3, 0);  // matrix instructions
+      __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);  // LDS reads
+    }
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  Fragments<4> even, odd;
+#pragma unroll
+  for (int h = 0; h < kStages - 1; ++h) fetch(k0 + h);
+  arrived();
+  fetch(k0 + kStages - 1);
+  read(even, k0);
+  __builtin_amdgcn_sched_barrier(0);
+  int k = k0 + 1;
+  for (; k + 1 < k1; k += 2) {
+    arrived();
+    fetch(k + kStages - 1);
+    read(odd, k);
+    multiply<4>(sum, even);
+    interleave();
+    arrived();
+    fetch(k + kStages);
+    read(even, k + 1);
+    multiply<4>(sum, odd);
+    interleave();
+  }
+  if (k < k1) {
+    arrived();
+    read(odd, k);
+    multiply<4>(sum, even);
+    multiply<4>(sum, odd);
+  } else {
+    multiply<4>(sum, even);
+  }
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // nothing lands once LDS holds something else
+}
+
+// A tile of 16 FRAG W on a side.  JOIN: the sums of k are those of g.parts parts.
+template <typename T, int FRAG, int W, int WK, PairEpilogue EPI, bool JOIN>
+__global__ __launch_bounds__(64 * W * W * WK, 1) void pair_kernel(const PairArgs g) {
+  constexpr int THREADS = 64 * W * W * WK, SIDE = 16 * FRAG;  // of a wave's tile
+  constexpr bool SPLIT = WK > 1;
+  static_assert(SPLIT ? W == 1 && WK == 4 : FRAG == 4, "four waves of one tile, or tiles of 64");
+  // 16 x 16 tiles of a wave's result: FRAG by FRAG, or its share of them
+  constexpr int RI = SPLIT ? 1 : FRAG, RJ = SPLIT ? FRAG * FRAG / WK : FRAG;
+  constexpr int SUMS = JOIN ? 0 : SPLIT ? WK * SIDE * SIDE : kStages * 2 * 4 * W * Blocks::kPair / 2;  // floats
+  constexpr int TILE = EPI == PAIR_BLOCKS ? W * W * SIDE * kTilePitch : 4;
+  __shared__ __attribute__((aligned(16))) float lds[SUMS > TILE ? SUMS : TILE];
   const int tid = threadIdx.x, lane = tid % 64, wave = __builtin_amdgcn_readfirstlane(tid / 64);
-  const int wk = wave % WK, wi = wave / WK / WJ, wj = wave / WK % WJ;
   int ti, tj;
   if (!find_tile(g, blockIdx.x, gridDim.x, ti, tj)) return;
-  const int64_t i0 = (int64_t(ti) * WI + wi) * kSide, j0 = (int64_t(tj) * WJ + wj) * kSide;
+  const int wi = SPLIT ? 0 : wave / W, wj = SPLIT ? 0 : wave % W;
+  const int64_t i0 = (int64_t(ti) * W + wi) * SIDE, j0 = (int64_t(tj) * W + wj) * SIDE;
   const bool inside = i0 < g.rows && j0 < g.cols;
+  const int first_i = SPLIT ? wave * RJ / FRAG : 0, first_j = SPLIT ? wave * RJ % FRAG : 0;
+  const int r = lane % 16, g4 = lane / 16;
+  typedef f16 f16x4 __attribute__((ext_vector_type(4)));
+  // A lane has four consecutive columns of a row; of D they are half a piece.
+  auto d_at = [&](int i, int j) {
+    const int row = 16 * (first_i + i), col = 16 * (first_j + j) + 4 * g4;
+    return g.d.at((i0 + row) / 16, (j0 + col) / 32) + (((j0 + col) % 32) / 8 * 16 + r) * 8 + col % 8;
+  };
+  f16x4 dh[SPLIT ? RI : 1][SPLIT ? RJ : 1], dl[SPLIT ? RI : 1][SPLIT ? RJ : 1];
+  float alpha, beta;
+  // What the result takes besides the sums, asked for before they are formed.
+  auto others = [&]() {
+    if constexpr (EPI != PAIR_PART) {
+      alpha = g.factors[0];
+      beta = g.factors[1];
+      if constexpr (SPLIT) {
+        if (g.d.data) {
+#pragma unroll
+          for (int i = 0; i < RI; ++i)
+#pragma unroll
+            for (int j = 0; j < RJ; ++j) {
+              dh[i][j] = *reinterpret_cast<const f16x4*>(d_at(i, j));
+              dl[i][j] = *reinterpret_cast<const f16x4*>(d_at(i, j) + Blocks::kBlock);
+            }
+        }
+      }
+    }
+  };
 
-  f32x4 acc[ROWS][kFrag];
+  f32x4 acc[RI][RJ];
   if constexpr (JOIN) {
+    others();
 #pragma unroll
-    for (int i = 0; i < ROWS; ++i)
+    for (int i = 0; i < RI; ++i)
 #pragma unroll
-      for (int j = 0; j < kFrag; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+      for (int j = 0; j < RJ; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     for (int part = 0; part < g.parts; ++part) {
-      const float* from = g.partial + (int64_t(part) * gridDim.x + blockIdx.x) * (THREADS * ROWS * kFrag * 4) + tid * 4;
+      const float* from = g.partial + (int64_t(part) * gridDim.x + blockIdx.x) * (THREADS * RI * RJ * 4) + tid * 4;
 #pragma unroll
-      for (int i = 0; i < ROWS; ++i)
+      for (int i = 0; i < RI; ++i)
 #pragma unroll
-        for (int j = 0; j < kFrag; ++j)
-          acc[i][j] += *reinterpret_cast<const f32x4*>(from + (i * kFrag + j) * THREADS * 4);
+        for (int j = 0; j < RJ; ++j) acc[i][j] += *reinterpret_cast<const f32x4*>(from + (i * RJ + j) * THREADS * 4);
     }
   } else {
-    f32x4 sum[kFrag][kFrag];
+    f32x4 sum[FRAG][FRAG];
 #pragma unroll
-    for (int i = 0; i < kFrag; ++i)
+    for (int i = 0; i < FRAG; ++i)
 #pragma unroll
-      for (int j = 0; j < kFrag; ++j) sum[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+      for (int j = 0; j < FRAG; ++j) sum[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     const int part = EPI == PAIR_PART ? int(blockIdx.y) : 0, parts = EPI == PAIR_PART ? g.parts : 1;
-    const int k0 = int(g.steps * part / parts) + wk, k1 = int(g.steps * (part + 1) / parts);
-    if (inside && k0 < k1) {
-      const int64_t a_row = g.a.across * Blocks::kPair, b_row = g.b.across * Blocks::kPair;
-      const f16* a = g.a.at(i0 / 16, k0) + lane * 8;
-      const f16* b = g.b.at(j0 / 16, k0) + lane * 8;
-      struct Set {
-        Pack<f16>::V ah[kFrag], al[kFrag], bh[kFrag], bl[kFrag];
-      } set[3];
-      auto load = [&](Set& f, int n) {  // past the end the last one again
-        const int64_t at = int64_t(min(n, (k1 - 1 - k0) / WK)) * (WK * Blocks::kPair);
+    const int k0 = int(g.steps * part / parts), k1 = int(g.steps * (part + 1) / parts);
+    if constexpr (!SPLIT) {
+      shared_sums<W>(sum, g, ti, tj, k0, k1, wave, lane, reinterpret_cast<f16*>(lds));
+      others();
 #pragma unroll
-        for (int i = 0; i < kFrag; ++i) {
-          f.ah[i] = *reinterpret_cast<const Pack<f16>::V*>(a + i * a_row + at);
-          f.al[i] = *reinterpret_cast<const Pack<f16>::V*>(a + i * a_row + at + Blocks::kBlock);
-          f.bh[i] = *reinterpret_cast<const Pack<f16>::V*>(b + i * b_row + at);
-          f.bl[i] = *reinterpret_cast<const Pack<f16>::V*>(b + i * b_row + at + Blocks::kBlock);
-        }
-        __builtin_amdgcn_sched_barrier(0);  // loads are asked for here, not where they are used
-      };
-      auto multiply = [&](const Set& f) {
+      for (int i = 0; i < FRAG; ++i)
 #pragma unroll
-        for (int p = 0; p < 3; ++p)
-#pragma unroll
-          for (int i = 0; i < kFrag; ++i)
-#pragma unroll
-            for (int j = 0; j < kFrag; ++j)
-              sum[i][j] = Mfma<f16>::run(p == 0 ? f.bl[j] : f.bh[j], p == 1 ? f.al[i] : f.ah[i], sum[i][j]);
-        __builtin_amdgcn_sched_barrier(0);
-      };
-      const int count = (k1 - k0 + WK - 1) / WK;
-      load(set[0], 0);
-      load(set[1], 1);
-      int n = 0;
-      for (; n + 2 < count; n += 3) {
-        load(set[2], n + 2);
-        multiply(set[0]);
-        load(set[0], n + 3);
-        multiply(set[1]);
-        load(set[1], n + 4);
-        multiply(set[2]);
-      }
-      if (n < count) multiply(set[0]);
-      if (n + 1 < count) multiply(set[1]);
-    }
-    if constexpr (WK == 1) {
-#pragma unroll
-      for (int i = 0; i < kFrag; ++i)
-#pragma unroll
-        for (int j = 0; j < kFrag; ++j) acc[i][j] = sum[i][j];
+        for (int j = 0; j < FRAG; ++j) acc[i][j] = sum[i][j];
+      __syncthreads();
     } else {
-      // wave w takes the 16-row tile w of the others
+      if (k0 + wave < k1)
+        split_sums<FRAG, WK>(sum, g, i0, j0, k0 + wave, k1, lane, others);
+      else
+        others();
 #pragma unroll
-      for (int i = 0; i < kFrag; ++i)
+      for (int i = 0; i < FRAG; ++i)
 #pragma unroll
-        for (int j = 0; j < kFrag; ++j)
-          *reinterpret_cast<f32x4*>(lds + ((wave * kFrag + i) * kFrag + j) * 256 + lane * 4) = sum[i][j];
+        for (int j = 0; j < FRAG; ++j)
+          *reinterpret_cast<f32x4*>(lds + ((wave * FRAG + i) * FRAG + j) * 256 + lane * 4) = sum[i][j];
       __syncthreads();
 #pragma unroll
-      for (int j = 0; j < kFrag; ++j) {
+      for (int j = 0; j < RJ; ++j) {
         acc[0][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
         for (int w = 0; w < WK; ++w)
-          acc[0][j] += *reinterpret_cast<const f32x4*>(lds + ((w * kFrag + wave) * kFrag + j) * 256 + lane * 4);
+          acc[0][j] += *reinterpret_cast<const f32x4*>(
+              lds + ((w * FRAG + first_i) * FRAG + first_j + j) * 256 + lane * 4);
+        arrive(acc[0][j]);  // the compiler moved these reads behind the barrier, where the tile is written over them
       }
       __syncthreads();
     }
   }
 
   if constexpr (EPI == PAIR_PART) {
-    float* to = g.partial + (int64_t(blockIdx.y) * gridDim.x + blockIdx.x) * (THREADS * ROWS * kFrag * 4) + tid * 4;
+    float* to = g.partial + (int64_t(blockIdx.y) * gridDim.x + blockIdx.x) * (THREADS * RI * RJ * 4) + tid * 4;
 #pragma unroll
-    for (int i = 0; i < ROWS; ++i)
+    for (int i = 0; i < RI; ++i)
 #pragma unroll
-      for (int j = 0; j < kFrag; ++j) *reinterpret_cast<f32x4*>(to + (i * kFrag + j) * THREADS * 4) = acc[i][j];
+      for (int j = 0; j < RJ; ++j) *reinterpret_cast<f32x4*>(to + (i * RJ + j) * THREADS * 4) = acc[i][j];
     return;
   }
 
-  // The fragments of B are not paired up: a lane has four consecutive columns of a row.
-  const int r = lane % 16, g4 = lane / 16;
-  const float alpha = g.factors[0], beta = g.factors[1];
-  float* tile = lds + (WK > 1 ? 0 : wave * kSide * kTilePitch);
+  float* tile = lds + (SPLIT ? 0 : wave * SIDE * kTilePitch);
   if (inside) {
 #pragma unroll
-    for (int i = 0; i < ROWS; ++i) {
-      const int row = 16 * (WK > 1 ? wave : i) + r;
+    for (int i = 0; i < RI; ++i) {
+      const int row = 16 * (first_i + i) + r;
 #pragma unroll
-      for (int j = 0; j < kFrag; ++j) {
-        const int col = 16 * j + 4 * g4;
+      for (int j = 0; j < RJ; ++j) {
+        const int col = 16 * (first_j + j) + 4 * g4;
         f32x4 c = alpha * acc[i][j];
         if (g.d.data) {
-          typedef f16 f16x4 __attribute__((ext_vector_type(4)));
-          const f16* d = g.d.at((i0 + row) / 16, (j0 + col) / 32) + ((col % 32) / 8 * 16 + r) * 8 + col % 8;
-          const f16x4 dh = *reinterpret_cast<const f16x4*>(d), dl = *reinterpret_cast<const f16x4*>(d + Blocks::kBlock);
+          f16x4 h, l;
+          if constexpr (SPLIT) {
+            h = dh[i][j];
+            l = dl[i][j];
+          } else {
+            h = *reinterpret_cast<const f16x4*>(d_at(i, j));
+            l = *reinterpret_cast<const f16x4*>(d_at(i, j) + Blocks::kBlock);
+          }
 #pragma unroll
-          for (int e = 0; e < 4; ++e) c[e] = fmaf(beta, float(dh[e]) + float(dl[e]), c[e]);
+          for (int e = 0; e < 4; ++e) c[e] = fmaf(beta, float(h[e]) + float(l[e]), c[e]);
         }
         if constexpr (EPI == PAIR_BLOCKS) {
           *reinterpret_cast<f32x4*>(tile + row * kTilePitch + col) = c;
@@ -365,17 +513,16 @@ __global__ __launch_bounds__(64 * WI * WJ * WK, 1) void pair_kernel(const PairAr
   if constexpr (EPI == PAIR_BLOCKS) {
     __syncthreads();
     if (!inside) return;
-    constexpr int SHARE = WK;  // waves that store the tile
-    store_blocks<false>(tile, g.out, i0, j0, lane, wk, SHARE);
-    if (g.symmetric) {
-      if (i0 != j0) store_blocks<true>(tile, g.out, j0, i0, lane, wk, SHARE);
-    } else {
-      store_blocks<true>(tile, g.across, j0, i0, lane, wk, SHARE);
-    }
+    const int mine = SPLIT ? wave : 0;
+    store_blocks<SIDE, false>(tile, g.out, i0, j0, lane, mine, WK);
+    if (!g.symmetric)
+      store_blocks<SIDE, true>(tile, g.across, j0, i0, lane, WK - 1 - mine, WK);
+    else if (i0 != j0)
+      store_blocks<SIDE, true>(tile, g.out, j0, i0, lane, WK - 1 - mine, WK);
   }
 }
 
-template <typename T, int W, int WK, PairEpilogue EPI>
+template <typename T, int FRAG, int W, int WK, PairEpilogue EPI>
 hipError_t run_tiles(PairArgs g, const PairCut& c, hipStream_t s) {
   g.tiles_i = int((g.rows + c.side - 1) / c.side);
   g.tiles_j = int((g.cols + c.side - 1) / c.side);
@@ -386,14 +533,14 @@ hipError_t run_tiles(PairArgs g, const PairCut& c, hipStream_t s) {
   while (g.band * g.band * 8 < int(blocks)) ++g.band;
   constexpr int THREADS = 64 * W * W * WK;
   if (c.parts == 1) {
-    pair_kernel<T, W, W, WK, EPI, false><<<blocks, THREADS, 0, s>>>(g);
+    pair_kernel<T, FRAG, W, WK, EPI, false><<<blocks, THREADS, 0, s>>>(g);
     return hipGetLastError();
   }
   if constexpr (EPI == PAIR_BLOCKS) {
-    pair_kernel<T, W, W, WK, PAIR_PART, false><<<dim3(blocks, uint32_t(c.parts)), THREADS, 0, s>>>(g);
+    pair_kernel<T, FRAG, W, WK, PAIR_PART, false><<<dim3(blocks, uint32_t(c.parts)), THREADS, 0, s>>>(g);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    pair_kernel<T, W, W, WK, PAIR_BLOCKS, true><<<blocks, THREADS, 0, s>>>(g);
+    pair_kernel<T, FRAG, W, WK, PAIR_BLOCKS, true><<<blocks, THREADS, 0, s>>>(g);
     return hipGetLastError();
   }
   return hipErrorInvalidValue;
@@ -402,8 +549,9 @@ hipError_t run_tiles(PairArgs g, const PairCut& c, hipStream_t s) {
 template <typename T, PairEpilogue EPI>
 hipError_t run_pair(const PairArgs& g, bool symmetric, hipStream_t s) {
   const PairCut c = cut_pair(g.rows, g.cols, g.steps, symmetric);
-  if (c.side == 64) return run_tiles<T, 1, 4, EPI>(g, c, s);
-  return run_tiles<T, 2, 1, EPI>(g, c, s);
+  if (c.side == 32) return run_tiles<T, 2, 1, 4, EPI>(g, c, s);
+  if (c.side == 64) return run_tiles<T, 4, 1, 4, EPI>(g, c, s);
+  return run_tiles<T, 4, 2, 1, EPI>(g, c, s);
 }
 
 template <typename T>
@@ -432,7 +580,7 @@ hipError_t run(const OrthogonalizeArgs& a, hipStream_t s) {
   for (int k = 0; k < a.steps; ++k) {
     const int now = k % 2, next = 1 - now;
     PairArgs g{};
-    g.partial = reinterpret_cast<float*>(base + p.partial);
+    g.partial = reinterpret_cast<float*>(base + p.x[next]);
     g.a = g.b = x[now];  // A = X X^T
     g.rows = g.cols = p.n_pad;
     g.steps = m_blocks;
