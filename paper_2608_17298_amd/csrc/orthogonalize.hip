@@ -13,32 +13,13 @@
 // bfloat16's rounding of the result.  Large float32 products run at 154 TFLOP/s on
 // this card and float16 ones at 1430, so three of those are a third of the time.
 // a X is added in float: inside P it would double the error.
-#include "blocks.h"
-#include "orthogonalize.h"
+#include "orthogonalize_small.h"
 #include "tile.h"
 
 namespace gart {
 namespace {
 
 constexpr int kThreads = 256;
-
-// ---- the matrix that is orthogonalised ----------------------------------------
-// x itself, or of a momentum step u = g + mu m (Nesterov) or m, with m already
-// stepped: the same operations wherever it is formed.
-template <typename T>
-struct Source {
-  const T* x;
-  int64_t ld;
-  const float* m;  // NULL: x itself
-  int64_t m_ld;
-  float momentum;
-  bool nesterov;
-  __device__ __forceinline__ float at(int64_t r, int64_t c) const {
-    if (!m) return float(x[r * ld + c]);
-    const float v = m[r * m_ld + c];
-    return nesterov ? fmaf(momentum, v, float(x[r * ld + c])) : v;
-  }
-};
 
 // m <- momentum m + g (if there is m), and the sum of squares of what is to be
 // orthogonalised, in 64 bits: float's squares would overflow from 2e19 on.
@@ -60,26 +41,6 @@ __global__ __launch_bounds__(kThreads) void squares_kernel(const Source<T> u, fl
   __syncthreads();
   if (threadIdx.x == 0) sums[blockIdx.x] = (s[0] + s[1]) + (s[2] + s[3]);
 }
-
-// A float as high + low.
-__device__ __forceinline__ void split(float v, f16& high, f16& low) {
-  high = f16(v);
-  low = f16(v - float(high));
-}
-
-// ---- matrices in the order of fragments ------------------------------------------
-// The matrix instruction takes 16 rows by 32 k of an operand, eight consecutive k of
-// row r = lane % 16 from k = 8 (lane / 16) in each lane.  X, A and P are stored in
-// such blocks, a kilobyte of high parts and one of low parts, side by side along k:
-// a wave loads a fragment as it stands, past LDS.  X is stored twice, as itself for
-// X X^T and transposed for P X; A and P are symmetric.
-struct Blocks {
-  f16* data;
-  int64_t across;  // blocks along k
-  static constexpr int kBlock = 16 * 32, kPair = 2 * kBlock;  // elements
-  // the block of rows 16 i and k 32 k
-  __device__ __forceinline__ f16* at(int64_t i, int64_t k) const { return data + (i * across + k) * kPair; }
-};
 
 // Of a tile in LDS, element (i, j) at tile[i * pitch + j], into blocks: those of rows
 // i, or, transposed, of rows j.  Values are split into two parts.
@@ -107,11 +68,6 @@ __device__ __forceinline__ void store_blocks(const float* tile, const Blocks& to
 
 // X and its transpose, zero in the padding, from u over its norm: 64 x 64 elements a
 // block; and the steps' factors, by the first one.
-struct Iteration {
-  float a, b, c, eps;
-  int steps;
-  Factors of_one;  // of values that start at 1
-};
 template <typename T>
 __global__ __launch_bounds__(kThreads) void prepare_kernel(const Source<T> u, int64_t n, int64_t m, bool tall,
                                                            const double* __restrict__ sums, const Iteration it,
@@ -126,15 +82,15 @@ __global__ __launch_bounds__(kThreads) void prepare_kernel(const Source<T> u, in
   for (int off = 32; off > 0; off >>= 1) t += __shfl_xor(t, off);
   if (lane == 0) s_sum[wave] = t;
   __syncthreads();
-  const double size = sqrt((s_sum[0] + s_sum[1]) + (s_sum[2] + s_sum[3])), norm = size + double(it.eps);
-  const bool tiny = size / norm < kNearOne;  // not if it is a NaN
-  const double inv = (tiny ? pair_scale(size / norm, kMostX) : double(it.of_one.x)) / norm;
+  const double size = sqrt((s_sum[0] + s_sum[1]) + (s_sum[2] + s_sum[3]));
+  bool tiny;
+  const double inv = first_scale(it, size, tiny);
   if (blockIdx.x == 0 && blockIdx.y == 0) {
     if (!tiny) {
       if (threadIdx.x < it.steps) factors[threadIdx.x] = it.of_one.step[threadIdx.x];
     } else if (threadIdx.x == 0) {
       float first;
-      step_factors(it.a, it.b, it.c, it.steps, size / norm, &first, factors);
+      step_factors(it.a, it.b, it.c, it.steps, size / (size + double(it.eps)), &first, factors);
     }
   }
   const int64_t i0 = int64_t(blockIdx.y) * 64, j0 = int64_t(blockIdx.x) * 64;
@@ -560,6 +516,7 @@ hipError_t run(const OrthogonalizeArgs& a, hipStream_t s) {
   const MatrixPlan p = matrix_plan(a.rows, a.cols);
   Iteration it{a.a, a.b, a.c, a.eps, a.steps, {}};
   if (!step_factors(a.a, a.b, a.c, a.steps, 1.0, &it.of_one.x, it.of_one.step)) return hipErrorInvalidValue;
+  if (small_fits(p)) return run_small<T>(a, p, it, s);
   char* base = static_cast<char*>(a.scratch);
   double* sums = reinterpret_cast<double*>(base + p.sums);
   StepFactors* factors = reinterpret_cast<StepFactors*>(base + p.factors);
