@@ -144,7 +144,7 @@ struct MatrixPlan {
   int64_t n_pad, m_pad;  // multiples of kTileSide
   size_t sums, factors, x[2], xt[2], a, p, total;
 };
-constexpr int64_t kSumBlocks = 256;  // partial sums of squares
+constexpr int64_t kSumBlocks = 1024;  // partial sums of squares, at most
 constexpr int64_t kMostTiles = int64_t(1) << 23;
 
 inline MatrixPlan matrix_plan(int64_t rows, int64_t cols) {

@@ -22,22 +22,48 @@ namespace {
 constexpr int kThreads = 256;
 
 // m <- momentum m + g (if there is m), and the sum of squares of what is to be
-// orthogonalised, in 64 bits: float's squares would overflow from 2e19 on.
-template <typename T>
-__global__ __launch_bounds__(kThreads) void squares_kernel(const Source<T> u, float* m, int64_t rows, int64_t cols,
-                                                           double* __restrict__ sums) {
+// orthogonalised, in 64 bits: float's squares would overflow from 2e19 on.  A row is
+// 2^log_lanes threads', a pack each at a time.
+template <typename T, bool MOMENTUM>
+__global__ __launch_bounds__(kThreads) void squares_kernel(const Source<T> u, float* __restrict__ m, int64_t rows,
+                                                           int64_t cols, int log_lanes, double* __restrict__ sums) {
+  constexpr int V = Pack<T>::N;
   __shared__ double s[kThreads / 64];
-  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+  const int lanes = 1 << log_lanes, lane = threadIdx.x % lanes, high = kThreads >> log_lanes;
   double t = 0.0;
-  for (int64_t r = int64_t(blockIdx.x) * (kThreads / 64) + wave; r < rows; r += int64_t(gridDim.x) * (kThreads / 64))
-    for (int64_t c = lane; c < cols; c += 64) {
-      if (m) m[r * u.m_ld + c] = fmaf(u.momentum, m[r * u.m_ld + c], float(u.x[r * u.ld + c]));
-      const double v = double(u.at(r, c));
-      t = fma(v, v, t);
+  for (int64_t r = int64_t(blockIdx.x) * high + (threadIdx.x >> log_lanes); r < rows; r += int64_t(gridDim.x) * high)
+    for (int64_t c = int64_t(lane) * V; c < cols; c += int64_t(lanes) * V) {
+      const int count = int(min(int64_t(V), cols - c));
+      const Pack<T> x = load_some(u.x + r * u.ld + c, count);
+      float w[V];
+      if constexpr (MOMENTUM) {
+        float* to = m + r * u.m_ld + c;
+#pragma unroll
+        for (int h = 0; h < V / 4; ++h) {
+          if (count <= 4 * h) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) w[4 * h + e] = 0.0f;
+            continue;
+          }
+          Pack<float> f = load_some(to + 4 * h, count - 4 * h);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float g = float(x.v[4 * h + e]);
+            f.v[e] = fmaf(u.momentum, f.v[e], g);
+            w[4 * h + e] = u.nesterov ? fmaf(u.momentum, f.v[e], g) : f.v[e];
+          }
+          store_some(to + 4 * h, f, count - 4 * h);
+        }
+      } else {
+#pragma unroll
+        for (int e = 0; e < V; ++e) w[e] = float(x.v[e]);
+      }
+#pragma unroll
+      for (int e = 0; e < V; ++e) t = fma(double(w[e]), double(w[e]), t);  // 0 past the end
     }
 #pragma unroll
   for (int off = 32; off > 0; off >>= 1) t += __shfl_xor(t, off);
-  if (lane == 0) s[wave] = t;
+  if (threadIdx.x % 64 == 0) s[threadIdx.x / 64] = t;
   __syncthreads();
   if (threadIdx.x == 0) sums[blockIdx.x] = (s[0] + s[1]) + (s[2] + s[3]);
 }
@@ -70,14 +96,24 @@ __device__ __forceinline__ void store_blocks(const float* tile, const Blocks& to
 // block; and the steps' factors, by the first one.
 template <typename T>
 __global__ __launch_bounds__(kThreads) void prepare_kernel(const Source<T> u, int64_t n, int64_t m, bool tall,
-                                                           const double* __restrict__ sums, const Iteration it,
+                                                           const double* __restrict__ sums, int count, const Iteration it,
                                                            StepFactors* __restrict__ factors, const Blocks x,
                                                            const Blocks xt) {
   __shared__ double s_sum[kThreads / 64];
   __shared__ float s_tile[64 * kTilePitch];
   const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-  static_assert(kSumBlocks == kThreads, "a partial sum a thread");
-  double t = sums[threadIdx.x];
+  const int64_t i0 = int64_t(blockIdx.y) * 64, j0 = int64_t(blockIdx.x) * 64;
+  // All of u is asked for first, lanes along its columns; past the end the last ones again.
+  constexpr int EACH = 64 * 64 / kThreads;
+  float v[EACH];
+#pragma unroll
+  for (int q = 0; q < EACH; ++q) {
+    const int k = wave + q * (kThreads / 64);
+    const int64_t i = min(i0 + (tall ? lane : k), n - 1), j = min(j0 + (tall ? k : lane), m - 1);
+    v[q] = tall ? u.at(j, i) : u.at(i, j);
+  }
+  double t = 0.0;
+  for (int q = threadIdx.x; q < count; q += kThreads) t += sums[q];
 #pragma unroll
   for (int off = 32; off > 0; off >>= 1) t += __shfl_xor(t, off);
   if (lane == 0) s_sum[wave] = t;
@@ -93,13 +129,11 @@ __global__ __launch_bounds__(kThreads) void prepare_kernel(const Source<T> u, in
       step_factors(it.a, it.b, it.c, it.steps, size / (size + double(it.eps)), &first, factors);
     }
   }
-  const int64_t i0 = int64_t(blockIdx.y) * 64, j0 = int64_t(blockIdx.x) * 64;
-  for (int k = wave; k < 64; k += kThreads / 64) {
-    // lanes along the source's columns
-    const int i = tall ? lane : k, j = tall ? k : lane;
-    float v = 0.0f;  // the padding stays 0 whatever the norm
-    if (i0 + i < n && j0 + j < m) v = float(double(tall ? u.at(j0 + j, i0 + i) : u.at(i0 + i, j0 + j)) * inv);
-    s_tile[i * kTilePitch + j] = v;
+#pragma unroll
+  for (int q = 0; q < EACH; ++q) {
+    const int k = wave + q * (kThreads / 64), i = tall ? lane : k, j = tall ? k : lane;
+    // the padding stays 0 whatever the norm
+    s_tile[i * kTilePitch + j] = i0 + i < n && j0 + j < m ? float(double(v[q]) * inv) : 0.0f;
   }
   __syncthreads();
   store_blocks<64, false>(s_tile, x, i0, j0, lane, wave, kThreads / 64);
@@ -527,11 +561,17 @@ hipError_t run(const OrthogonalizeArgs& a, hipStream_t s) {
   const Blocks gram = blocks(p.a, n_blocks), poly = blocks(p.p, n_blocks);
 
   Source<T> u{static_cast<const T*>(a.x), a.x_ld, a.m, a.m_ld, a.momentum, a.nesterov};
-  squares_kernel<T><<<uint32_t(kSumBlocks), kThreads, 0, s>>>(u, a.m, a.rows, a.cols, sums);
+  int log_lanes = 0;
+  while (log_lanes < 8 && int64_t(Pack<T>::N) << log_lanes < a.cols) ++log_lanes;
+  const int count = int(std::min<int64_t>(kSumBlocks, ceil_div64(a.rows << log_lanes, kThreads)));
+  if (a.m)
+    squares_kernel<T, true><<<uint32_t(count), kThreads, 0, s>>>(u, a.m, a.rows, a.cols, log_lanes, sums);
+  else
+    squares_kernel<T, false><<<uint32_t(count), kThreads, 0, s>>>(u, nullptr, a.rows, a.cols, log_lanes, sums);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   const dim3 grid(uint32_t(p.m_pad / 64), uint32_t(p.n_pad / 64));
-  prepare_kernel<T><<<grid, kThreads, 0, s>>>(u, p.n, p.m, p.tall, sums, it, factors, x[0], xt[0]);
+  prepare_kernel<T><<<grid, kThreads, 0, s>>>(u, p.n, p.m, p.tall, sums, count, it, factors, x[0], xt[0]);
   if ((e = hipGetLastError()) != hipSuccess) return e;
 
   for (int k = 0; k < a.steps; ++k) {

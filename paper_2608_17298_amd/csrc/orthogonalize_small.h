@@ -1,7 +1,7 @@
-// A small matrix through all its steps in one block: 48 x 64 f32 in one launch of
-// about 10 us instead of 17 of 3.5.
+// A small matrix through all its steps in one block: the step of a 48 x 64 f32 weight
+// in 15 us, where 17 launches take 60.
 //
-// X stays in registers, as floats, 16 FRAG x 16 FRAG tiles of it a wave; LDS holds its
+// X stays in registers, as floats, TX tiles a wave; LDS holds its
 // transpose in blocks and, one after the other, X itself, A and P.  What a wave adds
 // to its sums it has in registers: A's tile to P's, X's to the next X's.  Bound by the
 // chain of phases: each waits for LDS reads, a few dependent matrix instructions and
@@ -13,7 +13,7 @@
 namespace gart {
 namespace {
 
-constexpr int kSmallWaves = 16, kSmallThreads = 64 * kSmallWaves, kSmallTiles = 2;  // of X a wave, at most
+constexpr int kSmallWaves = 16, kSmallThreads = 64 * kSmallWaves;
 constexpr int64_t kSmallElements = 19456;  // of the padded matrix: two of them in LDS
 constexpr int64_t kSmallSide = 128;        // of A, which is one tile a wave at most
 
@@ -30,7 +30,7 @@ __device__ __forceinline__ void small_product(f32x4 (&sum)[FRAG][FRAG], const Bl
   for (int i = 0; i < FRAG; ++i)
 #pragma unroll
     for (int j = 0; j < FRAG; ++j) sum[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll 2
+#pragma unroll(FRAG == 1 ? 2 : 1)
   for (int k = 0; k < steps; ++k) {
     Pack<f16>::V ah[FRAG], al[FRAG], bh[FRAG], bl[FRAG];
 #pragma unroll
@@ -68,17 +68,55 @@ __device__ __forceinline__ void put_row(const Blocks& to, int row, int col, cons
   *reinterpret_cast<f16x4*>(p + Blocks::kBlock) = low;
 }
 __device__ __forceinline__ void put_column(const Blocks& to, int row, int col, const f32x4& v) {
+  f16* p = to.at(col / 16, row / 32) + (row % 32 / 8 * 16 + col % 16) * 8 + row % 8;
 #pragma unroll
-  for (int e = 0; e < 4; ++e) {
+  for (int e = 0; e < 4; ++e) {  // col is a multiple of 4: four rows of one block
     f16 h, l;
     split(v[e], h, l);
-    f16* p = to.at((col + e) / 16, row / 32) + (row % 32 / 8 * 16 + (col + e) % 16) * 8 + row % 8;
-    p[0] = h;
-    p[Blocks::kBlock] = l;
+    p[8 * e] = h;
+    p[8 * e + Blocks::kBlock] = l;
   }
 }
 
-template <typename T, int FRAG>
+// The four elements from (i, j) of X in x, or in its transpose; 0 past the first `count`.
+template <typename T>
+struct __attribute__((packed)) Four {
+  T v[4];
+};
+template <typename T>
+__device__ __forceinline__ f32x4 load_four(const T* x, int64_t ld, bool tall, int i, int j, int count) {
+  f32x4 r = {0.0f, 0.0f, 0.0f, 0.0f};
+  if (!tall && count == 4) {
+    const Four<T> f = *reinterpret_cast<const Four<T>*>(x + i * ld + j);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) r[e] = float(f.v[e]);
+  } else {
+    const T* p = tall ? x + j * ld + i : x + i * ld + j;
+    const int64_t step = tall ? ld : 1;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (e < count) r[e] = float(p[e * step]);
+  }
+  return r;
+}
+template <typename T>
+__device__ __forceinline__ void store_four(T* x, int64_t ld, bool tall, int i, int j, int count, const f32x4& r) {
+  if (!tall && count == 4) {
+    Four<T> f;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) f.v[e] = T(r[e]);
+    *reinterpret_cast<Four<T>*>(x + i * ld + j) = f;
+  } else {
+    T* p = tall ? x + j * ld + i : x + i * ld + j;
+    const int64_t step = tall ? ld : 1;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (e < count) p[e * step] = T(r[e]);
+  }
+}
+
+// 16 waves, with a tile of A and TX of X each at most.
+template <typename T, int FRAG, int TX>
 __global__ __launch_bounds__(kSmallThreads) void small_kernel(const Source<T> u, float* m, int64_t rows, int64_t cols,
                                                               bool tall, const Iteration it, T* y, int64_t y_ld,
                                                               float decay, float step) {
@@ -100,32 +138,46 @@ __global__ __launch_bounds__(kSmallThreads) void small_kernel(const Source<T> u,
     j = tile % along * SIDE + 16 * q + 4 * g4;
     return tile < down * along;
   };
-  f32x4 v[kSmallTiles][FRAG][FRAG];
-  double square = 0.0;
-#pragma unroll
-  for (int t = 0; t < kSmallTiles; ++t)
+  // f(p, q, i, j, how many of the four elements from (i, j) of X there are) in tile t
+  auto each = [&](int t, auto&& f) {
 #pragma unroll
     for (int p = 0; p < FRAG; ++p)
 #pragma unroll
       for (int q = 0; q < FRAG; ++q) {
         int i, j;
         const bool any = where(t, p, q, i, j);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          v[t][p][q][e] = 0.0f;
-          if (!any || i >= n || j + e >= k) continue;
-          const int64_t row = tall ? j + e : i, col = tall ? i : j + e;
-          float w = float(u.x[row * u.ld + col]);
-          if (m) {
-            const float next = fmaf(u.momentum, m[row * u.m_ld + col], w);
-            m[row * u.m_ld + col] = next;
-            w = u.nesterov ? fmaf(u.momentum, next, w) : next;
-          }
-          v[t][p][q][e] = w;
-        }
+        f(p, q, i, j, any && i < n ? max(0, min(4, k - j)) : 0);
       }
+  };
+  // A tile's loads are asked for before its first store, which they could not pass;
+  // the parameters at the start, if there are registers for them.
+  constexpr bool EARLY = FRAG == 1;
+  f32x4 v[TX][FRAG][FRAG], old[FRAG][FRAG], param[EARLY ? TX : 1][FRAG][FRAG];
+  auto load_param = [&](int t) {
+    each(t, [&](int p, int q, int i, int j, int count) {
+      param[EARLY ? t : 0][p][q] = load_four(y, y_ld, tall, i, j, count);
+    });
+  };
 #pragma unroll
-  for (int t = 0; t < kSmallTiles; ++t)
+  for (int t = 0; t < TX; ++t) {
+    each(t, [&](int p, int q, int i, int j, int count) { v[t][p][q] = load_four(u.x, u.ld, tall, i, j, count); });
+    if (!m) continue;
+    each(t, [&](int p, int q, int i, int j, int count) { old[p][q] = load_four(m, u.m_ld, tall, i, j, count); });
+    if (EARLY) load_param(t);
+    each(t, [&](int p, int q, int i, int j, int count) {
+      f32x4 next;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float g = v[t][p][q][e];
+        next[e] = fmaf(u.momentum, old[p][q][e], g);
+        v[t][p][q][e] = u.nesterov ? fmaf(u.momentum, next[e], g) : next[e];  // 0 where there is nothing
+      }
+      store_four(m, u.m_ld, tall, i, j, count, next);
+    });
+  }
+  double square = 0.0;
+#pragma unroll
+  for (int t = 0; t < TX; ++t)
 #pragma unroll
     for (int p = 0; p < FRAG; ++p)
 #pragma unroll
@@ -152,7 +204,7 @@ __global__ __launch_bounds__(kSmallThreads) void small_kernel(const Source<T> u,
   }
   auto place = [&]() {
 #pragma unroll
-    for (int t = 0; t < kSmallTiles; ++t)
+    for (int t = 0; t < TX; ++t)
 #pragma unroll
       for (int p = 0; p < FRAG; ++p)
 #pragma unroll
@@ -164,7 +216,7 @@ __global__ __launch_bounds__(kSmallThreads) void small_kernel(const Source<T> u,
         }
   };
 #pragma unroll
-  for (int t = 0; t < kSmallTiles; ++t)
+  for (int t = 0; t < TX; ++t)
 #pragma unroll
     for (int p = 0; p < FRAG; ++p)
 #pragma unroll
@@ -180,19 +232,20 @@ __global__ __launch_bounds__(kSmallThreads) void small_kernel(const Source<T> u,
 
   const int ai = wave / down, aj = wave % down;  // this wave's tile of A
   const bool has_a = wave < down * down;
+  f32x4 gram[FRAG][FRAG];
+  auto put_a = [&]() {
+    __syncthreads();  // what lies there has been read
+    if (has_a) {
+#pragma unroll
+      for (int p = 0; p < FRAG; ++p)
+#pragma unroll
+        for (int q = 0; q < FRAG; ++q) put_row(a, ai * SIDE + 16 * p + r, aj * SIDE + 16 * q + 4 * g4, gram[p][q]);
+    }
+    __syncthreads();
+  };
   for (int s = 0; s < it.steps; ++s) {
     const StepFactors f = s_factors[s];
-    f32x4 sum[FRAG][FRAG], gram[FRAG][FRAG];
-    auto put_a = [&](const f32x4(&c)[FRAG][FRAG]) {
-      __syncthreads();  // what lies there has been read
-      if (has_a) {
-#pragma unroll
-        for (int p = 0; p < FRAG; ++p)
-#pragma unroll
-          for (int q = 0; q < FRAG; ++q) put_row(a, ai * SIDE + 16 * p + r, aj * SIDE + 16 * q + 4 * g4, c[p][q]);
-      }
-      __syncthreads();
-    };
+    f32x4 sum[FRAG][FRAG];
     if (has_a) {  // A = X X^T
       small_product<FRAG>(sum, x, x, ai, aj, k_pad / 32, lane);
 #pragma unroll
@@ -200,7 +253,7 @@ __global__ __launch_bounds__(kSmallThreads) void small_kernel(const Source<T> u,
 #pragma unroll
         for (int q = 0; q < FRAG; ++q) gram[p][q] = f.gram * sum[p][q];
     }
-    put_a(gram);
+    put_a();
     if (has_a) {  // P = b A + c A A
       small_product<FRAG>(sum, a, a, ai, aj, n_pad / 32, lane);
 #pragma unroll
@@ -210,9 +263,9 @@ __global__ __launch_bounds__(kSmallThreads) void small_kernel(const Source<T> u,
 #pragma unroll
           for (int e = 0; e < 4; ++e) gram[p][q][e] = fmaf(f.linear, gram[p][q][e], f.square * sum[p][q][e]);
     }
-    put_a(gram);
+    put_a();
 #pragma unroll
-    for (int t = 0; t < kSmallTiles; ++t) {  // a X + P X
+    for (int t = 0; t < TX; ++t) {  // a X + P X
       const int tile = wave + t * kSmallWaves;
       if (tile >= down * along) continue;
       small_product<FRAG>(sum, a, xt, tile / along, tile % along, n_pad / 32, lane);
@@ -231,36 +284,37 @@ __global__ __launch_bounds__(kSmallThreads) void small_kernel(const Source<T> u,
   }
 
 #pragma unroll
-  for (int t = 0; t < kSmallTiles; ++t)
-#pragma unroll
-    for (int p = 0; p < FRAG; ++p)
-#pragma unroll
-      for (int q = 0; q < FRAG; ++q) {
-        int i, j;
-        if (!where(t, p, q, i, j)) continue;
+  for (int t = 0; t < TX; ++t) {
+    if (m) {
+      if (!EARLY) load_param(t);
+      each(t, [&](int p, int q, int, int, int) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          if (i >= n || j + e >= k) continue;
-          T* to = y + (tall ? (j + e) * y_ld + i : i * y_ld + j + e);
-          float o = v[t][p][q][e];
-          if (m) {
-            const float w = float(*to);
-            o = fmaf(-step, o, fmaf(-decay, w, w));
-          }
-          *to = T(o);
+          const float w = param[EARLY ? t : 0][p][q][e];
+          v[t][p][q][e] = fmaf(-step, v[t][p][q][e], fmaf(-decay, w, w));
         }
-      }
+      });
+    }
+    each(t, [&](int p, int q, int i, int j, int count) { store_four(y, y_ld, tall, i, j, count, v[t][p][q]); });
+  }
 }
 
 template <typename T>
 hipError_t run_small(const OrthogonalizeArgs& a, const MatrixPlan& p, const Iteration& it, hipStream_t s) {
   Source<T> u{static_cast<const T*>(a.x), a.x_ld, a.m, a.m_ld, a.momentum, a.nesterov};
   T* y = static_cast<T*>(a.y);
-  // tiles of 16 while there are two a wave at most, of X, and one of A
-  if (pad32(p.n) <= 64 && pad32(p.n) * pad32(p.m) <= kSmallTiles * kSmallWaves * 256)
-    small_kernel<T, 1><<<1, kSmallThreads, 0, s>>>(u, a.m, a.rows, a.cols, p.tall, it, y, a.y_ld, a.decay, a.step);
+  auto launch = [&](auto kernel) {
+    kernel<<<1, kSmallThreads, 0, s>>>(u, a.m, a.rows, a.cols, p.tall, it, y, a.y_ld, a.decay, a.step);
+  };
+  const int64_t n = pad32(p.n), elements = n * pad32(p.m);
+  // tiles of 16 where the waves suffice for them: half as many of 32 leave most waves
+  // idle (48 x 64 f32 with four waves: 27 us, so 15)
+  if (n <= 64 && elements <= kSmallWaves * 256)
+    launch(small_kernel<T, 1, 1>);
+  else if (n <= 64 && elements <= 2 * kSmallWaves * 256)
+    launch(small_kernel<T, 1, 2>);
   else
-    small_kernel<T, 2><<<1, kSmallThreads, 0, s>>>(u, a.m, a.rows, a.cols, p.tall, it, y, a.y_ld, a.decay, a.step);
+    launch(small_kernel<T, 2, 2>);
   return hipGetLastError();
 }
 
