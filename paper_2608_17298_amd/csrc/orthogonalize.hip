@@ -21,9 +21,35 @@ namespace {
 
 constexpr int kThreads = 256;
 
-// m <- momentum m + g (if there is m), and the sum of squares of what is to be
-// orthogonalised, in 64 bits: float's squares would overflow from 2e19 on.  A row is
-// 2^log_lanes threads', a pack each at a time.
+// The `count` elements from (r, c) of what is orthogonalised as floats, 0 behind
+// them.  STEP: m is stepped there first, m <- momentum m + g.
+template <typename T, bool MOMENTUM, bool STEP>
+__device__ __forceinline__ void load_source(float (&w)[Pack<T>::N], const Source<T>& u, float* m, int64_t r, int64_t c,
+                                            int count) {
+  constexpr int V = Pack<T>::N;
+  const Pack<T> x = load_some(u.x + r * u.ld + c, count);
+#pragma unroll
+  for (int e = 0; e < V; ++e) w[e] = float(x.v[e]);
+  if constexpr (MOMENTUM) {
+    float* at = m + r * u.m_ld + c;
+#pragma unroll
+    for (int h = 0; h < V / 4; ++h) {
+      if (count <= 4 * h) continue;
+      Pack<float> f = load_some(at + 4 * h, count - 4 * h);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float g = w[4 * h + e];
+        if (STEP) f.v[e] = fmaf(u.momentum, f.v[e], g);
+        w[4 * h + e] = u.nesterov ? fmaf(u.momentum, f.v[e], g) : f.v[e];
+      }
+      if (STEP) store_some(at + 4 * h, f, count - 4 * h);
+    }
+  }
+}
+
+// Steps m, if there is one, and sums the squares of what is to be orthogonalised in
+// 64 bits: float's squares would overflow from 2e19 on.  A row is 2^log_lanes
+// threads', a pack each at a time.
 template <typename T, bool MOMENTUM>
 __global__ __launch_bounds__(kThreads) void squares_kernel(const Source<T> u, float* __restrict__ m, int64_t rows,
                                                            int64_t cols, int log_lanes, double* __restrict__ sums) {
@@ -33,33 +59,10 @@ __global__ __launch_bounds__(kThreads) void squares_kernel(const Source<T> u, fl
   double t = 0.0;
   for (int64_t r = int64_t(blockIdx.x) * high + (threadIdx.x >> log_lanes); r < rows; r += int64_t(gridDim.x) * high)
     for (int64_t c = int64_t(lane) * V; c < cols; c += int64_t(lanes) * V) {
-      const int count = int(min(int64_t(V), cols - c));
-      const Pack<T> x = load_some(u.x + r * u.ld + c, count);
       float w[V];
-      if constexpr (MOMENTUM) {
-        float* to = m + r * u.m_ld + c;
+      load_source<T, MOMENTUM, true>(w, u, m, r, c, int(min(int64_t(V), cols - c)));
 #pragma unroll
-        for (int h = 0; h < V / 4; ++h) {
-          if (count <= 4 * h) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) w[4 * h + e] = 0.0f;
-            continue;
-          }
-          Pack<float> f = load_some(to + 4 * h, count - 4 * h);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const float g = float(x.v[4 * h + e]);
-            f.v[e] = fmaf(u.momentum, f.v[e], g);
-            w[4 * h + e] = u.nesterov ? fmaf(u.momentum, f.v[e], g) : f.v[e];
-          }
-          store_some(to + 4 * h, f, count - 4 * h);
-        }
-      } else {
-#pragma unroll
-        for (int e = 0; e < V; ++e) w[e] = float(x.v[e]);
-      }
-#pragma unroll
-      for (int e = 0; e < V; ++e) t = fma(double(w[e]), double(w[e]), t);  // 0 past the end
+      for (int e = 0; e < V; ++e) t = fma(double(w[e]), double(w[e]), t);
     }
 #pragma unroll
   for (int off = 32; off > 0; off >>= 1) t += __shfl_xor(t, off);
@@ -94,23 +97,23 @@ __device__ __forceinline__ void store_blocks(const float* tile, const Blocks& to
 
 // X and its transpose, zero in the padding, from u over its norm: 64 x 64 elements a
 // block; and the steps' factors, by the first one.
-template <typename T>
-__global__ __launch_bounds__(kThreads) void prepare_kernel(const Source<T> u, int64_t n, int64_t m, bool tall,
-                                                           const double* __restrict__ sums, int count, const Iteration it,
-                                                           StepFactors* __restrict__ factors, const Blocks x,
-                                                           const Blocks xt) {
+template <typename T, bool MOMENTUM>
+__global__ __launch_bounds__(kThreads) void prepare_kernel(const Source<T> u, int64_t rows, int64_t cols, bool tall,
+                                                           const double* __restrict__ sums, int count,
+                                                           const Iteration it, StepFactors* __restrict__ factors,
+                                                           const Blocks x, const Blocks xt) {
+  constexpr int V = Pack<T>::N, ACROSS = 64 / V, EACH = 64 * ACROSS / kThreads;  // packs a row, and a thread
   __shared__ double s_sum[kThreads / 64];
-  __shared__ float s_tile[64 * kTilePitch];
+  __shared__ __attribute__((aligned(16))) float s_tile[64 * kTilePitch];
   const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-  const int64_t i0 = int64_t(blockIdx.y) * 64, j0 = int64_t(blockIdx.x) * 64;
-  // All of u is asked for first, lanes along its columns; past the end the last ones again.
-  constexpr int EACH = 64 * 64 / kThreads;
-  float v[EACH];
+  const int64_t r0 = int64_t(blockIdx.y) * 64, c0 = int64_t(blockIdx.x) * 64;
+  float w[EACH][V];  // all asked for first
 #pragma unroll
   for (int q = 0; q < EACH; ++q) {
-    const int k = wave + q * (kThreads / 64);
-    const int64_t i = min(i0 + (tall ? lane : k), n - 1), j = min(j0 + (tall ? k : lane), m - 1);
-    v[q] = tall ? u.at(j, i) : u.at(i, j);
+    const int at = q * kThreads + threadIdx.x;
+    const int64_t r = r0 + at / ACROSS, c = c0 + at % ACROSS * V;
+    const int here = r < rows ? int(max(int64_t(0), min(int64_t(V), cols - c))) : 0;
+    load_source<T, MOMENTUM, false>(w[q], u, const_cast<float*>(u.m), r, c, here);
   }
   double t = 0.0;
   for (int q = threadIdx.x; q < count; q += kThreads) t += sums[q];
@@ -131,13 +134,20 @@ __global__ __launch_bounds__(kThreads) void prepare_kernel(const Source<T> u, in
   }
 #pragma unroll
   for (int q = 0; q < EACH; ++q) {
-    const int k = wave + q * (kThreads / 64), i = tall ? lane : k, j = tall ? k : lane;
-    // the padding stays 0 whatever the norm
-    s_tile[i * kTilePitch + j] = i0 + i < n && j0 + j < m ? float(double(v[q]) * inv) : 0.0f;
+    const int at = q * kThreads + threadIdx.x, r = at / ACROSS, c = at % ACROSS * V;
+    const int64_t left = r0 + r < rows ? cols - c0 - c : 0;  // the padding stays 0 whatever the norm
+#pragma unroll
+    for (int h = 0; h < V / 4; ++h) {
+      f32x4 f;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) f[e] = 4 * h + e < left ? float(double(w[q][4 * h + e]) * inv) : 0.0f;
+      *reinterpret_cast<f32x4*>(s_tile + r * kTilePitch + c + 4 * h) = f;
+    }
   }
   __syncthreads();
-  store_blocks<64, false>(s_tile, x, i0, j0, lane, wave, kThreads / 64);
-  store_blocks<64, true>(s_tile, xt, j0, i0, lane, wave, kThreads / 64);
+  // the rows of x are those of X, or of its transpose
+  store_blocks<64, false>(s_tile, tall ? xt : x, r0, c0, lane, wave, kThreads / 64);
+  store_blocks<64, true>(s_tile, tall ? x : xt, c0, r0, lane, wave, kThreads / 64);
 }
 
 // ---- products of pairs ----------------------------------------------------------
@@ -570,8 +580,11 @@ hipError_t run(const OrthogonalizeArgs& a, hipStream_t s) {
     squares_kernel<T, false><<<uint32_t(count), kThreads, 0, s>>>(u, nullptr, a.rows, a.cols, log_lanes, sums);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  const dim3 grid(uint32_t(p.m_pad / 64), uint32_t(p.n_pad / 64));
-  prepare_kernel<T><<<grid, kThreads, 0, s>>>(u, p.n, p.m, p.tall, sums, count, it, factors, x[0], xt[0]);
+  const dim3 grid(uint32_t((p.tall ? p.n_pad : p.m_pad) / 64), uint32_t((p.tall ? p.m_pad : p.n_pad) / 64));
+  if (a.m)
+    prepare_kernel<T, true><<<grid, kThreads, 0, s>>>(u, a.rows, a.cols, p.tall, sums, count, it, factors, x[0], xt[0]);
+  else
+    prepare_kernel<T, false><<<grid, kThreads, 0, s>>>(u, a.rows, a.cols, p.tall, sums, count, it, factors, x[0], xt[0]);
   if ((e = hipGetLastError()) != hipSuccess) return e;
 
   for (int k = 0; k < a.steps; ++k) {

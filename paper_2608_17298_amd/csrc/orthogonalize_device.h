@@ -19,11 +19,6 @@ struct Source {
   int64_t m_ld;
   float momentum;
   bool nesterov;
-  __device__ __forceinline__ float at(int64_t r, int64_t c) const {
-    if (!m) return float(x[r * ld + c]);
-    const float v = m[r * m_ld + c];
-    return nesterov ? fmaf(momentum, v, float(x[r * ld + c])) : v;
-  }
 };
 
 // A float as high + low.
