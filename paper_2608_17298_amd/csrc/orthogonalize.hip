@@ -202,9 +202,10 @@ __device__ __forceinline__ bool find_tile(const PairArgs& g, int b, int total, i
 //    multiplied; the waves meet when their sums are joined.  Bound by the bytes a CU
 //    takes in (100 a ns from its cache, 65 from another die's), for products with few
 //    tiles.
-//  - W x W waves of 64 x 64 that share the operands in LDS (tiles of 128).  Four
-//    blocks of k are there or on their way; the next fragments are read while the last
-//    ones are multiplied.
+//  - Two groups of W x W waves of 64 x 64 that share the operands in LDS (tiles of
+//    128) and take every other block of k: two waves a SIMD, of which one multiplies
+//    while the other reads its fragments (one wave that reads ahead instead: 1024 x
+//    1024 -> 4096 39 us, so TODO).
 template <int FRAG>
 struct Fragments {
   Pack<f16>::V ah[FRAG], al[FRAG], bh[FRAG], bl[FRAG];
@@ -259,13 +260,14 @@ __device__ __forceinline__ void split_sums(f32x4 (&sum)[FRAG][FRAG], const PairA
   if (n + 1 < count) product(set[1]);
 }
 
-constexpr int kStages = 4;
+// Wave `wave` of group `group`: every kGroups-th block of k.
+constexpr int kGroups = 2, kStages = 2;
 template <int W>
 __device__ __forceinline__ void shared_sums(f32x4 (&sum)[4][4], const PairArgs& g, int64_t ti, int64_t tj, int k0, int k1,
-                                            int wave, int lane, f16* lds) {
-  // a stage: 4 W row tiles of A, then of B, each a pair of blocks
-  constexpr int TILES = 4 * W, STAGE = 2 * TILES * Blocks::kPair, WAVES = W * W, MINE = TILES / WAVES;
-  static_assert(TILES % WAVES == 0, "whole tiles a wave");
+                                            int group, int wave, int lane, f16* lds) {
+  // a stage: kGroups blocks of k, each 4 W row tiles of A, then of B, pairs of blocks
+  constexpr int TILES = 4 * W, BLOCK = 2 * TILES * Blocks::kPair, STAGE = kGroups * BLOCK, MINE = TILES / (W * W);
+  static_assert(TILES % (W * W) == 0, "whole tiles a wave");
   typedef const __attribute__((address_space(1))) uint32_t* global_ptr;
   typedef __attribute__((address_space(3))) uint32_t* lds_ptr;
   const int64_t a_last = g.rows / 16 - 1, b_last = g.cols / 16 - 1;  // tiles past the end: the last one again
@@ -275,8 +277,9 @@ __device__ __forceinline__ void shared_sums(f32x4 (&sum)[4][4], const PairArgs& 
     a[u] = g.a.at(min(ti * TILES + wave * MINE + u, a_last), 0) + lane * 8;
     b[u] = g.b.at(min(tj * TILES + wave * MINE + u, b_last), 0) + lane * 8;
   }
-  auto fetch = [&](int k) {  // past the end the last one again: the waits below count on it
-    f16* to = lds + k % kStages * STAGE + wave * MINE * Blocks::kPair;
+  f16* mine = lds + group * BLOCK;
+  auto fetch = [&](int h, int k) {  // past the end the last one again: it is not used
+    f16* to = mine + h * STAGE + wave * MINE * Blocks::kPair;
     const int64_t at = int64_t(min(k, k1 - 1)) * Blocks::kPair;
 #pragma unroll
     for (int u = 0; u < MINE; ++u)
@@ -289,83 +292,49 @@ __device__ __forceinline__ void shared_sums(f32x4 (&sum)[4][4], const PairArgs& 
       }
   };
   const int wi = wave / W, wj = wave % W;
-  auto read = [&](Fragments<4>& f, int k) {
-    const f16* from = lds + k % kStages * STAGE + lane * 8;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const f16* p = from + (wi * 4 + i) * Blocks::kPair;
-      const f16* q = from + (TILES + wj * 4 + i) * Blocks::kPair;
-      f.ah[i] = *reinterpret_cast<const Pack<f16>::V*>(p);
-      f.al[i] = *reinterpret_cast<const Pack<f16>::V*>(p + Blocks::kBlock);
-      f.bh[i] = *reinterpret_cast<const Pack<f16>::V*>(q);
-      f.bl[i] = *reinterpret_cast<const Pack<f16>::V*>(q + Blocks::kBlock);
-    }
-  };
-  constexpr int LOADS = 4 * MINE;
-  auto arrived = [&]() {
-    // this wave's part of the oldest stage has landed, and it has read the one before
-    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((kStages - 2) * LOADS) : "memory");
+  int h = 0;
+  fetch(0, k0 + group);
+  for (int k = k0; k < k1; k += kGroups, h ^= 1) {
+    // this wave's part of the stage has landed, and it has read the one before
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
     __builtin_amdgcn_s_barrier();  // so has everyone's, and have they
     asm volatile("" ::: "memory");
-  };
-  // Reads of the next fragments among the products of the last.
-  auto interleave = [&]() {
+    if (k + kGroups < k1) fetch(h ^ 1, k + kGroups + group);
+    if (k + group < k1) {
+      const f16* from = mine + h * STAGE + lane * 8;
+      Fragments<4> f;
 #pragma unroll
-    for (int q = 0; q < 16; ++q) {
-      __builtin_amdgcn_sched_group_barrier(0x008, 3, 0);  // matrix instructions
-      __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);  // LDS reads
+      for (int i = 0; i < 4; ++i) {
+        const f16* p = from + (wi * 4 + i) * Blocks::kPair;
+        const f16* q = from + (TILES + wj * 4 + i) * Blocks::kPair;
+        f.ah[i] = *reinterpret_cast<const Pack<f16>::V*>(p);
+        f.al[i] = *reinterpret_cast<const Pack<f16>::V*>(p + Blocks::kBlock);
+        f.bh[i] = *reinterpret_cast<const Pack<f16>::V*>(q);
+        f.bl[i] = *reinterpret_cast<const Pack<f16>::V*>(q + Blocks::kBlock);
+      }
+      multiply<4>(sum, f);
     }
-    __builtin_amdgcn_sched_barrier(0);
-  };
-  Fragments<4> even, odd;
-#pragma unroll
-  for (int h = 0; h < kStages - 1; ++h) fetch(k0 + h);
-  arrived();
-  fetch(k0 + kStages - 1);
-  read(even, k0);
-  __builtin_amdgcn_sched_barrier(0);
-  int k = k0 + 1;
-  for (; k + 1 < k1; k += 2) {
-    arrived();
-    fetch(k + kStages - 1);
-    read(odd, k);
-    multiply<4>(sum, even);
-    interleave();
-    arrived();
-    fetch(k + kStages);
-    read(even, k + 1);
-    multiply<4>(sum, odd);
-    interleave();
   }
-  if (k < k1) {
-    arrived();
-    read(odd, k);
-    multiply<4>(sum, even);
-    multiply<4>(sum, odd);
-  } else {
-    multiply<4>(sum, even);
-  }
-  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // nothing lands once LDS holds something else
 }
 
 // A tile of 16 FRAG W on a side.  JOIN: the sums of k are those of g.parts parts.
 template <typename T, int FRAG, int W, int WK, PairEpilogue EPI, bool JOIN>
 __global__ __launch_bounds__(64 * W * W * WK, 1) void pair_kernel(const PairArgs g) {
   constexpr int THREADS = 64 * W * W * WK, SIDE = 16 * FRAG;  // of a wave's tile
-  constexpr bool SPLIT = WK > 1;
-  static_assert(SPLIT ? W == 1 && WK == 4 : FRAG == 4, "four waves of one tile, or tiles of 64");
-  // 16 x 16 tiles of a wave's result: FRAG by FRAG, or its share of them
-  constexpr int RI = SPLIT ? 1 : FRAG, RJ = SPLIT ? FRAG * FRAG / WK : FRAG;
-  constexpr int SUMS = JOIN ? 0 : SPLIT ? WK * SIDE * SIDE : kStages * 2 * 4 * W * Blocks::kPair / 2;  // floats
+  constexpr bool SPLIT = W == 1;
+  static_assert(SPLIT ? WK == 4 : FRAG == 4 && WK == kGroups, "four waves of one tile, or two groups of tiles of 64");
+  // 16 x 16 tiles of a wave's result: its share of FRAG by FRAG
+  constexpr int RJ = FRAG * FRAG / WK < FRAG ? FRAG * FRAG / WK : FRAG, RI = FRAG * FRAG / WK / RJ;
+  constexpr int SUMS = JOIN ? 0 : SPLIT ? WK * SIDE * SIDE : kStages * kGroups * 2 * 4 * W * Blocks::kPair / 2;  // floats
   constexpr int TILE = EPI == PAIR_BLOCKS ? W * W * SIDE * kTilePitch : 4;
   __shared__ __attribute__((aligned(16))) float lds[SUMS > TILE ? SUMS : TILE];
   const int tid = threadIdx.x, lane = tid % 64, wave = __builtin_amdgcn_readfirstlane(tid / 64);
   int ti, tj;
   if (!find_tile(g, blockIdx.x, gridDim.x, ti, tj)) return;
-  const int wi = SPLIT ? 0 : wave / W, wj = SPLIT ? 0 : wave % W;
+  const int wk = wave / (W * W), place = wave % (W * W), wi = place / W, wj = place % W;
   const int64_t i0 = (int64_t(ti) * W + wi) * SIDE, j0 = (int64_t(tj) * W + wj) * SIDE;
   const bool inside = i0 < g.rows && j0 < g.cols;
-  const int first_i = SPLIT ? wave * RJ / FRAG : 0, first_j = SPLIT ? wave * RJ % FRAG : 0;
+  const int first_i = wk * RI * RJ / FRAG, first_j = wk * RI * RJ % FRAG;
   const int r = lane % 16, g4 = lane / 16;
   typedef f16 f16x4 __attribute__((ext_vector_type(4)));
   // A lane has four consecutive columns of a row; of D they are half a piece.
@@ -373,23 +342,21 @@ __global__ __launch_bounds__(64 * W * W * WK, 1) void pair_kernel(const PairArgs
     const int row = 16 * (first_i + i), col = 16 * (first_j + j) + 4 * g4;
     return g.d.at((i0 + row) / 16, (j0 + col) / 32) + (((j0 + col) % 32) / 8 * 16 + r) * 8 + col % 8;
   };
-  f16x4 dh[SPLIT ? RI : 1][SPLIT ? RJ : 1], dl[SPLIT ? RI : 1][SPLIT ? RJ : 1];
+  f16x4 dh[RI][RJ], dl[RI][RJ];
   float alpha, beta;
   // What the result takes besides the sums, asked for before they are formed.
   auto others = [&]() {
     if constexpr (EPI != PAIR_PART) {
       alpha = g.factors[0];
       beta = g.factors[1];
-      if constexpr (SPLIT) {
-        if (g.d.data) {
+      if (g.d.data && inside) {
 #pragma unroll
-          for (int i = 0; i < RI; ++i)
+        for (int i = 0; i < RI; ++i)
 #pragma unroll
-            for (int j = 0; j < RJ; ++j) {
-              dh[i][j] = *reinterpret_cast<const f16x4*>(d_at(i, j));
-              dl[i][j] = *reinterpret_cast<const f16x4*>(d_at(i, j) + Blocks::kBlock);
-            }
-        }
+          for (int j = 0; j < RJ; ++j) {
+            dh[i][j] = *reinterpret_cast<const f16x4*>(d_at(i, j));
+            dl[i][j] = *reinterpret_cast<const f16x4*>(d_at(i, j) + Blocks::kBlock);
+          }
       }
     }
   };
@@ -417,35 +384,36 @@ __global__ __launch_bounds__(64 * W * W * WK, 1) void pair_kernel(const PairArgs
     const int part = EPI == PAIR_PART ? int(blockIdx.y) : 0, parts = EPI == PAIR_PART ? g.parts : 1;
     const int k0 = int(g.steps * part / parts), k1 = int(g.steps * (part + 1) / parts);
     if constexpr (!SPLIT) {
-      shared_sums<W>(sum, g, ti, tj, k0, k1, wave, lane, reinterpret_cast<f16*>(lds));
+      shared_sums<W>(sum, g, ti, tj, k0, k1, wk, place, lane, reinterpret_cast<f16*>(lds));
       others();
-#pragma unroll
-      for (int i = 0; i < FRAG; ++i)
-#pragma unroll
-        for (int j = 0; j < FRAG; ++j) acc[i][j] = sum[i][j];
       __syncthreads();
+    } else if (k0 + wk < k1) {
+      split_sums<FRAG, WK>(sum, g, i0, j0, k0 + wk, k1, lane, others);
     } else {
-      if (k0 + wave < k1)
-        split_sums<FRAG, WK>(sum, g, i0, j0, k0 + wave, k1, lane, others);
-      else
-        others();
-#pragma unroll
-      for (int i = 0; i < FRAG; ++i)
-#pragma unroll
-        for (int j = 0; j < FRAG; ++j)
-          *reinterpret_cast<f32x4*>(lds + ((wave * FRAG + i) * FRAG + j) * 256 + lane * 4) = sum[i][j];
-      __syncthreads();
-#pragma unroll
-      for (int j = 0; j < RJ; ++j) {
-        acc[0][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-        for (int w = 0; w < WK; ++w)
-          acc[0][j] += *reinterpret_cast<const f32x4*>(
-              lds + ((w * FRAG + first_i) * FRAG + first_j + j) * 256 + lane * 4);
-        arrive(acc[0][j]);  // the compiler moved these reads behind the barrier, where the tile is written over them
-      }
-      __syncthreads();
+      others();
     }
+    // each of the WK waves takes its share of the others' tiles
+    constexpr int SHARE = RI * RJ, ALL = FRAG * FRAG;
+    float* at = lds + place * (WK * ALL * 256) + lane * 4;
+#pragma unroll
+    for (int q = 0; q < ALL; ++q)
+      if (q / SHARE != wk) *reinterpret_cast<f32x4*>(at + (wk * ALL + q) * 256) = sum[q / FRAG][q % FRAG];
+    __syncthreads();
+#pragma unroll
+    for (int q = 0; q < SHARE; ++q) {
+      f32x4 t = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (int w = 0; w < WK; ++w) {
+        f32x4 own = t;
+#pragma unroll
+        for (int v = 0; v < WK; ++v)
+          if (v == w) own = sum[(v * SHARE + q) / FRAG][(v * SHARE + q) % FRAG];
+        t += w == wk ? own : *reinterpret_cast<const f32x4*>(at + (w * ALL + wk * SHARE + q) * 256);
+      }
+      arrive(t);  // the compiler moved these reads behind the barrier, where the tile is written over them
+      acc[q / RJ][q % RJ] = t;
+    }
+    __syncthreads();
   }
 
   if constexpr (EPI == PAIR_PART) {
@@ -457,7 +425,7 @@ __global__ __launch_bounds__(64 * W * W * WK, 1) void pair_kernel(const PairArgs
     return;
   }
 
-  float* tile = lds + (SPLIT ? 0 : wave * SIDE * kTilePitch);
+  float* tile = lds + place * SIDE * kTilePitch;
   if (inside) {
 #pragma unroll
     for (int i = 0; i < RI; ++i) {
@@ -467,16 +435,8 @@ __global__ __launch_bounds__(64 * W * W * WK, 1) void pair_kernel(const PairArgs
         const int col = 16 * (first_j + j) + 4 * g4;
         f32x4 c = alpha * acc[i][j];
         if (g.d.data) {
-          f16x4 h, l;
-          if constexpr (SPLIT) {
-            h = dh[i][j];
-            l = dl[i][j];
-          } else {
-            h = *reinterpret_cast<const f16x4*>(d_at(i, j));
-            l = *reinterpret_cast<const f16x4*>(d_at(i, j) + Blocks::kBlock);
-          }
 #pragma unroll
-          for (int e = 0; e < 4; ++e) c[e] = fmaf(beta, float(h[e]) + float(l[e]), c[e]);
+          for (int e = 0; e < 4; ++e) c[e] = fmaf(beta, float(dh[i][j][e]) + float(dl[i][j][e]), c[e]);
         }
         if constexpr (EPI == PAIR_BLOCKS) {
           *reinterpret_cast<f32x4*>(tile + row * kTilePitch + col) = c;
@@ -513,12 +473,11 @@ __global__ __launch_bounds__(64 * W * W * WK, 1) void pair_kernel(const PairArgs
   if constexpr (EPI == PAIR_BLOCKS) {
     __syncthreads();
     if (!inside) return;
-    const int mine = SPLIT ? wave : 0;
-    store_blocks<SIDE, false>(tile, g.out, i0, j0, lane, mine, WK);
+    store_blocks<SIDE, false>(tile, g.out, i0, j0, lane, wk, WK);
     if (!g.symmetric)
-      store_blocks<SIDE, true>(tile, g.across, j0, i0, lane, WK - 1 - mine, WK);
+      store_blocks<SIDE, true>(tile, g.across, j0, i0, lane, WK - 1 - wk, WK);
     else if (i0 != j0)
-      store_blocks<SIDE, true>(tile, g.out, j0, i0, lane, WK - 1 - mine, WK);
+      store_blocks<SIDE, true>(tile, g.out, j0, i0, lane, WK - 1 - wk, WK);
   }
 }
 
@@ -551,7 +510,7 @@ hipError_t run_pair(const PairArgs& g, bool symmetric, hipStream_t s) {
   const PairCut c = cut_pair(g.rows, g.cols, g.steps, symmetric);
   if (c.side == 32) return run_tiles<T, 2, 1, 4, EPI>(g, c, s);
   if (c.side == 64) return run_tiles<T, 4, 1, 4, EPI>(g, c, s);
-  return run_tiles<T, 4, 2, 1, EPI>(g, c, s);
+  return run_tiles<T, 4, 2, kGroups, EPI>(g, c, s);
 }
 
 template <typename T>
