@@ -166,7 +166,8 @@ struct PairArgs {
   int64_t steps;        // blocks along k
   int tiles_i, tiles_j, band;
   bool symmetric;       // C is: tiles above the diagonal are stored on both sides of it
-  int parts;            // of k: blockIdx.y
+  int tiles;            // launched for them, for each part of k
+  int parts;
   float* partial;       // their sums
   const float* factors; // alpha, beta
   Blocks out, across;   // PAIR_BLOCKS: C and, unless it is symmetric, its transpose
@@ -175,11 +176,11 @@ struct PairArgs {
   float decay, step;    // PAIR_STEP: y -= decay y + step C
 };
 
-// Blocks go to the eight XCDs in turn.  Each gets a run of tiles that covers a patch
-// of `band` rows, so that its cache takes in few rows of both operands.  A triangle of
-// tiles (i <= j) is folded to half as many rows: row r, then row n - 1 - r.
-__device__ __forceinline__ bool find_tile(const PairArgs& g, int b, int total, int& ti, int& tj) {
-  const int t = int(xcd_tile(b, total));
+// Blocks go to the eight XCDs in turn.  Each gets a run of tiles (xcd_tile), of one or
+// two parts of k, that covers a patch of `band` rows, so that its cache takes in few
+// rows of both operands.  A triangle of tiles (i <= j) is folded to half as many rows:
+// row r, then row n - 1 - r.
+__device__ __forceinline__ bool find_tile(const PairArgs& g, int t, int& ti, int& tj) {
   const int n = g.tiles_i, even = n + n % 2;
   const int rows = g.symmetric ? even / 2 : n, cols = g.symmetric ? even + 1 : g.tiles_j;
   const int top = t / (g.band * cols) * g.band, high = min(g.band, rows - top);
@@ -319,19 +320,23 @@ __device__ __forceinline__ void shared_sums(f32x4 (&sum)[4][4], const PairArgs& 
 
 // A tile of 16 FRAG W on a side.  JOIN: the sums of k are those of g.parts parts.
 template <typename T, int FRAG, int W, int WK, PairEpilogue EPI, bool JOIN>
-__global__ __launch_bounds__(64 * W * W * WK, 1) void pair_kernel(const PairArgs g) {
-  constexpr int THREADS = 64 * W * W * WK, SIDE = 16 * FRAG;  // of a wave's tile
+__global__ __launch_bounds__(64 * (JOIN ? 1 : W * W) * WK, 1) void pair_kernel(const PairArgs g) {
+  constexpr int PLACES = JOIN ? 1 : W * W;  // tiles of waves in a block: a join has one, to have more blocks
+  constexpr int THREADS = 64 * W * W * WK, SIDE = 16 * FRAG;
   constexpr bool SPLIT = W == 1;
   static_assert(SPLIT ? WK == 4 : FRAG == 4 && WK == kGroups, "four waves of one tile, or two groups of tiles of 64");
   // 16 x 16 tiles of a wave's result: its share of FRAG by FRAG
   constexpr int RJ = FRAG * FRAG / WK < FRAG ? FRAG * FRAG / WK : FRAG, RI = FRAG * FRAG / WK / RJ;
   constexpr int SUMS = JOIN ? 0 : SPLIT ? WK * SIDE * SIDE : kStages * kGroups * 2 * 4 * W * Blocks::kPair / 2;  // floats
-  constexpr int TILE = EPI == PAIR_BLOCKS ? W * W * SIDE * kTilePitch : 4;
+  constexpr int TILE = EPI == PAIR_BLOCKS ? PLACES * SIDE * kTilePitch : 4;
   __shared__ __attribute__((aligned(16))) float lds[SUMS > TILE ? SUMS : TILE];
-  const int tid = threadIdx.x, lane = tid % 64, wave = __builtin_amdgcn_readfirstlane(tid / 64);
+  const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+  const int at_xcd = int(xcd_tile(blockIdx.x, gridDim.x)), which = JOIN ? at_xcd / (W * W) : at_xcd;
+  const int part = which / g.tiles;  // 0 but for PAIR_PART
   int ti, tj;
-  if (!find_tile(g, blockIdx.x, gridDim.x, ti, tj)) return;
-  const int wk = wave / (W * W), place = wave % (W * W), wi = place / W, wj = place % W;
+  if (!find_tile(g, which - part * g.tiles, ti, tj)) return;
+  const int wk = wave / PLACES, place = JOIN ? at_xcd % (W * W) : wave % PLACES, wi = place / W, wj = place % W;
+  const int tid = (wk * W * W + place) * 64 + lane;  // of the block that sums
   const int64_t i0 = (int64_t(ti) * W + wi) * SIDE, j0 = (int64_t(tj) * W + wj) * SIDE;
   const bool inside = i0 < g.rows && j0 < g.cols;
   const int first_i = wk * RI * RJ / FRAG, first_j = wk * RI * RJ % FRAG;
@@ -368,8 +373,8 @@ __global__ __launch_bounds__(64 * W * W * WK, 1) void pair_kernel(const PairArgs
     for (int i = 0; i < RI; ++i)
 #pragma unroll
       for (int j = 0; j < RJ; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    for (int part = 0; part < g.parts; ++part) {
-      const float* from = g.partial + (int64_t(part) * gridDim.x + blockIdx.x) * (THREADS * RI * RJ * 4) + tid * 4;
+    for (int q = 0; q < g.parts; ++q) {
+      const float* from = g.partial + (int64_t(q) * g.tiles + which) * (THREADS * RI * RJ * 4) + tid * 4;
 #pragma unroll
       for (int i = 0; i < RI; ++i)
 #pragma unroll
@@ -381,7 +386,7 @@ __global__ __launch_bounds__(64 * W * W * WK, 1) void pair_kernel(const PairArgs
     for (int i = 0; i < FRAG; ++i)
 #pragma unroll
       for (int j = 0; j < FRAG; ++j) sum[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    const int part = EPI == PAIR_PART ? int(blockIdx.y) : 0, parts = EPI == PAIR_PART ? g.parts : 1;
+    const int parts = EPI == PAIR_PART ? g.parts : 1;
     const int k0 = int(g.steps * part / parts), k1 = int(g.steps * (part + 1) / parts);
     if constexpr (!SPLIT) {
       shared_sums<W>(sum, g, ti, tj, k0, k1, wk, place, lane, reinterpret_cast<f16*>(lds));
@@ -417,7 +422,7 @@ __global__ __launch_bounds__(64 * W * W * WK, 1) void pair_kernel(const PairArgs
   }
 
   if constexpr (EPI == PAIR_PART) {
-    float* to = g.partial + (int64_t(blockIdx.y) * gridDim.x + blockIdx.x) * (THREADS * RI * RJ * 4) + tid * 4;
+    float* to = g.partial + int64_t(which) * (THREADS * RI * RJ * 4) + tid * 4;
 #pragma unroll
     for (int i = 0; i < RI; ++i)
 #pragma unroll
@@ -425,7 +430,7 @@ __global__ __launch_bounds__(64 * W * W * WK, 1) void pair_kernel(const PairArgs
     return;
   }
 
-  float* tile = lds + place * SIDE * kTilePitch;
+  float* tile = lds + (JOIN ? 0 : place) * SIDE * kTilePitch;
   if (inside) {
 #pragma unroll
     for (int i = 0; i < RI; ++i) {
@@ -487,19 +492,19 @@ hipError_t run_tiles(PairArgs g, const PairCut& c, hipStream_t s) {
   g.tiles_j = int((g.cols + c.side - 1) / c.side);
   g.symmetric = c.symmetric;
   g.parts = c.parts;
-  const uint32_t blocks = uint32_t(blocks_of(g.rows, g.cols, c.side, c.symmetric));
+  g.tiles = int(blocks_of(g.rows, g.cols, c.side, c.symmetric));
   g.band = 1;
-  while (g.band * g.band * 8 < int(blocks)) ++g.band;
+  while (g.band * g.band * 8 < g.tiles) ++g.band;
   constexpr int THREADS = 64 * W * W * WK;
   if (c.parts == 1) {
-    pair_kernel<T, FRAG, W, WK, EPI, false><<<blocks, THREADS, 0, s>>>(g);
+    pair_kernel<T, FRAG, W, WK, EPI, false><<<uint32_t(g.tiles), THREADS, 0, s>>>(g);
     return hipGetLastError();
   }
   if constexpr (EPI == PAIR_BLOCKS) {
-    pair_kernel<T, FRAG, W, WK, PAIR_PART, false><<<dim3(blocks, uint32_t(c.parts)), THREADS, 0, s>>>(g);
+    pair_kernel<T, FRAG, W, WK, PAIR_PART, false><<<uint32_t(g.tiles * c.parts), THREADS, 0, s>>>(g);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    pair_kernel<T, FRAG, W, WK, PAIR_BLOCKS, true><<<blocks, THREADS, 0, s>>>(g);
+    pair_kernel<T, FRAG, W, WK, PAIR_BLOCKS, true><<<uint32_t(g.tiles * W * W), 64 * WK, 0, s>>>(g);
     return hipGetLastError();
   }
   return hipErrorInvalidValue;
