@@ -18,10 +18,14 @@ constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / 64;
 constexpr int64_t kMaxBlocks = int64_t(1) << 20;
 
-// 1 / sqrt(v) by the hardware's instruction, one unit of the last place off, which needs v above the subnormals
+// 1 / sqrt(v) by the hardware's instruction, which needs v above the subnormals and is
+// a unit of the last place off, the same for a whole row, and a step of Newton's.
 __device__ __forceinline__ float rsqrt_of(float v) {
   const bool small = v < 0x1p-100f;
-  return __builtin_amdgcn_rsqf(small ? v * 0x1p100f : v) * (small ? 0x1p50f : 1.0f);
+  if (small) v *= 0x1p100f;
+  const float r = __builtin_amdgcn_rsqf(v), e = fmaf(-(v * r), r, 1.0f);
+  const float q = e == e ? fmaf(0.5f * r, e, r) : r;  // of 0 and infinity as it is
+  return small ? q * 0x1p50f : q;
 }
 
 // s / n by n's reciprocal, the quotient set right by its own remainder: exact where
@@ -244,9 +248,10 @@ __global__ __launch_bounds__(THREADS) void block_rows_kernel(const LayerNormArgs
 }
 
 // The gradient: THREADS / G rows at a time, or one of a whole block (G = THREADS).
-// Lanes add dl h and dl of their columns up over the rows that the block takes, and
-// the block leaves its sums in sums[block] = [g_gain, g_bias], or, alone, the result.
-template <typename T, int G, int U, RowEnd END, int THREADS>
+// COLUMNS: lanes add dl h and dl of their columns up over the rows that the block takes,
+// and the block leaves its sums in sums[block] = [g_gain, g_bias], or, alone, the
+// result.  Else sums, if it is not NULL, takes the rows' mean and rstd.
+template <typename T, int G, int U, RowEnd END, int THREADS, bool COLUMNS>
 __global__ __launch_bounds__(THREADS) void rows_grad_kernel(const LayerNormArgs a, float* __restrict__ sums) {
   constexpr int V = Pack<T>::N, ROWS = THREADS / G, WAVES = THREADS / 64;
   constexpr bool BLOCK = G > 64;
@@ -257,7 +262,7 @@ __global__ __launch_bounds__(THREADS) void rows_grad_kernel(const LayerNormArgs 
   const T* gain = static_cast<const T*>(a.gain);
   Pack<T> g[U], x[U], dl[U];
   at.load_or(g, gain, 1.0f);
-  float g_gain[U][V] = {}, g_bias[U][V] = {};
+  float g_gain[COLUMNS ? U : 1][V] = {}, g_bias[COLUMNS ? U : 1][V] = {};
   const Count n(a.cols);
   const int64_t step = int64_t(gridDim.x) * ROWS;
   int64_t row = int64_t(blockIdx.x) * ROWS + threadIdx.x / G;
@@ -310,6 +315,7 @@ __global__ __launch_bounds__(THREADS) void rows_grad_kernel(const LayerNormArgs 
       for (int q = 0; q < 3; ++q) v[q] = group_sum<G>(v[q]);
     }
     const float rstd = rsqrt_of(n.mean(v[0]) + a.eps), mw = n.mean(v[1]), along = n.mean(v[2]) * rstd;
+    if (!COLUMNS && sums && threadIdx.x == 0) reinterpret_cast<float2*>(sums)[row] = make_float2(mean, rstd);
     renew();
     Pack<T> out[U];
     if (BLOCK || row < a.rows) {
@@ -319,8 +325,10 @@ __global__ __launch_bounds__(THREADS) void rows_grad_kernel(const LayerNormArgs 
         for (int e = 0; e < V; ++e) {
           const float h = (float(x[u].v[e]) - mean) * rstd, y = float(dl[u].v[e]);
           out[u].v[e] = T(rstd * fmaf(-h, along, weighted(u, e) - mw));
-          g_gain[u][e] = fmaf(y, h, g_gain[u][e]);
-          g_bias[u][e] += y;
+          if constexpr (COLUMNS) {
+            g_gain[u][e] = fmaf(y, h, g_gain[u][e]);
+            g_bias[u][e] += y;
+          }
         }
     }
     if (first + step < a.rows) load(row + step);  // before the stores, which it would wait for
@@ -331,6 +339,7 @@ __global__ __launch_bounds__(THREADS) void rows_grad_kernel(const LayerNormArgs 
     }
   }
 
+  if constexpr (!COLUMNS) return;
   auto put = [&](int which, int64_t c, float t) {
     T* result = static_cast<T*>(which ? a.g_bias : a.g_gain);
     if (!result) return;
@@ -345,7 +354,7 @@ __global__ __launch_bounds__(THREADS) void rows_grad_kernel(const LayerNormArgs 
     for (int u = 0; u < U; ++u) {
 #pragma unroll
       for (int e = 0; e < V; ++e) {
-        float t = which ? g_bias[u][e] : g_gain[u][e];
+        float t = which ? g_bias[COLUMNS ? u : 0][e] : g_gain[COLUMNS ? u : 0][e];
         if constexpr (BLOCK) {
           if (at.on(u) && at.counts(u, e)) put(which, at.at[u] + e, t);
         } else {
@@ -469,7 +478,8 @@ __global__ __launch_bounds__(kThreads) void long_rows_grad_kernel(const LayerNor
   }
 }
 
-// Sums over one part of the rows, for 64 packs of columns a block: sums[part] = [g_gain, g_bias]
+// Sums over one part of the rows, for 64 packs of columns a block: sums[part] =
+// [g_gain, g_bias], or, of all rows, the result.
 template <typename T>
 __global__ __launch_bounds__(kThreads) void column_grads_kernel(const LayerNormArgs a, const float2* __restrict__ stats,
                                                                 int64_t part, float* __restrict__ sums) {
@@ -499,7 +509,14 @@ __global__ __launch_bounds__(kThreads) void column_grads_kernel(const LayerNormA
       __syncthreads();
       for (int c = threadIdx.x; c < 64 * V; c += kThreads)
         if (j0 + c < a.cols)
-          sums[(int64_t(blockIdx.x) * 2 + which) * a.cols + j0 + c] = (s[0][c] + s[1][c]) + (s[2][c] + s[3][c]);
+{
+          const float t = (s[0][c] + s[1][c]) + (s[2][c] + s[3][c]);
+          T* result = static_cast<T*>(which ? a.g_bias : a.g_gain);
+          if (gridDim.x > 1)
+            sums[(int64_t(blockIdx.x) * 2 + which) * a.cols + j0 + c] = t;
+          else if (result)
+            result[j0 + c] = T(t);
+        }
       __syncthreads();
     }
   }
@@ -613,7 +630,7 @@ void with_grad_lanes(int64_t packs, F&& f) {
   f(Int<64>{}, Int<2>{});
 }
 // Longer rows, up to 8192 columns; past those the blocks would be one a CU.
-constexpr int64_t kGradCols = 8192;
+constexpr int64_t kGradCols = 8192, kManyRows = 1024;
 template <typename F>
 void with_grad_block(int64_t packs, F&& f) {
   if (packs <= 256) return f(Int<256>{}, Int<1>{});
@@ -628,11 +645,14 @@ struct Plan {
   int64_t part;    // rows of a part (not fused)
   size_t stats, total;
 };
-constexpr int64_t kPartRows = 16, kMaxParts = 2048, kCardPacks = 256 * 1024;
+constexpr int64_t kFewColumnRows = 128, kPartRows = 16, kMaxParts = 2048, kCardPacks = 256 * 1024;
 Plan plan_of(int64_t rows, int64_t cols, int64_t es) {
   Plan p{};
   const int64_t V = 16 / es, packs = ceil_div64(cols, V);
-  p.fused = cols <= kGradCols;
+  // Rows of a block each are summed as they are read where there are many, a launch
+  // later where their blocks would have few (64 x 16384 f16: 43 us, so 19; 64 x 4096
+  // bf16 13.9 and 12.5).
+  p.fused = packs <= kWavePacks || (cols <= kGradCols && rows >= kManyRows);
   if (p.fused) {
     int64_t at_once = 1, lanes = 0;  // rows a block takes at a time; its threads times their packs
     if (packs <= kWavePacks)
@@ -653,11 +673,12 @@ Plan plan_of(int64_t rows, int64_t cols, int64_t es) {
     p.total = p.stats;
     return p;
   }
-  // blocks of the column sums fill the card, with 16 rows each at least
+  // Blocks of the column sums take all of few rows; else they fill the card.
   const int64_t across = ceil_div64(packs, 64);
-  p.part = std::max(kPartRows, ceil_div64(rows, std::max<int64_t>(1, kMaxParts / across)));
+  p.part = rows <= kFewColumnRows ? std::max<int64_t>(1, rows)
+                                  : std::max(kPartRows, ceil_div64(rows, std::max<int64_t>(1, kMaxParts / across)));
   p.parts = ceil_div64(rows, p.part);
-  p.stats = size_t(ceil_div64(p.parts * 2 * cols * 4, 16)) * 16;
+  p.stats = p.parts > 1 ? size_t(ceil_div64(p.parts * 2 * cols * 4, 16)) * 16 : 0;
   p.total = p.stats + size_t(rows) * sizeof(float2);
   return p;
 }
@@ -671,18 +692,47 @@ hipError_t rows_grad(const LayerNormArgs& a, const Plan& p, float* sums, hipStre
     with_grad_lanes(packs, [&](auto g, auto u) {
       constexpr int G = decltype(g)::value, U = decltype(u)::value;
       if (a.cols < V) {
-        if constexpr (G == 1) rows_grad_kernel<T, 1, 1, END_TINY, kGradThreads><<<grid, kGradThreads, 0, s>>>(a, sums);
+        if constexpr (G == 1) rows_grad_kernel<T, 1, 1, END_TINY, kGradThreads, true><<<grid, kGradThreads, 0, s>>>(a, sums);
       } else if (a.cols == G * U * V) {
-        rows_grad_kernel<T, G, U, END_EXACT, kGradThreads><<<grid, kGradThreads, 0, s>>>(a, sums);
+        rows_grad_kernel<T, G, U, END_EXACT, kGradThreads, true><<<grid, kGradThreads, 0, s>>>(a, sums);
       } else {
-        rows_grad_kernel<T, G, U, END_SHARED, kGradThreads><<<grid, kGradThreads, 0, s>>>(a, sums);
+        rows_grad_kernel<T, G, U, END_SHARED, kGradThreads, true><<<grid, kGradThreads, 0, s>>>(a, sums);
       }
     });
   else
     with_grad_block(packs, [&](auto t, auto u) {
       constexpr int THREADS = decltype(t)::value;
-      rows_grad_kernel<T, THREADS, decltype(u)::value, END_SHARED, THREADS><<<grid, THREADS, 0, s>>>(a, sums);
+      rows_grad_kernel<T, THREADS, decltype(u)::value, END_SHARED, THREADS, true><<<grid, THREADS, 0, s>>>(a, sums);
     });
+  return hipGetLastError();
+}
+
+// g_x and the rows' mean and rstd.  Registers hold 16384 columns: with four 16-bit
+// packs a lane 1024 threads would spill.
+template <typename T>
+constexpr int64_t kAlonePacks = sizeof(T) == 4 ? 4096 : 2048;
+template <typename T>
+hipError_t rows_alone(const LayerNormArgs& a, float2* stats, hipStream_t s) {
+  const int64_t packs = ceil_div64(a.cols, Pack<T>::N);
+  const uint32_t grid = uint32_t(std::min(a.rows, kMaxBlocks));
+  auto launch = [&](auto t, auto u) {
+    constexpr int THREADS = decltype(t)::value;
+    rows_grad_kernel<T, THREADS, decltype(u)::value, END_SHARED, THREADS, false>
+        <<<grid, THREADS, 0, s>>>(a, reinterpret_cast<float*>(stats));
+  };
+  if (packs <= 256)
+    launch(Int<256>{}, Int<1>{});
+  else if (packs <= 512)
+    launch(Int<256>{}, Int<2>{});
+  else if (packs <= 1024)
+    launch(Int<512>{}, Int<2>{});
+  else if (packs <= 2048)
+    launch(Int<1024>{}, Int<2>{});
+  else if (packs <= kAlonePacks<T>) {
+    if constexpr (kAlonePacks<T> > 2048) launch(Int<1024>{}, Int<4>{});
+  } else {
+    long_rows_grad_kernel<T><<<grid, kThreads, 0, s>>>(a, stats);
+  }
   return hipGetLastError();
 }
 
@@ -698,13 +748,11 @@ hipError_t backward(const LayerNormArgs& a, hipStream_t s) {
       if ((e = rows_grad<T>(a, p, sums, s)) != hipSuccess || p.parts == 1) return e;
     } else {
       float2* stats = reinterpret_cast<float2*>(static_cast<char*>(a.scratch) + p.stats);
-      const uint32_t grid = uint32_t(std::min(a.rows, kMaxBlocks));
-      long_rows_grad_kernel<T><<<grid, kThreads, 0, s>>>(a, columns ? stats : nullptr);
-      if ((e = hipGetLastError()) != hipSuccess) return e;
+      if ((e = rows_alone<T>(a, columns ? stats : nullptr, s)) != hipSuccess) return e;
       if (columns) {
         const dim3 parts(uint32_t(p.parts), uint32_t(std::min<int64_t>(ceil_div64(a.cols, 64 * Pack<T>::N), 65535)));
         column_grads_kernel<T><<<parts, kThreads, 0, s>>>(a, stats, p.part, sums);
-        if ((e = hipGetLastError()) != hipSuccess) return e;
+        if ((e = hipGetLastError()) != hipSuccess || p.parts == 1) return e;
       }
     }
   }

@@ -74,7 +74,8 @@ def test_layer_norm_backward(rows, cols, dtype, gain, pad):
 
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("rows,cols,pad", [(70001, 8, 0), (300007, 2, 0), (100000, 34, 3), (20000, 256, 0),
-                                           (20001, 510, 8), (3000, 2046, 1), (1000, 9000, 0), (300, 17000, 0)])
+                                           (20001, 510, 8), (3000, 2046, 1), (1100, 3000, 3), (1000, 9000, 0), (300, 17000, 0),
+                                           (129, 5000, 1), (128, 5000, 0)])
 def test_column_sums_are_exact_in_whole_numbers(rows, cols, pad, dtype):
     """Rows of as many 1 as -1 with eps = 0: mean 0, variance 1 and h = x exactly, so the sums over rows are of whole
     numbers below 2^24, exact in float in any order, and rounded once: every row is in them, once."""
