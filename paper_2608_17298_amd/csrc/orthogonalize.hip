@@ -373,12 +373,28 @@ __global__ __launch_bounds__(64 * (JOIN ? 1 : W * W) * WK, 1) void pair_kernel(c
     for (int i = 0; i < RI; ++i)
 #pragma unroll
       for (int j = 0; j < RJ; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    for (int q = 0; q < g.parts; ++q) {
-      const float* from = g.partial + (int64_t(q) * g.tiles + which) * (THREADS * RI * RJ * 4) + tid * 4;
+    // Four parts' sums are asked for before the first is added; past the end the last one again.
+    constexpr int AHEAD = 4;
+    f32x4 next[AHEAD][RI][RJ];
+    auto load = [&](f32x4(&to)[RI][RJ], int q) {
+      const float* from = g.partial + (int64_t(min(q, g.parts - 1)) * g.tiles + which) * (THREADS * RI * RJ * 4) + tid * 4;
 #pragma unroll
       for (int i = 0; i < RI; ++i)
 #pragma unroll
-        for (int j = 0; j < RJ; ++j) acc[i][j] += *reinterpret_cast<const f32x4*>(from + (i * RJ + j) * THREADS * 4);
+        for (int j = 0; j < RJ; ++j) to[i][j] = *reinterpret_cast<const f32x4*>(from + (i * RJ + j) * THREADS * 4);
+    };
+    for (int q = 0; q < g.parts; q += AHEAD) {
+#pragma unroll
+      for (int h = 0; h < AHEAD; ++h) load(next[h], q + h);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int h = 0; h < AHEAD; ++h) {
+        if (q + h >= g.parts) break;
+#pragma unroll
+        for (int i = 0; i < RI; ++i)
+#pragma unroll
+          for (int j = 0; j < RJ; ++j) acc[i][j] += next[h][i][j];
+      }
     }
   } else {
     f32x4 sum[FRAG][FRAG];
