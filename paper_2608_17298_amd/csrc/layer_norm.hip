@@ -303,7 +303,8 @@ __global__ __launch_bounds__(THREADS) void rows_grad_kernel(const LayerNormArgs 
     for (int u = 0; u < U; ++u)
 #pragma unroll
       for (int e = 0; e < V; ++e) {
-        const float d = float(x[u].v[e]) - mean, w = at.weighed(u, e, weighted(u, e));
+        // a choice, no weight: an infinite dl makes no NaN of its row
+        const float d = float(x[u].v[e]) - mean, w = at.counts(u, e) ? weighted(u, e) : 0.0f;
         v[0] = fmaf(at.weighed(u, e, d), d, v[0]);
         v[1] += w;
         v[2] = fmaf(w, d, v[2]);

@@ -106,7 +106,7 @@ __global__ __launch_bounds__(kThreads) void prepare_kernel(const Source<T> u, in
   __shared__ double s_sum[kThreads / 64];
   __shared__ __attribute__((aligned(16))) float s_tile[64 * kTilePitch];
   const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-  const int64_t r0 = int64_t(blockIdx.y) * 64, c0 = int64_t(blockIdx.x) * 64;
+  const int64_t tiles = (cols + 63) / 64, r0 = blockIdx.x / tiles * 64, c0 = blockIdx.x % tiles * 64;
   float w[EACH][V];  // all asked for first
 #pragma unroll
   for (int q = 0; q < EACH; ++q) {
@@ -124,7 +124,7 @@ __global__ __launch_bounds__(kThreads) void prepare_kernel(const Source<T> u, in
   const double size = sqrt((s_sum[0] + s_sum[1]) + (s_sum[2] + s_sum[3]));
   bool tiny;
   const double inv = first_scale(it, size, tiny);
-  if (blockIdx.x == 0 && blockIdx.y == 0) {
+  if (blockIdx.x == 0) {
     if (!tiny) {
       if (threadIdx.x < it.steps) factors[threadIdx.x] = it.of_one.step[threadIdx.x];
     } else if (threadIdx.x == 0) {
@@ -560,7 +560,7 @@ hipError_t run(const OrthogonalizeArgs& a, hipStream_t s) {
     squares_kernel<T, false><<<uint32_t(count), kThreads, 0, s>>>(u, nullptr, a.rows, a.cols, log_lanes, sums);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  const dim3 grid(uint32_t((p.tall ? p.n_pad : p.m_pad) / 64), uint32_t((p.tall ? p.m_pad : p.n_pad) / 64));
+  const uint32_t grid = uint32_t(p.n_pad / 64 * (p.m_pad / 64));
   if (a.m)
     prepare_kernel<T, true><<<grid, kThreads, 0, s>>>(u, a.rows, a.cols, p.tall, sums, count, it, factors, x[0], xt[0]);
   else

@@ -50,6 +50,10 @@ __device__ __forceinline__ void small_product(f32x4 (&sum)[FRAG][FRAG], const Bl
         for (int j = 0; j < FRAG; ++j)
           sum[i][j] = Mfma<f16>::run(p == 0 ? bl[j] : bh[j], p == 1 ? al[i] : ah[i], sum[i][j]);
   }
+#pragma unroll
+  for (int i = 0; i < FRAG; ++i)
+#pragma unroll
+    for (int j = 0; j < FRAG; ++j) arrive(sum[i][j]);  // read before the barrier behind which LDS is written again
 }
 
 // Four consecutive columns of a row into blocks, and into those of the transpose.

@@ -249,6 +249,25 @@ def test_nonfinite_stays_in_its_row(rows, cols, value, dtype):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("cols", [6, 13, 50, 130, 1023, 2047, 5001, 9001])
+def test_infinite_dl_is_the_same_at_both_ends_of_a_row(cols, dtype):
+    """Packs overlap at a row's end: what is infinite there counts once, as at the beginning.  With dl = (inf, 1, 1 ..)
+    mean(w) is infinite, so g_x is the NaN or the infinity that the formula has."""
+    import torch
+    rng = np.random.default_rng(cols)
+    x, x64 = _rows(rng, 3, cols, dtype)
+    for at in (0, cols - 1, cols - 2):
+        dl = torch.ones_like(x)
+        dl[1, at] = float("inf")
+        gx, gg, gb = _grads(x, dl, None, dtype)
+        with np.errstate(invalid="ignore"):
+            want, want_gain, _ = ref.norm_grads(x64, dl.cpu().double().numpy(), None, EPS32)
+        assert np.array_equal(np.isnan(gx), np.isnan(want)) and np.array_equal(np.isinf(gx), np.isinf(want))
+        assert np.isinf(gb[at]) and np.isfinite(np.delete(gb, at)).all() and np.isfinite(np.delete(gg, at)).all()
+        assert not np.isnan(gg[at])
+
+
+@pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("rows,cols,pad", [(33, 5, 3), (100, 48, 0), (9, 1023, 1), (5, 5000, 8), (3, 17001, 3),
                                            (2, 70001, 0)])
 def test_in_place_and_repeated_rows(rows, cols, pad, dtype):

@@ -85,6 +85,32 @@ def test_steps(rows, cols, steps):
     _exact_as_float32(_orthogonalize(x, "f32", steps=steps), x64, "f32", steps=steps)
 
 
+@pytest.mark.parametrize("rows,cols", [(30, 50), (100, 128), (300, 200), (1100, 1000)])
+def test_most_steps(rows, cols):
+    """64 steps of polynomials that settle at 1: the result's singular values are 1, as nearly as float32's steps'."""
+    rng = np.random.default_rng(rows)
+    x, x64 = _device(rng.standard_normal((rows, cols)), "f32")
+    abc = (1.875, -1.25, 0.375)
+    got = _orthogonalize(x, "f32", steps=64, abc=abc)
+    _exact_as_float32(got, x64, "f32", steps=64, abc=list(abc))
+
+
+def test_more_tiles_of_rows_than_a_grid_is_high():
+    """Four million rows of two columns: 65626 tiles of 64."""
+    import torch
+    from paper_2608_17298_amd import gart
+    if torch.cuda.mem_get_info()[0] < 12 << 30:
+        pytest.skip("needs 9 GB of device memory")
+    rng = np.random.default_rng(8)
+    x, x64 = _device(rng.standard_normal((4_200_001, 2)).astype(np.float32), "bf16")
+    y = torch.empty_like(x)
+    gart.gart_orthogonalize(x, y, _how(gart), _scratch(gart.gart_orthogonalize_scratch_bytes(*x.shape, x.dtype)))
+    want = ref.orthogonalize(x64)
+    got = y.cpu().double().numpy()
+    # sums of 4.2 million terms, in parts of at most 131250 blocks of 32: their relative error stays below 2^-8 / 4
+    assert (np.abs(got - want) <= 1.25 * blocks_ref.U["bf16"] * np.abs(want) + 1e-9).all()
+
+
 @pytest.mark.parametrize("abc", [(1.5, -0.5, 0.0), (1.875, -1.25, 0.375), (2.0, -1.5, 0.5), (0.5, 0.0, 0.0),
                                  (0.8, 0.0, 0.2), (-3.0, 4.0, -1.5), (0.0, 0.0, 0.0), (4.0, 0.0, 0.0)])
 @pytest.mark.parametrize("rows,cols", [(20, 30), (70, 300), (300, 200), (400, 1000)])
