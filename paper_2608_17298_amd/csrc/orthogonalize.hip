@@ -8,7 +8,7 @@
 //
 // Products run on the float16 matrix cores with operands in two parts
 // (orthogonalize.h): high high + high low + low high, sums in float, so that the
-// result is float32's (2-norm 2.4e-6 off at 512 x 512, as the same steps in float32
+// result is float32's (2-norm 2.4e-6 off at 256 x 256, as the same steps in float32
 // are).  With operands rounded once to float16 it is 1e-3 to 4e-3 off, more than
 // bfloat16's rounding of the result.  Large float32 products run at 154 TFLOP/s on
 // this card and float16 ones at 1430, so three of those are a third of the time.
