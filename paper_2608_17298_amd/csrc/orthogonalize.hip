@@ -10,8 +10,8 @@
 // (orthogonalize.h): high high + high low + low high, sums in float, so that the
 // result is float32's (2-norm 2.4e-6 off at 256 x 256, as the same steps in float32
 // are).  With operands rounded once to float16 it is 1e-3 to 4e-3 off, more than
-// bfloat16's rounding of the result.  Large float32 products run at 154 TFLOP/s on
-// this card and float16 ones at 1430, so three of those are a third of the time.
+// bfloat16's rounding of the result.  A large product runs at 153 TFLOP/s in float32 on
+// this card and at 1106 in float16, so three of those take less than half the time.
 // a X is added in float: inside P it would double the error.
 #include "orthogonalize_small.h"
 #include "tile.h"
@@ -96,7 +96,8 @@ __device__ __forceinline__ void store_blocks(const float* tile, const Blocks& to
 }
 
 // X and its transpose, zero in the padding, from u over its norm: 64 x 64 elements a
-// block; and the steps' factors, by the first one.
+// block; and the steps' factors, by the first one.  Bound by bytes and the two orders
+// of the stores: 1024 x 4096 bf16 in 15 us.
 template <typename T, bool MOMENTUM>
 __global__ __launch_bounds__(kThreads) void prepare_kernel(const Source<T> u, int64_t rows, int64_t cols, bool tall,
                                                            const double* __restrict__ sums, int count,
@@ -319,6 +320,8 @@ __device__ __forceinline__ void shared_sums(f32x4 (&sum)[4][4], const PairArgs& 
 }
 
 // A tile of 16 FRAG W on a side.  JOIN: the sums of k are those of g.parts parts.
+// 1024 x 4096: X X^T in seven parts 20 us and their join 8, A A 12, P X 33, of which 10
+// are its stores and 31 % matrix instructions; its LDS reads take as long as those.
 template <typename T, int FRAG, int W, int WK, PairEpilogue EPI, bool JOIN>
 __global__ __launch_bounds__(64 * (JOIN ? 1 : W * W) * WK, 1) void pair_kernel(const PairArgs g) {
   constexpr int PLACES = JOIN ? 1 : W * W;  // tiles of waves in a block: a join has one, to have more blocks
