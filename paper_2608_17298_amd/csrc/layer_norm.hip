@@ -390,14 +390,24 @@ __global__ __launch_bounds__(THREADS) void rows_grad_kernel(const LayerNormArgs 
 }
 
 // ---- rows of any length: a block a row, read once for each sum -----------------
+constexpr int kLongThreads = 1024, kLongWaves = kLongThreads / 64;
+// f(first column, columns) of a thread's packs, four whole ones at a time as long as
+// there are, so that four loads are on their way (with 256 threads and one at a time
+// 1000 x 65536 f16 100 us, so 76; 64 x 1000003 f32 1511 and 478).  Bound by reading x
+// again, out of the caches while all blocks' rows fit them.
 template <typename T, typename F>
 __device__ __forceinline__ void for_packs(int64_t cols, F&& f) {
-  for (int64_t c = int64_t(threadIdx.x) * Pack<T>::N; c < cols; c += kThreads * Pack<T>::N)
-    f(c, int(min(int64_t(Pack<T>::N), cols - c)));
+  constexpr int N = Pack<T>::N, STEP = kLongThreads * N;
+  int64_t c = int64_t(threadIdx.x) * N;
+  for (; c + 3 * STEP + N <= cols; c += 4 * STEP) {
+#pragma unroll
+    for (int u = 0; u < 4; ++u) f(c + u * STEP, N);
+  }
+  for (; c < cols; c += STEP) f(c, int(min(int64_t(N), cols - c)));
 }
 
 template <typename T>
-__device__ __forceinline__ float row_mean(const T* x, int64_t cols, float (&s)[kWaves][1]) {
+__device__ __forceinline__ float row_mean(const T* x, int64_t cols, float (&s)[kLongWaves][1]) {
   float v[1] = {0.0f};
   for_packs<T>(cols, [&](int64_t c, int count) {
     const Pack<T> p = load_some(x + c, count);
@@ -409,8 +419,8 @@ __device__ __forceinline__ float row_mean(const T* x, int64_t cols, float (&s)[k
 }
 
 template <typename T>
-__global__ __launch_bounds__(kThreads) void long_rows_kernel(const LayerNormArgs a) {
-  __shared__ float s[kWaves][1];
+__global__ __launch_bounds__(kLongThreads) void long_rows_kernel(const LayerNormArgs a) {
+  __shared__ float s[kLongWaves][1];
   const T* gain = static_cast<const T*>(a.gain);
   const T* bias = static_cast<const T*>(a.bias);
   for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
@@ -446,8 +456,8 @@ __global__ __launch_bounds__(kThreads) void long_rows_kernel(const LayerNormArgs
 
 // g_x, and the rows' mean and rstd for the column sums
 template <typename T>
-__global__ __launch_bounds__(kThreads) void long_rows_grad_kernel(const LayerNormArgs a, float2* __restrict__ stats) {
-  __shared__ float s1[kWaves][1], s3[kWaves][3];
+__global__ __launch_bounds__(kLongThreads) void long_rows_grad_kernel(const LayerNormArgs a, float2* __restrict__ stats) {
+  __shared__ float s1[kLongWaves][1], s3[kLongWaves][3];
   const T* gain = static_cast<const T*>(a.gain);
   for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
     const T* x = static_cast<const T*>(a.x) + row * a.x_ld;
@@ -617,7 +627,7 @@ hipError_t forward(const LayerNormArgs& a, hipStream_t s) {
     });
     return hipGetLastError();
   }
-  long_rows_kernel<T><<<uint32_t(std::min(a.rows, kMaxBlocks)), kThreads, 0, s>>>(a);
+  long_rows_kernel<T><<<uint32_t(std::min(a.rows, kMaxBlocks)), kLongThreads, 0, s>>>(a);
   return hipGetLastError();
 }
 
@@ -741,7 +751,7 @@ hipError_t rows_alone(const LayerNormArgs& a, float2* stats, hipStream_t s) {
   else if (packs <= kAlonePacks<T>) {
     if constexpr (kAlonePacks<T> > 2048) launch(Int<1024>{}, Int<4>{});
   } else {
-    long_rows_grad_kernel<T><<<grid, kThreads, 0, s>>>(a, stats);
+    long_rows_grad_kernel<T><<<grid, kLongThreads, 0, s>>>(a, stats);
   }
   return hipGetLastError();
 }
