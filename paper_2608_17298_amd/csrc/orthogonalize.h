@@ -109,6 +109,45 @@ inline int64_t blocks_of(int64_t rows, int64_t cols, int side, bool symmetric) {
   const int64_t i = (rows + side - 1) / side, j = (cols + side - 1) / side, even = i + i % 2;
   return symmetric ? even / 2 * (even + 1) : i * j;
 }
+
+// The tiles of a product.  Blocks go to the eight XCDs in turn; each XCD gets a run of
+// tiles, of one or two parts of k, that covers a patch of `band` rows, so that its
+// cache takes in few rows of both operands.  A triangle of tiles (i <= j) is folded to
+// half as many rows: row r, then row n - 1 - r.
+struct TileOrder {
+  int tiles_i, tiles_j, band;
+  bool symmetric;
+};
+inline TileOrder tile_order(int64_t rows, int64_t cols, int side, bool symmetric) {
+  TileOrder o{int((rows + side - 1) / side), int((cols + side - 1) / side), 1, symmetric};
+  const int tiles = int(blocks_of(rows, cols, side, symmetric));
+  while (o.band * o.band * 8 < tiles) ++o.band;
+  return o;
+}
+// Tile t of those launched; false where there is none.
+GART_HOST_DEVICE inline bool find_tile(const TileOrder& o, int t, int& ti, int& tj) {
+  const int n = o.tiles_i, even = n + n % 2;
+  const int rows = o.symmetric ? even / 2 : n, cols = o.symmetric ? even + 1 : o.tiles_j;
+  const int top = t / (o.band * cols) * o.band, high = o.band < rows - top ? o.band : rows - top;
+  const int in = t - top * cols, r = top + in % high, c = in / high;
+  ti = r;
+  tj = c;
+  if (o.symmetric) {
+    const bool folded = c >= even - r;
+    ti = folded ? even - 1 - r : r;
+    tj = folded ? ti + c - (even - r) : r + c;
+  }
+  return ti < n && tj < o.tiles_j;
+}
+// Whether the part of a tile from (i0, j0) is a result.  Each wave stores what it has
+// formed of a symmetric product on both sides of the diagonal.  A tile on the diagonal
+// that several waves share has a part below it: the one above stores that one too, and
+// its own sums would not be the same bits, as they add the low parts' products in the
+// other order.
+GART_HOST_DEVICE inline bool is_result(const TileOrder& o, int64_t rows, int64_t cols, int64_t i0, int64_t j0) {
+  return i0 < rows && j0 < cols && !(o.symmetric && i0 > j0);
+}
+
 inline PairCut cut_pair(int64_t rows, int64_t cols, int64_t steps, bool symmetric) {
   // measured: us of a block of k for each tile, and of what surrounds the sums
   constexpr int kSides[3] = {32, 64, 128};

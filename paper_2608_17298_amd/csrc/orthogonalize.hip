@@ -165,8 +165,7 @@ struct PairArgs {
   Blocks a, b, d;       // d.data may be NULL
   int64_t rows, cols;   // of C
   int64_t steps;        // blocks along k
-  int tiles_i, tiles_j, band;
-  bool symmetric;       // C is: tiles above the diagonal are stored on both sides of it
+  TileOrder order;      // symmetric: C is, tiles above the diagonal are stored on both sides of it
   int tiles;            // launched for them, for each part of k
   int parts;
   float* partial;       // their sums
@@ -176,25 +175,6 @@ struct PairArgs {
   int64_t y_ld, y_rows, y_cols;
   float decay, step;    // PAIR_STEP: y -= decay y + step C
 };
-
-// Blocks go to the eight XCDs in turn.  Each gets a run of tiles (xcd_tile), of one or
-// two parts of k, that covers a patch of `band` rows, so that its cache takes in few
-// rows of both operands.  A triangle of tiles (i <= j) is folded to half as many rows:
-// row r, then row n - 1 - r.
-__device__ __forceinline__ bool find_tile(const PairArgs& g, int t, int& ti, int& tj) {
-  const int n = g.tiles_i, even = n + n % 2;
-  const int rows = g.symmetric ? even / 2 : n, cols = g.symmetric ? even + 1 : g.tiles_j;
-  const int top = t / (g.band * cols) * g.band, high = min(g.band, rows - top);
-  const int in = t - top * cols, r = top + in % high, c = in / high;
-  ti = r;
-  tj = c;
-  if (g.symmetric) {
-    const bool folded = c >= even - r;
-    ti = folded ? even - 1 - r : r;
-    tj = folded ? ti + c - (even - r) : r + c;
-  }
-  return ti < n && tj < g.tiles_j;
-}
 
 // The sums of a product, two ways:
 //
@@ -337,11 +317,11 @@ __global__ __launch_bounds__(64 * (JOIN ? 1 : W * W) * WK, 1) void pair_kernel(c
   const int at_xcd = int(xcd_tile(blockIdx.x, gridDim.x)), which = JOIN ? at_xcd / (W * W) : at_xcd;
   const int part = which / g.tiles;  // 0 but for PAIR_PART
   int ti, tj;
-  if (!find_tile(g, which - part * g.tiles, ti, tj)) return;
+  if (!find_tile(g.order, which - part * g.tiles, ti, tj)) return;
   const int wk = wave / PLACES, place = JOIN ? at_xcd % (W * W) : wave % PLACES, wi = place / W, wj = place % W;
   const int tid = (wk * W * W + place) * 64 + lane;  // of the block that sums
   const int64_t i0 = (int64_t(ti) * W + wi) * SIDE, j0 = (int64_t(tj) * W + wj) * SIDE;
-  const bool inside = i0 < g.rows && j0 < g.cols;
+  const bool inside = is_result(g.order, g.rows, g.cols, i0, j0);
   const int first_i = wk * RI * RJ / FRAG, first_j = wk * RI * RJ % FRAG;
   const int r = lane % 16, g4 = lane / 16;
   typedef f16 f16x4 __attribute__((ext_vector_type(4)));
@@ -498,7 +478,7 @@ __global__ __launch_bounds__(64 * (JOIN ? 1 : W * W) * WK, 1) void pair_kernel(c
     __syncthreads();
     if (!inside) return;
     store_blocks<SIDE, false>(tile, g.out, i0, j0, lane, wk, WK);
-    if (!g.symmetric)
+    if (!g.order.symmetric)
       store_blocks<SIDE, true>(tile, g.across, j0, i0, lane, WK - 1 - wk, WK);
     else if (i0 != j0)
       store_blocks<SIDE, true>(tile, g.out, j0, i0, lane, WK - 1 - wk, WK);
@@ -507,13 +487,9 @@ __global__ __launch_bounds__(64 * (JOIN ? 1 : W * W) * WK, 1) void pair_kernel(c
 
 template <typename T, int FRAG, int W, int WK, PairEpilogue EPI>
 hipError_t run_tiles(PairArgs g, const PairCut& c, hipStream_t s) {
-  g.tiles_i = int((g.rows + c.side - 1) / c.side);
-  g.tiles_j = int((g.cols + c.side - 1) / c.side);
-  g.symmetric = c.symmetric;
+  g.order = tile_order(g.rows, g.cols, c.side, c.symmetric);
   g.parts = c.parts;
   g.tiles = int(blocks_of(g.rows, g.cols, c.side, c.symmetric));
-  g.band = 1;
-  while (g.band * g.band * 8 < g.tiles) ++g.band;
   constexpr int THREADS = 64 * W * W * WK;
   if (c.parts == 1) {
     pair_kernel<T, FRAG, W, WK, EPI, false><<<uint32_t(g.tiles), THREADS, 0, s>>>(g);
