@@ -54,13 +54,13 @@ GART_HOST_DEVICE inline double step_scales(double a, double b, double c, double 
   if (!(p <= kMaxPolynomial)) return HUGE_VAL;
   // p'(s) = a + 3 b t + 5 c t^2 = 0 with t = s^2
   double next = sqrt(s2) * fabs(a + b * s2 + c * s2 * s2);
+  // by the sum that does not cancel, so that a small c (or 0) leaves the root -a / 3b
   double t[2] = {-1.0, -1.0};
   const double disc = 9.0 * b * b - 20.0 * a * c;
-  if (c != 0.0 && disc >= 0.0) {
-    t[0] = (-3.0 * b - sqrt(disc)) / (10.0 * c);
-    t[1] = (-3.0 * b + sqrt(disc)) / (10.0 * c);
-  } else if (c == 0.0 && b != 0.0) {
-    t[0] = -a / (3.0 * b);
+  if (disc >= 0.0) {
+    const double q = -0.5 * (3.0 * b + copysign(sqrt(disc), b));
+    if (c != 0.0) t[0] = q / (5.0 * c);
+    if (q != 0.0) t[1] = a / q;
   }
   for (int k = 0; k < 2; ++k)
     if (t[k] > 0.0 && t[k] < s2) next = larger(next, sqrt(t[k]) * fabs(a + b * t[k] + c * t[k] * t[k]));

@@ -29,3 +29,17 @@ def test_one_step_element_by_element(rows, cols, dtype):
     rng = np.random.default_rng(rows + 5 * cols)
     x, x64 = _device(_gradient(rng, rows, cols, "normal"), dtype, 1)
     _within(_orthogonalize(x, dtype, 3, steps=1), ref.orthogonalize(x64, 1), ref.one_step_tolerance(x64, dtype))
+
+
+@pytest.mark.parametrize("abc", [(3.0, -2.9, 1e-17), (3.0, -3.0, -1e-20), (2.0, -1.9, 1e-30), (-2.0, 1e-25, 2.0)])
+@pytest.mark.parametrize("rows,cols", [(2, 5), (20, 30), (70, 300), (300, 200), (500, 700)])
+@pytest.mark.parametrize("size", [1.0, 1e-9])
+def test_polynomials_with_a_small_coefficient(rows, cols, size, abc):
+    """Two singular values of 0.7, in an element each, which the polynomial takes past 1 where the largest of its values
+    lies; and, with eps as large, smaller ones."""
+    x = np.zeros((rows, cols))
+    x[0, 0] = x[1, cols - 1] = size
+    t, x64 = _device(x, "f32")
+    got = _orthogonalize(t, "f32", steps=3, abc=abc)
+    assert np.isfinite(got).all()
+    _exact_as_float32(got, x64, "f32", steps=3, abc=[float(np.float32(v)) for v in abc])
