@@ -120,8 +120,8 @@ struct TileOrder {
 };
 inline TileOrder tile_order(int64_t rows, int64_t cols, int side, bool symmetric) {
   TileOrder o{int((rows + side - 1) / side), int((cols + side - 1) / side), 1, symmetric};
-  const int tiles = int(blocks_of(rows, cols, side, symmetric));
-  while (o.band * o.band * 8 < tiles) ++o.band;
+  const int tiles = int(blocks_of(rows, cols, side, symmetric)), most = symmetric ? (o.tiles_i + 1) / 2 : o.tiles_i;
+  while (o.band < most && o.band * o.band * 8 < tiles) ++o.band;  // find_tile multiplies it by the columns
   return o;
 }
 // Tile t of those launched; false where there is none.

@@ -55,3 +55,25 @@ def test_every_block_of_a_product_has_one_writer(tmp_path, side):
     any_size = [(64 * n, 64 * m, side, 0) for n in (1, 2, 3, 7, 16, 33) for m in (1, 2, 5, 8, 31, 200)]
     for q, got in zip(square + any_size, _ask(tmp_path, WRITERS, square + any_size)):
         assert got == (1, 1), q
+
+
+ORDER = """
+int main() {
+  long long rows, cols;
+  int side, symmetric;
+  while (std::scanf("%lld %lld %d %d", &rows, &cols, &side, &symmetric) == 4) {
+    const TileOrder o = tile_order(rows, cols, side, symmetric != 0);
+    std::printf("%d %d %d\\n", o.tiles_i, o.tiles_j, o.band);
+  }
+}
+"""
+
+
+def test_order_of_the_most_tiles_stays_in_32_bits(tmp_path):
+    """Up to 2^23 tiles of 64 x 64 in all, in one row of tiles as well: what find_tile multiplies fits an int."""
+    queries = [(64 * n, 64 * (2 ** 23 // n), side, 0) for n in (1, 2, 3, 5, 64, 2896, 2 ** 22, 2 ** 23)
+               for side in (32, 64, 128)]
+    queries += [(64 * n, 64 * n, side, 1) for n in (1, 2, 63, 1000, 2896) for side in (32, 64, 128)]
+    for q, (i, j, band) in zip(queries, _ask(tmp_path, ORDER, queries)):
+        rows, cols = ((i + i % 2) // 2, i + i % 2 + 1) if q[3] else (i, j)
+        assert 1 <= band <= rows and rows * cols < 2 ** 31 and band * cols < 2 ** 31, q
