@@ -578,8 +578,9 @@ size_t gart_orthogonalize_scratch_bytes(int64_t rows, int64_t cols, gart_dtype d
 
 /* y = the iteration's result for x; y may be x.  Products are formed of operands
  * of 22 bits with float32 sums and rounded to the type once, at the end, so the
- * result is as exact as the same steps in float32.  x = 0 gives 0 (NaN with
- * eps = 0); an x that holds a NaN or an infinity gives NaN throughout.
+ * result is as exact as the same steps in float32 (elements below 2^-122
+ * aside).  x = 0 gives 0 (NaN with eps = 0); an x that holds a NaN or an infinity
+ * gives NaN throughout.
  * INVALID_ARG also for coefficients whose steps may take a singular value of 1
  * or less past 1024.  UNSUPPORTED for more than 2^23 tiles of 64 x 64. */
 gart_status gart_orthogonalize(const gart_matrix* x, const gart_newton_schulz* how, gart_dtype dtype,

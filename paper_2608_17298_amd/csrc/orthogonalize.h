@@ -34,13 +34,15 @@ struct StepScales {
 };
 
 // The power of two by which numbers up to `bound` are multiplied.  Beyond the clamps
-// a result of float has nothing left (X), or the matrix adds nothing to a X (A, P).
+// a result of float has nothing left (X; A and P with a small a; 2^-122, where the
+// product's last factor ends, counts as nothing), or the matrix adds nothing to a X
+// (A and P with |P| below 2^-24 |a|).
 GART_HOST_DEVICE inline double pair_scale(double bound, int most) {
   if (!(bound > 0.0)) return 1.0;
   const int e = 13 - ilogb(bound);
   return ldexp(1.0, e > most ? most : e < -60 ? -60 : e);
 }
-constexpr int kMostX = 120, kMostA = 60;
+constexpr int kMostX = 120, kMostA = 60, kMostAlone = 120;
 
 GART_HOST_DEVICE inline double larger(double a, double b) { return a > b ? a : b; }
 
@@ -50,7 +52,8 @@ GART_HOST_DEVICE inline double step_scales(double a, double b, double c, double 
   double p = fabs(b * s2 + c * s2 * s2);
   const double top = c != 0.0 ? -b / (2.0 * c) : -1.0;
   if (top > 0.0 && top < s2) p = larger(p, fabs(b * top + c * top * top));
-  *out = StepScales{pair_scale(bound, kMostX), pair_scale(s2, kMostA), pair_scale(p, kMostA)};
+  const int most = fabs(a) < 0x1p24 * p ? kMostAlone : kMostA;
+  *out = StepScales{pair_scale(bound, kMostX), pair_scale(s2, most), pair_scale(p, most)};
   if (!(p <= kMaxPolynomial)) return HUGE_VAL;
   // p'(s) = a + 3 b t + 5 c t^2 = 0 with t = s^2
   double next = sqrt(s2) * fabs(a + b * s2 + c * s2 * s2);

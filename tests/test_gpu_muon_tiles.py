@@ -43,3 +43,14 @@ def test_polynomials_with_a_small_coefficient(rows, cols, size, abc):
     got = _orthogonalize(t, "f32", steps=3, abc=abc)
     assert np.isfinite(got).all()
     _exact_as_float32(got, x64, "f32", steps=3, abc=[float(np.float32(v)) for v in abc])
+
+
+@pytest.mark.parametrize("abc", [(0.0, 1.5, -0.5), (1e-20, 1.5, -0.5)])
+@pytest.mark.parametrize("rows,cols", [(20, 30), (70, 300), (300, 200)])
+@pytest.mark.parametrize("size", [1e-13, 1e-18, 1e-19])
+def test_small_matrices_where_the_linear_term_is_small(rows, cols, size, abc):
+    """A matrix far smaller than eps, whose a X does not hide what P X has lost."""
+    rng = np.random.default_rng(rows)
+    x, x64 = _device(rng.standard_normal((rows, cols)) * size / (rows * cols) ** 0.5, "f32")
+    _exact_as_float32(_orthogonalize(x, "f32", steps=1, abc=abc), x64, "f32", steps=1,
+                      abc=[float(np.float32(v)) for v in abc])
