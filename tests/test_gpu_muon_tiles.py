@@ -4,9 +4,10 @@ import numpy as np
 import pytest
 
 import muon_ref as ref
+import test_gpu_muon as plain
 from muon_sizes import SIZES
-from test_gpu_blocks import TYPES, _within
-from test_gpu_muon import _device, _exact_as_float32, _gradient, _orthogonalize
+from test_gpu_blocks import TYPES, _scratch, _within
+from test_gpu_muon import _device, _exact_as_float32, _gradient, _muon_h, _orthogonalize
 
 pytestmark = pytest.mark.gpu
 
@@ -29,6 +30,42 @@ def test_one_step_element_by_element(rows, cols, dtype):
     rng = np.random.default_rng(rows + 5 * cols)
     x, x64 = _device(_gradient(rng, rows, cols, "normal"), dtype, 1)
     _within(_orthogonalize(x, dtype, 3, steps=1), ref.orthogonalize(x64, 1), ref.one_step_tolerance(x64, dtype))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,cols", AT)
+@pytest.mark.parametrize("nesterov,pad,scale", [(True, 0, 1.0), (False, 3, 1.7)])
+def test_muon_step(rows, cols, dtype, nesterov, pad, scale):
+    plain.test_muon_step(rows, cols, dtype, nesterov, pad, scale)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,cols", [(48, 64), (300, 200), (500, 1500), (960, 2560), (2560, 960)])
+def test_muon_leaves_the_gradient(rows, cols, dtype):
+    import torch
+    from paper_2608_17298_amd import gart
+    rng = np.random.default_rng(6)
+    p, g = (_device(_gradient(rng, rows, cols), dtype, 3)[0] for _ in range(2))
+    m = _device(_gradient(rng, rows, cols), "f32")[0]
+    before = g.clone()
+    gart.gart_muon_step(p, g, m, _muon_h(gart, 1.0, True), _scratch(gart.gart_muon_scratch_bytes(rows, cols, p.dtype)))
+    assert torch.equal(g, before)
+
+
+@pytest.mark.parametrize("rows,cols,pad", [(960, 2560, 3), (2560, 960, 8), (1472, 1472, 0), (4090, 390, 1), (1000, 1100, 3)])
+def test_uses_nothing_around_its_inputs(rows, cols, pad):
+    plain.test_uses_nothing_around_its_inputs(rows, cols, pad, "bf16")
+
+
+@pytest.mark.parametrize("value", [float("nan"), float("inf")])
+@pytest.mark.parametrize("rows,cols", [(960, 2560), (2560, 960), (1930, 1921), (450, 3072)])
+def test_nonfinite(rows, cols, value):
+    plain.test_nonfinite(rows, cols, value, "f32")
+
+
+@pytest.mark.parametrize("rows,cols", [(1000, 2700), (2560, 960), (1930, 1921)])
+def test_another_stream_and_graphs(rows, cols):
+    plain.test_another_stream_and_graphs(rows, cols)
 
 
 @pytest.mark.parametrize("abc", [(3.0, -2.9, 1e-17), (3.0, -3.0, -1e-20), (2.0, -1.9, 1e-30), (-2.0, 1e-25, 2.0)])

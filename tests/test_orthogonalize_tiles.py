@@ -4,6 +4,9 @@ import subprocess
 
 import pytest
 
+import muon_sizes
+import test_gpu_muon
+
 CSRC = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2608_17298_amd", "csrc")
 
 
@@ -77,3 +80,40 @@ def test_order_of_the_most_tiles_stays_in_32_bits(tmp_path):
     for q, (i, j, band) in zip(queries, _ask(tmp_path, ORDER, queries)):
         rows, cols = ((i + i % 2) // 2, i + i % 2 + 1) if q[3] else (i, j)
         assert 1 <= band <= rows and rows * cols < 2 ** 31 and band * cols < 2 ** 31, q
+
+
+CUTS = """
+int main() {
+  long long rows, cols;
+  while (std::scanf("%lld %lld", &rows, &cols) == 2) {
+    const MatrixPlan p = matrix_plan(rows, cols);
+    const int64_t n = p.n_pad, m = p.m_pad;
+    const PairCut c[4] = {cut_pair(n, n, m / 32, true), cut_pair(n, n, n / 32, true), cut_pair(n, m, n / 32, false),
+                          p.tall ? cut_pair(m, n, n / 32, false) : cut_pair(n, m, n / 32, false)};
+    for (const PairCut& q : c) std::printf("%d %d ", q.side, q.parts);
+    std::printf("\\n");
+  }
+}
+"""
+
+
+def _cuts(tmp_path, sizes):
+    """of each size, by product: the tile's side, and whether the sums are cut into parts"""
+    return [[(v[2 * k], v[2 * k + 1] > 1) for k in range(4)] for v in _ask(tmp_path, CUTS, sizes)]
+
+
+def test_every_tile_is_reached_on_the_gpu(tmp_path):
+    """The tests' sizes take the tiles that they are listed for, and among them are all that any size takes."""
+    listed = _cuts(tmp_path, [s[:2] for s in muon_sizes.SIZES])
+    for (rows, cols, want), got in zip(muon_sizes.SIZES, listed):
+        assert tuple(got) == (*want, want[2]), (rows, cols)
+    steps = range(64, 2200, 64)
+    every = [(n, m) for n in steps for m in (*steps, *range(2240, 6000, 256), 20000, 100000)]
+    every += [(m, n) for n, m in every]
+    reached = {(k, rows > cols, *c) for (rows, cols), q in zip(test_gpu_muon.SIZES + [s[:2] for s in muon_sizes.SIZES],
+                                                                _cuts(tmp_path, test_gpu_muon.SIZES) + listed)
+               for k, c in enumerate(q)}
+    some = {(k, rows > cols, *c) for (rows, cols), q in zip(every, _cuts(tmp_path, every)) for k, c in enumerate(q)}
+    # A's and P's products do not know which way x lies
+    one_way = lambda s: {c if c[0] > 1 else (c[0], False, *c[2:]) for c in s}  # noqa: E731
+    assert one_way(some) <= one_way(reached), one_way(some) - one_way(reached)
