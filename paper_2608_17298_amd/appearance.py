@@ -20,8 +20,6 @@ import torch
 
 from . import gart
 
-WEIGHTS = ("w1", "b1", "w2", "b2")
-NORM = ("gain", "shift")
 NORM_EPS = 1e-5
 
 
