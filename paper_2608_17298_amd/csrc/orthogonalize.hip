@@ -187,7 +187,7 @@ struct PairArgs {
 //  - Two groups of W x W waves of 64 x 64 that share the operands in LDS (tiles of
 //    128) and take every other block of k: two waves a SIMD, of which one multiplies
 //    while the other reads its fragments (one wave that reads ahead instead: 1024 x
-//    1024 -> 4096 39 us, these 34).
+//    1024 -> 4096 39 us, these 34 on the same card).
 template <int FRAG>
 struct Fragments {
   Pack<f16>::V ah[FRAG], al[FRAG], bh[FRAG], bl[FRAG];
@@ -300,7 +300,7 @@ __device__ __forceinline__ void shared_sums(f32x4 (&sum)[4][4], const PairArgs& 
 }
 
 // A tile of 16 FRAG W on a side.  JOIN: the sums of k are those of g.parts parts.
-// 1024 x 4096: X X^T in seven parts 20 us and their join 8, A A 12, P X 33, of which 10
+// 1024 x 4096: X X^T in seven parts 20 us and their join 9, A A 12, P X 35, of which 10
 // are its stores and 31 % matrix instructions; its LDS reads take as long as those.
 template <typename T, int FRAG, int W, int WK, PairEpilogue EPI, bool JOIN>
 __global__ __launch_bounds__(64 * (JOIN ? 1 : W * W) * WK, 1) void pair_kernel(const PairArgs g) {

@@ -14,7 +14,7 @@ namespace gart {
 namespace {
 
 constexpr int kSmallWaves = 16, kSmallThreads = 64 * kSmallWaves;
-constexpr int64_t kSmallElements = 19456;  // of the padded matrix: two of them in LDS
+constexpr int64_t kSmallElements = 19456;  // of the matrix padded to 32, up to 64 x 288, say: two of them in LDS
 constexpr int64_t kSmallSide = 128;        // of A, which is one tile a wave at most
 
 inline int64_t pad32(int64_t v) { return (v + 31) / 32 * 32; }
@@ -119,7 +119,8 @@ __device__ __forceinline__ void store_four(T* x, int64_t ld, bool tall, int i, i
   }
 }
 
-// 16 waves, with a tile of A and TX of X each at most.
+// 16 waves, with a tile of A and TX of X each at most.  <T, 2, 2> spills 7 or 8
+// registers: 128 x 128 f32 49 us (128 x 129, past what it takes, 65).
 template <typename T, int FRAG, int TX>
 __global__ __launch_bounds__(kSmallThreads) void small_kernel(const Source<T> u, float* m, int64_t rows, int64_t cols,
                                                               bool tall, const Iteration it, T* y, int64_t y_ld,

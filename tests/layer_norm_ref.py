@@ -6,8 +6,8 @@ from blocks_ref import TINY, U, U32
 
 
 def _steps(cols):
-    """Additions that any element of a row's sum passes: a lane adds up to 64 elements of its own, or every 256th pack
-    of a long row, and lanes and waves are joined in at most 16 more."""
+    """Additions that any element of a row's sum passes: a lane adds up to 64 elements of its own, or one in 1024
+    packs of a long row (fewer than cols / 256), and lanes and waves are joined in at most 16 more."""
     return 80 + cols / 256
 
 

@@ -9,7 +9,7 @@ from test_gpu_blocks import GUARD, TYPES, _Out, _inside, _mat, _scratch, _torch,
 
 pytestmark = pytest.mark.gpu
 
-# sizes on both sides of every border where another kernel, tile or cut of the sums is taken
+# sizes on both sides of the borders between the kernels, and of those of small tiles; the large tiles': muon_sizes.py
 SIZES = [(1, 1), (1, 7), (5, 1), (2, 3), (3, 2), (16, 16), (17, 33), (33, 17), (48, 64), (64, 32), (32, 64), (65, 63),
          (64, 65), (7, 300), (300, 7), (1, 4096), (4096, 1), (100, 129), (129, 100), (128, 128), (96, 200), (200, 96),
          (40, 1000), (1000, 40), (255, 255), (256, 130), (130, 700), (700, 130), (512, 300), (300, 512), (500, 1500),
